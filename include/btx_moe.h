@@ -380,6 +380,115 @@ int btx_mix_experts(const void* W1, const void* W3, const void* W2, int dtype, i
 int btx_adamw_step(float* master, float* m, float* v, const void* grad, int grad_dtype, void* lowp, int64_t numel,
                    int step, float lr, float beta1, float beta2, float eps, float weight_decay, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * btx_moe_group_route - routing from logits, for mixtures of many experts: softmax or sigmoid
+ * scores, a bias that balances the experts' loads and that only the selection sees, groups of
+ * experts of which the best are kept, top-k, renormalised and scaled gates; then the same token ->
+ * expert grouping as btx_moe_route's, so that btx_moe_ff_forward, btx_moe_ff_forward_mx4 and
+ * btx_moe_ff_backward_gates take its outputs.
+ *     s = sigmoid(l) or softmax(l)                      (of a token's E logits l)
+ *     v = s + bias                                      (bias NULL: s)
+ *     a group's value = its largest v, or the sum of its two largest; the topk_groups groups of the
+ *     largest values are kept; the k experts of the largest v in them are chosen
+ *     gates_j = scale * s_j / (sum_j s_j + 1e-20)       (renorm 0: scale * s_j)
+ *
+ *   logits     [T,E]   logits_dtype (BTX_F32 or BTX_BF16): the router's product, made by the caller
+ *   bias       [E]     fp32, may be NULL
+ *   score_fn           btx_score_fn
+ *   n_groups           groups of E / n_groups consecutive experts; 1: no groups
+ *   topk_groups        groups kept, 1 <= topk_groups <= n_groups
+ *   group_score        btx_group_score (ignored with one group)
+ * The selection is that of v and of the groups' values in double precision; ties go to the lower
+ * index; topk_idx lists the chosen experts by descending v.  A logit of -inf masks its expert: its
+ * score is 0 and it is chosen only where the kept groups have fewer than k others (TOP2 adds nothing for a
+ * masked one; a group of masked experts only is behind all others).  A NaN logit counts as -inf, +inf as the
+ * largest float; whatever the logits hold, a token's experts are in range and distinct.
+ * Outputs
+ *   topk_idx   [T,k]   int32 expert ids
+ *   gates      [T,k]   fp32
+ *   scores     [T,E]   fp32 s, may be NULL
+ *   counts, offsets, perm, inv_pos: as btx_moe_route's (without a capacity limit)
+ * Requirements: E <= 256, n_groups <= 16, n_groups divides E, 1 <= k <= min(16, topk_groups * E / n_groups);
+ * T*k < 2^31; scale finite.  workspace >= btx_moe_group_route_workspace_bytes(T,E,k) (16-byte aligned; may be NULL
+ * where that is 0, which it is up to 64 tokens).
+ */
+typedef enum { BTX_SCORE_SOFTMAX = 0, BTX_SCORE_SIGMOID = 1 } btx_score_fn;
+typedef enum { BTX_GROUP_MAX = 0, BTX_GROUP_TOP2 = 1 } btx_group_score;
+size_t btx_moe_group_route_workspace_bytes(int T, int E, int k);
+int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias, int T, int E, int k, int score_fn,
+                        int n_groups, int topk_groups, int group_score, int renorm, float scale, int32_t* topk_idx,
+                        float* gates, float* scores, int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv_pos,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * btx_moe_group_route_backward - gradient of the logits from those of the gates (and of the scores),
+ * with the selection held fixed; the bias has none.
+ *   logits, score_fn, renorm, scale: as given to btx_moe_group_route;  topk_idx [T,k] as it wrote them
+ *   dgates   [T,k]  fp32
+ *   dscores  [T,E]  fp32, may be NULL: gradient that reaches the scores directly (an auxiliary loss)
+ *   dlogits  [T,E]  logits_dtype, out; may alias logits
+ * A masked expert's gradient is 0.  Entries of topk_idx outside 0..E-1 are passed over.
+ * Requirements: as btx_moe_group_route; no workspace.
+ */
+int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int32_t* topk_idx, const float* dgates,
+                                 const float* dscores, int T, int E, int k, int score_fn, int renorm, float scale,
+                                 void* dlogits, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * btx_moe_ff_backward_gates - btx_moe_ff_backward for gates of another router than btx_moe_route's: the
+ * gradients of <dY, out> with respect to the gates, x and the experts' weights.  What the router adds to
+ * x's gradient is the caller's (for btx_moe_group_route: dlogits W_router^T).
+ *   dX     [T,d]  dtype  out: through the experts alone
+ *   dgates [T,k]  fp32   out: <dY[t], FF_{idx[t,j]}(x[t])>; 0 for a dropped pair
+ * The other arguments, limits and the workspace's size as btx_moe_ff_backward's.
+ */
+int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype,
+                              int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d, int f, int E, int k,
+                              const float* gates, const int32_t* offsets, const int32_t* perm, const int32_t* inv_pos,
+                              const void* save_h1, const void* save_h3, void* dX, float* dgates, void* dW1, void* dW3,
+                              void* dW2, int dW_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit floats (MXFP4): values 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives (e2m1), of which 32
+ * consecutive ones along the quantised axis (of length K) share a power of two (e8m0).
+ *   codes   [.., n, K/2]   uint8: element 2i of a row in the low half of byte i, element 2i+1 in the high half
+ *   scales  [.., n, btx_mx4_scale_pitch(K)]   uint8: byte b stands for 2^(b-127), 255 for NaN; the K/32 scales of a
+ *           row, then zeros up to a multiple of 16 bytes
+ * btx_mx4_quantize: a block's scale is 2^(floor(log2 of its largest magnitude) - 2), at least 2^-127; its values divided
+ * by that are rounded to the nearest code, ties to the even one, and saturate at 6.  A block that holds an infinity or a NaN gets
+ * the scale 255: all its values are NaN.
+ * btx_mx4_dequantize: code value * scale, exact in fp32 and, down to 2^-133, in bf16.
+ *   x, out  [batch, rows, cols]  dtype (BTX_F32 or BTX_BF16)
+ *   axis    1: blocks along the rows: K = cols, n = rows (activations: [T,d] with batch 1)
+ *           0: blocks down the columns: K = rows, n = cols; codes and scales are [batch, cols, ..].  So are the
+ *              experts' weights quantised whose products sum over their rows: W1, W3 [E,d,f] and W2 [E,f,d].
+ * Requirements: K a multiple of 32, n >= 0, batch >= 0 (nothing to do where one of them is 0); x, out, codes, scales on
+ * 16-byte boundaries.  batch * rows * cols < 2^40.  axis 0: batch <= 65535 and cols <= 4194240 (BTX_ERR_UNSUPPORTED).
+ */
+int64_t btx_mx4_scale_pitch(int64_t K);
+int btx_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, uint8_t* codes,
+                     uint8_t* scales, void* stream);
+int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int64_t batch, int64_t rows, int64_t cols,
+                       int axis, void* out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * btx_moe_ff_forward_mx4 - the layer of 4-bit experts, for serving (forward only): btx_moe_ff_forward with both
+ * operands of every product in microscaled 4-bit floats.  Token rows are quantised along d once each; per expert
+ *     act = silu(xq W1_e) * (xq W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
+ *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
+ *   x [T,d] bf16;  residual [T,d] bf16, may be NULL;  out [T,d] bf16; aliasing as in btx_moe_ff_forward
+ *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
+ *   btx_mx4_quantize (axis 0) writes them
+ *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
+ * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, everything on 16-byte boundaries.
+ */
+size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k);
+int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t* W1_scales, const uint8_t* W3_codes,
+                           const uint8_t* W3_scales, const uint8_t* W2_codes, const uint8_t* W2_scales, int T, int d, int f,
+                           int E, int k, const float* gates, const int32_t* offsets, const int32_t* perm,
+                           const int32_t* inv_pos, const void* residual, void* out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

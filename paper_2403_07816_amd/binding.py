@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
@@ -53,6 +54,15 @@ _SIGNATURES = {
     "btx_merge_average": (_i, [ctypes.POINTER(_vp), _i, _vp, _i64, _i, _vp]),
     "btx_merge_weighted": (_i, [ctypes.POINTER(_vp), ctypes.POINTER(ctypes.c_float), _i, _vp, _i64, _i, _vp]),
     "btx_adamw_step": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _i64, _i, _f, _f, _f, _f, _f, _vp]),
+    "btx_moe_group_route_workspace_bytes": (_sz, [_i] * 3),
+    "btx_moe_group_route": (_i, [_vp, _i, _vp] + [_i] * 8 + [_f] + [_vp] * 8 + [_sz, _vp]),
+    "btx_moe_group_route_backward": (_i, [_vp, _i, _vp, _vp, _vp] + [_i] * 5 + [_f, _vp, _vp]),
+    "btx_moe_ff_backward_gates": (_i, [_vp] * 5 + [_i, _i64, _i64] + [_i] * 5 + [_vp] * 11 + [_i, _vp, _sz, _vp]),
+    "btx_mx4_scale_pitch": (_i64, [_i64]),
+    "btx_mx4_quantize": (_i, [_vp, _i, _i64, _i64, _i64, _i, _vp, _vp, _vp]),
+    "btx_mx4_dequantize": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _i, _vp, _vp]),
+    "btx_moe_ff_forward_mx4_workspace_bytes": (_sz, [_i] * 5),
+    "btx_moe_ff_forward_mx4": (_i, [_vp] * 7 + [_i] * 5 + [_vp] * 7 + [_sz, _vp]),
     "btx_mix_experts": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
 }
 
@@ -124,6 +134,10 @@ def _workspace(nbytes: int, device, workspace: Optional[torch.Tensor]) -> torch.
     if workspace is not None and workspace.numel() * workspace.element_size() >= nbytes:
         return workspace
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def _nbytes(t: Optional[torch.Tensor]) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
 
 
 def _run(entry: str, what: str, x: torch.Tensor, workspace: Optional[torch.Tensor], args: tuple) -> None:
@@ -263,6 +277,203 @@ def btx_moe_ff_backward(dY: torch.Tensor, x: torch.Tensor, W_router: torch.Tenso
     _run("backward", "btx_moe_ff_backward", x, workspace,
          (dY, x, W_router, W1, W3, W2, routing, h1, h3, route_mode, lb_mode, lb_alpha, lb_grad_scale, flags, noise, tau, out.dX,
           out.dW_router, out.db_router, out.dW1, out.dW3, out.dW2, dW_dtype == torch.float32))
+    return out
+
+
+# ---- routing from logits, for many experts; the experts' gradients under such a router -------------------------
+
+BTX_SCORE_SOFTMAX, BTX_SCORE_SIGMOID = 0, 1
+BTX_GROUP_MAX, BTX_GROUP_TOP2 = 0, 1
+
+
+@dataclass
+class GroupRouting:
+    topk_idx: torch.Tensor   # [T,k] int32
+    gates: torch.Tensor      # [T,k] fp32
+    scores: Optional[torch.Tensor]   # [T,E] fp32
+    counts: torch.Tensor     # [E] int32
+    offsets: torch.Tensor    # [E+1] int32
+    perm: torch.Tensor       # [T*k] int32
+    inv_pos: torch.Tensor    # [T,k] int32
+
+
+def alloc_group_routing(T: int, E: int, k: int, device, scores: bool = True) -> GroupRouting:
+    i32, f32 = dict(dtype=torch.int32, device=device), dict(dtype=torch.float32, device=device)
+    return GroupRouting(torch.empty((T, k), **i32), torch.empty((T, k), **f32), torch.empty((T, E), **f32) if scores else None,
+                        torch.zeros(E, **i32), torch.zeros(E + 1, **i32), torch.empty(T * k, **i32), torch.empty((T, k), **i32))
+
+
+def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str):
+    """Device address of a contiguous tensor of this dtype and shape (None: NULL)."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what} is {str(dtype)[6:]} {tuple(shape)}")
+    return _ptr(t)
+
+
+def btx_moe_group_route(logits: torch.Tensor, k: int, score_fn: int = BTX_SCORE_SIGMOID, bias: Optional[torch.Tensor] = None,
+                        n_groups: int = 1, topk_groups: int = 1, group_score: int = BTX_GROUP_TOP2, renorm: bool = True,
+                        scale: float = 1.0, out: Optional[GroupRouting] = None,
+                        workspace: Optional[torch.Tensor] = None) -> GroupRouting:
+    """Route on a router's logits [T,E].  An `out` without scores leaves them out."""
+    lib = load_library()
+    T, E = logits.shape
+    r = out if out is not None else alloc_group_routing(T, E, k, logits.device)
+    i32, f32 = torch.int32, torch.float32
+    nbytes = lib.btx_moe_group_route_workspace_bytes(T, E, k)
+    ws = _workspace(nbytes, logits.device, workspace) if nbytes else None
+    st = lib.btx_moe_group_route(_ptr(logits), _dtype_code(logits), _typed(bias, f32, (E,), "bias"), T, E, k, score_fn, n_groups, topk_groups,
+                                 group_score, int(renorm), scale, _typed(r.topk_idx, i32, (T, k), "topk_idx"),
+                                 _typed(r.gates, f32, (T, k), "gates"), _typed(r.scores, f32, (T, E), "scores"),
+                                 _typed(r.counts, i32, (E,), "counts"), _typed(r.offsets, i32, (E + 1,), "offsets"),
+                                 _typed(r.perm, i32, (T * k,), "perm"), _typed(r.inv_pos, i32, (T, k), "inv_pos"), _ptr(ws),
+                                 _nbytes(ws), _stream())
+    _check(st, "btx_moe_group_route")
+    return r
+
+
+def btx_moe_group_route_backward(logits: torch.Tensor, routing, dgates: torch.Tensor, score_fn: int = BTX_SCORE_SIGMOID,
+                                 renorm: bool = True, scale: float = 1.0, dscores: Optional[torch.Tensor] = None,
+                                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dlogits [T,E]; routing: of btx_moe_group_route on these logits (its topk_idx is read)."""
+    lib = load_library()
+    T, E = logits.shape
+    k = routing.topk_idx.shape[1]
+    out = out if out is not None else torch.empty_like(logits)
+    st = lib.btx_moe_group_route_backward(_ptr(logits), _dtype_code(logits), _typed(routing.topk_idx, torch.int32, (T, k), "topk_idx"),
+                                          _typed(dgates, torch.float32, (T, k), "dgates"),
+                                          _typed(dscores, torch.float32, (T, E), "dscores"), T, E, k, score_fn, int(renorm), scale,
+                                          _typed(out, logits.dtype, (T, E), "dlogits"), _stream())
+    _check(st, "btx_moe_group_route_backward")
+    return out
+
+
+def _stacked(t: Optional[torch.Tensor]):
+    """Device address of stacked expert matrices, each contiguous, the experts any distance apart."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2], "stacked expert matrices only"
+    return t.data_ptr()
+
+
+@dataclass
+class ExpertGrads:
+    dX: torch.Tensor
+    dgates: torch.Tensor
+    dW1: Optional[torch.Tensor]
+    dW3: Optional[torch.Tensor]
+    dW2: Optional[torch.Tensor]
+
+
+def btx_moe_ff_backward_gates(dY: torch.Tensor, x: torch.Tensor, W1: torch.Tensor, W3: torch.Tensor, W2: torch.Tensor, routing,
+                              h1: torch.Tensor, h3: torch.Tensor, dW_dtype: Optional[torch.dtype] = None,
+                              frozen_experts: bool = False, out: Optional[ExpertGrads] = None,
+                              workspace: Optional[torch.Tensor] = None) -> ExpertGrads:
+    """Gradients of x, the gates and the experts; what the router adds to dX is the caller's."""
+    lib = load_library()
+    T, d = x.shape
+    E, f, k, dt = W1.shape[0], W1.shape[2], routing.topk_idx.shape[1], x.dtype
+    dW_dtype = dt if dW_dtype is None else dW_dtype
+    assert W1.shape == (E, d, f) and W3.shape == (E, d, f) and W2.shape == (E, f, d) and W1.dtype == W3.dtype == W2.dtype == dt
+    assert E == 1 or W3.stride(0) == W1.stride(0), "W3 is stacked like W1"
+    if out is None:
+        mk = (lambda W: None) if frozen_experts else (
+            lambda W: torch.empty_strided(W.shape, W.stride(), dtype=dW_dtype, device=x.device))
+        out = ExpertGrads(torch.empty_like(x), torch.empty((T, k), dtype=torch.float32, device=x.device), mk(W1), mk(W3), mk(W2))
+    for dW, W in ((out.dW1, W1), (out.dW3, W3), (out.dW2, W2)):
+        assert dW is None or (dW.shape == W.shape and dW.stride() == W.stride() and dW.dtype == dW_dtype), "dW is stacked like W"
+    i32, f32 = torch.int32, torch.float32
+    ws = _workspace(lib.btx_moe_ff_backward_workspace_bytes(T, d, f, E, k, _dtype_code(x)), x.device, workspace)
+    st = lib.btx_moe_ff_backward_gates(_typed(dY, dt, (T, d), "dY"), _ptr(x), _stacked(W1), _stacked(W3), _stacked(W2), _dtype_code(x),
+                                       W1.stride(0), W2.stride(0), T, d, f, E, k, _typed(routing.gates, f32, (T, k), "gates"),
+                                       _typed(routing.offsets, i32, (E + 1,), "offsets"), _typed(routing.perm, i32, (T * k,), "perm"),
+                                       _typed(routing.inv_pos, i32, (T, k), "inv_pos"), _typed(h1, dt, (T * k, f), "h1"),
+                                       _typed(h3, dt, (T * k, f), "h3"), _typed(out.dX, dt, (T, d), "dX"),
+                                       _typed(out.dgates, f32, (T, k), "dgates"), _stacked(out.dW1), _stacked(out.dW3),
+                                       _stacked(out.dW2), BTX_F32 if dW_dtype == f32 else BTX_BF16, _ptr(ws), _nbytes(ws), _stream())
+    _check(st, "btx_moe_ff_backward_gates")
+    return out
+
+
+# ---- microscaled 4-bit floats, and the layer of experts that are kept in them ---------------------------------
+
+
+@dataclass
+class Mx4:
+    codes: torch.Tensor      # [.., n, K/2] uint8
+    scales: torch.Tensor     # [.., n, 16-byte rows] uint8
+    K: int                   # length of the quantised axis
+
+
+def alloc_mx4(shape, axis: int, device) -> Mx4:
+    """For a tensor of this shape ([.., rows, cols]), quantised along its last axis (-1) or the one before (-2)."""
+    *batch, rows, cols = shape
+    K, n = (cols, rows) if axis == -1 else (rows, cols)
+    u8 = dict(dtype=torch.uint8, device=device)
+    return Mx4(torch.empty((*batch, n, K // 2), **u8), torch.empty((*batch, n, load_library().btx_mx4_scale_pitch(K)), **u8), K)
+
+
+def _mx4_shape(q: Mx4, batch, n: int, what: str) -> None:
+    pitch = load_library().btx_mx4_scale_pitch(q.K)
+    _typed(q.codes, torch.uint8, (*batch, n, q.K // 2), what + ".codes")
+    _typed(q.scales, torch.uint8, (*batch, n, pitch), what + ".scales")
+
+
+def _mx4_axis(axis: int) -> int:
+    if axis not in (-1, -2):
+        raise ValueError("axis is -1 or -2")
+    return axis + 2
+
+
+def btx_mx4_quantize(x: torch.Tensor, axis: int = -1, out: Optional[Mx4] = None) -> Mx4:
+    """[.., rows, cols] in blocks of 32 along axis -1 (activations) or -2 (the experts' weights [E, K, N])."""
+    lib = load_library()
+    ax = _mx4_axis(axis)
+    *batch, rows, cols = x.shape
+    K, n = (cols, rows) if axis == -1 else (rows, cols)
+    out = out if out is not None else alloc_mx4(x.shape, axis, x.device)
+    if out.K != K:
+        raise ValueError(f"out.K is {K}")
+    _mx4_shape(out, batch, n, "out")
+    st = lib.btx_mx4_quantize(_ptr(x), _dtype_code(x), math.prod(batch), rows, cols, ax, _ptr(out.codes), _ptr(out.scales), _stream())
+    _check(st, "btx_mx4_quantize")
+    return out
+
+
+def btx_mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, axis: int = -1, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of q as a tensor; axis: as given to btx_mx4_quantize."""
+    lib = load_library()
+    ax = _mx4_axis(axis)
+    *batch, n, _ = q.codes.shape
+    _mx4_shape(q, batch, n, "q")
+    rows, cols = (n, q.K) if axis == -1 else (q.K, n)
+    out = out if out is not None else torch.empty((*batch, rows, cols), dtype=dtype, device=q.codes.device)
+    st = lib.btx_mx4_dequantize(_ptr(q.codes), _ptr(q.scales), _dtype_code(out), math.prod(batch), rows, cols, ax,
+                                _typed(out, dtype, (*batch, rows, cols), "out"), _stream())
+    _check(st, "btx_mx4_dequantize")
+    return out
+
+
+def btx_moe_ff_forward_mx4(x: torch.Tensor, W1: Mx4, W3: Mx4, W2: Mx4, routing, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[T,d] of the layer of 4-bit experts: W1, W3, W2 as btx_mx4_quantize(W, axis=-2) returns them; routing of btx_moe_route or
+    btx_moe_group_route."""
+    lib = load_library()
+    T, d = x.shape
+    E, f, k = W1.codes.shape[0], W2.K, routing.topk_idx.shape[1]
+    bf16, i32 = torch.bfloat16, torch.int32
+    for q, K, n, what in ((W1, d, f, "W1"), (W3, d, f, "W3"), (W2, f, d, "W2")):
+        if q.K != K:
+            raise ValueError(f"{what}.K is {K}")
+        _mx4_shape(q, (E,), n, what)
+    out = out if out is not None else torch.empty_like(x)
+    ws = _workspace(lib.btx_moe_ff_forward_mx4_workspace_bytes(T, d, f, E, k), x.device, workspace)
+    st = lib.btx_moe_ff_forward_mx4(_typed(x, bf16, (T, d), "x"), _ptr(W1.codes), _ptr(W1.scales), _ptr(W3.codes), _ptr(W3.scales),
+                                    _ptr(W2.codes), _ptr(W2.scales), T, d, f, E, k,
+                                    _typed(routing.gates, torch.float32, (T, k), "gates"), _typed(routing.offsets, i32, (E + 1,), "offsets"),
+                                    _typed(routing.perm, i32, (T * k,), "perm"), _typed(routing.inv_pos, i32, (T, k), "inv_pos"),
+                                    _typed(residual, bf16, (T, d), "residual"), _typed(out, bf16, (T, d), "out"), _ptr(ws), _nbytes(ws),
+                                    _stream())
+    _check(st, "btx_moe_ff_forward_mx4")
     return out
 
 

@@ -6,6 +6,8 @@
 #include "common.h"
 #include "gemm_f32.h"
 #include "gemm_mfma.h"
+#include "group_route.h"
+#include "mx4.h"
 #include "router_ds.h"
 
 using namespace btx;
@@ -301,6 +303,77 @@ size_t btx_moe_ff_backward_workspace_bytes(int T, int d, int f, int E, int k, in
   return carve_backward(nullptr, T, d, f, E, k, dtype).bytes;
 }
 
+namespace {
+// The gradients of the experts and of what feeds them; the gates' go to the router of btx_moe_route (router: what it needs, the rest is
+// filled in here) or to the caller (dgates).
+int backward_impl(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype, int64_t w13_expert_stride,
+                  int64_t w2_expert_stride, int T, int d, int f, int E, int k, const float* gates, const int32_t* offsets, const int32_t* perm,
+                  const int32_t* inv_pos, const void* save_h1, const void* save_h3, void* dX, void* dW1, void* dW3, void* dW2, int dW_dtype,
+                  void* workspace, size_t workspace_bytes, void* stream, RouterBwdArgs* router, float* dgates) {
+  const int n_dw = (dW1 != nullptr) + (dW3 != nullptr) + (dW2 != nullptr);
+  if (!shapes_supported(dtype, T, d, f, E, k)) return BTX_ERR_UNSUPPORTED;
+  const int R = T * k;
+  const FfShapes sh{R, d, f, E, w13_expert_stride, w2_expert_stride};
+  const bool fused = ff_gather_fused(dtype, T, d), direct = ff_dw_direct(dtype, dW_dtype, sh, fused);
+  if (n_dw == 3 && !ff_dw_supported(dtype, sh, direct)) return BTX_ERR_UNSUPPORTED;
+  if (!dY || !x || !W1 || !W3 || !W2 || !gates || !offsets || !perm || !inv_pos || !save_h1 || !save_h3 || !dX || !workspace)
+    return BTX_ERR_INVALID_ARG;
+  if (router ? !router->W_router || !router->topk_idx || !router->probs || !router->gate_sum || !router->prob_sum || !router->counts ||
+                   !router->dW_router
+             : !dgates)
+    return BTX_ERR_INVALID_ARG;
+  if (!aligned16(dY, x, W1, W3, W2, save_h1, save_h3, dX, dW1, dW3, dW2, workspace) || w13_expert_stride % 8 ||
+      w2_expert_stride % 8)
+    return BTX_ERR_INVALID_ARG;
+  const BwdWs w = carve_backward(workspace, T, d, f, E, k, dtype);
+  if (workspace_bytes < w.bytes) return BTX_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!fused) BTX_STAGE(BTX_STAGE_GATHER_DY, launch_gather_rows(dY, w.dys, perm, R, k, d, dtype, s));
+  const RowSource dys = fused ? RowSource{dY, perm, k} : RowSource{w.dys, nullptr, 1};
+  // of weight gradients that read token rows: all of them, or (tiles) dW2
+  const bool dw2_rows = !direct && ff_dw2_rows(dtype, T, sh);
+  uint32_t* row_bytes = n_dw == 3 && (direct || dw2_rows) ? w.row_bytes : nullptr;
+  BTX_STAGE(BTX_STAGE_BWD_ACT, launch_bwd_act(dtype, dys, W2, save_h1, save_h3, gates, perm, offsets, sh, w.dh1,
+                                              w.dh3, w.ga, n_dw == 3, !direct, row_bytes, w.dg_part, s));
+  const int n_part = bwd_act_partials(dtype, sh);
+  if (router) {
+    router->dg_part = w.dg_part;
+    router->n_part = n_part;
+    router->dxs = w.dxs;
+    router->workspace = w.router;
+  }
+  const bool ds_rides = router && n_dw == 3 && direct && router_ds_rides(T, d, E, dtype == BTX_F32);
+  const RouterDs rd = ds_rides ? router_ds_args(*router) : RouterDs{};
+  const RouterDs* const ds = ds_rides ? &rd : nullptr;
+  const RowSource dw_x{x, perm, k}, dw_dy{dY, perm, k};
+  if (n_dw == 3 && dtype == BTX_F32) {
+    BTX_STAGE(BTX_STAGE_BWD_DX, f32_bwd_dx_dw(dw_x, dw_dy, w.dh1, w.dh3, w.ga, W1, W3, offsets, sh, row_bytes, w.dxs, w.partial,
+                                                 dW1, dW3, dW2, ds, s));
+    BTX_STAGE(BTX_STAGE_DW13, BTX_OK);                   // events with nothing between them
+    BTX_STAGE(BTX_STAGE_DW2, BTX_OK);
+  } else {
+    BTX_STAGE(BTX_STAGE_BWD_DX, launch_bwd_dx(dtype, w.dh1, w.dh3, W1, W3, offsets, sh, w.dxs, w.partial, s));
+  }
+  if (n_dw == 3 && dtype == BTX_BF16 && direct) {
+    BTX_STAGE(BTX_STAGE_DW13, mfma_bwd_dw_direct(dW_dtype, dw_x, dw_dy, w.dh1, w.dh3, w.ga, offsets, sh, row_bytes, dW1, dW3, dW2, ds, s));
+    BTX_STAGE(BTX_STAGE_DW2, BTX_OK);
+  } else if (n_dw == 3 && dtype == BTX_BF16) {
+    BTX_STAGE(BTX_STAGE_GATHER_X_BWD,
+              launch_gather_rows_t(x, w.xsT, dw2_rows ? nullptr : dY, w.dysT, perm, offsets, R, k, d, E, ff_dw_pitch(R, E), s));
+    BTX_STAGE(BTX_STAGE_DW13, mfma_bwd_dw13(dW_dtype, {w.xsT, nullptr, 1}, w.dh1, w.dh3, offsets, sh, dW1, dW3, s));
+    BTX_STAGE(BTX_STAGE_DW2, mfma_bwd_dw2(dW_dtype, w.ga, dw2_rows ? dw_dy : RowSource{w.dysT, nullptr, 1}, offsets, sh, row_bytes, dW2, s));
+  }
+  if (router) {
+    BTX_STAGE(BTX_STAGE_ROUTER_BWD, launch_router_bwd(*router, ds_rides, s));
+  } else {
+    BTX_STAGE(BTX_STAGE_ROUTER_BWD, launch_gate_grads(w.dg_part, n_part, inv_pos, R, dgates, s));
+    BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.dxs, nullptr, 1, nullptr, inv_pos, nullptr, dX, T, k, d, dtype, s));
+  }
+  return BTX_OK;
+}
+}  // namespace
+
+
 int btx_moe_ff_backward(const void* dY, const void* x, const float* W_router, const void* W1, const void* W3,
                         const void* W2, int dtype, int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d,
                         int f, int E, int k, int route_mode, int lb_mode, float lb_alpha, float lb_grad_scale,
@@ -323,52 +396,141 @@ int btx_moe_ff_backward(const void* dY, const void* x, const float* W_router, co
   const int n_dw = (dW1 != nullptr) + (dW3 != nullptr) + (dW2 != nullptr);
   if (n_dw != 0 && n_dw != 3) return BTX_ERR_INVALID_ARG;
   if (T == 0) return BTX_OK;
-  if (!shapes_supported(dtype, T, d, f, E, k)) return BTX_ERR_UNSUPPORTED;
-  const int R = T * k;
-  const FfShapes sh{R, d, f, E, w13_expert_stride, w2_expert_stride};
-  const bool fused = ff_gather_fused(dtype, T, d), direct = ff_dw_direct(dtype, dW_dtype, sh, fused);
-  if (n_dw == 3 && !ff_dw_supported(dtype, sh, direct)) return BTX_ERR_UNSUPPORTED;
-  if (!dY || !x || !W_router || !W1 || !W3 || !W2 || !topk_idx || !gates || !probs || !offsets || !perm || !inv_pos ||
-      !gate_sum || !prob_sum || !counts || !save_h1 || !save_h3 || !dX || !dW_router || !workspace)
+  RouterBwdArgs ra{x, dtype, W_router, T, d, E, k, route_mode, lb_mode, lb_alpha, lb_grad_scale, flags, noise, tau,
+                   topk_idx, gates, probs, inv_pos, gate_sum, prob_sum, counts, nullptr, 0, nullptr, dX, dW_router, db_router, nullptr};
+  return backward_impl(dY, x, W1, W3, W2, dtype, w13_expert_stride, w2_expert_stride, T, d, f, E, k, gates, offsets, perm, inv_pos, save_h1,
+                       save_h3, dX, dW1, dW3, dW2, dW_dtype, workspace, workspace_bytes, stream, &ra, nullptr);
+}
+
+int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype,
+                              int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d, int f, int E, int k, const float* gates,
+                              const int32_t* offsets, const int32_t* perm, const int32_t* inv_pos, const void* save_h1, const void* save_h3,
+                              void* dX, float* dgates, void* dW1, void* dW3, void* dW2, int dW_dtype, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(dW_dtype) || !shapes_ok(T, d, f, E, k)) return BTX_ERR_INVALID_ARG;
+  if (dW_dtype != dtype && dW_dtype != BTX_F32) return BTX_ERR_INVALID_ARG;
+  if (w13_expert_stride < (int64_t)d * f || w2_expert_stride < (int64_t)d * f) return BTX_ERR_INVALID_ARG;
+  const int n_dw = (dW1 != nullptr) + (dW3 != nullptr) + (dW2 != nullptr);
+  if (n_dw != 0 && n_dw != 3) return BTX_ERR_INVALID_ARG;
+  if (T == 0) return BTX_OK;
+  return backward_impl(dY, x, W1, W3, W2, dtype, w13_expert_stride, w2_expert_stride, T, d, f, E, k, gates, offsets, perm, inv_pos, save_h1,
+                       save_h3, dX, dW1, dW3, dW2, dW_dtype, workspace, workspace_bytes, stream, nullptr, dgates);
+}
+
+size_t btx_moe_group_route_workspace_bytes(int T, int E, int k) {
+  if (T <= 0 || E < 1 || E > kGroupMaxExperts || k < 1 || k > E || k > kGroupMaxK) return 0;
+  return group_route_workspace_bytes(T, E);
+}
+
+int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias, int T, int E, int k, int score_fn, int n_groups,
+                        int topk_groups, int group_score, int renorm, float scale, int32_t* topk_idx, float* gates, float* scores,
+                        int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv_pos, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+  if (!dtype_ok(logits_dtype) || T < 0 || E < 1 || E > kGroupMaxExperts || k < 1 || k > kGroupMaxK) return BTX_ERR_INVALID_ARG;
+  if (n_groups < 1 || n_groups > kGroupMaxGroups || E % n_groups != 0 || topk_groups < 1 || topk_groups > n_groups) return BTX_ERR_INVALID_ARG;
+  if (k > topk_groups * (E / n_groups) || (int64_t)T * k >= (int64_t)1 << 31) return BTX_ERR_INVALID_ARG;
+  if (score_fn != BTX_SCORE_SOFTMAX && score_fn != BTX_SCORE_SIGMOID) return BTX_ERR_INVALID_ARG;
+  if (group_score != BTX_GROUP_MAX && group_score != BTX_GROUP_TOP2) return BTX_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return BTX_ERR_INVALID_ARG;
+  if (T == 0) return BTX_OK;
+  const size_t need = group_route_workspace_bytes(T, E);
+  if (!logits || !topk_idx || !gates || !counts || !offsets || !perm || !inv_pos || (need && !workspace)) return BTX_ERR_INVALID_ARG;
+  if (!aligned16(logits, scores, workspace)) return BTX_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return BTX_ERR_WORKSPACE;
+  GroupRouteArgs a{logits, logits_dtype, bias, T, E, k, score_fn, n_groups, topk_groups, group_score, renorm, scale, topk_idx, gates, scores,
+                   counts, offsets, perm, inv_pos, static_cast<int*>(workspace), 0, 0, 0, 0, 0};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  BTX_STAGE(BTX_STAGE_ROUTE, launch_group_route(a, s));
+  return BTX_OK;
+}
+
+int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int32_t* topk_idx, const float* dgates, const float* dscores,
+                                 int T, int E, int k, int score_fn, int renorm, float scale, void* dlogits, void* stream) {
+  if (!dtype_ok(logits_dtype) || T < 0 || E < 1 || E > kGroupMaxExperts || k < 1 || k > kGroupMaxK || k > E) return BTX_ERR_INVALID_ARG;
+  if ((int64_t)T * k >= (int64_t)1 << 31) return BTX_ERR_INVALID_ARG;
+  if (score_fn != BTX_SCORE_SOFTMAX && score_fn != BTX_SCORE_SIGMOID) return BTX_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return BTX_ERR_INVALID_ARG;
+  if (T == 0) return BTX_OK;
+  if (!logits || !topk_idx || !dgates || !dlogits) return BTX_ERR_INVALID_ARG;
+  if (!aligned16(logits, dscores, dlogits)) return BTX_ERR_INVALID_ARG;
+  GroupRouteBwdArgs a{logits, logits_dtype, topk_idx, dgates, dscores, T, E, k, score_fn, renorm, scale, dlogits};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  BTX_STAGE(BTX_STAGE_ROUTER_BWD, launch_group_route_bwd(a, s));
+  return BTX_OK;
+}
+
+int64_t btx_mx4_scale_pitch(int64_t K) { return K > 0 && K % kMxBlock == 0 ? mx4_pitch(K) : 0; }
+
+namespace {
+int mx4_tensor_ok(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, const uint8_t* codes, const uint8_t* scales) {
+  if (!dtype_ok(dtype) || batch < 0 || rows < 0 || cols < 0 || (axis != 0 && axis != 1)) return BTX_ERR_INVALID_ARG;
+  if ((axis == 1 ? cols : rows) % kMxBlock != 0) return BTX_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0 || cols == 0) return BTX_OK;
+  if (rows >= (int64_t)1 << 40 || cols >= ((int64_t)1 << 40) / rows || batch >= ((int64_t)1 << 40) / (rows * cols)) return BTX_ERR_INVALID_ARG;
+  if (!x || !codes || !scales || !aligned16(x, codes, scales)) return BTX_ERR_INVALID_ARG;
+  return BTX_OK;
+}
+}  // namespace
+
+int btx_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, uint8_t* codes, uint8_t* scales,
+                     void* stream) {
+  if (int rc = mx4_tensor_ok(x, dtype, batch, rows, cols, axis, codes, scales)) return rc;
+  if (batch == 0 || rows == 0 || cols == 0) return BTX_OK;
+  return launch_mx4_quantize(x, dtype, batch, rows, cols, axis, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, void* out,
+                       void* stream) {
+  if (int rc = mx4_tensor_ok(out, dtype, batch, rows, cols, axis, codes, scales)) return rc;
+  if (batch == 0 || rows == 0 || cols == 0) return BTX_OK;
+  return launch_mx4_dequantize(codes, scales, dtype, batch, rows, cols, axis, out, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+bool mx4_shapes_ok(int T, int d, int f, int E, int k) {
+  return T >= 0 && d > 0 && f > 0 && E >= 1 && E <= kMx4MaxExperts && k >= 1 && k <= E && d % kMxBlock == 0 && f % kMxBlock == 0 &&
+         (int64_t)T * k < (int64_t)1 << 31 && (int64_t)T * k * (int64_t)(d > f ? d : f) < (int64_t)1 << 40 &&
+         (int64_t)E * d * f < (int64_t)1 << 40;
+}
+struct Mx4Ws { uint8_t *x_codes, *x_scales, *act_codes, *act_scales; void* y; size_t bytes; };
+Mx4Ws carve_mx4(void* ws, int T, int d, int f, int k) {
+  const size_t R = (size_t)T * k;
+  Carver c(ws);
+  Mx4Ws w;
+  w.x_codes = static_cast<uint8_t*>(c.take((size_t)T * (d / 2)));
+  w.x_scales = static_cast<uint8_t*>(c.take((size_t)T * mx4_pitch(d)));
+  w.act_codes = static_cast<uint8_t*>(c.take(R * (f / 2)));
+  w.act_scales = static_cast<uint8_t*>(c.take(R * mx4_pitch(f)));
+  w.y = c.take(R * d * 2);
+  w.bytes = c.used;
+  return w;
+}
+}  // namespace
+
+size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k) {
+  if (!mx4_shapes_ok(T, d, f, E, k) || T == 0) return 0;
+  return carve_mx4(nullptr, T, d, f, k).bytes;
+}
+
+int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t* W1_scales, const uint8_t* W3_codes, const uint8_t* W3_scales,
+                           const uint8_t* W2_codes, const uint8_t* W2_scales, int T, int d, int f, int E, int k, const float* gates,
+                           const int32_t* offsets, const int32_t* perm, const int32_t* inv_pos, const void* residual, void* out,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (!mx4_shapes_ok(T, d, f, E, k)) return BTX_ERR_INVALID_ARG;
+  if (T == 0) return BTX_OK;
+  if (!x || !W1_codes || !W1_scales || !W3_codes || !W3_scales || !W2_codes || !W2_scales || !gates || !offsets || !perm || !inv_pos || !out ||
+      !workspace)
     return BTX_ERR_INVALID_ARG;
-  if (!aligned16(dY, x, W1, W3, W2, save_h1, save_h3, dX, dW1, dW3, dW2, workspace) || w13_expert_stride % 8 ||
-      w2_expert_stride % 8)
-    return BTX_ERR_INVALID_ARG;
-  const BwdWs w = carve_backward(workspace, T, d, f, E, k, dtype);
+  if (!aligned16(x, W1_codes, W1_scales, W3_codes, W3_scales, W2_codes, W2_scales, residual, out, workspace)) return BTX_ERR_INVALID_ARG;
+  const Mx4Ws w = carve_mx4(workspace, T, d, f, k);
   if (workspace_bytes < w.bytes) return BTX_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (!fused) BTX_STAGE(BTX_STAGE_GATHER_DY, launch_gather_rows(dY, w.dys, perm, R, k, d, dtype, s));
-  const RowSource dys = fused ? RowSource{dY, perm, k} : RowSource{w.dys, nullptr, 1};
-  // of weight gradients that read token rows: all of them, or (tiles) dW2
-  const bool dw2_rows = !direct && ff_dw2_rows(dtype, T, sh);
-  uint32_t* row_bytes = n_dw == 3 && (direct || dw2_rows) ? w.row_bytes : nullptr;
-  BTX_STAGE(BTX_STAGE_BWD_ACT, launch_bwd_act(dtype, dys, W2, save_h1, save_h3, gates, perm, offsets, sh, w.dh1,
-                                              w.dh3, w.ga, n_dw == 3, !direct, row_bytes, w.dg_part, s));
-  RouterBwdArgs ra{x, dtype, W_router, T, d, E, k, route_mode, lb_mode, lb_alpha, lb_grad_scale, flags, noise, tau,
-                   topk_idx, gates, probs, inv_pos, gate_sum, prob_sum, counts, w.dg_part, bwd_act_partials(dtype, sh), w.dxs, dX,
-                   dW_router, db_router, w.router};
-  const bool ds_rides = n_dw == 3 && direct && router_ds_rides(T, d, E, dtype == BTX_F32);
-  const RouterDs rd = ds_rides ? router_ds_args(ra) : RouterDs{};
-  const RouterDs* const ds = ds_rides ? &rd : nullptr;
-  const RowSource dw_x{x, perm, k}, dw_dy{dY, perm, k};
-  if (n_dw == 3 && dtype == BTX_F32) {
-    BTX_STAGE(BTX_STAGE_BWD_DX, f32_bwd_dx_dw(dw_x, dw_dy, w.dh1, w.dh3, w.ga, W1, W3, offsets, sh, row_bytes, w.dxs, w.partial,
-                                                 dW1, dW3, dW2, ds, s));
-    BTX_STAGE(BTX_STAGE_DW13, BTX_OK);                   // events with nothing between them
-    BTX_STAGE(BTX_STAGE_DW2, BTX_OK);
-  } else {
-    BTX_STAGE(BTX_STAGE_BWD_DX, launch_bwd_dx(dtype, w.dh1, w.dh3, W1, W3, offsets, sh, w.dxs, w.partial, s));
-  }
-  if (n_dw == 3 && dtype == BTX_BF16 && direct) {
-    BTX_STAGE(BTX_STAGE_DW13, mfma_bwd_dw_direct(dW_dtype, dw_x, dw_dy, w.dh1, w.dh3, w.ga, offsets, sh, row_bytes, dW1, dW3, dW2, ds, s));
-    BTX_STAGE(BTX_STAGE_DW2, BTX_OK);
-  } else if (n_dw == 3 && dtype == BTX_BF16) {
-    BTX_STAGE(BTX_STAGE_GATHER_X_BWD,
-              launch_gather_rows_t(x, w.xsT, dw2_rows ? nullptr : dY, w.dysT, perm, offsets, R, k, d, E, ff_dw_pitch(R, E), s));
-    BTX_STAGE(BTX_STAGE_DW13, mfma_bwd_dw13(dW_dtype, {w.xsT, nullptr, 1}, w.dh1, w.dh3, offsets, sh, dW1, dW3, s));
-    BTX_STAGE(BTX_STAGE_DW2, mfma_bwd_dw2(dW_dtype, w.ga, dw2_rows ? dw_dy : RowSource{w.dysT, nullptr, 1}, offsets, sh, row_bytes, dW2, s));
-  }
-  BTX_STAGE(BTX_STAGE_ROUTER_BWD, launch_router_bwd(ra, ds_rides, s));
+  const Mx4Shapes sh{T, d, f, E, k};
+  BTX_STAGE(BTX_STAGE_GATHER_X, launch_mx4_quantize(x, BTX_BF16, 1, T, d, 1, w.x_codes, w.x_scales, s));
+  BTX_STAGE(BTX_STAGE_UP, launch_mx4_up({w.x_codes, w.x_scales}, {W1_codes, W1_scales}, {W3_codes, W3_scales}, offsets, perm, sh, w.act_codes,
+                                        w.act_scales, s));
+  BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down({w.act_codes, w.act_scales}, {W2_codes, W2_scales}, offsets, sh, w.y, s));
+  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, nullptr, 1, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
   return BTX_OK;
 }
 

@@ -1,0 +1,628 @@
+// Routing from logits for mixtures of many experts: softmax or sigmoid scores, a bias that only the selection sees, groups of
+// which the best are kept, top-k, renormalised and scaled gates, and the stable grouping of the (token, slot) pairs by expert.
+// Up to 64 tokens one launch, else two:
+//   1. group_select   16 lanes (one DPP row) take a token, four tokens a wavefront, 64 a workgroup at a time: scores, the groups'
+//                     values and ranks, the k largest one after another; then the workgroup ranks its pairs among those of the same
+//                     expert and leaves how many of each it has.
+//   2. group_scatter  every workgroup adds those counts up (of the workgroups before it, and of all) and writes its pairs' places.
+// The selection is the one of the scores in double precision.  It is done in float, with a bound of each value's error; a token with two
+// values, or two groups, nearer to each other than that is done again in double (group_pick<double>), by the same lanes: a few in a
+// thousand of ordinary logits, all of them where all logits are equal.
+#include "group_route.h"
+
+namespace btx {
+namespace {
+
+constexpr int kLanes = 16;                     // of a token
+constexpr int kTokWave = kWave / kLanes;
+constexpr int kThreadsMost = 1024, kTokPass = kThreadsMost / kLanes;
+constexpr int kSlots = kGroupMaxK + 1;         // the k chosen and the one behind them
+constexpr float kMaskedF = -1e30f;             // value of a masked expert in float
+constexpr float kUlp = 1.1920929e-7f;          // 2^-23
+
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) { return (uint32_t)dpp_i32<CTRL>((int)v); }
+// over the 16 lanes of a row
+__device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
+  v = max(v, dpp_u32<kDppXor1>(v));
+  v = max(v, dpp_u32<kDppXor2>(v));
+  v = max(v, dpp_u32<kDppRor4>(v));
+  return max(v, dpp_u32<kDppRor8>(v));
+}
+__device__ __forceinline__ float row_max_f32(float v) {
+  v = fmaxf(v, dpp_f32<kDppXor1>(v));
+  v = fmaxf(v, dpp_f32<kDppXor2>(v));
+  v = fmaxf(v, dpp_f32<kDppRor4>(v));
+  return fmaxf(v, dpp_f32<kDppRor8>(v));
+}
+// (mirrors, not rotations: both halves of every addition are the same two sums, so that all lanes have the same bits, and equal
+// logits in different lanes equal scores)
+constexpr int kDppHalfMirror = 0x141, kDppMirror = 0x140;   // lane i of 8 (of 16): lane 7 - i (15 - i)
+__device__ __forceinline__ float row_sum_f32(float v) {
+  v += dpp_f32<kDppXor1>(v);
+  v += dpp_f32<kDppXor2>(v);
+  v += dpp_f32<kDppHalfMirror>(v);
+  return v + dpp_f32<kDppMirror>(v);
+}
+__device__ __forceinline__ uint32_t row_or_u32(uint32_t v) {
+  v |= dpp_u32<kDppXor1>(v);
+  v |= dpp_u32<kDppXor2>(v);
+  v |= dpp_u32<kDppRor4>(v);
+  return v | dpp_u32<kDppRor8>(v);
+}
+// a float's bits in an order that unsigned integers have; above 0 for every float
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// NaN: masked, as -inf is; +inf: the largest float
+__device__ __forceinline__ float clean(float l) { return l == l ? fminf(l, 3.402823e38f) : -INFINITY; }
+
+__device__ __forceinline__ float load_logit(const float* p) { return clean(*p); }
+__device__ __forceinline__ float load_logit(const bf16_t* p) { return clean(bf16_to_f32(*p)); }
+__device__ __forceinline__ void load_logits4(const float* p, float* v) {
+  const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = clean(w[i]);
+}
+__device__ __forceinline__ void load_logits4(const bf16_t* p, float* v) {
+  const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { v[2 * i] = clean(bf16lo(w[i])); v[2 * i + 1] = clean(bf16hi(w[i])); }
+}
+
+// Which experts a lane has: group g's are dealt to 2^log2_lanes lanes of the row, `per_lane` consecutive ones each
+struct Deal {
+  int first, n, group;       // of this lane
+  __device__ __forceinline__ Deal(const GroupRouteArgs& a, int sub) {
+    group = sub >> a.log2_lanes;
+    const int part = sub & ((1 << a.log2_lanes) - 1), from = part * a.per_lane;
+    first = group * a.per_group + from;
+    n = group < a.G ? max(0, min(a.per_lane, a.per_group - from)) : 0;
+  }
+};
+
+// Scores of one token: max and 1 / sum of exp for softmax
+struct RowStat { float m, inv; };
+template <int SCORE> __device__ __forceinline__ float score_f(float l, const RowStat& st) {
+  if (SCORE == BTX_SCORE_SIGMOID) return sigmoid_f(l);
+  return l == -INFINITY ? 0.f : __expf(l - st.m) * st.inv;
+}
+// bound of the error of score + bias = v in float: the argument of exp is rounded (|l| 2^-24 log2(e) of its value, at most), the
+// hardware's exp2 and reciprocal add an ulp each, softmax's sum one for every addition in line (36 at most), the bias another
+template <int SCORE> __device__ __forceinline__ float score_err(float l, float s, float v, const RowStat& st) {
+  if (l == -INFINITY) return 0.f;
+  if (SCORE == BTX_SCORE_SIGMOID) return kUlp * (s * ((1.f - s) * (fabsf(l) + 2.f) + 3.f) + fabsf(v));
+  return kUlp * (s * (fabsf(l - st.m) + 26.f) + fabsf(v));
+}
+
+__device__ __forceinline__ double shfl_f64(double v, int lane) {
+  const int lo = __shfl(__double2loint(v), lane, kWave), hi = __shfl(__double2hiint(v), lane, kWave);
+  return __hiloint2double(hi, lo);
+}
+
+// what lanes of this wavefront have put into LDS is there for the others
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The selection in double, by the 16 lanes of a token: slot[j] = expert of slot j.  logits: the token's.  (Not inlined, and it reads the
+// logits again: its registers are not the fast path's.)
+template <typename XT, int P, int SCORE>
+__device__ __attribute__((noinline)) void group_pick_f64(const GroupRouteArgs& a, const XT* logits, int sub, int row_base, int* slot) {
+  const Deal mine(a, sub);
+  float l[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) l[i] = i < mine.n ? load_logit(logits + mine.first + i) : -INFINITY;
+  double v[P];
+  double m = -INFINITY, sum = 0.0;
+  if (SCORE == BTX_SCORE_SOFTMAX) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) m = fmax(m, (double)l[i]);
+    for (int d = 1; d < kLanes; d *= 2) m = fmax(m, shfl_f64(m, row_base + (sub ^ d)));
+#pragma unroll
+    for (int i = 0; i < P; ++i) sum += i < mine.n && l[i] != -INFINITY ? exp((double)l[i] - m) : 0.0;
+    for (int d = 1; d < kLanes; d *= 2) sum += shfl_f64(sum, row_base + (sub ^ d));
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (i < mine.n && l[i] != -INFINITY) {
+      const double s = SCORE == BTX_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - m) / sum;
+      v[i] = s + (a.bias ? (double)a.bias[mine.first + i] : 0.0);
+      if (!(v[i] == v[i])) v[i] = -INFINITY;
+    } else {
+      v[i] = -INFINITY;
+    }
+  }
+  uint32_t left = mine.n >= 32 ? 0xffffffffu : (1u << mine.n) - 1u;     // experts that may be chosen
+  if (a.G > 1) {
+    double b1 = -INFINITY, b2 = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      b2 = fmax(b2, fmin(b1, v[i]));
+      b1 = fmax(b1, v[i]);
+    }
+    for (int d = 1; d < (1 << a.log2_lanes); d *= 2) {
+      const double o1 = shfl_f64(b1, row_base + (sub ^ d)), o2 = shfl_f64(b2, row_base + (sub ^ d));
+      b2 = fmax(fmax(b2, o2), fmin(b1, o1));
+      b1 = fmax(b1, o1);
+    }
+    const double value = a.group_score == BTX_GROUP_TOP2 && b2 != -INFINITY ? b1 + b2 : b1;
+    int better = 0;
+    for (int h = 0; h < a.G; ++h) {
+      const double o = shfl_f64(value, row_base + (h << a.log2_lanes));
+      better += h != mine.group && (o > value || (o == value && h < mine.group));
+    }
+    if (better >= a.keep) left = 0;
+  }
+  for (int j = 0; j < a.k; ++j) {
+    double best = -INFINITY;
+    int at = -1;                                                        // any expert that is left, masked ones too, before none
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if ((left >> i & 1) && (at < 0 || v[i] > best)) { best = v[i]; at = i; }
+    double top = best;
+    int who = at < 0 ? kWave : sub;
+    for (int d = 1; d < kLanes; d *= 2) {
+      const double o = shfl_f64(top, row_base + (sub ^ d));
+      const int w = __shfl(who, row_base + (sub ^ d), kWave);
+      if (w < kWave && (who == kWave || o > top || (o == top && w < who))) { top = o; who = w; }
+    }
+    if (who == sub) {
+      left &= ~(1u << at);
+      slot[j] = mine.first + at;
+    }
+  }
+}
+
+// grid: blocks of `tokens` tokens.  LDS: slots of the tokens of a pass; counts of [64 pairs][expert].
+template <typename XT, int P, int SCORE>
+__global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteArgs a) {
+  __shared__ int s_slot[kTokPass][kSlots];
+  __shared__ int s_idx[kTokPass * kGroupMaxK];                          // of the pass' pairs
+  __shared__ uint16_t s_count[kTokPass * kGroupMaxK / kWave][kGroupMaxExperts];
+  __shared__ int s_base[kGroupMaxExperts], s_off[kGroupMaxExperts], s_wave[kGroupMaxExperts / kWave];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, sub = lane & (kLanes - 1), row_base = lane & ~(kLanes - 1);
+  const int in_pass = threadIdx.x / kLanes, pass_tokens = blockDim.x / kLanes;
+  const Deal mine(a, sub);
+  const XT* const logits = static_cast<const XT*>(a.logits);
+  for (int e = threadIdx.x; e < a.E; e += blockDim.x) s_base[e] = 0;
+  const int t_begin = blockIdx.x * a.tokens, t_end = min(a.T, t_begin + a.tokens);
+  for (int t0 = t_begin; t0 < t_end; t0 += pass_tokens) {
+    const int t = t0 + in_pass;
+    const int n_tok = min(pass_tokens, t_end - t0), rounds = (n_tok * a.k + kWave - 1) / kWave;
+    for (int i = threadIdx.x; i < rounds * a.E; i += blockDim.x) s_count[i / a.E][i % a.E] = 0;
+    if (t < t_end) {
+      // ---- scores ----
+      float l[P];
+      const XT* const from = logits + (size_t)t * a.E + mine.first;
+      if (P % 4 == 0 && a.vector) {
+#pragma unroll
+        for (int i = 0; i + 3 < P; i += 4) {
+          if (i < mine.n) load_logits4(from + i, l + i);
+          else l[i] = l[i + 1] = l[i + 2] = l[i + 3] = -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) l[i] = i < mine.n ? load_logit(from + i) : -INFINITY;
+      }
+      RowStat st{0.f, 0.f};
+      if (SCORE == BTX_SCORE_SOFTMAX) {
+        float m = l[0];
+#pragma unroll
+        for (int i = 1; i < P; ++i) m = fmaxf(m, l[i]);
+        st.m = row_max_f32(m);
+        if (st.m == -INFINITY) st.m = 0.f;                              // every expert masked
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) sum += __expf(l[i] - st.m);
+        sum = row_sum_f32(sum);
+        st.inv = sum > 0.f ? 1.f / sum : 0.f;
+      }
+      float v[P], s[P], err = 0.f, b1 = kMaskedF, b2 = kMaskedF;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        s[i] = score_f<SCORE>(l[i], st);
+        v[i] = kMaskedF;
+        if (l[i] != -INFINITY) {
+          const float x = a.bias ? s[i] + a.bias[mine.first + i] : s[i];
+          v[i] = fmaxf(x, kMaskedF);                                    // (also of a NaN)
+        }
+        err = fmaxf(err, score_err<SCORE>(l[i], s[i], v[i], st));
+        b2 = fmaxf(b2, fminf(b1, v[i]));
+        b1 = fmaxf(b1, v[i]);
+      }
+      if (a.scores) {
+        float* const to = a.scores + (size_t)t * a.E + mine.first;
+        if (P % 4 == 0 && a.vector) {
+#pragma unroll
+          for (int i = 0; i + 3 < P; i += 4)
+            if (i < mine.n) *reinterpret_cast<f32x4*>(to + i) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < P; ++i)
+            if (i < mine.n) to[i] = s[i];
+        }
+      }
+      // ---- groups ----
+      bool in = true, unsure = false;
+      if (a.G > 1) {
+        for (int d = 1; d < (1 << a.log2_lanes); d *= 2) {
+          const float o1 = __shfl_xor(b1, d, kWave), o2 = __shfl_xor(b2, d, kWave);
+          b2 = fmaxf(fmaxf(b2, o2), fminf(b1, o1));
+          b1 = fmaxf(b1, o1);
+        }
+        float e2 = row_max_f32(err);                                    // of every value of the token
+        const bool two = a.group_score == BTX_GROUP_TOP2 && b2 > kMaskedF;
+        const float value = two ? b1 + b2 : b1;
+        e2 = 4.f * e2 + 2.f * kUlp * fabsf(value);                      // of the difference of two groups' values
+        int above = 0, maybe = 0;                                       // groups that are better, or may be
+        for (int h = 0; h < a.G; ++h) {
+          const float d = __shfl(value, row_base + (h << a.log2_lanes), kWave) - value;
+          if (h != mine.group) {
+            above += d > e2;
+            maybe += d >= -e2;
+          }
+        }
+        in = maybe < a.keep;
+        unsure = mine.group < a.G && !in && above < a.keep;
+      }
+      // ---- the k largest, and the next ----
+      uint32_t key[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) key[i] = in && i < mine.n ? ordered(v[i]) : 0u;
+      int* const slot = s_slot[in_pass];
+      int taken = 0, found = 0;
+      for (int j = 0; j <= a.k; ++j) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int i = 1; i < P; ++i) best = max(best, key[i]);
+        const uint32_t top = row_max_u32(best);
+        const uint32_t have = (uint32_t)(__ballot(best == top) >> row_base) & 0xffffu;
+        found += top != 0u;
+        if (sub == __ffs(have) - 1) {                                   // the first lane of those that have it
+          int at = -1 - mine.first;
+          if (top) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+              const bool hit = key[i] == top;                           // (more than one: `taken` tells)
+              at = hit ? i : at;
+              taken += hit;
+              key[i] = hit ? 0u : key[i];
+            }
+          }
+          slot[j] = mine.first + at;                                    // -1: none is left
+        }
+      }
+      unsure |= row_sum_f32((float)taken) > (float)found;               // equal values of one lane went together
+      wave_lds_fence();
+      // lane j: slot j
+      int e = -1;
+      float ls = -INFINITY, ss = 0.f;
+      if (sub < a.k) {
+        e = slot[sub];
+        const int n = slot[sub + 1];
+        if (e >= 0) {
+          ls = load_logit(logits + (size_t)t * a.E + e);
+          ss = score_f<SCORE>(ls, st);
+        }
+        if (e < 0) {
+          unsure = true;
+        } else if (n >= 0) {                                            // nearer to the next one than the errors of both?
+          const float ln = load_logit(logits + (size_t)t * a.E + n), sn = score_f<SCORE>(ln, st);
+          const float be = a.bias ? a.bias[e] : 0.f, bn = a.bias ? a.bias[n] : 0.f;
+          const float ve = ls == -INFINITY ? kMaskedF : ss + be, vn = ln == -INFINITY ? kMaskedF : sn + bn;
+          const bool near = !(ve - vn > score_err<SCORE>(ls, ss, ve, st) + score_err<SCORE>(ln, sn, vn, st));
+          unsure |= near && !(ls == ln && be == bn);                    // (the same value: the lower index, which came first)
+        }
+      }
+      if (row_or_u32(unsure)) {
+        group_pick_f64<XT, P, SCORE>(a, logits + (size_t)t * a.E, sub, row_base, slot);
+        wave_lds_fence();
+        if (sub < a.k) {
+          e = slot[sub];
+          ss = score_f<SCORE>(load_logit(logits + (size_t)t * a.E + e), st);
+        }
+      }
+      // ---- gates ----
+      const float sum = row_sum_f32(sub < a.k ? ss : 0.f);
+      if (sub < a.k) {
+        a.gates[(size_t)t * a.k + sub] = a.renorm ? a.scale * (ss / (sum + 1e-20f)) : a.scale * ss;
+        a.topk_idx[(size_t)t * a.k + sub] = e;
+        s_idx[in_pass * a.k + sub] = e;
+      }
+    }
+    __syncthreads();
+    // ---- ranks of the pass' pairs among those of their expert: a wavefront takes 64 pairs ----
+    const int n_pairs = n_tok * a.k;
+    for (int r = wave; r < rounds; r += blockDim.x / kWave) {
+      const int p = r * kWave + lane;
+      const int e = p < n_pairs ? s_idx[p] : -1;
+      unsigned long long same = ~0ull;
+#pragma unroll
+      for (int b = 0; b < 9; ++b) {                                     // (-1 has all bits, no expert bit 8)
+        const unsigned long long set = __ballot(e >> b & 1);
+        same &= (e >> b & 1) ? set : ~set;
+      }
+      const int rank = __popcll(same & ((1ull << lane) - 1ull));
+      if (e >= 0) {
+        if (rank == 0) s_count[r][e] = (uint16_t)__popcll(same);
+        s_idx[p] = e | rank << 16;
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += blockDim.x) {               // counts -> pairs of the block in front of these 64
+      int n = s_base[e];
+      for (int r = 0; r < rounds; ++r) {
+        const int c = s_count[r][e];
+        s_count[r][e] = (uint16_t)(n - s_base[e]);
+        n += c;
+      }
+      s_off[e] = s_base[e];
+      s_base[e] = n;
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < n_pairs; p += blockDim.x) {
+      const int w = s_idx[p], e = w & 0xffff;
+      a.inv_pos[(size_t)t0 * a.k + p] = (w >> 16) + s_off[e] + s_count[p / kWave][e];    // the rank inside the block
+    }
+    __syncthreads();
+  }
+  if (gridDim.x > 1) {
+    for (int e = threadIdx.x; e < a.E; e += blockDim.x) a.hist[(size_t)blockIdx.x * a.E + e] = s_base[e];
+    return;
+  }
+  // one block: its counts are all there are
+  group_offsets(a, s_base, s_off, s_wave);
+  for (int p = threadIdx.x; p < a.T * a.k; p += blockDim.x) {           // (the same thread wrote inv_pos[p])
+    const int pos = s_off[a.topk_idx[p]] + a.inv_pos[p];
+    a.inv_pos[p] = pos;
+    a.perm[pos] = p;
+  }
+}
+
+constexpr int kScatterThreads = 1024;
+__global__ __launch_bounds__(kScatterThreads) void group_scatter_kernel(GroupRouteArgs a, int blocks) {
+  __shared__ int s_part[kScatterThreads], s_upto[kScatterThreads];
+  __shared__ int s_base[kGroupMaxExperts], s_off[kGroupMaxExperts], s_wave[kGroupMaxExperts / kWave];
+  // segment s of the blocks' counts for each of 256 experts
+  const int e = threadIdx.x % kGroupMaxExperts, seg = threadIdx.x / kGroupMaxExperts, segs = kScatterThreads / kGroupMaxExperts;
+  const int b0 = (int)((int64_t)seg * blocks / segs), b1 = (int)((int64_t)(seg + 1) * blocks / segs);
+  int all = 0, upto = 0;
+  if (e < a.E) {
+#pragma unroll 8
+    for (int b = b0; b < b1; ++b) {
+      const int c = a.hist[(size_t)b * a.E + e];
+      all += c;
+      upto += b < (int)blockIdx.x ? c : 0;
+    }
+  }
+  s_part[threadIdx.x] = all;
+  s_upto[threadIdx.x] = upto;
+  __syncthreads();
+  for (int x = threadIdx.x; x < a.E; x += blockDim.x) {
+    int n = 0;
+    for (int s = 0; s < segs; ++s) n += s_part[s * kGroupMaxExperts + x];
+    s_base[x] = n;
+  }
+  __syncthreads();
+  group_offsets(a, s_base, s_off, s_wave);                              // every block works them out, the first writes them
+  for (int x = threadIdx.x; x < a.E; x += blockDim.x)
+    for (int s = 0; s < segs; ++s) s_off[x] += s_upto[s * kGroupMaxExperts + x];
+  __syncthreads();
+  const size_t p0 = (size_t)blockIdx.x * a.tokens * a.k, p1 = min(p0 + (size_t)a.tokens * a.k, (size_t)a.T * a.k);
+  for (size_t p = p0 + threadIdx.x; p < p1; p += blockDim.x) {
+    const int pos = s_off[a.topk_idx[p]] + a.inv_pos[p];
+    a.inv_pos[p] = pos;
+    a.perm[pos] = (int32_t)p;
+  }
+}
+
+// ---- backward ----
+// dL/dlogits from dL/dgates (and dL/dscores), 16 lanes a token, four experts at a time a lane (vector) or one.  With
+//   w_j = s_{e_j},  g_j = scale w_j / Z,  Z = sum w + 1e-20:   dw_j = (scale dg_j - sum_i dg_i g_i) / Z      (or scale dg_j)
+//   ds = dscores + the dw at their experts;   sigmoid: dl = ds s (1 - s);   softmax: dl = s (ds - sum ds s)
+// Bound by what it reads and writes; a sigmoid router without dscores reads only the chosen logits.
+constexpr int kBwdThreads = 256, kBwdTokens = kBwdThreads / kLanes;
+__device__ __forceinline__ void store_grad4(float* p, const float* v) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void store_grad4(bf16_t* p, const float* v) {
+  *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+template <typename XT, int SCORE, bool DSCORES, bool VEC>
+__global__ __launch_bounds__(kBwdThreads) void group_route_bwd_kernel(GroupRouteBwdArgs a) {
+  constexpr int P = kGroupMaxExperts / kLanes, W = VEC ? 4 : 1;
+  __shared__ __attribute__((aligned(16))) float s_dw[kBwdTokens][kGroupMaxExperts];
+  const int lane = threadIdx.x & (kWave - 1), sub = lane & (kLanes - 1), in_block = threadIdx.x / kLanes;
+  const int t = blockIdx.x * kBwdTokens + in_block;
+  if (t >= a.T) return;                                                 // (whole rows of 16 lanes)
+  const XT* const logits = static_cast<const XT*>(a.logits) + (size_t)t * a.E;
+  constexpr bool ALL = SCORE == BTX_SCORE_SOFTMAX || DSCORES;           // every logit is needed
+  float* const dw = s_dw[in_block];
+#pragma unroll
+  for (int i = 0; i < P; i += W) {
+    const int e = (i / W * kLanes + sub) * W;
+    if (e < a.E) {
+#pragma unroll
+      for (int x = 0; x < W; ++x) dw[e + x] = 0.f;
+    }
+  }
+  float l[P];
+  RowStat st{0.f, 0.f};
+  if (ALL) {
+#pragma unroll
+    for (int i = 0; i < P; i += W) {
+      const int e = (i / W * kLanes + sub) * W;
+      if (e < a.E) {
+        if constexpr (VEC) load_logits4(logits + e, l + i);
+        else l[i] = load_logit(logits + e);
+      } else {
+#pragma unroll
+        for (int x = 0; x < W; ++x) l[i + x] = -INFINITY;
+      }
+    }
+  }
+  if (SCORE == BTX_SCORE_SOFTMAX) {
+    float m = l[0];
+#pragma unroll
+    for (int i = 1; i < P; ++i) m = fmaxf(m, l[i]);
+    st.m = row_max_f32(m);
+    if (st.m == -INFINITY) st.m = 0.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) sum += __expf(l[i] - st.m);
+    sum = row_sum_f32(sum);
+    st.inv = sum > 0.f ? 1.f / sum : 0.f;
+  }
+  int e = -1;
+  float w = 0.f, dg = 0.f, slope = 0.f;                                 // slot sub
+  if (sub < a.k) {
+    e = a.topk_idx[(size_t)t * a.k + sub];
+    dg = a.dgates[(size_t)t * a.k + sub];
+    if ((unsigned)e < (unsigned)a.E) {
+      const float x = load_logit(logits + e);
+      w = score_f<SCORE>(x, st);
+      const float z = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + z);
+      slope = z * r * r;                                                // s (1 - s), also where s rounds to 1
+    } else {
+      e = -1;
+    }
+  }
+  float d = a.scale * dg;
+  if (a.renorm) {
+    const float inv_z = 1.f / (row_sum_f32(w) + 1e-20f), mean = row_sum_f32(dg * (w * inv_z));
+    d = a.scale * (dg - mean) * inv_z;
+  }
+  wave_lds_fence();
+  if (e >= 0) dw[e] = SCORE == BTX_SCORE_SIGMOID && !DSCORES ? d * slope : d;
+  wave_lds_fence();
+  XT* const out = static_cast<XT*>(a.dlogits) + (size_t)t * a.E;
+  float ds[P];
+#pragma unroll
+  for (int i = 0; i < P; i += W) {
+    const int x0 = (i / W * kLanes + sub) * W;
+#pragma unroll
+    for (int x = 0; x < W; ++x) ds[i + x] = x0 < a.E ? dw[x0 + x] : 0.f;
+    if (DSCORES && x0 < a.E) {
+      if constexpr (VEC) {
+        const f32x4 q = *reinterpret_cast<const f32x4*>(a.dscores + (size_t)t * a.E + x0);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) ds[i + x] += q[x];
+      } else {
+        ds[i] += a.dscores[(size_t)t * a.E + x0];
+      }
+    }
+  }
+  float mean = 0.f;
+  if (SCORE == BTX_SCORE_SOFTMAX) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) mean += ds[i] * score_f<SCORE>(l[i], st);
+    mean = row_sum_f32(mean);
+  }
+#pragma unroll
+  for (int i = 0; i < P; i += W) {
+    const int x0 = (i / W * kLanes + sub) * W;
+    if (x0 >= a.E) continue;
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      if (SCORE == BTX_SCORE_SOFTMAX) {
+        ds[i + x] = score_f<SCORE>(l[i + x], st) * (ds[i + x] - mean);
+      } else if (DSCORES) {
+        const float z = __expf(-fabsf(l[i + x])), r = __builtin_amdgcn_rcpf(1.f + z);
+        ds[i + x] *= z * r * r;
+      }
+    }
+    if constexpr (VEC) store_grad4(out + x0, ds + i);
+    else Elem<XT>::st(out + x0, ds[i]);
+  }
+}
+
+// 16 lanes a pair
+__global__ __launch_bounds__(kBwdThreads) void gate_grads_kernel(const float* __restrict__ part, int n_part, const int32_t* __restrict__ inv_pos, int R,
+                                                                 float* __restrict__ dgates) {
+  const int sub = threadIdx.x & (kLanes - 1);
+  const int64_t p = (int64_t)blockIdx.x * kBwdTokens + threadIdx.x / kLanes;
+  if (p >= R) return;
+  const int r = inv_pos[p];
+  float sum = 0.f;
+  if (r >= 0)
+    for (int i = sub; i < n_part; i += kLanes) sum += part[(size_t)r * n_part + i];
+  sum = row_sum_f32(sum);
+  if (sub == 0) dgates[p] = sum;
+}
+
+}  // namespace
+
+int launch_gate_grads(const float* dg_part, int n_part, const int32_t* inv_pos, int R, float* dgates, hipStream_t s) {
+  gate_grads_kernel<<<ceil_div(R, kBwdTokens), kBwdThreads, 0, s>>>(dg_part, n_part, inv_pos, R, dgates);
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+
+// tokens of a workgroup: 64, or more where that would be over 512 workgroups, whose counts every workgroup of the second launch adds up
+static int block_tokens(int T) { return T <= 512 * kTokPass ? kTokPass : ceil_div(ceil_div(T, 512), kTokPass) * kTokPass; }
+
+size_t group_route_workspace_bytes(int T, int E) {
+  // (of the most workgroups that fewer tokens have: never less for more tokens)
+  return T > kTokPass ? (size_t)std::min(512, ceil_div(T, kTokPass)) * E * sizeof(int) : 0;
+}
+
+int launch_group_route(GroupRouteArgs a, hipStream_t s) {
+  a.per_group = a.E / a.G;
+  a.log2_lanes = 0;                                     // as many lanes a group as there are for the next power of two of groups
+  while (a.G << (a.log2_lanes + 1) <= kLanes) ++a.log2_lanes;
+  a.per_lane = ceil_div(a.per_group, 1 << a.log2_lanes);
+  a.tokens = block_tokens(a.T);
+  if (a.per_lane > 4 || a.per_group % 4 == 0) a.per_lane = (a.per_lane + 3) & ~3;   // whole vectors, where rows have them
+  const int lsize = a.dtype == BTX_BF16 ? 2 : 4;
+  a.vector = a.per_group % 4 == 0 && a.per_lane % 4 == 0 && ((uintptr_t)a.logits % (4 * lsize)) == 0 && ((uintptr_t)a.scores & 15) == 0;
+  const int blocks = ceil_div(a.T, a.tokens);
+  const int threads = std::min(kThreadsMost, ceil_div(std::min(a.T, a.tokens), kTokWave) * kWave);
+  auto go = [&](auto tag, auto per, auto score) {
+    group_select_kernel<decltype(tag), decltype(per)::value, decltype(score)::value><<<blocks, threads, 0, s>>>(a);
+  };
+  auto with_p = [&](auto tag, auto score) {
+    if (a.per_lane <= 4) go(tag, std::integral_constant<int, 4>{}, score);
+    else if (a.per_lane <= 8) go(tag, std::integral_constant<int, 8>{}, score);
+    else if (a.per_lane <= 16) go(tag, std::integral_constant<int, 16>{}, score);
+    else go(tag, std::integral_constant<int, 32>{}, score);
+  };
+  auto with_score = [&](auto tag) {
+    if (a.score_fn == BTX_SCORE_SIGMOID) with_p(tag, std::integral_constant<int, BTX_SCORE_SIGMOID>{});
+    else with_p(tag, std::integral_constant<int, BTX_SCORE_SOFTMAX>{});
+  };
+  if (a.dtype == BTX_BF16) with_score(bf16_t{});
+  else with_score(float{});
+  BTX_LAUNCH_CHECK();
+  if (blocks > 1) {
+    group_scatter_kernel<<<blocks, kScatterThreads, 0, s>>>(a, blocks);
+    BTX_LAUNCH_CHECK();
+  }
+  return BTX_OK;
+}
+
+int launch_group_route_bwd(const GroupRouteBwdArgs& a, hipStream_t s) {
+  const int lsize = a.dtype == BTX_BF16 ? 2 : 4, blocks = ceil_div(a.T, kBwdTokens);
+  const bool vec = a.E % 4 == 0 && (((uintptr_t)a.logits | (uintptr_t)a.dlogits) % (4 * lsize)) == 0 && ((uintptr_t)a.dscores & 15) == 0;
+  auto go = [&](auto tag, auto score) {
+    using XT = decltype(tag);
+    constexpr int SC = decltype(score)::value;
+    if (a.dscores) {
+      if (vec) group_route_bwd_kernel<XT, SC, true, true><<<blocks, kBwdThreads, 0, s>>>(a);
+      else group_route_bwd_kernel<XT, SC, true, false><<<blocks, kBwdThreads, 0, s>>>(a);
+    } else {
+      if (vec) group_route_bwd_kernel<XT, SC, false, true><<<blocks, kBwdThreads, 0, s>>>(a);
+      else group_route_bwd_kernel<XT, SC, false, false><<<blocks, kBwdThreads, 0, s>>>(a);
+    }
+  };
+  auto with_score = [&](auto tag) {
+    if (a.score_fn == BTX_SCORE_SIGMOID) go(tag, std::integral_constant<int, BTX_SCORE_SIGMOID>{});
+    else go(tag, std::integral_constant<int, BTX_SCORE_SOFTMAX>{});
+  };
+  if (a.dtype == BTX_BF16) with_score(bf16_t{});
+  else with_score(float{});
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+
+}  // namespace btx

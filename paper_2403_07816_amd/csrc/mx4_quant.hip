@@ -1,0 +1,199 @@
+// Tensors to microscaled 4-bit floats and back (layout: mx4.h).  Both directions are bound by the bytes they move: 2 (bf16) or 4 (fp32)
+// of an element on one side, 17/32 on the other.
+//   axis 1: blocks lie along the rows.  A thread has 8 consecutive elements, four threads a block: its largest magnitude by two DPP steps.
+//   axis 0: blocks run down the columns, as the expert weights [K, N] are quantised, whose products sum over K; rows of the result
+//           are the columns of the tensor.  A thread has the 32 elements of a block in two neighbouring columns, so the magnitude needs no other
+//           lane; 64 columns x 256 rows go through LDS, so that 128 consecutive bytes of a row of codes are written at once.
+#include "mx4.h"
+
+namespace btx {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---- axis 1: [rows, K] --------------------------------------------------------------------------------------
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const XT* __restrict__ x, int64_t rows, int64_t K, uint32_t* __restrict__ codes,
+                                                                 uint8_t* __restrict__ scales, int64_t pitch) {
+  // a row is cut into pieces of 8 elements, and rows are as long as their scales' pitch (whole 512 elements): what lies behind K
+  // only writes the zeros behind the scales
+  const int64_t per_row = pitch * 4, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t r = i / per_row;
+  if (r >= rows) return;                               // whole blocks of four threads
+  const int64_t p = i - r * per_row;
+  float v[8];
+  uint32_t amax = 0;
+  const bool inside = p * 8 < K;
+  if (inside) {
+    RowVec<XT, 8>::ld_stream(x + r * K + p * 8, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) amax = max(amax, magnitude(v[q]));
+  }
+  amax = max(amax, (uint32_t)dpp_i32<kDppXor1>((int)amax));
+  amax = max(amax, (uint32_t)dpp_i32<kDppXor2>((int)amax));
+  const uint32_t byte = mx4_scale_byte(amax);
+  if (inside) codes[r * (K / 8) + p] = byte == 255u ? 0u : mx4_codes8(v, mx4_scale(byte));
+  if ((threadIdx.x & 3) == 0) scales[r * pitch + p / 4] = inside ? (uint8_t)byte : 0;
+}
+
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows,
+                                                                   int64_t K, int64_t pitch, XT* __restrict__ out);
+
+// the value of code c
+__device__ __forceinline__ float code_value(uint32_t c) {
+  const uint32_t m = c & 7u;                            // 0 .5 1 1.5 2 3 4 6: an exponent of two bits and one of the mantissa
+  const float mag = m < 2u ? 0.5f * (float)m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
+  return (c & 8u) ? -mag : mag;
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte); }
+// the eight values of a word of codes; bf16: past its range (6 * 2^127 ...) or precision (below 2^-126) rounded once
+__device__ __forceinline__ void decode8(uint32_t w, float scale, float* v) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = code_value(w >> (4 * q) & 15u) * scale;
+}
+
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows,
+                                                                   int64_t K, int64_t pitch, XT* __restrict__ out) {
+  const int64_t per_row = K / 8, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t r = i / per_row;
+  if (r >= rows) return;
+  const int64_t p = i - r * per_row;
+  float v[8];
+  decode8(codes[i], scale_value(scales[r * pitch + p / 4]), v);
+  RowVec<XT, 8>::st_stream(out + r * K + p * 8, v);
+}
+
+// ---- axis 0: [batch, K, N] -> rows [batch, N] of K ------------------------------------------------------------
+constexpr int kCols = 64, kBlocks = 8;                  // columns, blocks of 32 rows of a workgroup: 32 threads x 8
+// grid: (pieces of 256 rows, pieces of 64 columns, batch)
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void quantize_cols_kernel(const XT* __restrict__ x, int64_t K, int64_t N, u32x4* __restrict__ codes,
+                                                                 uint8_t* __restrict__ scales, int64_t pitch) {
+  __shared__ u32x4 s_codes[kCols][kBlocks + 1];
+  __shared__ uint8_t s_scales[kCols][kBlocks];
+  const int c = (threadIdx.x & 31) * 2, b = threadIdx.x / 32;
+  const int64_t col = (int64_t)blockIdx.y * kCols + c, blk = (int64_t)blockIdx.x * kBlocks + b, n_blk = K / kMxBlock;
+  const int64_t batch = blockIdx.z;
+  x += batch * K * N;
+  if (blk < n_blk && col < N) {
+    const XT* from = x + blk * kMxBlock * N + col;
+    const bool both = col + 1 < N;
+    float v[2][kMxBlock];
+#pragma unroll
+    for (int q = 0; q < kMxBlock; ++q) {
+      v[0][q] = Elem<XT>::ld(from + (int64_t)q * N);
+      v[1][q] = both ? Elem<XT>::ld(from + (int64_t)q * N + 1) : 0.f;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t amax = 0;
+#pragma unroll
+      for (int q = 0; q < kMxBlock; ++q) amax = max(amax, magnitude(v[h][q]));
+      const uint32_t byte = mx4_scale_byte(amax);
+      const float scale = mx4_scale(byte);
+      u32x4 w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = byte == 255u ? 0u : mx4_codes8(v[h] + 8 * q, scale);
+      s_codes[c + h][b] = w;
+      s_scales[c + h][b] = (uint8_t)byte;
+    }
+  }
+  __syncthreads();
+  codes += batch * N * n_blk;
+  scales += batch * N * pitch;
+#pragma unroll
+  for (int i = threadIdx.x; i < kCols * kBlocks; i += kThreads) {
+    const int q = i % kBlocks;
+    const int64_t n = (int64_t)blockIdx.y * kCols + i / kBlocks, k = (int64_t)blockIdx.x * kBlocks + q;
+    if (n >= N) continue;
+    if (k < n_blk) codes[n * n_blk + k] = s_codes[i / kBlocks][q];
+    if (k < pitch) scales[n * pitch + k] = k < n_blk ? s_scales[i / kBlocks][q] : 0;
+  }
+}
+
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void dequantize_cols_kernel(const u32x4* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t K, int64_t N,
+                                                                   int64_t pitch, XT* __restrict__ out) {
+  __shared__ u32x4 s_codes[kCols][kBlocks + 1];
+  __shared__ uint8_t s_scales[kCols][kBlocks];
+  const int64_t n_blk = K / kMxBlock, batch = blockIdx.z;
+  codes += batch * N * n_blk;
+  scales += batch * N * pitch;
+#pragma unroll
+  for (int i = threadIdx.x; i < kCols * kBlocks; i += kThreads) {
+    const int q = i % kBlocks;
+    const int64_t n = (int64_t)blockIdx.y * kCols + i / kBlocks, k = (int64_t)blockIdx.x * kBlocks + q;
+    if (n < N && k < n_blk) {
+      s_codes[i / kBlocks][q] = codes[n * n_blk + k];
+      s_scales[i / kBlocks][q] = scales[n * pitch + k];
+    }
+  }
+  __syncthreads();
+  const int c = (threadIdx.x & 31) * 2, b = threadIdx.x / 32;
+  const int64_t col = (int64_t)blockIdx.y * kCols + c, blk = (int64_t)blockIdx.x * kBlocks + b;
+  if (blk >= n_blk || col >= N) return;
+  const bool both = col + 1 < N;
+  XT* to = out + batch * K * N + blk * kMxBlock * N + col;
+  const float sc[2] = {scale_value(s_scales[c][b]), both ? scale_value(s_scales[c + 1][b]) : 0.f};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float v[2][8];
+    decode8(s_codes[c][b][q], sc[0], v[0]);
+    decode8(both ? s_codes[c + 1][b][q] : 0u, sc[1], v[1]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      Elem<XT>::st(to + (int64_t)(8 * q + j) * N, v[0][j]);
+      if (both) Elem<XT>::st(to + (int64_t)(8 * q + j) * N + 1, v[1][j]);
+    }
+  }
+}
+
+}  // namespace
+
+int launch_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, uint8_t* codes, uint8_t* scales,
+                        hipStream_t s) {
+  const int64_t K = axis == 1 ? cols : rows, pitch = mx4_pitch(K);
+  if (axis == 1) {
+    const int64_t n = batch * rows, blocks = (n * pitch * 4 + kThreads - 1) / kThreads;
+    if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
+    if (dtype == BTX_BF16)
+      quantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(static_cast<const bf16_t*>(x), n, K, reinterpret_cast<uint32_t*>(codes), scales, pitch);
+    else
+      quantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(static_cast<const float*>(x), n, K, reinterpret_cast<uint32_t*>(codes), scales, pitch);
+  } else {
+    const int64_t gx = (pitch + kBlocks - 1) / kBlocks, gy = (cols + kCols - 1) / kCols;
+    if (!grid_fits(gx, kThreads) || gy > 65535 || batch > 65535) return BTX_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)gx, (unsigned)gy, (unsigned)batch);
+    if (dtype == BTX_BF16)
+      quantize_cols_kernel<<<grid, kThreads, 0, s>>>(static_cast<const bf16_t*>(x), K, cols, reinterpret_cast<u32x4*>(codes), scales, pitch);
+    else
+      quantize_cols_kernel<<<grid, kThreads, 0, s>>>(static_cast<const float*>(x), K, cols, reinterpret_cast<u32x4*>(codes), scales, pitch);
+  }
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+
+int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, void* out,
+                          hipStream_t s) {
+  const int64_t K = axis == 1 ? cols : rows, pitch = mx4_pitch(K);
+  if (axis == 1) {
+    const int64_t n = batch * rows, blocks = (n * (K / 8) + kThreads - 1) / kThreads;
+    if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
+    const uint32_t* const c = reinterpret_cast<const uint32_t*>(codes);
+    if (dtype == BTX_BF16) dequantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(c, scales, n, K, pitch, static_cast<bf16_t*>(out));
+    else dequantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(c, scales, n, K, pitch, static_cast<float*>(out));
+  } else {
+    const int64_t gx = (K / kMxBlock + kBlocks - 1) / kBlocks, gy = (cols + kCols - 1) / kCols;
+    if (!grid_fits(gx, kThreads) || gy > 65535 || batch > 65535) return BTX_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)gx, (unsigned)gy, (unsigned)batch);
+    const u32x4* const c = reinterpret_cast<const u32x4*>(codes);
+    if (dtype == BTX_BF16) dequantize_cols_kernel<<<grid, kThreads, 0, s>>>(c, scales, K, cols, pitch, static_cast<bf16_t*>(out));
+    else dequantize_cols_kernel<<<grid, kThreads, 0, s>>>(c, scales, K, cols, pitch, static_cast<float*>(out));
+  }
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+
+}  // namespace btx
