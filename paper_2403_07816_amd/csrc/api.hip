@@ -197,6 +197,7 @@ int btx_moe_route(const void* x, int x_dtype, const float* W_router, const float
 int btx_init(void) {
   void* p = nullptr;
   if (int rc = static_scratch(&p)) return rc;   // also looks up this device's copy of the fixed workspace
+  if (int rc = mx4_prepare()) return rc;
   return ff_prepare();
 }
 

@@ -36,6 +36,7 @@ int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype
                           hipStream_t s);
 
 // The layer of 4-bit experts (mx4_gemm.hip)
+int mx4_prepare();                     // one-time set-up on the current device (not capturable)
 struct Mx4Shapes { int T, d, f, E, k; };
 struct Mx4Matrix { const uint8_t* codes; const uint8_t* scales; };
 // act = silu(xq W1) * (xq W3), quantised along f: rows in grouped order, xq's rows found by perm
