@@ -493,8 +493,8 @@ bool mx4_shapes_ok(int T, int d, int f, int E, int k) {
          (int64_t)T * k < (int64_t)1 << 31 && (int64_t)T * k * (int64_t)(d > f ? d : f) < (int64_t)1 << 40 &&
          (int64_t)E * d * f < (int64_t)1 << 40;
 }
-struct Mx4Ws { uint8_t *x_codes, *x_scales, *act_codes, *act_scales; void* y; size_t bytes; };
-Mx4Ws carve_mx4(void* ws, int T, int d, int f, int k) {
+struct Mx4Ws { uint8_t *x_codes, *x_scales, *act_codes, *act_scales; int32_t* tokens; TileInfo* tiles; void* y; size_t bytes; };
+Mx4Ws carve_mx4(void* ws, int T, int d, int f, int E, int k) {
   const size_t R = (size_t)T * k;
   Carver c(ws);
   Mx4Ws w;
@@ -502,6 +502,8 @@ Mx4Ws carve_mx4(void* ws, int T, int d, int f, int k) {
   w.x_scales = static_cast<uint8_t*>(c.take((size_t)T * mx4_pitch(d)));
   w.act_codes = static_cast<uint8_t*>(c.take(R * (f / 2)));
   w.act_scales = static_cast<uint8_t*>(c.take(R * mx4_pitch(f)));
+  w.tokens = static_cast<int32_t*>(c.take(R * sizeof(int32_t)));
+  w.tiles = static_cast<TileInfo*>(c.take((1 + (size_t)mx4_most_tiles((int)R, E)) * sizeof(TileInfo)));
   w.y = c.take(R * d * 2);
   w.bytes = c.used;
   return w;
@@ -510,7 +512,7 @@ Mx4Ws carve_mx4(void* ws, int T, int d, int f, int k) {
 
 size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k) {
   if (!mx4_shapes_ok(T, d, f, E, k) || T == 0) return 0;
-  return carve_mx4(nullptr, T, d, f, k).bytes;
+  return carve_mx4(nullptr, T, d, f, E, k).bytes;
 }
 
 int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t* W1_scales, const uint8_t* W3_codes, const uint8_t* W3_scales,
@@ -523,14 +525,14 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
       !workspace)
     return BTX_ERR_INVALID_ARG;
   if (!aligned16(x, W1_codes, W1_scales, W3_codes, W3_scales, W2_codes, W2_scales, residual, out, workspace)) return BTX_ERR_INVALID_ARG;
-  const Mx4Ws w = carve_mx4(workspace, T, d, f, k);
+  const Mx4Ws w = carve_mx4(workspace, T, d, f, E, k);
   if (workspace_bytes < w.bytes) return BTX_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Mx4Shapes sh{T, d, f, E, k};
-  BTX_STAGE(BTX_STAGE_GATHER_X, launch_mx4_quantize(x, BTX_BF16, 1, T, d, 1, w.x_codes, w.x_scales, s));
-  BTX_STAGE(BTX_STAGE_UP, launch_mx4_up({w.x_codes, w.x_scales}, {W1_codes, W1_scales}, {W3_codes, W3_scales}, offsets, perm, sh, w.act_codes,
-                                        w.act_scales, s));
-  BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down({w.act_codes, w.act_scales}, {W2_codes, W2_scales}, offsets, sh, w.y, s));
+  const Mx4Layer l{{w.x_codes, w.x_scales}, w.tokens, w.tiles, w.act_codes, w.act_scales, w.y};
+  BTX_STAGE(BTX_STAGE_GATHER_X, launch_mx4_begin(x, perm, offsets, sh, w.x_codes, w.x_scales, w.tokens, w.tiles, s));
+  BTX_STAGE(BTX_STAGE_UP, launch_mx4_up(l, {W1_codes, W1_scales}, {W3_codes, W3_scales}, offsets, sh, s));
+  BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down(l, {W2_codes, W2_scales}, offsets, sh, s));
   BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, nullptr, 1, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
   return BTX_OK;
 }

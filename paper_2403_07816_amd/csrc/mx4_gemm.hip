@@ -14,17 +14,21 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// one step of K = 128; S: which byte of the scale words
-template <int S> __device__ __forceinline__ f32x4 mfma_mx4(const u32x4& w, const u32x4& x, const f32x4& acc, uint32_t w_scale, uint32_t x_scale) {
+// one step of K = 128; SW, SX: which byte of the scale words
+template <int SW, int SX = SW> __device__ __forceinline__ f32x4 mfma_mx4(const u32x4& w, const u32x4& x, const f32x4& acc, uint32_t w_scale, uint32_t x_scale) {
   const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}, b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, S, (int)w_scale, S, (int)x_scale);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, SW, (int)w_scale, SX, (int)x_scale);
 }
 
 struct Mx4Args {
   Mx4Matrix a, b0, b1;                  // token rows; weights (b1: W3)
-  const int32_t* offsets; const int32_t* perm; int k;   // perm: row r of the product is row perm[r] / k of a (NULL: row r)
-  int E, N, K;                          // columns, depth
+  const int32_t* offsets; int E;
+  const int32_t* tokens;                // row r of the product is row tokens[r] of a (NULL: row r)
+  const TileInfo* tiles;                // row tiles (tile kernel): the first entry's row0 is their number
+  int a_rows;                           // of a (tile kernel: their scales' order, see mx4_scale_at())
+  int N, K;                             // columns, depth
   uint8_t* act_codes; uint8_t* act_scales; bf16_t* y;
+  int R;
 };
 
 // Row tiles of up to 256 experts (RowTiles has 64): lane x looks at experts 4x .. 4x + 3
@@ -82,7 +86,7 @@ __global__ __launch_bounds__(NW* kWave) void mx4_few_kernel(Mx4Args g) {
   const int n_blk = g.K / kMxBlock;
   const int64_t pitch = mx4_pitch(g.K);
   int64_t row = min(row0 + r, row_end - 1);
-  if (g.perm) row = g.perm[row] / g.k;
+  if (g.tokens) row = g.tokens[row];
   const u32x4* const a = reinterpret_cast<const u32x4*>(g.a.codes) + row * n_blk;
   const uint8_t* const a_sc = g.a.scales + row * pitch;
   const u32x4* w[PANELS * 2];
@@ -167,12 +171,15 @@ template <bool UP> int launch_few(const Mx4Args& g, int R, hipStream_t s) {
 // ---- many rows: 256 x 256 tiles --------------------------------------------------------------------------------
 // Bound by the matrix cores and by what feeds them from LDS.  A tile is [row][128 bytes] per operand and k tile (256 elements), 8 wavefronts
 // have 128 x 64 of the result each (UP: 32 columns of either panel, one block of the activations), 128 accumulator registers.
-//   * global -> LDS copies are direct, 16 bytes a lane; two stages of both operands (128 KB), and two of the scales, which come for two
-//     k tiles at a time: 16 bytes a row (2 x 8 KB).
+//   * global -> LDS copies are direct, 16 bytes a lane, two stages of both operands (128 KB).
 //   * 16-byte chunks are XOR-swizzled by row (by choosing which chunk a lane fetches), so that the 16 rows of a fragment read meet no
-//     bank twice.  Step s of a k tile takes chunks 2g + s of lane group g: the two scales that a lane needs of a row are neighbours.
-//   * The two wavefronts of a SIMD alternate between a memory phase (fragment reads of half a k tile) and a compute phase (32 products),
-//     half a period apart, with a barrier at every boundary; the copies of the next k tile are issued in the first memory phase.
+//     bank twice.  Step s of a k tile takes chunk 2g + s of lane group g.
+//   * The two wavefronts of a SIMD alternate between a memory phase and a compute phase (32 products), half a period apart, with a barrier at
+//     every boundary.  The first memory phase of a k tile reads all fragments of B and those of half of A's rows, the second the other
+//     half's: B's stage and half of A's are free half a k tile early, and the copies of the k tile after the next go there.
+//   * Scales: a lane's two of B for a k tile are neighbours and read as 16 bits.  A's, which only these kernels read, lie in an order
+//     (mx4_scale_at()) in which the four of two k tiles are one word, and 16 bytes of every row for two k tiles beside each other.  (With
+//     A's like B's, 12 words a lane and two k tiles dealt out by v_permlane32_swap and v_perm, the products of a k tile waited 260 cycles for it.)
 //   * Tiles are dealt so that the ones an XCD runs at a time share row and column panels in its L2.
 __device__ __forceinline__ void copy16(uint64_t base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory");
@@ -186,6 +193,14 @@ __device__ __forceinline__ void copy64(uint64_t base, const uint32_t (&off)[4], 
       :
       : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3])
       : "memory");
+}
+
+constexpr uint32_t kCopyBias2 = 1024;
+__device__ __forceinline__ void copy32(uint64_t base, uint32_t off0, uint32_t off1, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024"
+               :
+               : "s"(lds), "s"(base), "v"(off0), "v"(off1)
+               : "memory");
 }
 
 constexpr int kSup = 16, kXcdRows = 4, kXcds = 8;       // supertile of 16 x 16 tiles; of it an XCD has 4 x 8
@@ -215,9 +230,25 @@ __device__ __forceinline__ bool tile_of(int id, int n_rt, int n_ct, int& tm, int
 }
 
 constexpr int kTileRows = 256, kTileCols = 256, kTileWaves = 8, kTileK = 256;   // (UP: 128 columns of W1, 128 of W3)
-constexpr uint32_t kStage = 32768, kScaleStage = 8192;
-constexpr uint32_t kB0 = 2 * kStage, kScale0 = 4 * kStage;
-constexpr int kTileLds = 4 * kStage + 2 * kScaleStage;
+constexpr uint32_t kStage = 32768, kScaleAStage = 4096, kScaleBStage = 8192;   // scales: of 2 (A) and 4 (B) k tiles
+constexpr uint32_t kB0 = 2 * kStage, kScaleA0 = 4 * kStage, kScaleB0 = kScaleA0 + 2 * kScaleAStage;
+constexpr int kTileLds = kScaleB0 + 2 * kScaleBStage;
+constexpr int kTileGrid = 256;                          // compute units; a multiple of kXcds
+
+// Chunk c of a row lies at chunk c ^ tile_swz(row).  A 16-byte read of 64 lanes takes four passes, of lanes 0-3, 12-15 and 20-27, of 4-11, 16-19 and
+// 28-31, and so on; with chunks 2g of lane group g, (row >> 1) & 7 alone put 0-3 and 12-15 in the banks of 20-27 (16384 tokens of the
+// 7B-shaped layer 2.60 / 2.45 ms).
+__device__ __forceinline__ int tile_swz(int row) {
+  const int i = (row >> 1) & 7;
+  return i ^ ((i & 2) << 1);
+}
+
+// the same number, worked on where it is used: what follows from a lane's index for a tile's begin and end is not kept in registers over
+// its k loop (spilt registers are read back behind all copies and stores on their way: 18 us a tile)
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
 template <bool UP>
 __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args g, int n_ct) {
@@ -226,220 +257,341 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave >> 2, wn = wave & 3, grp = wm;     // the wavefronts of a SIMD are w and w + 4
-  int e, row0, row_end, tn;
-  {
-    const ManyRowTiles tiles(g.offsets, g.E, kTileRows, lane);
-    int tm;
-    if (!tile_of(blockIdx.x, tiles.count(), n_ct, tm, tn) || tm >= tiles.count()) return;
-    tiles.find(tm, e, row0, row_end);
-  }
-  const int col0 = tn * COLS;
   const int n_blk = g.K / kMxBlock, nk = (g.K + kTileK - 1) / kTileK, tail = n_blk - (nk - 1) * 8;   // blocks of the last k tile
   const int64_t pitch = mx4_pitch(g.K), row_bytes = g.K / 2;
-
-  // ---- copies: wavefront w has rows 32 w .. of either operand, 8 lanes a row, 8 rows an instruction
-  uint32_t a_off[4], b_off[4];
-  int chunk[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int row = wave * 32 + q * 8 + lane / 8;
-    chunk[q] = (lane & 7) ^ ((row >> 1) & 7);
-    const int gr = min(row0 + row, row_end - 1);
-    const uint32_t a_row = g.perm ? (uint32_t)(g.perm[gr] / g.k) : (uint32_t)(gr - row0);
-    a_off[q] = a_row * (uint32_t)row_bytes + chunk[q] * 16 + (kCopyBias4 - 1024 * q);
-    const int col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
-    b_off[q] = (uint32_t)col * (uint32_t)row_bytes + chunk[q] * 16 + (kCopyBias4 - 1024 * q);
-  }
-  const Mx4Matrix& bm = UP && wave >= 4 ? g.b1 : g.b0;
-  uint64_t a_from = uniform64(g.a.codes + (g.perm ? 0 : (int64_t)row0 * row_bytes)) - kCopyBias4;
-  uint64_t b_from = uniform64(bm.codes + ((int64_t)e * g.N + col0) * row_bytes) - kCopyBias4;
-  // scales: row 64 w + lane of A's 256 rows and B's 256 columns
-  uint64_t s_from;
-  uint32_t s_off;
-  {
-    const int row = (wave & 3) * 64 + lane;
-    if (wave < 4) {
-      const int gr = min(row0 + row, row_end - 1);
-      s_off = (uint32_t)(g.perm ? g.perm[gr] / g.k : gr - row0) * (uint32_t)pitch;
-      s_from = uniform64(g.a.scales + (g.perm ? 0 : (int64_t)row0 * pitch));
-    } else {
-      const int col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
-      s_off = (uint32_t)col * (uint32_t)pitch;
-      const Mx4Matrix& m = UP && wave >= 6 ? g.b1 : g.b0;
-      s_from = uniform64(m.scales + ((int64_t)e * g.N + col0) * pitch);
-    }
-  }
+  const int quads = (nk + 3) / 4;                        // pieces of 32 bytes in a row's scales
   const uint32_t base = (uint32_t)(uintptr_t)smem;
-  uint32_t to = base + wave * 4096;                      // of A; B's is kB0 behind
-  const uint32_t s_to = base + kScale0 + wave * 1024;
-  auto copy_scales = [&](int pair) { copy16(s_from + (uint64_t)pair * 16, s_off, s_to + (pair & 1) * kScaleStage); };
-  auto copy_tile = [&](bool last) {                      // last: chunks behind K are re-pointed at the row's first of this tile
-    uint32_t ao[4], bo[4];
+
+  // ---- the tile
+  const int n_rt = g.tiles[0].row0, most = n_rt * n_ct + kXcds;
+  int e, row0, row_end, col0, id = blockIdx.x;
+  auto find_tile = [&]() -> bool {                       // `id`, or the next one of this workgroup that names a tile
+    int tm, tn;
+    for (; id < most; id += gridDim.x)
+      if (tile_of(id, n_rt, n_ct, tm, tn)) {
+        const TileInfo t = g.tiles[1 + tm];
+        e = t.e;
+        row0 = t.row0;
+        row_end = t.row_end;
+        col0 = tn * COLS;
+        return true;
+      }
+    return false;
+  };
+
+  // ---- copies.  Rows 0-63 and 128-191 of A are its first half (A0), which the first memory phase reads, the others the second (A1): a
+  // wavefront has 16 rows of either and 32 rows of B, 8 lanes a row, 8 rows an instruction; 64 rows of A's scales, or of B's (2 lanes a row).
+  auto chunk = [](int ln, int q) { return (ln & 7) ^ tile_swz(ln / 8 + 8 * (q & 1)); };
+  auto s_half = [](int ln) { return (ln & 1) ^ (ln >> 4 & 1); };   // the halves of rows 8 .. 15 of 16 change places (banks)
+  const int a_row = wm * 128 + wn * 16;
+  uint32_t a_off[4], b_off[4], s_off[2];                 // a_off: A0, A0, A1, A1
+  uint64_t a_from, b_from, s_from;                       // a, b: of the k tile behind the next (A1: the one before)
+  auto set_rows = [&] {                                  // (as indexes of rows, for now)
+    const int ln = here(lane);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const uint32_t back = last && chunk[q] >= tail ? chunk[q] * 16 : 0;
-      ao[q] = a_off[q] - back;
-      bo[q] = b_off[q] - back;
+      const int gr = min(row0 + a_row + (q >> 1) * 64 + (q & 1) * 8 + ln / 8, row_end - 1);
+      a_off[q] = (uint32_t)(g.tokens ? g.tokens[gr] : gr - row0);
     }
-    copy64(a_from, ao, to);
-    copy64(b_from, bo, to + kB0);
+    if (wm == 0) {
+      const int gr = min(row0 + wn * 64 + ln, row_end - 1);
+      s_off[0] = (uint32_t)(g.tokens ? g.tokens[gr] : gr - row0);
+    }
   };
-  auto next_tile = [&] {
-    a_from += kTileK / 2;
-    b_from += kTileK / 2;
-    to ^= kStage;                                        // (LDS of the launch starts at a multiple of two stages)
+  const uint32_t s_step = wm == 0 ? (uint32_t)g.a_rows * 16 : 32;     // to the scales of the next two k tiles (B: four)
+  auto set_sources = [&] {
+    const int ln = here(lane);
+    // (asm: one register for each of these for the whole loop, not the pair that their 64-bit products are in)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      a_off[q] = a_off[q] * (uint32_t)row_bytes + chunk(ln, q) * 16 + (kCopyBias2 - 1024 * (q & 1));
+      const int row = wave * 32 + q * 8 + ln / 8, col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
+      b_off[q] = (uint32_t)col * (uint32_t)row_bytes + chunk(ln, q) * 16 + (kCopyBias4 - 1024 * q);
+      asm volatile("" : "+v"(a_off[q]), "+v"(b_off[q]));
+    }
+    const Mx4Matrix& bm = UP && wave >= 4 ? g.b1 : g.b0;
+    a_from = uniform64(g.a.codes + (g.tokens ? 0 : (int64_t)row0 * row_bytes)) - kCopyBias2;
+    b_from = uniform64(bm.codes + ((int64_t)e * g.N + col0) * row_bytes) - kCopyBias4;
+    if (wm == 0) {
+      s_off[0] *= 16;
+      s_off[1] = 0;
+      s_from = uniform64(g.a.scales + (g.tokens ? 0 : (int64_t)row0 * 16));
+    } else {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int row = wn * 64 + q * 32 + ln / 2, col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
+        s_off[q] = (uint32_t)col * (uint32_t)pitch + s_half(ln) * 16;
+      }
+      s_from = uniform64((UP && wn >= 2 ? g.b1 : g.b0).scales + ((int64_t)e * g.N + col0) * pitch);
+    }
+    asm volatile("" : "+v"(s_off[0]), "+v"(s_off[1]));
+  };
+  const uint32_t to_a = base + a_row * 128, to_b = base + kB0 + wave * 4096;
+  const uint32_t to_s = base + (wm == 0 ? kScaleA0 + wn * 1024 : kScaleB0 + wn * 2048);
+  // the last k tile's chunks behind K are re-pointed at the row's first of that tile
+  auto back = [&](int ln, int q) -> uint32_t { return chunk(ln, q) >= tail ? chunk(ln, q) * 16 : 0; };
+  auto copy_a0b = [&](int kt) {                          // a_from, b_from: of k tile kt
+    if (kt + 1 == nk && tail < 8) {
+      const int ln = here(lane);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q < 2) a_off[q] -= back(ln, q);
+        b_off[q] -= back(ln, q);
+      }
+    }
+    copy32(a_from, a_off[0], a_off[1], to_a + (kt & 1) * kStage);
+    copy64(b_from, b_off, to_b + (kt & 1) * kStage);
+  };
+  auto copy_a1 = [&](int kt, uint64_t from) {
+    if (kt + 1 == nk && tail < 8) {
+      const int ln = here(lane);
+      a_off[2] -= back(ln, 2);
+      a_off[3] -= back(ln, 3);
+    }
+    copy32(from, a_off[2], a_off[3], to_a + (kt & 1) * kStage + 64 * 128);
+  };
+  // One instruction for every two k tiles: A's scales of k tiles 2 pair, 2 pair + 1 (the wavefronts of wm 0), and of B's for four k tiles one half of
+  // the rows.  (Behind the last ones: anything.  A row of B's may end in the middle of its last 32 bytes.)
+  auto copy_scales_a = [&](int pair) {
+    copy16(s_from + (uint64_t)min(pair, (nk - 1) / 2) * s_step, s_off[0], to_s + (pair & 1) * kScaleAStage);
+  };
+  auto copy_scales_b = [&](int quad, int q) {
+    const int from = min(quad, (nk - 1) / 4);
+    const uint32_t less = from * 32 + 16 >= (int)pitch ? s_half(here(lane)) * 16 : 0;
+    copy16(s_from + (uint64_t)from * 32, (q ? s_off[1] : s_off[0]) - less, to_s + (quad & 1) * kScaleBStage + q * 1024);
   };
 
-  // ---- fragments: lane l has row l % 16 and chunks 2 (l / 16) + step
+  // ---- fragments: lane l has row l % 16
   const int r = lane & 15, lg = lane >> 4;
   typedef const __attribute__((address_space(3))) u32x4* lds_frag;
   typedef const __attribute__((address_space(3))) uint32_t* lds_word;
-  uint32_t at_a = base + (wm * 128 + r) * 128 + (((2 * lg) ^ ((r >> 1) & 7)) << 4);
-  uint32_t at_b = base + kB0 + (wn * (TNH * 16) + r) * 128 + (((2 * lg) ^ ((r >> 1) & 7)) << 4);
-  const uint32_t sc_a = base + kScale0 + (wm * 128 + r) * 16 + 4 * (lg >> 1);
-  const uint32_t sc_b = base + kScale0 + (256 + wn * (TNH * 16) + r) * 16 + 4 * (lg >> 1);
-  const uint32_t sc_shift = 16 * (lg & 1);
-  f32x4 acc[TM][TN] = {};
-  u32x4 fa[TM], fb[TN];
+  typedef const __attribute__((address_space(3))) uint16_t* lds_half;
+  const uint32_t at_a = base + (wm * 128 + r) * 128 + ((2 * lg) ^ tile_swz(r)) * 16;
+  const uint32_t at_b = base + kB0 + (wn * (TNH * 16) + r) * 128 + ((2 * lg) ^ tile_swz(r)) * 16;
+  const uint32_t sc_a = base + kScaleA0 + (wm * 128 + r) * 16 + 4 * lg;
+  const uint32_t sc_b = base + kScaleB0 + (wn * (TNH * 16) + r) * 32 + 2 * lg;
+  const uint32_t sc_half = (r >> 3) * 16;                // where the first half of a row of B's is
+  f32x4 acc[TM][TN];
+  u32x4 fa[TM / 2][2], fb[TN][2];                        // (of one half of A)
   uint32_t xa[TM], xb[TN];
-  auto read_frags = [&](int step) {
-    const uint32_t a = at_a ^ (step << 4), b = at_b ^ (step << 4);
+  auto read_a = [&](int stage, int half) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) fa[i] = *(lds_frag)(uintptr_t)(a + i * 2048);
+    for (int i = 0; i < TM / 2; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j] = *(lds_frag)(uintptr_t)(b + (j / TNH) * (128 * 128) + (j % TNH) * 2048);
+      for (int st = 0; st < 2; ++st) fa[i][st] = *(lds_frag)(uintptr_t)((at_a ^ (st << 4)) + stage * kStage + (half * 4 + i) * 2048);
   };
-  auto read_scales = [&](int kt) {
-    const uint32_t where = ((kt >> 1) & 1) * kScaleStage + (kt & 1) * 8;
+  auto read_b = [&](int stage) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) xa[i] = *(lds_word)(uintptr_t)(sc_a + where + i * 256);
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) xb[j] = *(lds_word)(uintptr_t)(sc_b + where + (j / TNH) * 2048 + (j % TNH) * 256);
+      for (int st = 0; st < 2; ++st)
+        fb[j][st] = *(lds_frag)(uintptr_t)((at_b ^ (st << 4)) + stage * kStage + (j / TNH) * (128 * 128) + (j % TNH) * 2048);
   };
-  auto k_tile = [&](auto fast_tag, int kt) {
-    constexpr bool fast = decltype(fast_tag)::value;
+  auto read_scales = [&](int kt, bool a) {
+    if (a) {                                             // kt even: of it and the next
+      const uint32_t at = sc_a + ((kt >> 1) & 1) * kScaleAStage;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) xa[i] = *(lds_word)(uintptr_t)(at + i * 256);
+    }
+    const uint32_t at = sc_b + ((kt >> 2) & 1) * kScaleBStage + (sc_half ^ ((kt & 2) << 3)) + (kt & 1) * 8;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) xb[j] = *(lds_half)(uintptr_t)(at + (j / TNH) * 4096 + (j % TNH) * 512);
+  };
+  // Copies: in the first memory phase of k tile kt A1 of kt + 1 (2 instructions), in the second A0 and B of kt + 2 (2 and 4) and in odd ones one of
+  // scales.  What they overwrite was read last in the memory phases before, and they have four phases or more to land.
+  auto k_tile = [&](auto odd_tag, int kt) {
+    constexpr int odd = decltype(odd_tag)::value;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (h == 0 && (fast || kt + 1 < nk)) {
-        next_tile();
-        copy_tile(!fast && kt + 2 == nk);
-        if (kt & 1) copy_scales((kt + 1) >> 1);
+      // ---- memory phase
+      read_a(odd, h);
+      if (h == 0) {
+        read_b(odd);
+        read_scales(kt, !odd);
+        if (kt + 1 < nk) copy_a1(kt + 1, a_from - kTileK / 2);
+      } else {
+        if (kt + 2 < nk) {
+          copy_a0b(kt + 2);
+          a_from += kTileK / 2;
+          b_from += kTileK / 2;
+          if (odd) {
+            if (wm == 0) copy_scales_a((kt + 1) / 2 + 1);
+            else copy_scales_b(((kt + 1) >> 2) + 1, kt & 2 ? 0 : 1);
+          }
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      read_frags(h);
-      if (h == 0) read_scales(kt);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_waitcnt(0xC07F);                // lgkmcnt(0)
-      if (h == 0) {
+      if (kt + 1 == nk && tail < 8) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) xa[i] >>= sc_shift;
+        for (int st = 0; st < 2; ++st) {
+          const uint32_t keep = 2 * (here(lane) >> 4) + st < tail ? ~0u : 0u;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) xb[j] >>= sc_shift;
+          for (int i = 0; i < TM / 2; ++i) fa[i][st] &= keep;
+        }
       }
-      if (!fast && kt + 1 == nk && 2 * lg + h >= tail) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fa[i] = u32x4{0u, 0u, 0u, 0u};
-      }
-      if (h == 1 && grp == 1) wait_vmcnt<0>();
+      // What the next memory phases read has landed: behind h == 0, A1 of this k tile; behind h == 1, A0, B and scales of the next.  What has
+      // been issued since may be outstanding.
+      auto landed = [&] {
+        if (h == 0) {
+          if (kt + 1 < nk) wait_vmcnt<9 - odd>(); else wait_vmcnt<0>();
+        } else {
+          if (kt + 2 < nk) wait_vmcnt<8 + odd>(); else wait_vmcnt<2>();
+        }
+      };
+      if (grp == 1) landed();
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
+      // ---- compute phase
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = h == 0 ? mfma_mx4<0>(fb[j], fa[i], acc[i][j], xb[j], xa[i]) : mfma_mx4<1>(fb[j], fa[i], acc[i][j], xb[j], xa[i]);
-      if (h == 1 && grp == 0) wait_vmcnt<0>();
-      if (h == 1) {
-        at_a ^= kStage;
-        at_b ^= kStage;
-      }
+        for (int i = 0; i < TM / 2; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            f32x4& c = acc[h * 4 + i][j];
+            c = st == 0 ? mfma_mx4<0, 2 * odd>(fb[j][0], fa[i][0], c, xb[j], xa[h * 4 + i])
+                        : mfma_mx4<1, 2 * odd + 1>(fb[j][1], fa[i][1], c, xb[j], xa[h * 4 + i]);
+          }
+#pragma unroll
+      for (int i = 0; i < TM / 2; ++i)                   // here, and not where the sums are needed next: behind the next phases' barriers
+#pragma unroll
+        for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(acc[h * 4 + i][j]));
+      if (grp == 0) landed();
       __builtin_amdgcn_sched_barrier(0);
-      if (fast || !(grp == 1 && h == 1 && kt + 1 == nk)) __builtin_amdgcn_s_barrier();
+      if (!(grp == 1 && h == 1 && kt + 1 == nk)) __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  copy_tile(nk == 1);
-  copy_scales(0);
-  wait_vmcnt<0>();
-  __builtin_amdgcn_s_barrier();
-  if (grp == 1) __builtin_amdgcn_s_barrier();            // group 1 is a phase behind
-  int kt = 0;
-#pragma unroll 1
-  for (; kt < nk - 2; ++kt) k_tile(std::true_type{}, kt);
-#pragma unroll 1
-  for (; kt < nk; ++kt) k_tile(std::false_type{}, kt);
 
-  // ---- epilogue: acc[i][j][v] is row wm 128 + 16 i + l % 16, column 16 j + 4 (l / 16) + v of the wavefront's.  The operand stages are dead
-  // (group 0's last barrier comes after group 1's last read).
-  if constexpr (UP) {
-    // a wavefront's 32 columns are one block; codes [256 rows][64 bytes] and scales [256][4] are put together in LDS
+  if (!find_tile()) return;
+  set_rows();
+  auto start = [&] {                                     // into the first stages: k tile 0, and scales
+    set_sources();
+    if (wm == 0) {
+      copy_scales_a(0);
+    } else {
+      copy_scales_b(0, 0);
+      copy_scales_b(0, 1);
+    }
+    copy_a0b(0);
+    copy_a1(0, a_from);
+    a_from += kTileK / 2;
+    b_from += kTileK / 2;
+  };
+  start();
+  for (;;) {
+    if (nk > 1) {                                        // into the second stages, as k tile -1 would have
+      copy_a0b(1);
+      a_from += kTileK / 2;
+      b_from += kTileK / 2;
+      if (wm == 0) copy_scales_a(1);
+      else copy_scales_b(1, 0);
+      wait_vmcnt<7>();
+    } else {
+      wait_vmcnt<0>();
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    if (grp == 1) __builtin_amdgcn_s_barrier();          // group 1 is a phase behind
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+    for (int kt = 0; kt < nk; kt += 2) {
+      k_tile(std::integral_constant<int, 0>{}, kt);
+      if (kt + 1 < nk) k_tile(std::integral_constant<int, 1>{}, kt + 1);
+    }
+
+    // ---- epilogue: acc[i][j][v] is row wm 128 + 16 i + l % 16, column 16 j + 4 (l / 16) + v of the wavefront's.  All of LDS is free (group
+    // 0's last barrier comes after group 1's last read); the result goes through the second stage of A, and the first stages are filled
+    // for the workgroup's next tile beside it.
+    const int out_row0 = row0, out_end = row_end, out_col0 = col0;
+    const int ln = here(lane), r = ln & 15, lg = ln >> 4, tid = wave * kWave + ln;
     __syncthreads();
-    char* const s_codes = smem;
-    char* const s_scales = smem + 256 * 64;
+    id += gridDim.x;
+    const bool more = find_tile();
+    if (more) set_rows();
+    char* const out = smem + kStage;
+    if constexpr (UP) {
+      // a wavefront's 32 columns are one block; codes [256 rows][64 bytes] and scales [256][4] are put together in LDS
+      char* const s_scales = out + 256 * 64;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int row = wm * 128 + i * 16 + r;
-      float v[2][4];
-      uint32_t amax = 0;
+      for (int i = 0; i < TM; ++i) {
+        const int row = wm * 128 + i * 16 + r;
+        float v[2][4];
+        uint32_t amax = 0;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          v[j][x] = silu_f(acc[i][j][x]) * acc[i][j + 2][x];
-          amax = max(amax, magnitude(v[j][x]));
+          for (int x = 0; x < 4; ++x) {
+            v[j][x] = silu_f(acc[i][j][x]) * acc[i][j + 2][x];
+            amax = max(amax, magnitude(v[j][x]));
+          }
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, kWave));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, kWave));
+        const uint32_t byte = mx4_scale_byte(amax);
+        const float scale = mx4_scale(byte);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t w = 0;
+          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[j][0], v[j][1], scale, 0);
+          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[j][2], v[j][3], scale, 1);
+          *reinterpret_cast<uint16_t*>(out + row * 64 + wn * 16 + j * 8 + lg * 2) = byte == 255u ? 0 : (uint16_t)w;
         }
-      amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, kWave));
-      amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, kWave));
-      const uint32_t byte = mx4_scale_byte(amax);
-      const float scale = mx4_scale(byte);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t w = 0;
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[j][0], v[j][1], scale, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[j][2], v[j][3], scale, 1);
-        *reinterpret_cast<uint16_t*>(s_codes + row * 64 + wn * 16 + j * 8 + lg * 2) = byte == 255u ? 0 : (uint16_t)w;
+        if (lg == 0) s_scales[row * 4 + wn] = out_col0 + wn * 32 < g.N ? (char)byte : 0;
       }
-      if (lg == 0) s_scales[row * 4 + wn] = col0 + wn * 32 < g.N ? (char)byte : 0;
-    }
-    __syncthreads();
-    const int64_t out_row = g.N / 2, out_pitch = mx4_pitch(g.N);
+      if (more) start();
+      __syncthreads();
+      const int64_t out_row = g.N / 2, out_pitch = mx4_pitch(g.N);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int idx = q * 512 + threadIdx.x, row = idx >> 2, c = idx & 3;
-      if (row0 + row < row_end && col0 + c * 32 < g.N)
-        *reinterpret_cast<u32x4*>(g.act_codes + (int64_t)(row0 + row) * out_row + col0 / 2 + c * 16) =
-            *reinterpret_cast<const u32x4*>(s_codes + row * 64 + c * 16);
-    }
-    if (threadIdx.x < 256 && row0 + (int)threadIdx.x < row_end) {
-      uint8_t* const to_scales = g.act_scales + (int64_t)(row0 + threadIdx.x) * out_pitch;
-      *reinterpret_cast<uint32_t*>(to_scales + col0 / 32) = *reinterpret_cast<const uint32_t*>(s_scales + threadIdx.x * 4);
-      if (col0 + COLS >= g.N)                            // the zeros behind them
-        for (int z = col0 / 32 + 4; z < (int)out_pitch; z += 4) *reinterpret_cast<uint32_t*>(to_scales + z) = 0;
-    }
-  } else {
-    // 32 rows of the wavefront's 64 columns at a time (128 bytes a row) through its own piece of LDS, chunks swizzled by row
-    __syncthreads();
-    char* const band = smem + wave * 4096;
-    const int n0 = col0 + wn * 64;
+      for (int q = 0; q < 2; ++q) {
+        const int idx = q * 512 + tid, row = idx >> 2, c = idx & 3;
+        if (out_row0 + row < out_end && out_col0 + c * 32 < g.N)
+          *reinterpret_cast<u32x4*>(g.act_codes + (int64_t)(out_row0 + row) * out_row + out_col0 / 2 + c * 16) =
+              *reinterpret_cast<const u32x4*>(out + row * 64 + c * 16);
+      }
+      if (tid < 256 && out_row0 + tid < out_end) {
+        const uint32_t four = *reinterpret_cast<const uint32_t*>(s_scales + tid * 4);
+        auto put = [&](int b, uint32_t w) {              // blocks b, b + 1; b a multiple of 2
+          *reinterpret_cast<uint16_t*>(g.act_scales + mx4_scale_at(g.R, out_row0 + tid, b)) = (uint16_t)w;
+        };
+        put(out_col0 / 32, four);
+        put(out_col0 / 32 + 2, four >> 16);
+        if (out_col0 + COLS >= g.N)                      // the zeros behind them
+          for (int z = out_col0 / 32 + 4; z < (int)out_pitch; z += 2) put(z, 0);
+      }
+    } else {
+      if (more) start();
+      // 32 rows of the wavefront's 64 columns at a time (128 bytes a row) through its own piece of LDS, chunks swizzled by row
+      char* const band = out + wave * 4096;
+      const int n0 = out_col0 + wn * 64;
 #pragma unroll
-    for (int ib = 0; ib < TM / 2; ++ib) {
+      for (int ib = 0; ib < TM / 2; ++ib) {
 #pragma unroll
-      for (int i2 = 0; i2 < 2; ++i2)
+        for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4& v = acc[2 * ib + i2][j];
-          const int row = i2 * 16 + r, byte = (j * 16 + 4 * lg) * 2;
-          *reinterpret_cast<u32x2*>(band + row * 128 + ((byte >> 4 ^ (row & 7)) << 4) + (byte & 15)) =
-              u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+          for (int j = 0; j < 4; ++j) {
+            const f32x4& v = acc[2 * ib + i2][j];
+            const int row = i2 * 16 + r, byte = (j * 16 + 4 * lg) * 2;
+            *reinterpret_cast<u32x2*>(band + row * 128 + ((byte >> 4 ^ (row & 7)) << 4) + (byte & 15)) =
+                u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+          }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int row = q * 8 + ln / 8, c = ln & 7, m = out_row0 + wm * 128 + ib * 32 + row;
+          const u32x4 w = *reinterpret_cast<const u32x4*>(band + row * 128 + ((c ^ (row & 7)) << 4));
+          if (m < out_end && n0 + c * 8 < g.N) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(g.y + (int64_t)m * g.N + n0 + c * 8));
         }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = q * 8 + lane / 8, c = lane & 7, m = row0 + wm * 128 + ib * 32 + row;
-        const u32x4 w = *reinterpret_cast<const u32x4*>(band + row * 128 + ((c ^ (row & 7)) << 4));
-        if (m < row_end && n0 + c * 8 < g.N) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(g.y + (int64_t)m * g.N + n0 + c * 8));
+        __builtin_amdgcn_wave_barrier();
       }
     }
+    if (!more) return;
+    __syncthreads();                                     // the second stages are free
   }
 }
 
@@ -461,15 +613,10 @@ template <bool UP> int launch_tiles(const Mx4Args& g, int R, hipStream_t s) {
   const int n_ct = ceil_div(g.N, UP ? 128 : 256);
   const int64_t tiles = ((int64_t)ceil_div(R, kTileRows) + std::min(g.E, R)) * n_ct + kXcds;
   if (!grid_fits(tiles, kTileWaves * kWave)) return BTX_ERR_UNSUPPORTED;
-  mx4_tile_kernel<UP><<<(unsigned)tiles, kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
+  // a workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end
+  mx4_tile_kernel<UP><<<(unsigned)std::min<int64_t>(tiles, kTileGrid), kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
-}
-
-// gathered rows are found with 32-bit offsets
-bool tiles_ok(const Mx4Args& g, int T) { return !g.perm || (int64_t)T * (g.K / 2) + kTileK < (int64_t)1 << 32; }
-template <bool UP> int launch(const Mx4Args& g, int T, int R, hipStream_t s) {
-  return R / g.E >= 64 && tiles_ok(g, T) ? launch_tiles<UP>(g, R, s) : launch_few<UP>(g, R, s);
 }
 
 }  // namespace
@@ -479,15 +626,23 @@ int mx4_prepare() {
   return raise_lds<mx4_tile_kernel<false>>();
 }
 
-int launch_mx4_up(const Mx4Matrix& xq, const Mx4Matrix& W1, const Mx4Matrix& W3, const int32_t* offsets, const int32_t* perm,
-                  const Mx4Shapes& sh, uint8_t* act_codes, uint8_t* act_scales, hipStream_t s) {
-  const Mx4Args g{xq, W1, W3, offsets, perm, sh.k, sh.E, sh.f, sh.d, act_codes, act_scales, nullptr};
-  return launch<true>(g, sh.T, sh.T * sh.k, s);
+// 256-row tiles: from 64 rows an expert on average; rows of x are found with 32-bit offsets there
+bool mx4_use_tiles(const Mx4Shapes& sh) {
+  return (int64_t)sh.T * sh.k / sh.E >= 64 && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 &&
+         ((int64_t)sh.T * sh.k + 256) * 16 < (int64_t)1 << 32;
 }
 
-int launch_mx4_down(const Mx4Matrix& act, const Mx4Matrix& W2, const int32_t* offsets, const Mx4Shapes& sh, void* y, hipStream_t s) {
-  const Mx4Args g{act, W2, {nullptr, nullptr}, offsets, nullptr, 1, sh.E, sh.d, sh.f, nullptr, nullptr, static_cast<bf16_t*>(y)};
-  return launch<false>(g, sh.T, sh.T * sh.k, s);
+int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const int32_t* offsets, const Mx4Shapes& sh, hipStream_t s) {
+  const int R = sh.T * sh.k;
+  const Mx4Args g{l.x, W1, W3, offsets, sh.E, l.tokens, l.tiles, sh.T, sh.f, sh.d, l.act_codes, l.act_scales, nullptr, R};
+  return mx4_use_tiles(sh) ? launch_tiles<true>(g, R, s) : launch_few<true>(g, R, s);
+}
+
+int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const int32_t* offsets, const Mx4Shapes& sh, hipStream_t s) {
+  const int R = sh.T * sh.k;
+  const Mx4Args g{{l.act_codes, l.act_scales}, W2, {nullptr, nullptr}, offsets, sh.E, nullptr, l.tiles, R, sh.d, sh.f, nullptr, nullptr,
+                  static_cast<bf16_t*>(l.y), R};
+  return mx4_use_tiles(sh) ? launch_tiles<false>(g, R, s) : launch_few<false>(g, R, s);
 }
 
 }  // namespace btx

@@ -12,12 +12,13 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---- axis 1: [rows, K] --------------------------------------------------------------------------------------
-template <typename XT>
-__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const XT* __restrict__ x, int64_t rows, int64_t K, uint32_t* __restrict__ codes,
-                                                                 uint8_t* __restrict__ scales, int64_t pitch) {
+// TILES: scales in mx4_scale_at()'s order
+template <typename XT, bool TILES>
+__device__ __forceinline__ void quantize_rows(int64_t block, const XT* __restrict__ x, int64_t rows, int64_t K, uint32_t* __restrict__ codes,
+                                              uint8_t* __restrict__ scales, int64_t pitch) {
   // a row is cut into pieces of 8 elements, and rows are as long as their scales' pitch (whole 512 elements): what lies behind K
   // only writes the zeros behind the scales
-  const int64_t per_row = pitch * 4, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t per_row = pitch * 4, i = block * kThreads + threadIdx.x;
   const int64_t r = i / per_row;
   if (r >= rows) return;                               // whole blocks of four threads
   const int64_t p = i - r * per_row;
@@ -33,12 +34,41 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const XT* __res
   amax = max(amax, (uint32_t)dpp_i32<kDppXor2>((int)amax));
   const uint32_t byte = mx4_scale_byte(amax);
   if (inside) codes[r * (K / 8) + p] = byte == 255u ? 0u : mx4_codes8(v, mx4_scale(byte));
-  if ((threadIdx.x & 3) == 0) scales[r * pitch + p / 4] = inside ? (uint8_t)byte : 0;
+  if ((threadIdx.x & 3) == 0) scales[TILES ? mx4_scale_at(rows, r, (int)(p / 4)) : r * pitch + p / 4] = inside ? (uint8_t)byte : 0;
+}
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const XT* __restrict__ x, int64_t rows, int64_t K, uint32_t* __restrict__ codes,
+                                                                 uint8_t* __restrict__ scales, int64_t pitch) {
+  quantize_rows<XT, false>(blockIdx.x, x, rows, K, codes, scales, pitch);
 }
 
-template <typename XT>
-__global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows,
-                                                                   int64_t K, int64_t pitch, XT* __restrict__ out);
+// The layer's first launch: its rows quantised, and beside them (the first blocks) the token of every grouped row and the row tiles
+template <bool TILES>
+__global__ __launch_bounds__(kThreads) void layer_begin_kernel(const bf16_t* __restrict__ x, int64_t T, int64_t d, uint32_t* __restrict__ codes,
+                                                               uint8_t* __restrict__ scales, int64_t pitch, const int32_t* __restrict__ perm,
+                                                               int R, int k, int token_blocks, int32_t* __restrict__ tokens,
+                                                               const int32_t* __restrict__ offsets, int E, TileInfo* __restrict__ tiles) {
+  const int n_first = token_blocks + (TILES ? 1 : 0);
+  if ((int)blockIdx.x >= n_first) {
+    quantize_rows<bf16_t, TILES>((int64_t)blockIdx.x - n_first, x, T, d, codes, scales, pitch);
+    return;
+  }
+  if ((int)blockIdx.x < token_blocks) {
+    const int r = blockIdx.x * kThreads + threadIdx.x;
+    if (r < R) tokens[r] = perm[r] / k;
+    return;
+  }
+  __shared__ int s_wave[kThreads / kWave];              // thread e: expert e (E <= 256)
+  const int e = threadIdx.x, lane = e & (kWave - 1);
+  const int o0 = e < E ? offsets[e] : 0, o1 = e < E ? offsets[e + 1] : 0, n = (o1 - o0 + kMx4TileRows - 1) / kMx4TileRows;
+  const int incl = wave_incl_scan_i32(n, lane);
+  if (lane == kWave - 1) s_wave[e / kWave] = incl;
+  __syncthreads();
+  int at = 1 + incl - n;
+  for (int w = 0; w < e / kWave; ++w) at += s_wave[w];
+  for (int i = 0; i < n; ++i) tiles[at + i] = TileInfo{e, o0 + i * kMx4TileRows, o1, 0};
+  if (e == kThreads - 1) tiles[0] = TileInfo{0, at + n - 1, 0, 0};
+}
 
 // the value of code c
 __device__ __forceinline__ float code_value(uint32_t c) {
@@ -171,6 +201,24 @@ int launch_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, i
     else
       quantize_cols_kernel<<<grid, kThreads, 0, s>>>(static_cast<const float*>(x), K, cols, reinterpret_cast<u32x4*>(codes), scales, pitch);
   }
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+
+int launch_mx4_begin(const void* x, const int32_t* perm, const int32_t* offsets, const Mx4Shapes& sh, uint8_t* x_codes, uint8_t* x_scales,
+                     int32_t* tokens, TileInfo* tiles, hipStream_t s) {
+  static_assert(kMx4MaxExperts <= kThreads, "one thread an expert");
+  const int R = sh.T * sh.k, token_blocks = ceil_div(R, kThreads);
+  const int64_t pitch = mx4_pitch(sh.d), blocks = token_blocks + 1 + ((int64_t)sh.T * pitch * 4 + kThreads - 1) / kThreads;
+  if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
+  const bf16_t* const xp = static_cast<const bf16_t*>(x);
+  uint32_t* const codes = reinterpret_cast<uint32_t*>(x_codes);
+  if (mx4_use_tiles(sh))
+    layer_begin_kernel<true><<<(unsigned)blocks, kThreads, 0, s>>>(xp, sh.T, sh.d, codes, x_scales, pitch, perm, R, sh.k, token_blocks, tokens, offsets,
+                                                                   sh.E, tiles);
+  else
+    layer_begin_kernel<false><<<(unsigned)blocks - 1, kThreads, 0, s>>>(xp, sh.T, sh.d, codes, x_scales, pitch, perm, R, sh.k, token_blocks, tokens,
+                                                                        offsets, sh.E, tiles);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
