@@ -39,11 +39,10 @@ int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype
 int mx4_prepare();                     // one-time set-up on the current device (not capturable)
 struct Mx4Shapes { int T, d, f, E, k; };
 struct Mx4Matrix { const uint8_t* codes; const uint8_t* scales; };
-constexpr int kMx4TileRows = 256;
-struct TileInfo { int e, row0, row_end, unused; };      // rows of a row tile
-inline int mx4_most_tiles(int R, int E) { return (int)((int64_t)R / kMx4TileRows + std::min(E, R)); }
-// the products take 256-row tiles (else 16 rows at a time); x and act then have their scales in another order, mx4_scale_at()
-bool mx4_use_tiles(const Mx4Shapes& sh);
+struct TileInfo { int e, row0, row_end, unused; };      // of an expert's rows the tile has those from row0 on, row_end is the expert's end
+inline int mx4_most_tiles(int R, int E, int tile_rows) { return (int)std::min<int64_t>((int64_t)R / tile_rows + std::min(E, R), R); }
+// Rows of a row tile: 256 (the products take tiles of them; x and act have their scales in another order then, mx4_scale_at()), 64, 32 or 16
+int mx4_tile_rows(const Mx4Shapes& sh);
 // Where the scale of block b of a row is in that order: 16 bytes of every row for 16 blocks (two k tiles), in them those of blocks 2g, 2g + 1,
 // 8 + 2g and 9 + 2g together, which lane group g takes.
 inline __device__ int64_t mx4_scale_at(int64_t rows, int64_t row, int b) {
@@ -54,8 +53,8 @@ struct Mx4Layer { Mx4Matrix x; const int32_t* tokens; const TileInfo* tiles; uin
 int launch_mx4_begin(const void* x, const int32_t* perm, const int32_t* offsets, const Mx4Shapes& sh, uint8_t* x_codes, uint8_t* x_scales,
                      int32_t* tokens, TileInfo* tiles, hipStream_t s);
 // act = silu(xq W1) * (xq W3), quantised along f: rows in grouped order
-int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const int32_t* offsets, const Mx4Shapes& sh, hipStream_t s);
+int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const Mx4Shapes& sh, hipStream_t s);
 // y = act W2, [T*k, d] bf16
-int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const int32_t* offsets, const Mx4Shapes& sh, hipStream_t s);
+int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const Mx4Shapes& sh, hipStream_t s);
 
 }  // namespace btx

@@ -22,148 +22,140 @@ template <int SW, int SX = SW> __device__ __forceinline__ f32x4 mfma_mx4(const u
 
 struct Mx4Args {
   Mx4Matrix a, b0, b1;                  // token rows; weights (b1: W3)
-  const int32_t* offsets; int E;
   const int32_t* tokens;                // row r of the product is row tokens[r] of a (NULL: row r)
-  const TileInfo* tiles;                // row tiles (tile kernel): the first entry's row0 is their number
+  const TileInfo* tiles;                // row tiles: the first entry's row0 is their number
   int a_rows;                           // of a (tile kernel: their scales' order, see mx4_scale_at())
   int N, K;                             // columns, depth
   uint8_t* act_codes; uint8_t* act_scales; bf16_t* y;
   int R;
 };
 
-// Row tiles of up to 256 experts (RowTiles has 64): lane x looks at experts 4x .. 4x + 3
-struct ManyRowTiles {
-  int off[5], nt[4], incl, bm;
-  __device__ __forceinline__ ManyRowTiles(const int32_t* __restrict__ offsets, int E, int BM, int lane) : bm(BM) {
-#pragma unroll
-    for (int q = 0; q < 5; ++q) off[q] = offsets[min(4 * lane + q, E)];
-    int n = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      nt[q] = (off[q + 1] - off[q] + BM - 1) / BM;
-      n += nt[q];
-    }
-    incl = wave_incl_scan_i32(n, lane);
-  }
-  __device__ __forceinline__ int count() const { return __builtin_amdgcn_readlane(incl, kWave - 1); }
-  // tile id < count(): its expert, and rows row0 .. row_end - 1 of which the tile takes the first bm
-  __device__ __forceinline__ void find(int id, int& expert, int& row0, int& row_end) const {
-    const int owner = __ffsll((long long)__ballot(incl > id)) - 1;
-    int n[4], o[5], left = id - __builtin_amdgcn_readlane(incl, owner);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      n[q] = __builtin_amdgcn_readlane(nt[q], owner);
-      left += n[q];
-    }
-#pragma unroll
-    for (int q = 0; q < 5; ++q) o[q] = __builtin_amdgcn_readlane(off[q], owner);
-    int q = 0;
-    while (q < 3 && left >= n[q]) left -= n[q++];
-    expert = 4 * owner + q;
-    int begin = o[0], end = o[1];
-    if (q == 1) { begin = o[1]; end = o[2]; }
-    if (q == 2) { begin = o[2]; end = o[3]; }
-    if (q == 3) { begin = o[3]; end = o[4]; }
-    row0 = begin + left * bm;
-    row_end = end;
-  }
-};
-
-// ---- few rows: 16 rows x 32 columns a workgroup, whose wavefronts share K ------------------------------------
-// Bound by reading the weights.  They go from memory to the registers that the products take: a lane reads 64 consecutive bytes
-// of a row (4 blocks) and their four scales in a word, 512 elements of 16 rows a wavefront at a time.
-constexpr int kFewRows = 16, kFewCols = 32;
-template <bool UP, int NW>
-__global__ __launch_bounds__(NW* kWave) void mx4_few_kernel(Mx4Args g) {
+// ---- few rows: up to 64 rows x 32 columns a workgroup, whose wavefronts share K ---------------------------------
+// Bound by reading the weights.  They go from memory to the registers that the products take, 512 elements of 16 rows a wavefront at a time: in
+// step s lane group g has chunk 4s + g, so that a load covers 64 bytes of a row; of the row's 16 scales a lane picks every fourth.  RB blocks of
+// 16 rows meet each fragment of the weights.  With 4 wavefronts and at most 128 registers three workgroups are on a compute unit and begin and end beside
+// each other (one token, 2 experts of 4096 x 11008: UP with 8 wavefronts, one workgroup at a time, 29 us).
+constexpr int kFewCols = 32;
+// byte g of each of four words; pick: g | (4 + g) << 8
+__device__ __forceinline__ uint32_t every_fourth(const u32x4& v, uint32_t pick) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[3], v[2], pick), __builtin_amdgcn_perm(v[1], v[0], pick), 0x05040100u);
+}
+template <bool UP, int RB, int NW>
+__global__ __launch_bounds__(NW* kWave, UP && RB == 4 ? 2 : 3) void mx4_few_kernel(Mx4Args g) {
   constexpr int PANELS = UP ? 2 : 1;
-  __shared__ f32x4 s_sum[NW][PANELS * 2][kWave];
+  __shared__ f32x4 s_sum[NW][RB][PANELS * 2][kWave];
+  if ((int)blockIdx.x >= g.tiles[0].row0) return;
+  const TileInfo tile = g.tiles[1 + blockIdx.x];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const ManyRowTiles tiles(g.offsets, g.E, kFewRows, lane);
-  if ((int)blockIdx.y >= tiles.count()) return;
-  int e, row0, row_end;
-  tiles.find(blockIdx.y, e, row0, row_end);
-  const int n0 = blockIdx.x * kFewCols, r = lane & 15, grp = lane >> 4;
+  const int n0 = blockIdx.y * kFewCols, r = lane & 15, grp = lane >> 4;
   const int n_blk = g.K / kMxBlock;
   const int64_t pitch = mx4_pitch(g.K);
-  int64_t row = min(row0 + r, row_end - 1);
-  if (g.tokens) row = g.tokens[row];
-  const u32x4* const a = reinterpret_cast<const u32x4*>(g.a.codes) + row * n_blk;
-  const uint8_t* const a_sc = g.a.scales + row * pitch;
-  const u32x4* w[PANELS * 2];
-  const uint8_t* w_sc[PANELS * 2];
+  const uint32_t pick = (uint32_t)grp | (uint32_t)(4 + grp) << 8;
+  const u32x4* const a = reinterpret_cast<const u32x4*>(g.a.codes);
+  uint32_t row[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    row[rb] = (uint32_t)min(tile.row0 + rb * 16 + r, tile.row_end - 1);
+    if (g.tokens) row[rb] = (uint32_t)g.tokens[row[rb]];
+  }
+  // the weights by one base for every 16 columns, and a lane's offset of 32 bits
+  const char* w[PANELS * 2];
+  const char* w_sc[PANELS * 2];
 #pragma unroll
   for (int p = 0; p < PANELS * 2; ++p) {
     const Mx4Matrix& m = p < 2 ? g.b0 : g.b1;
-    const int64_t n = (int64_t)e * g.N + n0 + 16 * (p & 1) + r;
-    w[p] = reinterpret_cast<const u32x4*>(m.codes) + n * n_blk;
-    w_sc[p] = m.scales + n * pitch;
+    const int64_t n = (int64_t)tile.e * g.N + n0 + 16 * (p & 1);
+    w[p] = reinterpret_cast<const char*>(m.codes) + n * n_blk * 16;
+    w_sc[p] = reinterpret_cast<const char*>(m.scales) + n * pitch;
   }
-  f32x4 acc[PANELS * 2] = {};
+  const uint32_t w_row = (uint32_t)r * (uint32_t)n_blk * 16, sc_row = (uint32_t)r * (uint32_t)pitch;
+  f32x4 acc[RB][PANELS * 2] = {};
+#pragma unroll 1
   for (int b0 = 16 * wave; b0 < n_blk; b0 += 16 * NW) {
-    const int at = b0 + 4 * grp;                       // (scale rows are whole 16 bytes; behind K / 32 they are zero)
-    u32x4 xv[4], wv[PANELS * 2][4];
-    uint32_t xs, ws[PANELS * 2];
-    xs = *reinterpret_cast<const uint32_t*>(a_sc + at);
-#pragma unroll
-    for (int p = 0; p < PANELS * 2; ++p) ws[p] = *reinterpret_cast<const uint32_t*>(w_sc[p] + at);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const bool in = at + s < n_blk;
-      xv[s] = in ? a[at + s] : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int p = 0; p < PANELS * 2; ++p) wv[p][s] = in ? w[p][at + s] : u32x4{0u, 0u, 0u, 0u};
-    }
+    const int at = b0 + grp;                           // (scale rows are whole 16 bytes; behind K / 32 they are zero)
+    u32x4 wv[PANELS * 2][4];
+    uint32_t ws[PANELS * 2];
 #pragma unroll
     for (int p = 0; p < PANELS * 2; ++p) {
-      acc[p] = mfma_mx4<0>(wv[p][0], xv[0], acc[p], ws[p], xs);
-      acc[p] = mfma_mx4<1>(wv[p][1], xv[1], acc[p], ws[p], xs);
-      acc[p] = mfma_mx4<2>(wv[p][2], xv[2], acc[p], ws[p], xs);
-      acc[p] = mfma_mx4<3>(wv[p][3], xv[3], acc[p], ws[p], xs);
+      ws[p] = every_fourth(*reinterpret_cast<const u32x4*>(w_sc[p] + (sc_row + b0)), pick);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        wv[p][s] = at + 4 * s < n_blk ? *reinterpret_cast<const u32x4*>(w[p] + (w_row + (at + 4 * s) * 16u)) : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      if (rb > 0 && tile.row0 + rb * 16 >= tile.row_end) break;
+      const uint32_t xs = every_fourth(*reinterpret_cast<const u32x4*>(g.a.scales + row[rb] * pitch + b0), pick);
+      u32x4 xv[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) xv[s] = at + 4 * s < n_blk ? a[(int64_t)row[rb] * n_blk + at + 4 * s] : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int p = 0; p < PANELS * 2; ++p) {
+        acc[rb][p] = mfma_mx4<0>(wv[p][0], xv[0], acc[rb][p], ws[p], xs);
+        acc[rb][p] = mfma_mx4<1>(wv[p][1], xv[1], acc[rb][p], ws[p], xs);
+        acc[rb][p] = mfma_mx4<2>(wv[p][2], xv[2], acc[rb][p], ws[p], xs);
+        acc[rb][p] = mfma_mx4<3>(wv[p][3], xv[3], acc[rb][p], ws[p], xs);
+      }
     }
   }
 #pragma unroll
-  for (int p = 0; p < PANELS * 2; ++p) s_sum[wave][p][lane] = acc[p];
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int p = 0; p < PANELS * 2; ++p) s_sum[wave][rb][p][lane] = acc[rb][p];
   __syncthreads();
-  // thread t < 256: row t / 16, columns 2 (t % 16) and the next: lane 16 (c % 16 / 4) + row of fragment c / 16, element c % 4
-  if (threadIdx.x >= 256) return;
-  const int out_row = threadIdx.x / 16, c = 2 * (threadIdx.x % 16), m = row0 + out_row;
+  // thread t of 256: rows t / 16 of every block, columns 2 (t % 16) and the next: lane 16 (c % 16 / 4) + row of fragment c / 16, element c % 4
+  const int out_row = (threadIdx.x & 255) / 16, c = 2 * (threadIdx.x % 16);
   const int from = 16 * ((c & 15) >> 2) + out_row, half = c >> 4, el = c & 3;
-  float sum[PANELS][2] = {};
+  for (int rb = threadIdx.x / 256; rb < RB; rb += NW * kWave / 256) {
+    const int m = tile.row0 + rb * 16 + out_row;
+    if (m - out_row >= tile.row_end) break;
+    float sum[PANELS][2] = {};
 #pragma unroll
-  for (int x = 0; x < NW; ++x)
+    for (int x = 0; x < NW; ++x)
 #pragma unroll
-    for (int p = 0; p < PANELS; ++p) {
-      const f32x2* v = reinterpret_cast<const f32x2*>(&s_sum[x][2 * p + half][from]);
-      sum[p][0] += v[el >> 1][0];
-      sum[p][1] += v[el >> 1][1];
+      for (int p = 0; p < PANELS; ++p) {
+        const f32x2* v = reinterpret_cast<const f32x2*>(&s_sum[x][rb][2 * p + half][from]);
+        sum[p][0] += v[el >> 1][0];
+        sum[p][1] += v[el >> 1][1];
+      }
+    const bool live = m < tile.row_end;
+    if constexpr (UP) {
+      const float v0 = silu_f(sum[0][0]) * sum[1][0], v1 = silu_f(sum[0][1]) * sum[1][1];
+      uint32_t amax = max(magnitude(v0), magnitude(v1));
+      amax = max(amax, (uint32_t)dpp_i32<kDppXor1>((int)amax));
+      amax = max(amax, (uint32_t)dpp_i32<kDppXor2>((int)amax));
+      amax = max(amax, (uint32_t)dpp_i32<kDppRor4>((int)amax));
+      amax = max(amax, (uint32_t)dpp_i32<kDppRor8>((int)amax));
+      const uint32_t byte = mx4_scale_byte(amax);
+      const uint32_t code = byte == 255u ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v0, v1, mx4_scale(byte), 0) & 255u;
+      if (live) {
+        const int64_t act_pitch = mx4_pitch(g.N);
+        g.act_codes[(int64_t)m * (g.N / 2) + (n0 + c) / 2] = (uint8_t)code;
+        if (c == 0) g.act_scales[(int64_t)m * act_pitch + n0 / kMxBlock] = (uint8_t)byte;
+        // the zeros behind the scales of a row
+        if (n0 + kFewCols == g.N)
+          for (int64_t z = g.N / kMxBlock + c / 2; z < act_pitch; z += 16) g.act_scales[(int64_t)m * act_pitch + z] = 0;
+      }
+    } else {
+      if (live) *reinterpret_cast<uint32_t*>(g.y + (int64_t)m * g.N + n0 + c) = pack_bf16x2(sum[0][0], sum[0][1]);
     }
-  const bool live = m < row_end;
-  if constexpr (UP) {
-    const float v0 = silu_f(sum[0][0]) * sum[1][0], v1 = silu_f(sum[0][1]) * sum[1][1];
-    uint32_t amax = max(magnitude(v0), magnitude(v1));
-    amax = max(amax, (uint32_t)dpp_i32<kDppXor1>((int)amax));
-    amax = max(amax, (uint32_t)dpp_i32<kDppXor2>((int)amax));
-    amax = max(amax, (uint32_t)dpp_i32<kDppRor4>((int)amax));
-    amax = max(amax, (uint32_t)dpp_i32<kDppRor8>((int)amax));
-    const uint32_t byte = mx4_scale_byte(amax);
-    const uint32_t code = byte == 255u ? 0u : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v0, v1, mx4_scale(byte), 0) & 255u;
-    if (live) {
-      const int64_t act_pitch = mx4_pitch(g.N);
-      g.act_codes[(int64_t)m * (g.N / 2) + (n0 + c) / 2] = (uint8_t)code;
-      if (c == 0) g.act_scales[(int64_t)m * act_pitch + n0 / kMxBlock] = (uint8_t)byte;
-      // the zeros behind the scales of a row
-      if (n0 + kFewCols == g.N)
-        for (int64_t z = g.N / kMxBlock + c / 2; z < act_pitch; z += 16) g.act_scales[(int64_t)m * act_pitch + z] = 0;
-    }
-  } else {
-    if (live) *reinterpret_cast<uint32_t*>(g.y + (int64_t)m * g.N + n0 + c) = pack_bf16x2(sum[0][0], sum[0][1]);
   }
 }
 
-template <bool UP> int launch_few(const Mx4Args& g, int R, hipStream_t s) {
-  const int64_t tiles = (int64_t)ceil_div(R, kFewRows) + std::min(g.E, R);    // at most: every expert may have a partly filled one
-  if (tiles > 65535) return BTX_ERR_UNSUPPORTED;
-  mx4_few_kernel<UP, 8><<<dim3(g.N / kFewCols, (unsigned)tiles), 8 * kWave, 0, s>>>(g);
+template <bool UP> int launch_few(const Mx4Args& g, int tile_rows, int E, hipStream_t s) {
+  const int tiles = mx4_most_tiles(g.R, E, tile_rows), cols = g.N / kFewCols;
+  if (cols > 65535) return BTX_ERR_UNSUPPORTED;
+  auto go = [&](auto rb, auto nw) {
+    mx4_few_kernel<UP, decltype(rb)::value, decltype(nw)::value><<<dim3((unsigned)tiles, (unsigned)cols), decltype(nw)::value * kWave, 0, s>>>(g);
+  };
+  auto rows = [&](auto nw) {
+    if (tile_rows == 16) go(std::integral_constant<int, 1>{}, nw);
+    else if (tile_rows == 32) go(std::integral_constant<int, 2>{}, nw);
+    else go(std::integral_constant<int, 4>{}, nw);
+  };
+  // 8 wavefronts where each has two pieces of 512 elements or more
+  if (g.K >= 16 * 512) rows(std::integral_constant<int, 8>{});
+  else rows(std::integral_constant<int, 4>{});
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
@@ -229,7 +221,7 @@ __device__ __forceinline__ bool tile_of(int id, int n_rt, int n_ct, int& tm, int
   return true;
 }
 
-constexpr int kTileRows = 256, kTileCols = 256, kTileWaves = 8, kTileK = 256;   // (UP: 128 columns of W1, 128 of W3)
+constexpr int kTileRows = 256, kTileWaves = 8, kTileK = 256;   // x 256 columns (UP: 128 of W1, 128 of W3)
 constexpr uint32_t kStage = 32768, kScaleAStage = 4096, kScaleBStage = 8192;   // scales: of 2 (A) and 4 (B) k tiles
 constexpr uint32_t kB0 = 2 * kStage, kScaleA0 = 4 * kStage, kScaleB0 = kScaleA0 + 2 * kScaleAStage;
 constexpr int kTileLds = kScaleB0 + 2 * kScaleBStage;
@@ -608,15 +600,20 @@ template <auto KERNEL> int raise_lds() {
   return BTX_OK;
 }
 
-template <bool UP> int launch_tiles(const Mx4Args& g, int R, hipStream_t s) {
+template <bool UP> int launch_tiles(const Mx4Args& g, int E, hipStream_t s) {
   if (int rc = raise_lds<mx4_tile_kernel<UP>>()) return rc;
   const int n_ct = ceil_div(g.N, UP ? 128 : 256);
-  const int64_t tiles = ((int64_t)ceil_div(R, kTileRows) + std::min(g.E, R)) * n_ct + kXcds;
-  if (!grid_fits(tiles, kTileWaves * kWave)) return BTX_ERR_UNSUPPORTED;
+  const int64_t tiles = (int64_t)mx4_most_tiles(g.R, E, kTileRows) * n_ct + kXcds;
+  if (tiles >= (int64_t)1 << 31) return BTX_ERR_UNSUPPORTED;
   // a workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end
   mx4_tile_kernel<UP><<<(unsigned)std::min<int64_t>(tiles, kTileGrid), kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
+}
+
+template <bool UP> int launch(const Mx4Args& g, const Mx4Shapes& sh, hipStream_t s) {
+  const int rows = mx4_tile_rows(sh);
+  return rows == kTileRows ? launch_tiles<UP>(g, sh.E, s) : launch_few<UP>(g, rows, sh.E, s);
 }
 
 }  // namespace
@@ -626,23 +623,24 @@ int mx4_prepare() {
   return raise_lds<mx4_tile_kernel<false>>();
 }
 
-// 256-row tiles: from 64 rows an expert on average; rows of x are found with 32-bit offsets there
-bool mx4_use_tiles(const Mx4Shapes& sh) {
-  return (int64_t)sh.T * sh.k / sh.E >= 64 && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 &&
-         ((int64_t)sh.T * sh.k + 256) * 16 < (int64_t)1 << 32;
+// How many rows a row tile has: 256 from 64 rows an expert on average on (rows of x, a tile's rows and their scales are found with 32-bit offsets there).
+// Below, 16, 32 or 64, so that few experts have more rows than the average and a tile's: those read their weights twice.
+int mx4_tile_rows(const Mx4Shapes& sh) {
+  const int64_t R = (int64_t)sh.T * sh.k, avg = R / sh.E;
+  if (avg >= 64 && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 && (R + 256) * 16 < (int64_t)1 << 32 && sh.d <= 1 << 21 &&
+      sh.f <= 1 << 21)
+    return kTileRows;
+  return avg <= 8 ? 16 : avg <= 22 ? 32 : 64;
 }
 
-int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const int32_t* offsets, const Mx4Shapes& sh, hipStream_t s) {
-  const int R = sh.T * sh.k;
-  const Mx4Args g{l.x, W1, W3, offsets, sh.E, l.tokens, l.tiles, sh.T, sh.f, sh.d, l.act_codes, l.act_scales, nullptr, R};
-  return mx4_use_tiles(sh) ? launch_tiles<true>(g, R, s) : launch_few<true>(g, R, s);
+int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const Mx4Shapes& sh, hipStream_t s) {
+  return launch<true>(Mx4Args{l.x, W1, W3, l.tokens, l.tiles, sh.T, sh.f, sh.d, l.act_codes, l.act_scales, nullptr, sh.T * sh.k}, sh, s);
 }
 
-int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const int32_t* offsets, const Mx4Shapes& sh, hipStream_t s) {
+int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const Mx4Shapes& sh, hipStream_t s) {
   const int R = sh.T * sh.k;
-  const Mx4Args g{{l.act_codes, l.act_scales}, W2, {nullptr, nullptr}, offsets, sh.E, nullptr, l.tiles, R, sh.d, sh.f, nullptr, nullptr,
-                  static_cast<bf16_t*>(l.y), R};
-  return mx4_use_tiles(sh) ? launch_tiles<false>(g, R, s) : launch_few<false>(g, R, s);
+  return launch<false>(Mx4Args{{l.act_codes, l.act_scales}, W2, {nullptr, nullptr}, nullptr, l.tiles, R, sh.d, sh.f, nullptr, nullptr,
+                               static_cast<bf16_t*>(l.y), R}, sh, s);
 }
 
 }  // namespace btx

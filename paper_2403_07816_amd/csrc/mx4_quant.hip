@@ -47,8 +47,8 @@ template <bool TILES>
 __global__ __launch_bounds__(kThreads) void layer_begin_kernel(const bf16_t* __restrict__ x, int64_t T, int64_t d, uint32_t* __restrict__ codes,
                                                                uint8_t* __restrict__ scales, int64_t pitch, const int32_t* __restrict__ perm,
                                                                int R, int k, int token_blocks, int32_t* __restrict__ tokens,
-                                                               const int32_t* __restrict__ offsets, int E, TileInfo* __restrict__ tiles) {
-  const int n_first = token_blocks + (TILES ? 1 : 0);
+                                                               const int32_t* __restrict__ offsets, int E, int tile_rows, TileInfo* __restrict__ tiles) {
+  const int n_first = token_blocks + 1;
   if ((int)blockIdx.x >= n_first) {
     quantize_rows<bf16_t, TILES>((int64_t)blockIdx.x - n_first, x, T, d, codes, scales, pitch);
     return;
@@ -60,13 +60,13 @@ __global__ __launch_bounds__(kThreads) void layer_begin_kernel(const bf16_t* __r
   }
   __shared__ int s_wave[kThreads / kWave];              // thread e: expert e (E <= 256)
   const int e = threadIdx.x, lane = e & (kWave - 1);
-  const int o0 = e < E ? offsets[e] : 0, o1 = e < E ? offsets[e + 1] : 0, n = (o1 - o0 + kMx4TileRows - 1) / kMx4TileRows;
+  const int o0 = e < E ? offsets[e] : 0, o1 = e < E ? offsets[e + 1] : 0, n = (o1 - o0 + tile_rows - 1) / tile_rows;
   const int incl = wave_incl_scan_i32(n, lane);
   if (lane == kWave - 1) s_wave[e / kWave] = incl;
   __syncthreads();
   int at = 1 + incl - n;
   for (int w = 0; w < e / kWave; ++w) at += s_wave[w];
-  for (int i = 0; i < n; ++i) tiles[at + i] = TileInfo{e, o0 + i * kMx4TileRows, o1, 0};
+  for (int i = 0; i < n; ++i) tiles[at + i] = TileInfo{e, o0 + i * tile_rows, o1, 0};
   if (e == kThreads - 1) tiles[0] = TileInfo{0, at + n - 1, 0, 0};
 }
 
@@ -213,12 +213,13 @@ int launch_mx4_begin(const void* x, const int32_t* perm, const int32_t* offsets,
   if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
   const bf16_t* const xp = static_cast<const bf16_t*>(x);
   uint32_t* const codes = reinterpret_cast<uint32_t*>(x_codes);
-  if (mx4_use_tiles(sh))
+  const int tile_rows = mx4_tile_rows(sh);
+  if (tile_rows == 256)
     layer_begin_kernel<true><<<(unsigned)blocks, kThreads, 0, s>>>(xp, sh.T, sh.d, codes, x_scales, pitch, perm, R, sh.k, token_blocks, tokens, offsets,
-                                                                   sh.E, tiles);
+                                                                   sh.E, tile_rows, tiles);
   else
-    layer_begin_kernel<false><<<(unsigned)blocks - 1, kThreads, 0, s>>>(xp, sh.T, sh.d, codes, x_scales, pitch, perm, R, sh.k, token_blocks, tokens,
-                                                                        offsets, sh.E, tiles);
+    layer_begin_kernel<false><<<(unsigned)blocks, kThreads, 0, s>>>(xp, sh.T, sh.d, codes, x_scales, pitch, perm, R, sh.k, token_blocks, tokens, offsets,
+                                                                    sh.E, tile_rows, tiles);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
