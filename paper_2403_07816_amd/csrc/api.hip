@@ -504,7 +504,7 @@ Mx4Ws carve_mx4(void* ws, int T, int d, int f, int E, int k) {
   w.act_scales = static_cast<uint8_t*>(c.take(R * mx4_pitch(f)));
   w.tokens = static_cast<int32_t*>(c.take(R * sizeof(int32_t)));
   w.tiles = static_cast<TileInfo*>(c.take((1 + (size_t)mx4_most_tiles((int)R, E, 16)) * sizeof(TileInfo)));
-  w.y = c.take(R * d * 2);
+  w.y = c.take(mx4_y_bytes((int64_t)R, d));
   w.bytes = c.used;
   return w;
 }
@@ -532,8 +532,9 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
   const Mx4Layer l{{w.x_codes, w.x_scales}, w.tokens, w.tiles, w.act_codes, w.act_scales, w.y};
   BTX_STAGE(BTX_STAGE_GATHER_X, launch_mx4_begin(x, perm, offsets, sh, w.x_codes, w.x_scales, w.tokens, w.tiles, s));
   BTX_STAGE(BTX_STAGE_UP, launch_mx4_up(l, {W1_codes, W1_scales}, {W3_codes, W3_scales}, sh, s));
-  BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down(l, {W2_codes, W2_scales}, sh, s));
-  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, nullptr, 1, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
+  int slices = 1;
+  BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down(l, {W2_codes, W2_scales}, sh, &slices, s));
+  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, static_cast<const float*>(w.y), slices, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
   return BTX_OK;
 }
 

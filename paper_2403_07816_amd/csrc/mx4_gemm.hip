@@ -28,6 +28,7 @@ struct Mx4Args {
   int N, K;                             // columns, depth
   uint8_t* act_codes; uint8_t* act_scales; bf16_t* y;
   int R;
+  int slices;                           // DOWN in tiles: K ranges of a tile; more than one: sums [slice][R][N] in fp32, in y's place
 };
 
 // ---- few rows: up to 64 rows x 32 columns a workgroup, whose wavefronts share K ---------------------------------
@@ -41,7 +42,7 @@ __device__ __forceinline__ uint32_t every_fourth(const u32x4& v, uint32_t pick) 
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[3], v[2], pick), __builtin_amdgcn_perm(v[1], v[0], pick), 0x05040100u);
 }
 template <bool UP, int RB, int NW>
-__global__ __launch_bounds__(NW* kWave, UP && RB == 4 ? 2 : 3) void mx4_few_kernel(Mx4Args g) {
+__global__ __launch_bounds__(NW* kWave, RB == 4 ? 2 : 3) void mx4_few_kernel(Mx4Args g) {
   constexpr int PANELS = UP ? 2 : 1;
   __shared__ f32x4 s_sum[NW][RB][PANELS * 2][kWave];
   if ((int)blockIdx.x >= g.tiles[0].row0) return;
@@ -249,18 +250,23 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave >> 2, wn = wave & 3, grp = wm;     // the wavefronts of a SIMD are w and w + 4
-  const int n_blk = g.K / kMxBlock, nk = (g.K + kTileK - 1) / kTileK, tail = n_blk - (nk - 1) * 8;   // blocks of the last k tile
+  const int nk_all = (g.K + kTileK - 1) / kTileK, slices = UP ? 1 : g.slices;
   const int64_t pitch = mx4_pitch(g.K), row_bytes = g.K / 2;
-  const int quads = (nk + 3) / 4;                        // pieces of 32 bytes in a row's scales
   const uint32_t base = (uint32_t)(uintptr_t)smem;
 
   // ---- the tile
   const int n_rt = g.tiles[0].row0, most = n_rt * n_ct + kXcds;
-  int e, row0, row_end, col0, id = blockIdx.x;
+  int e, row0, row_end, col0, slice, id = blockIdx.x;
+  int k_first, nk, tail;                                 // its k tiles: k_first (a multiple of four, as scales are copied) .. + nk - 1; blocks of the last
   auto find_tile = [&]() -> bool {                       // `id`, or the next one of this workgroup that names a tile
     int tm, tn;
-    for (; id < most; id += gridDim.x)
-      if (tile_of(id, n_rt, n_ct, tm, tn)) {
+    for (; id < most * slices; id += gridDim.x)
+      if (tile_of(id % most, n_rt, n_ct, tm, tn)) {
+        const int quads = (nk_all + 3) / 4;
+        slice = id / most;
+        k_first = slice * quads / slices * 4;
+        nk = min((slice + 1) * quads / slices * 4, nk_all) - k_first;
+        tail = min(g.K / kMxBlock - (k_first + nk - 1) * 8, 8);
         const TileInfo t = g.tiles[1 + tm];
         e = t.e;
         row0 = t.row0;
@@ -302,19 +308,19 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
       asm volatile("" : "+v"(a_off[q]), "+v"(b_off[q]));
     }
     const Mx4Matrix& bm = UP && wave >= 4 ? g.b1 : g.b0;
-    a_from = uniform64(g.a.codes + (g.tokens ? 0 : (int64_t)row0 * row_bytes)) - kCopyBias2;
-    b_from = uniform64(bm.codes + ((int64_t)e * g.N + col0) * row_bytes) - kCopyBias4;
+    a_from = uniform64(g.a.codes + (g.tokens ? 0 : (int64_t)row0 * row_bytes)) - kCopyBias2 + (uint64_t)k_first * (kTileK / 2);
+    b_from = uniform64(bm.codes + ((int64_t)e * g.N + col0) * row_bytes) - kCopyBias4 + (uint64_t)k_first * (kTileK / 2);
     if (wm == 0) {
       s_off[0] *= 16;
       s_off[1] = 0;
-      s_from = uniform64(g.a.scales + (g.tokens ? 0 : (int64_t)row0 * 16));
+      s_from = uniform64(g.a.scales + (g.tokens ? 0 : (int64_t)row0 * 16)) + (uint64_t)(k_first / 2) * s_step;
     } else {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const int row = wn * 64 + q * 32 + ln / 2, col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
         s_off[q] = (uint32_t)col * (uint32_t)pitch + s_half(ln) * 16;
       }
-      s_from = uniform64((UP && wn >= 2 ? g.b1 : g.b0).scales + ((int64_t)e * g.N + col0) * pitch);
+      s_from = uniform64((UP && wn >= 2 ? g.b1 : g.b0).scales + ((int64_t)e * g.N + col0) * pitch) + (uint64_t)k_first * 8;
     }
     asm volatile("" : "+v"(s_off[0]), "+v"(s_off[1]));
   };
@@ -349,7 +355,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
   };
   auto copy_scales_b = [&](int quad, int q) {
     const int from = min(quad, (nk - 1) / 4);
-    const uint32_t less = from * 32 + 16 >= (int)pitch ? s_half(here(lane)) * 16 : 0;
+    const uint32_t less = k_first * 8 + from * 32 + 16 >= (int)pitch ? s_half(here(lane)) * 16 : 0;
     copy16(s_from + (uint64_t)from * 32, (q ? s_off[1] : s_off[0]) - less, to_s + (quad & 1) * kScaleBStage + q * 1024);
   };
 
@@ -501,7 +507,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
     // ---- epilogue: acc[i][j][v] is row wm 128 + 16 i + l % 16, column 16 j + 4 (l / 16) + v of the wavefront's.  All of LDS is free (group
     // 0's last barrier comes after group 1's last read); the result goes through the second stage of A, and the first stages are filled
     // for the workgroup's next tile beside it.
-    const int out_row0 = row0, out_end = row_end, out_col0 = col0;
+    const int out_row0 = row0, out_end = row_end, out_col0 = col0, out_slice = slice;
     const int ln = here(lane), r = ln & 15, lg = ln >> 4, tid = wave * kWave + ln;
     __syncthreads();
     id += gridDim.x;
@@ -558,6 +564,19 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
       }
     } else {
       if (more) start();
+      if (slices > 1) {                                  // four columns a lane, as they are
+        float* const sums = reinterpret_cast<float*>(g.y) + ((int64_t)out_slice * g.R + out_row0) * g.N;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const int m = wm * 128 + i * 16 + r, n = out_col0 + wn * 64 + j * 16 + 4 * lg;
+            if (out_row0 + m < out_end && n < g.N) *reinterpret_cast<f32x4*>(sums + (int64_t)m * g.N + n) = acc[i][j];
+          }
+        if (!more) return;
+        __syncthreads();
+        continue;
+      }
       // 32 rows of the wavefront's 64 columns at a time (128 bytes a row) through its own piece of LDS, chunks swizzled by row
       char* const band = out + wave * 4096;
       const int n0 = out_col0 + wn * 64;
@@ -600,13 +619,23 @@ template <auto KERNEL> int raise_lds() {
   return BTX_OK;
 }
 
+// K ranges of DOWN's tiles: as many as fill the chip where the tiles alone do not, of eight k tiles or more each; no more than whoever
+// combines the rows adds, and than there is room for
+int down_slices(const Mx4Args& g, const Mx4Shapes& sh) {
+  const int64_t busy = std::min<int64_t>(sh.E, g.R), tiles = busy * ceil_div(ceil_div(g.R, busy), kTileRows) * ceil_div(g.N, 256);
+  const int64_t fit = (int64_t)mx4_y_bytes(g.R, g.N) / ((int64_t)g.R * g.N * 4);
+  return (int)std::max<int64_t>(std::min({kTileGrid / tiles, (int64_t)ceil_div(g.K, kTileK) / 8, fit, (int64_t)combine_most_slices(sh.T, sh.k, BTX_BF16)}), 1);
+}
+
 template <bool UP> int launch_tiles(const Mx4Args& g, int E, hipStream_t s) {
   if (int rc = raise_lds<mx4_tile_kernel<UP>>()) return rc;
   const int n_ct = ceil_div(g.N, UP ? 128 : 256);
-  const int64_t tiles = (int64_t)mx4_most_tiles(g.R, E, kTileRows) * n_ct + kXcds;
+  const int64_t tiles = ((int64_t)mx4_most_tiles(g.R, E, kTileRows) * n_ct + kXcds) * g.slices;
   if (tiles >= (int64_t)1 << 31) return BTX_ERR_UNSUPPORTED;
-  // a workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end
-  mx4_tile_kernel<UP><<<(unsigned)std::min<int64_t>(tiles, kTileGrid), kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
+  // A workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end.  Of less than two
+  // rounds each has its own: a few ids name no tile, and their compute units take the ones behind the 256th.
+  const int64_t grid = tiles <= 2 * kTileGrid ? tiles : kTileGrid;
+  mx4_tile_kernel<UP><<<(unsigned)grid, kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
@@ -634,13 +663,15 @@ int mx4_tile_rows(const Mx4Shapes& sh) {
 }
 
 int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const Mx4Shapes& sh, hipStream_t s) {
-  return launch<true>(Mx4Args{l.x, W1, W3, l.tokens, l.tiles, sh.T, sh.f, sh.d, l.act_codes, l.act_scales, nullptr, sh.T * sh.k}, sh, s);
+  return launch<true>(Mx4Args{l.x, W1, W3, l.tokens, l.tiles, sh.T, sh.f, sh.d, l.act_codes, l.act_scales, nullptr, sh.T * sh.k, 1}, sh, s);
 }
 
-int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const Mx4Shapes& sh, hipStream_t s) {
+int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const Mx4Shapes& sh, int* slices, hipStream_t s) {
   const int R = sh.T * sh.k;
-  return launch<false>(Mx4Args{{l.act_codes, l.act_scales}, W2, {nullptr, nullptr}, nullptr, l.tiles, R, sh.d, sh.f, nullptr, nullptr,
-                               static_cast<bf16_t*>(l.y), R}, sh, s);
+  Mx4Args g{{l.act_codes, l.act_scales}, W2, {nullptr, nullptr}, nullptr, l.tiles, R, sh.d, sh.f, nullptr, nullptr, static_cast<bf16_t*>(l.y), R, 1};
+  if (mx4_tile_rows(sh) == kTileRows) g.slices = down_slices(g, sh);
+  *slices = g.slices;
+  return launch<false>(g, sh, s);
 }
 
 }  // namespace btx
