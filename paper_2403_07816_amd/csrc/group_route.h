@@ -11,9 +11,9 @@ constexpr int kGroupMaxExperts = 256, kGroupMaxK = 16, kGroupMaxGroups = 16;
 struct GroupRouteArgs {
   const void* logits; int dtype; const float* bias; int T, E, k, score_fn, G, keep, group_score, renorm; float scale;
   int32_t* topk_idx; float* gates; float* scores; int32_t* counts; int32_t* offsets; int32_t* perm; int32_t* inv_pos;
-  int* hist;                       // workspace: [blocks][E] pairs of every expert
-  // by the launcher: experts of a group; lanes it has (log2) of a token's 16, experts a lane; rows in pieces of four; tokens of a block
-  int per_group, log2_lanes, per_lane, vector, tokens;
+  int* hist;                       // workspace: [blocks][hist_pitch] pairs of every expert
+  // by the launcher: E, rounded up; experts of a group; lanes it has (log2) of a token's 16, experts a lane; rows in pieces of four; tokens of a block
+  int hist_pitch, per_group, log2_lanes, per_lane, vector, tokens;
 };
 size_t group_route_workspace_bytes(int T, int E);
 int launch_group_route(GroupRouteArgs a, hipStream_t s);

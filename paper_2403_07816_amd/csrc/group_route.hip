@@ -6,8 +6,8 @@
 //                     expert and leaves how many of each it has.
 //   2. group_scatter  every workgroup adds those counts up (of the workgroups before it, and of all) and writes its pairs' places.
 // The selection is the one of the scores in double precision.  It is done in float, with a bound of each value's error; a token with two
-// values, or two groups, nearer to each other than that is done again in double (group_pick<double>), by the same lanes: a few in a
-// thousand of ordinary logits, all of them where all logits are equal.
+// values, or two groups, nearer to each other than that is done again in double (group_pick_f64), by its wavefront: a few in a
+// thousand of ordinary logits.
 #include "group_route.h"
 
 namespace btx {
@@ -88,17 +88,31 @@ template <int SCORE> __device__ __forceinline__ float score_f(float l, const Row
   if (SCORE == BTX_SCORE_SIGMOID) return sigmoid_f(l);
   return l == -INFINITY ? 0.f : __expf(l - st.m) * st.inv;
 }
-// bound of the error of score + bias = v in float: the argument of exp is rounded (|l| 2^-24 log2(e) of its value, at most), the
-// hardware's exp2 and reciprocal add an ulp each, softmax's sum one for every addition in line (36 at most), the bias another
-template <int SCORE> __device__ __forceinline__ float score_err(float l, float s, float v, const RowStat& st) {
+// bound of the error, in 2^-23, of a score in float: the argument of exp is rounded (|l| 2^-24 log2(e) of its value, at most), the
+// hardware's exp2 and reciprocal add an ulp each, softmax's sum one for every addition in line (36 at most)
+template <int SCORE> __device__ __forceinline__ float score_err(float l, float s) {
   if (l == -INFINITY) return 0.f;
-  if (SCORE == BTX_SCORE_SIGMOID) return kUlp * (s * ((1.f - s) * (fabsf(l) + 2.f) + 3.f) + fabsf(v));
-  return kUlp * (s * (fabsf(l - st.m) + 26.f) + fabsf(v));
+  if (SCORE == BTX_SCORE_SIGMOID) return s * ((1.f - s) * (fabsf(l) + 2.f) + 3.f);
+  return s * (fabsf(l) + 26.f);                                         // l: less the row's largest
+}
+template <int SCORE> __device__ __forceinline__ float score_err(float l, float s, const RowStat& st) {
+  return score_err<SCORE>(SCORE == BTX_SCORE_SOFTMAX && l != -INFINITY ? l - st.m : l, s);
 }
 
-__device__ __forceinline__ double shfl_f64(double v, int lane) {
-  const int lo = __shfl(__double2loint(v), lane, kWave), hi = __shfl(__double2hiint(v), lane, kWave);
+__device__ __forceinline__ double xor_f64(double v, int d) {
+  const int lo = __shfl_xor(__double2loint(v), d, kWave), hi = __shfl_xor(__double2hiint(v), d, kWave);
   return __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double read_lane_f64(double v, int lane) {   // lane: of all lanes the same
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+// over the wavefront
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = row_max_u32(v);
+  uint32_t top = 0u;
+#pragma unroll
+  for (int r = 0; r < kWave; r += kLanes) top = max(top, (uint32_t)__builtin_amdgcn_readlane((int)v, r));
+  return top;
 }
 
 // what lanes of this wavefront have put into LDS is there for the others
@@ -107,71 +121,79 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The selection in double, by the 16 lanes of a token: slot[j] = expert of slot j.  logits: the token's.  (Not inlined, and it reads the
-// logits again: its registers are not the fast path's.)
+// The selection of one token in double, by the whole wavefront: slot[j] = expert of slot j.  logits: the token's.  64 lanes and not the
+// token's 16, since such a token is the last one of its workgroup, and of the launch: over 16384 tokens of 256 experts without any, those
+// of random logits took 12 us more with 16 lanes and take 2 us more with 64.
 template <typename XT, int P, int SCORE>
-__device__ __attribute__((noinline)) void group_pick_f64(const GroupRouteArgs& a, const XT* logits, int sub, int row_base, int* slot) {
-  const Deal mine(a, sub);
-  float l[P];
-#pragma unroll
-  for (int i = 0; i < P; ++i) l[i] = i < mine.n ? load_logit(logits + mine.first + i) : -INFINITY;
-  double v[P];
+__device__ __forceinline__ void group_pick_f64(const GroupRouteArgs& a, const XT* logits, int lane, int* slot) {
+  constexpr int Q = P / kTokWave;                                       // four times the lanes have a group
+  const int shift = a.log2_lanes + 2, per = (a.per_group + (1 << shift) - 1) >> shift;
+  const int group = lane >> shift, from = (lane & ((1 << shift) - 1)) * per;
+  const int first = group * a.per_group + from, n = group < a.G ? max(0, min(per, a.per_group - from)) : 0;
+  double v[Q];
   double m = -INFINITY, sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < Q; ++i) v[i] = i < n ? (double)load_logit(logits + first + i) : -INFINITY;
   if (SCORE == BTX_SCORE_SOFTMAX) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) m = fmax(m, (double)l[i]);
-    for (int d = 1; d < kLanes; d *= 2) m = fmax(m, shfl_f64(m, row_base + (sub ^ d)));
+    for (int i = 0; i < Q; ++i) m = fmax(m, v[i]);
+    for (int d = 1; d < kWave; d *= 2) m = fmax(m, xor_f64(m, d));
 #pragma unroll
-    for (int i = 0; i < P; ++i) sum += i < mine.n && l[i] != -INFINITY ? exp((double)l[i] - m) : 0.0;
-    for (int d = 1; d < kLanes; d *= 2) sum += shfl_f64(sum, row_base + (sub ^ d));
+    for (int i = 0; i < Q; ++i) {
+      v[i] = v[i] != -INFINITY ? exp(v[i] - m) : -INFINITY;
+      sum += v[i] != -INFINITY ? v[i] : 0.0;
+    }
+    for (int d = 1; d < kWave; d *= 2) sum += xor_f64(sum, d);
   }
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    if (i < mine.n && l[i] != -INFINITY) {
-      const double s = SCORE == BTX_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - m) / sum;
-      v[i] = s + (a.bias ? (double)a.bias[mine.first + i] : 0.0);
+  for (int i = 0; i < Q; ++i) {
+    if (v[i] != -INFINITY) {
+      v[i] = SCORE == BTX_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-v[i])) : v[i] / sum;
+      if (a.bias) v[i] += (double)a.bias[first + i];
       if (!(v[i] == v[i])) v[i] = -INFINITY;
-    } else {
-      v[i] = -INFINITY;
     }
   }
-  uint32_t left = mine.n >= 32 ? 0xffffffffu : (1u << mine.n) - 1u;     // experts that may be chosen
+  bool in = group < a.G;
   if (a.G > 1) {
     double b1 = -INFINITY, b2 = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
+    for (int i = 0; i < Q; ++i) {
       b2 = fmax(b2, fmin(b1, v[i]));
       b1 = fmax(b1, v[i]);
     }
-    for (int d = 1; d < (1 << a.log2_lanes); d *= 2) {
-      const double o1 = shfl_f64(b1, row_base + (sub ^ d)), o2 = shfl_f64(b2, row_base + (sub ^ d));
+    for (int d = 1; d < (1 << shift); d *= 2) {
+      const double o1 = xor_f64(b1, d), o2 = xor_f64(b2, d);
       b2 = fmax(fmax(b2, o2), fmin(b1, o1));
       b1 = fmax(b1, o1);
     }
     const double value = a.group_score == BTX_GROUP_TOP2 && b2 != -INFINITY ? b1 + b2 : b1;
     int better = 0;
     for (int h = 0; h < a.G; ++h) {
-      const double o = shfl_f64(value, row_base + (h << a.log2_lanes));
-      better += h != mine.group && (o > value || (o == value && h < mine.group));
+      const double o = read_lane_f64(value, h << shift);
+      better += h != group && (o > value || (o == value && h < group));
     }
-    if (better >= a.keep) left = 0;
+    in &= better < a.keep;
+  }
+  unsigned long long key[Q];                                            // 0: cannot be chosen; masked experts can, after all others
+#pragma unroll
+  for (int i = 0; i < Q; ++i) {
+    const unsigned long long u = __double_as_longlong(v[i] == 0.0 ? 0.0 : v[i]);
+    key[i] = in && i < n ? (u >> 63 ? ~u : u | 1ull << 63) : 0ull;
   }
   for (int j = 0; j < a.k; ++j) {
-    double best = -INFINITY;
-    int at = -1;                                                        // any expert that is left, masked ones too, before none
+    unsigned long long best = key[0];
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-      if ((left >> i & 1) && (at < 0 || v[i] > best)) { best = v[i]; at = i; }
-    double top = best;
-    int who = at < 0 ? kWave : sub;
-    for (int d = 1; d < kLanes; d *= 2) {
-      const double o = shfl_f64(top, row_base + (sub ^ d));
-      const int w = __shfl(who, row_base + (sub ^ d), kWave);
-      if (w < kWave && (who == kWave || o > top || (o == top && w < who))) { top = o; who = w; }
-    }
-    if (who == sub) {
-      left &= ~(1u << at);
-      slot[j] = mine.first + at;
+    for (int i = 1; i < Q; ++i) best = max(best, key[i]);
+    const uint32_t hi = wave_max_u32((uint32_t)(best >> 32));
+    const uint32_t lo = wave_max_u32((uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
+    const unsigned long long top = (unsigned long long)hi << 32 | lo;
+    if (lane == __ffsll(__ballot(best == top)) - 1) {                   // the first lane of those that have it, the first of its experts
+      int at = 0;
+#pragma unroll
+      for (int i = Q - 1; i >= 0; --i) at = key[i] == top ? i : at;
+#pragma unroll
+      for (int i = 0; i < Q; ++i) key[i] = i == at ? 0ull : key[i];
+      slot[j] = first + at;
     }
   }
 }
@@ -193,56 +215,67 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
     const int t = t0 + in_pass;
     const int n_tok = min(pass_tokens, t_end - t0), rounds = (n_tok * a.k + kWave - 1) / kWave;
     for (int i = threadIdx.x; i < rounds * a.E; i += blockDim.x) s_count[i / a.E][i % a.E] = 0;
-    if (t < t_end) {
+    if (t0 + wave * kTokWave < t_end) {                                 // (the rows behind the last token do its work again)
+      const bool live = t < t_end;
+      const XT* const row = logits + (size_t)min(t, t_end - 1) * a.E;
       // ---- scores ----
-      float l[P];
-      const XT* const from = logits + (size_t)t * a.E + mine.first;
+      float l[P], v[P];
+      const XT* const from = row + mine.first;
       if (P % 4 == 0 && a.vector) {
 #pragma unroll
         for (int i = 0; i + 3 < P; i += 4) {
           if (i < mine.n) load_logits4(from + i, l + i);
           else l[i] = l[i + 1] = l[i + 2] = l[i + 3] = -INFINITY;
+          f32x4 b{0.f, 0.f, 0.f, 0.f};
+          if (a.bias && i < mine.n) b = *reinterpret_cast<const f32x4*>(a.bias + mine.first + i);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[i + x] = b[x];
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < P; ++i) l[i] = i < mine.n ? load_logit(from + i) : -INFINITY;
+        for (int i = 0; i < P; ++i) {
+          l[i] = i < mine.n ? load_logit(from + i) : -INFINITY;
+          v[i] = a.bias && i < mine.n ? a.bias[mine.first + i] : 0.f;
+        }
       }
+      float l_max = l[0];
+#pragma unroll
+      for (int i = 1; i < P; ++i) l_max = fmaxf(l_max, l[i]);
+      l_max = row_max_f32(l_max);
       RowStat st{0.f, 0.f};
       if (SCORE == BTX_SCORE_SOFTMAX) {
-        float m = l[0];
-#pragma unroll
-        for (int i = 1; i < P; ++i) m = fmaxf(m, l[i]);
-        st.m = row_max_f32(m);
-        if (st.m == -INFINITY) st.m = 0.f;                              // every expert masked
+        st.m = l_max == -INFINITY ? 0.f : l_max;                        // (every expert masked)
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < P; ++i) sum += __expf(l[i] - st.m);
         sum = row_sum_f32(sum);
         st.inv = sum > 0.f ? 1.f / sum : 0.f;
       }
-      float v[P], s[P], err = 0.f, b1 = kMaskedF, b2 = kMaskedF;
+      // No score's error is more than that of the largest logit's and a twentieth: softmax's bound rises with the logit, sigmoid's
+      // s (3 + (1 - s) (|l| + 2)) up to l = 2.5, where it is 3.09, and falls to 3 from there.
+      const float all_err = 1.05f * score_err<SCORE>(l_max, score_f<SCORE>(l_max, st), st);
+      float b1 = kMaskedF, b2 = kMaskedF;
+      float* const to = a.scores ? a.scores + (size_t)t * a.E + mine.first : nullptr;
+      const bool store = to && live;
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        s[i] = score_f<SCORE>(l[i], st);
-        v[i] = kMaskedF;
-        if (l[i] != -INFINITY) {
-          const float x = a.bias ? s[i] + a.bias[mine.first + i] : s[i];
-          v[i] = fmaxf(x, kMaskedF);                                    // (also of a NaN)
+      for (int i = 0; i < P; i += 4) {
+        float s[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          s[x] = score_f<SCORE>(l[i + x], st);
+          const float y = fmaxf(s[x] + v[i + x], kMaskedF);             // (also of a NaN)
+          v[i + x] = l[i + x] == -INFINITY ? kMaskedF : y;
+          b2 = fmaxf(b2, fminf(b1, v[i + x]));
+          b1 = fmaxf(b1, v[i + x]);
         }
-        err = fmaxf(err, score_err<SCORE>(l[i], s[i], v[i], st));
-        b2 = fmaxf(b2, fminf(b1, v[i]));
-        b1 = fmaxf(b1, v[i]);
-      }
-      if (a.scores) {
-        float* const to = a.scores + (size_t)t * a.E + mine.first;
-        if (P % 4 == 0 && a.vector) {
+        if (store) {
+          if (P % 4 == 0 && a.vector) {
+            if (i < mine.n) *reinterpret_cast<f32x4*>(to + i) = f32x4{s[0], s[1], s[2], s[3]};
+          } else {
 #pragma unroll
-          for (int i = 0; i + 3 < P; i += 4)
-            if (i < mine.n) *reinterpret_cast<f32x4*>(to + i) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
-        } else {
-#pragma unroll
-          for (int i = 0; i < P; ++i)
-            if (i < mine.n) to[i] = s[i];
+            for (int x = 0; x < 4; ++x)
+              if (i + x < mine.n) to[i + x] = s[x];
+          }
         }
       }
       // ---- groups ----
@@ -253,16 +286,18 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
           b2 = fmaxf(fmaxf(b2, o2), fminf(b1, o1));
           b1 = fmaxf(b1, o1);
         }
-        float e2 = row_max_f32(err);                                    // of every value of the token
+        // errors of the difference of two groups' values: four of scores, the roundings of v (of a lower v than the group's best: what it
+        // is lower by makes up for it), of two sums and of the difference
+        const float most = row_max_f32(fmaxf(b1 > kMaskedF ? fabsf(b1) : 0.f, b2 > kMaskedF ? fabsf(b2) : 0.f));
+        const float e2 = kUlp * (4.f * all_err + 8.f * most);
         const bool two = a.group_score == BTX_GROUP_TOP2 && b2 > kMaskedF;
         const float value = two ? b1 + b2 : b1;
-        e2 = 4.f * e2 + 2.f * kUlp * fabsf(value);                      // of the difference of two groups' values
         int above = 0, maybe = 0;                                       // groups that are better, or may be
         for (int h = 0; h < a.G; ++h) {
           const float d = __shfl(value, row_base + (h << a.log2_lanes), kWave) - value;
           if (h != mine.group) {
             above += d > e2;
-            maybe += d >= -e2;
+            maybe += !(d < -e2);                                        // (also infinity less itself)
           }
         }
         in = maybe < a.keep;
@@ -271,63 +306,83 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
       // ---- the k largest, and the next ----
       uint32_t key[P];
 #pragma unroll
-      for (int i = 0; i < P; ++i) key[i] = in && i < mine.n ? ordered(v[i]) : 0u;
+      for (int i = 0; i < P; ++i) key[i] = i < mine.n ? ordered(v[i]) : 0u;
       int* const slot = s_slot[in_pass];
-      int taken = 0, found = 0;
       for (int j = 0; j <= a.k; ++j) {
         uint32_t best = key[0];
 #pragma unroll
         for (int i = 1; i < P; ++i) best = max(best, key[i]);
+        best = in ? best : 0u;
         const uint32_t top = row_max_u32(best);
         const uint32_t have = (uint32_t)(__ballot(best == top) >> row_base) & 0xffffu;
-        found += top != 0u;
         if (sub == __ffs(have) - 1) {                                   // the first lane of those that have it
-          int at = -1 - mine.first;
-          if (top) {
+          uint32_t hits = 0u;
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
-              const bool hit = key[i] == top;                           // (more than one: `taken` tells)
-              at = hit ? i : at;
-              taken += hit;
-              key[i] = hit ? 0u : key[i];
-            }
+          for (int i = P - 1; i >= 0; --i) {
+            const bool hit = key[i] == top;
+            hits = hits + hits + hit;
+            key[i] = hit ? 0u : key[i];
           }
-          slot[j] = mine.first + at;                                    // -1: none is left
+          const uint32_t more = hits & (hits - 1u);                     // equal values: the first one only
+          if (more) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) key[i] = more >> i & 1 ? top : key[i];
+          }
+          slot[j] = top ? mine.first + __ffs(hits) - 1 : -1;            // -1: none is left
         }
       }
-      unsure |= row_sum_f32((float)taken) > (float)found;               // equal values of one lane went together
       wave_lds_fence();
       // lane j: slot j
       int e = -1;
-      float ls = -INFINITY, ss = 0.f;
+      float ls = -INFINITY, ss = 0.f, ve = 0.f, room = 0.f;
+      bool tied = false;
       if (sub < a.k) {
         e = slot[sub];
         const int n = slot[sub + 1];
         if (e >= 0) {
-          ls = load_logit(logits + (size_t)t * a.E + e);
+          ls = load_logit(row + e);
           ss = score_f<SCORE>(ls, st);
         }
         if (e < 0) {
           unsure = true;
         } else if (n >= 0) {                                            // nearer to the next one than the errors of both?
-          const float ln = load_logit(logits + (size_t)t * a.E + n), sn = score_f<SCORE>(ln, st);
+          const float ln = load_logit(row + n), sn = score_f<SCORE>(ln, st);
           const float be = a.bias ? a.bias[e] : 0.f, bn = a.bias ? a.bias[n] : 0.f;
-          const float ve = ls == -INFINITY ? kMaskedF : ss + be, vn = ln == -INFINITY ? kMaskedF : sn + bn;
-          const bool near = !(ve - vn > score_err<SCORE>(ls, ss, ve, st) + score_err<SCORE>(ln, sn, vn, st));
-          unsure |= near && !(ls == ln && be == bn);                    // (the same value: the lower index, which came first)
+          ve = ls == -INFINITY ? kMaskedF : fmaxf(ss + be, kMaskedF);
+          const float vn = ln == -INFINITY ? kMaskedF : fmaxf(sn + bn, kMaskedF);
+          const bool last = sub == a.k - 1;                             // behind it any that is left may be the next
+          float err = score_err<SCORE>(ls, ss, st) + (last ? all_err : score_err<SCORE>(ln, sn, st));
+          err += (ve > kMaskedF ? fabsf(ve) : 0.f) + (vn > kMaskedF ? fabsf(vn) : 0.f);
+          room = kUlp * err;
+          const bool near = !(ve - vn > room), same = ls == ln && be == bn;
+          tied = near && same && last && !a.bias;
+          unsure |= near && !(same && (!last || tied));                 // (the same value: the lower index, which came first)
         }
       }
-      if (row_or_u32(unsure)) {
-        group_pick_f64<XT, P, SCORE>(a, logits + (size_t)t * a.E, sub, row_base, slot);
+      if (__ballot(tied)) {
+        // The last slot's logit once more, left out: of all that are left, only that very logit may be so near.
+        const int at = row_base + a.k - 1;
+        const float l_last = __shfl(ls, at, kWave), least = __shfl(ve - room, at, kWave);
+        const bool here = in && __shfl((int)tied, at, kWave);
+#pragma unroll
+        for (int i = 0; i < P; ++i) if (here && key[i]) unsure |= load_logit(from + i) != l_last && !(v[i] < least);
+      }
+      unsigned long long again = __ballot(unsure && live);
+      if (again) {
+        for (int r = 0; r < kTokWave; ++r)
+          if (again >> (r * kLanes) & 0xffff) {
+            const int w = wave * kTokWave + r;
+            group_pick_f64<XT, P, SCORE>(a, logits + (size_t)(t0 + w) * a.E, lane, s_slot[w]);
+          }
         wave_lds_fence();
-        if (sub < a.k) {
+        if (sub < a.k && live) {
           e = slot[sub];
-          ss = score_f<SCORE>(load_logit(logits + (size_t)t * a.E + e), st);
+          ss = score_f<SCORE>(load_logit(row + e), st);
         }
       }
       // ---- gates ----
       const float sum = row_sum_f32(sub < a.k ? ss : 0.f);
-      if (sub < a.k) {
+      if (sub < a.k && live) {
         a.gates[(size_t)t * a.k + sub] = a.renorm ? a.scale * (ss / (sum + 1e-20f)) : a.scale * ss;
         a.topk_idx[(size_t)t * a.k + sub] = e;
         s_idx[in_pass * a.k + sub] = e;
@@ -370,7 +425,7 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
     __syncthreads();
   }
   if (gridDim.x > 1) {
-    for (int e = threadIdx.x; e < a.E; e += blockDim.x) a.hist[(size_t)blockIdx.x * a.E + e] = s_base[e];
+    for (int e = threadIdx.x; e < a.E; e += blockDim.x) a.hist[(size_t)blockIdx.x * a.hist_pitch + e] = s_base[e];
     return;
   }
   // one block: its counts are all there are
@@ -382,34 +437,40 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
   }
 }
 
+// The counts are read in pieces of four experts, 16 rows or so a thread at once: one by one, 64 rows a thread, the launch took 8.8 us for
+// 256 workgroups, 6.6 so.
 constexpr int kScatterThreads = 1024;
 __global__ __launch_bounds__(kScatterThreads) void group_scatter_kernel(GroupRouteArgs a, int blocks) {
-  __shared__ int s_part[kScatterThreads], s_upto[kScatterThreads];
+  constexpr int kFours = kGroupMaxExperts / 4, kSegs = kScatterThreads / kFours;
+  __shared__ __attribute__((aligned(16))) int s_part[kSegs][kGroupMaxExperts], s_upto[kSegs][kGroupMaxExperts];
   __shared__ int s_base[kGroupMaxExperts], s_off[kGroupMaxExperts], s_wave[kGroupMaxExperts / kWave];
-  // segment s of the blocks' counts for each of 256 experts
-  const int e = threadIdx.x % kGroupMaxExperts, seg = threadIdx.x / kGroupMaxExperts, segs = kScatterThreads / kGroupMaxExperts;
-  const int b0 = (int)((int64_t)seg * blocks / segs), b1 = (int)((int64_t)(seg + 1) * blocks / segs);
-  int all = 0, upto = 0;
-  if (e < a.E) {
-#pragma unroll 8
-    for (int b = b0; b < b1; ++b) {
-      const int c = a.hist[(size_t)b * a.E + e];
+  const int e4 = threadIdx.x % kFours * 4, seg = threadIdx.x / kFours;
+  u32x4 all{0, 0, 0, 0}, upto{0, 0, 0, 0};
+  if (e4 < a.E) {
+#pragma unroll 16
+    for (int b = seg; b < blocks; b += kSegs) {
+      const u32x4 c = *reinterpret_cast<const u32x4*>(a.hist + (size_t)b * a.hist_pitch + e4);
       all += c;
-      upto += b < (int)blockIdx.x ? c : 0;
+      if (b < (int)blockIdx.x) upto += c;
     }
   }
-  s_part[threadIdx.x] = all;
-  s_upto[threadIdx.x] = upto;
+  *reinterpret_cast<u32x4*>(&s_part[seg][e4]) = all;
+  *reinterpret_cast<u32x4*>(&s_upto[seg][e4]) = upto;
   __syncthreads();
   for (int x = threadIdx.x; x < a.E; x += blockDim.x) {
     int n = 0;
-    for (int s = 0; s < segs; ++s) n += s_part[s * kGroupMaxExperts + x];
+#pragma unroll
+    for (int s = 0; s < kSegs; ++s) n += s_part[s][x];
     s_base[x] = n;
   }
   __syncthreads();
   group_offsets(a, s_base, s_off, s_wave);                              // every block works them out, the first writes them
-  for (int x = threadIdx.x; x < a.E; x += blockDim.x)
-    for (int s = 0; s < segs; ++s) s_off[x] += s_upto[s * kGroupMaxExperts + x];
+  for (int x = threadIdx.x; x < a.E; x += blockDim.x) {
+    int n = s_off[x];
+#pragma unroll
+    for (int s = 0; s < kSegs; ++s) n += s_upto[s][x];
+    s_off[x] = n;
+  }
   __syncthreads();
   const size_t p0 = (size_t)blockIdx.x * a.tokens * a.k, p1 = min(p0 + (size_t)a.tokens * a.k, (size_t)a.T * a.k);
   for (size_t p = p0 + threadIdx.x; p < p1; p += blockDim.x) {
@@ -562,9 +623,11 @@ int launch_gate_grads(const float* dg_part, int n_part, const int32_t* inv_pos, 
 // tokens of a workgroup: 64, or more where that would be over 512 workgroups, whose counts every workgroup of the second launch adds up
 static int block_tokens(int T) { return T <= 512 * kTokPass ? kTokPass : ceil_div(ceil_div(T, 512), kTokPass) * kTokPass; }
 
+static int hist_pitch(int E) { return (E + 3) & ~3; }            // (whole pieces of 16 bytes)
+
 size_t group_route_workspace_bytes(int T, int E) {
   // (of the most workgroups that fewer tokens have: never less for more tokens)
-  return T > kTokPass ? (size_t)std::min(512, ceil_div(T, kTokPass)) * E * sizeof(int) : 0;
+  return T > kTokPass ? (size_t)std::min(512, ceil_div(T, kTokPass)) * hist_pitch(E) * sizeof(int) : 0;
 }
 
 int launch_group_route(GroupRouteArgs a, hipStream_t s) {
@@ -573,9 +636,11 @@ int launch_group_route(GroupRouteArgs a, hipStream_t s) {
   while (a.G << (a.log2_lanes + 1) <= kLanes) ++a.log2_lanes;
   a.per_lane = ceil_div(a.per_group, 1 << a.log2_lanes);
   a.tokens = block_tokens(a.T);
+  a.hist_pitch = hist_pitch(a.E);
   if (a.per_lane > 4 || a.per_group % 4 == 0) a.per_lane = (a.per_lane + 3) & ~3;   // whole vectors, where rows have them
   const int lsize = a.dtype == BTX_BF16 ? 2 : 4;
-  a.vector = a.per_group % 4 == 0 && a.per_lane % 4 == 0 && ((uintptr_t)a.logits % (4 * lsize)) == 0 && ((uintptr_t)a.scores & 15) == 0;
+  a.vector = a.per_group % 4 == 0 && a.per_lane % 4 == 0 && ((uintptr_t)a.logits % (4 * lsize)) == 0 &&
+             (((uintptr_t)a.scores | (uintptr_t)a.bias) & 15) == 0;
   const int blocks = ceil_div(a.T, a.tokens);
   const int threads = std::min(kThreadsMost, ceil_div(std::min(a.T, a.tokens), kTokWave) * kWave);
   auto go = [&](auto tag, auto per, auto score) {
