@@ -12,7 +12,6 @@ from __future__ import annotations
 
 import ctypes
 import importlib
-import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
@@ -315,19 +314,9 @@ def btx_moe_group_route(logits: torch.Tensor, k: int, score_fn: int = BTX_SCORE_
                         scale: float = 1.0, out: Optional[GroupRouting] = None,
                         workspace: Optional[torch.Tensor] = None) -> GroupRouting:
     """Route on a router's logits [T,E].  An `out` without scores leaves them out."""
-    lib = load_library()
-    T, E = logits.shape
-    r = out if out is not None else alloc_group_routing(T, E, k, logits.device)
-    i32, f32 = torch.int32, torch.float32
-    nbytes = lib.btx_moe_group_route_workspace_bytes(T, E, k)
-    ws = _workspace(nbytes, logits.device, workspace) if nbytes else None
-    st = lib.btx_moe_group_route(_ptr(logits), _dtype_code(logits), _typed(bias, f32, (E,), "bias"), T, E, k, score_fn, n_groups, topk_groups,
-                                 group_score, int(renorm), scale, _typed(r.topk_idx, i32, (T, k), "topk_idx"),
-                                 _typed(r.gates, f32, (T, k), "gates"), _typed(r.scores, f32, (T, E), "scores"),
-                                 _typed(r.counts, i32, (E,), "counts"), _typed(r.offsets, i32, (E + 1,), "offsets"),
-                                 _typed(r.perm, i32, (T * k,), "perm"), _typed(r.inv_pos, i32, (T, k), "inv_pos"), _ptr(ws),
-                                 _nbytes(ws), _stream())
-    _check(st, "btx_moe_group_route")
+    r = out if out is not None else alloc_group_routing(*logits.shape, k, logits.device)
+    _run("group_route", "btx_moe_group_route", logits, workspace,
+         (logits, k, score_fn, bias, n_groups, topk_groups, group_score, renorm, scale, r))
     return r
 
 
@@ -335,15 +324,9 @@ def btx_moe_group_route_backward(logits: torch.Tensor, routing, dgates: torch.Te
                                  renorm: bool = True, scale: float = 1.0, dscores: Optional[torch.Tensor] = None,
                                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dlogits [T,E]; routing: of btx_moe_group_route on these logits (its topk_idx is read)."""
-    lib = load_library()
-    T, E = logits.shape
-    k = routing.topk_idx.shape[1]
     out = out if out is not None else torch.empty_like(logits)
-    st = lib.btx_moe_group_route_backward(_ptr(logits), _dtype_code(logits), _typed(routing.topk_idx, torch.int32, (T, k), "topk_idx"),
-                                          _typed(dgates, torch.float32, (T, k), "dgates"),
-                                          _typed(dscores, torch.float32, (T, E), "dscores"), T, E, k, score_fn, int(renorm), scale,
-                                          _typed(out, logits.dtype, (T, E), "dlogits"), _stream())
-    _check(st, "btx_moe_group_route_backward")
+    _run("group_route_backward", "btx_moe_group_route_backward", logits, None,
+         (logits, routing, dgates, score_fn, renorm, scale, dscores, out))
     return out
 
 
@@ -412,12 +395,6 @@ def alloc_mx4(shape, axis: int, device) -> Mx4:
     return Mx4(torch.empty((*batch, n, K // 2), **u8), torch.empty((*batch, n, load_library().btx_mx4_scale_pitch(K)), **u8), K)
 
 
-def _mx4_shape(q: Mx4, batch, n: int, what: str) -> None:
-    pitch = load_library().btx_mx4_scale_pitch(q.K)
-    _typed(q.codes, torch.uint8, (*batch, n, q.K // 2), what + ".codes")
-    _typed(q.scales, torch.uint8, (*batch, n, pitch), what + ".scales")
-
-
 def _mx4_axis(axis: int) -> int:
     if axis not in (-1, -2):
         raise ValueError("axis is -1 or -2")
@@ -426,30 +403,22 @@ def _mx4_axis(axis: int) -> int:
 
 def btx_mx4_quantize(x: torch.Tensor, axis: int = -1, out: Optional[Mx4] = None) -> Mx4:
     """[.., rows, cols] in blocks of 32 along axis -1 (activations) or -2 (the experts' weights [E, K, N])."""
-    lib = load_library()
     ax = _mx4_axis(axis)
-    *batch, rows, cols = x.shape
-    K, n = (cols, rows) if axis == -1 else (rows, cols)
     out = out if out is not None else alloc_mx4(x.shape, axis, x.device)
-    if out.K != K:
-        raise ValueError(f"out.K is {K}")
-    _mx4_shape(out, batch, n, "out")
-    st = lib.btx_mx4_quantize(_ptr(x), _dtype_code(x), math.prod(batch), rows, cols, ax, _ptr(out.codes), _ptr(out.scales), _stream())
-    _check(st, "btx_mx4_quantize")
+    _run("mx4_quantize", "btx_mx4_quantize", x, None, (x, ax, out))
     return out
 
 
 def btx_mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, axis: int = -1, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values of q as a tensor; axis: as given to btx_mx4_quantize."""
-    lib = load_library()
     ax = _mx4_axis(axis)
     *batch, n, _ = q.codes.shape
-    _mx4_shape(q, batch, n, "q")
-    rows, cols = (n, q.K) if axis == -1 else (q.K, n)
-    out = out if out is not None else torch.empty((*batch, rows, cols), dtype=dtype, device=q.codes.device)
-    st = lib.btx_mx4_dequantize(_ptr(q.codes), _ptr(q.scales), _dtype_code(out), math.prod(batch), rows, cols, ax,
-                                _typed(out, dtype, (*batch, rows, cols), "out"), _stream())
-    _check(st, "btx_mx4_dequantize")
+    shape = (*batch, n, q.K) if axis == -1 else (*batch, q.K, n)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.codes.device)
+    elif out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"out is {str(dtype)[6:]} {shape}")
+    _run("mx4_dequantize", "btx_mx4_dequantize", out, None, (q, ax, out))
     return out
 
 
@@ -457,23 +426,8 @@ def btx_moe_ff_forward_mx4(x: torch.Tensor, W1: Mx4, W3: Mx4, W2: Mx4, routing, 
                            workspace: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[T,d] of the layer of 4-bit experts: W1, W3, W2 as btx_mx4_quantize(W, axis=-2) returns them; routing of btx_moe_route or
     btx_moe_group_route."""
-    lib = load_library()
-    T, d = x.shape
-    E, f, k = W1.codes.shape[0], W2.K, routing.topk_idx.shape[1]
-    bf16, i32 = torch.bfloat16, torch.int32
-    for q, K, n, what in ((W1, d, f, "W1"), (W3, d, f, "W3"), (W2, f, d, "W2")):
-        if q.K != K:
-            raise ValueError(f"{what}.K is {K}")
-        _mx4_shape(q, (E,), n, what)
     out = out if out is not None else torch.empty_like(x)
-    ws = _workspace(lib.btx_moe_ff_forward_mx4_workspace_bytes(T, d, f, E, k), x.device, workspace)
-    st = lib.btx_moe_ff_forward_mx4(_typed(x, bf16, (T, d), "x"), _ptr(W1.codes), _ptr(W1.scales), _ptr(W3.codes), _ptr(W3.scales),
-                                    _ptr(W2.codes), _ptr(W2.scales), T, d, f, E, k,
-                                    _typed(routing.gates, torch.float32, (T, k), "gates"), _typed(routing.offsets, i32, (E + 1,), "offsets"),
-                                    _typed(routing.perm, i32, (T * k,), "perm"), _typed(routing.inv_pos, i32, (T, k), "inv_pos"),
-                                    _typed(residual, bf16, (T, d), "residual"), _typed(out, bf16, (T, d), "out"), _ptr(ws), _nbytes(ws),
-                                    _stream())
-    _check(st, "btx_moe_ff_forward_mx4")
+    _run("forward_mx4", "btx_moe_ff_forward_mx4", x, workspace, (x, W1, W3, W2, routing, residual, out))
     return out
 
 

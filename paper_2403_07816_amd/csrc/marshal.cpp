@@ -1,6 +1,7 @@
-// Argument marshalling of the four entry points that a program calls once or more for every layer (routing with and without the
-// normalisation, forward, backward), for binding.py: the checks and addresses of up to thirty tensors and the call itself.  In
-// Python these are 0.2 us a tensor and 0.1 us an argument, 7 us of a call that launches two kernels.  Nothing is kept from one call
+// Argument marshalling of the entry points that a program calls once or more for every layer (routing with and without the
+// normalisation or from logits, forward, backward, those of 4-bit floats), for binding.py: the checks and addresses of up to thirty tensors and the call itself.  In
+// Python these are 0.2 us a tensor and 0.1 us an argument (0.6 where its shape and dtype are checked), 7 us of a call that launches two
+// kernels.  Nothing is kept from one call
 // for the next but the addresses of the library's functions.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -9,6 +10,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <string>
 #include <type_traits>
 
 #include "btx_moe.h"
@@ -23,6 +25,14 @@ struct Library {
   decltype(&btx_moe_ff_forward) forward;
   decltype(&btx_moe_ff_backward_workspace_bytes) backward_bytes;
   decltype(&btx_moe_ff_backward) backward;
+  decltype(&btx_moe_group_route_workspace_bytes) group_route_bytes;
+  decltype(&btx_moe_group_route) group_route;
+  decltype(&btx_moe_group_route_backward) group_route_backward;
+  decltype(&btx_mx4_scale_pitch) mx4_pitch;
+  decltype(&btx_mx4_quantize) mx4_quantize;
+  decltype(&btx_mx4_dequantize) mx4_dequantize;
+  decltype(&btx_moe_ff_forward_mx4_workspace_bytes) forward_mx4_bytes;
+  decltype(&btx_moe_ff_forward_mx4) forward_mx4;
 } lib{};
 
 struct PyError {};                       // a Python exception has been set
@@ -58,6 +68,18 @@ int dtype_code(const at::Tensor& t) {
   if (t.scalar_type() == at::kFloat) return BTX_F32;
   if (t.scalar_type() == at::kBFloat16) return BTX_BF16;
   fail(PyExc_TypeError, "unsupported dtype");
+}
+// address() of a tensor of this dtype and shape
+template <typename T> T* typed(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const std::string& what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() != type || t.sizes() != shape) {
+    std::string text = what + " is " + (type == at::kInt ? "int32" : type == at::kFloat ? "float32" : type == at::kByte ? "uint8" : "bfloat16") + " (";
+    for (const int64_t n : shape) text += std::to_string(n) + ", ";
+    if (!shape.empty()) text.resize(text.size() - 2);
+    fail(PyExc_ValueError, (text + ")").c_str());
+  }
+  return address_of<T>(o);
 }
 const at::Tensor& matrix(PyObject* o) {
   const at::Tensor& t = tensor(o);
@@ -108,6 +130,38 @@ struct RoutingPtrs {
   }
 };
 
+// an attribute; the object holds on to it, too
+struct Attr {
+  PyObject* o;
+  Attr(PyObject* of, const char* name) : o(PyObject_GetAttrString(of, name)) {
+    if (!o) throw PyError{};
+  }
+  ~Attr() { Py_DECREF(o); }
+  Attr(const Attr&) = delete;
+  Attr& operator=(const Attr&) = delete;
+  operator PyObject*() const { return o; }
+};
+// codes [.., n, K/2] and scales of an Mx4
+struct Mx4Ptrs {
+  uint8_t *codes, *scales;
+  Mx4Ptrs(PyObject* q, at::IntArrayRef batch, int64_t n, int64_t K, const std::string& what) {
+    const Attr c(q, "codes"), s(q, "scales"), k(q, "K");
+    if (integer(k) != K) fail(PyExc_ValueError, (what + ".K is " + std::to_string(K)).c_str());
+    at::DimVector shape(batch.begin(), batch.end());
+    shape.append({n, K / 2});
+    codes = typed<uint8_t>(c, at::kByte, shape, what + ".codes");
+    shape.back() = lib.mx4_pitch(K);
+    scales = typed<uint8_t>(s, at::kByte, shape, what + ".scales");
+  }
+};
+
+template <typename Call> PyObject* called(Call call) {
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = call();
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
 // The call with this workspace, or, where it is too small or there is none, minus the bytes that one has to have
 template <typename Call> PyObject* with_workspace(PyObject* workspace, size_t bytes, Call call) {
   if (workspace != Py_None) {
@@ -234,6 +288,105 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// logits, k, score_fn, bias, n_groups, topk_groups, group_score, renorm, scale, routing, workspace, stream
+PyObject* group_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&] {
+    const at::Tensor& logits = matrix(a[0]);
+    const int64_t T = logits.size(0), E = logits.size(1);
+    const int k = int32(a[1]), score_fn = int32(a[2]), groups = int32(a[4]), keep = int32(a[5]), group_score = int32(a[6]), renorm = int32(a[7]);
+    const float scale = real(a[8]);
+    const int dt = dtype_code(logits);
+    const void* const l = address(a[0]);
+    const float* const bias = typed<float>(a[3], at::kFloat, {E}, "bias");
+    const Attr o_idx(a[9], "topk_idx"), o_gates(a[9], "gates"), o_scores(a[9], "scores"), o_counts(a[9], "counts"), o_offsets(a[9], "offsets"),
+        o_perm(a[9], "perm"), o_inv(a[9], "inv_pos");
+    int32_t* const idx = typed<int32_t>(o_idx, at::kInt, {T, k}, "topk_idx");
+    float *const gates = typed<float>(o_gates, at::kFloat, {T, k}, "gates"), *const scores = typed<float>(o_scores, at::kFloat, {T, E}, "scores");
+    int32_t *const counts = typed<int32_t>(o_counts, at::kInt, {E}, "counts"), *const offsets = typed<int32_t>(o_offsets, at::kInt, {E + 1}, "offsets");
+    int32_t *const perm = typed<int32_t>(o_perm, at::kInt, {T * k}, "perm"), *const inv = typed<int32_t>(o_inv, at::kInt, {T, k}, "inv_pos");
+    void* const stream = reinterpret_cast<void*>(integer(a[11]));
+    const auto call = [&](void* ws, size_t bytes) {
+      return lib.group_route(l, dt, bias, (int)T, (int)E, k, score_fn, groups, keep, group_score, renorm, scale, idx, gates, scores, counts, offsets,
+                             perm, inv, ws, bytes, stream);
+    };
+    const size_t bytes = lib.group_route_bytes((int)T, (int)E, k);
+    if (!bytes) return called([&] { return call(nullptr, 0); });
+    return with_workspace(a[10], bytes, call);
+  });
+}
+
+// logits, routing, dgates, score_fn, renorm, scale, dscores, dlogits, workspace (none), stream
+PyObject* group_route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    const at::Tensor& logits = matrix(a[0]);
+    const int64_t T = logits.size(0), E = logits.size(1);
+    const int dt = dtype_code(logits), score_fn = int32(a[3]), renorm = int32(a[4]);
+    const float scale = real(a[5]);
+    const Attr o_idx(a[1], "topk_idx");
+    const int64_t k = matrix(o_idx).size(1);
+    const void* const l = address(a[0]);
+    const int32_t* const idx = typed<int32_t>(o_idx, at::kInt, {T, k}, "topk_idx");
+    const float *const dgates = typed<float>(a[2], at::kFloat, {T, k}, "dgates"), *const dscores = typed<float>(a[6], at::kFloat, {T, E}, "dscores");
+    void* const out = typed<void>(a[7], logits.scalar_type(), {T, E}, "dlogits");
+    void* const stream = reinterpret_cast<void*>(integer(a[9]));
+    return called([&] {
+      return lib.group_route_backward(l, dt, idx, dgates, dscores, (int)T, (int)E, (int)k, score_fn, renorm, scale, out, stream);
+    });
+  });
+}
+
+// x, axis (of the library), out, workspace (none), stream
+PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const at::Tensor& x = tensor(a[0]);
+    if (x.dim() < 2) fail(PyExc_ValueError, "a matrix or a stack of them is expected");
+    const int axis = int32(a[1]), dt = dtype_code(x);
+    const at::IntArrayRef batch = x.sizes().slice(0, x.dim() - 2);
+    const int64_t rows = x.size(-2), cols = x.size(-1), K = axis ? cols : rows;
+    const Mx4Ptrs q(a[2], batch, axis ? rows : cols, K, "out");
+    const void* const from = address(a[0]);
+    void* const stream = reinterpret_cast<void*>(integer(a[4]));
+    return called([&] { return lib.mx4_quantize(from, dt, c10::multiply_integers(batch), rows, cols, axis, q.codes, q.scales, stream); });
+  });
+}
+
+// q, axis, out, workspace (none), stream
+PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const at::Tensor& out = tensor(a[2]);
+    if (out.dim() < 2) fail(PyExc_ValueError, "a matrix or a stack of them is expected");
+    const int axis = int32(a[1]), dt = dtype_code(out);
+    const at::IntArrayRef batch = out.sizes().slice(0, out.dim() - 2);
+    const int64_t rows = out.size(-2), cols = out.size(-1);
+    const Mx4Ptrs q(a[0], batch, axis ? rows : cols, axis ? cols : rows, "q");
+    void* const to = address(a[2]);
+    void* const stream = reinterpret_cast<void*>(integer(a[4]));
+    return called([&] { return lib.mx4_dequantize(q.codes, q.scales, dt, c10::multiply_integers(batch), rows, cols, axis, to, stream); });
+  });
+}
+
+// x, W1, W3, W2, routing, residual, out, workspace, stream
+PyObject* forward_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&] {
+    const at::Tensor& x = matrix(a[0]);
+    const int64_t T = x.size(0), d = x.size(1);
+    const Attr w1_codes(a[1], "codes"), w2_K(a[3], "K"), o_idx(a[4], "topk_idx");
+    const int64_t E = tensor(w1_codes).dim() ? tensor(w1_codes).size(0) : 0, f = integer(w2_K), k = matrix(o_idx).size(1);
+    const Mx4Ptrs W1(a[1], {E}, f, d, "W1"), W3(a[2], {E}, f, d, "W3"), W2(a[3], {E}, d, f, "W2");
+    const Attr o_gates(a[4], "gates"), o_offsets(a[4], "offsets"), o_perm(a[4], "perm"), o_inv(a[4], "inv_pos");
+    const void *const from = typed<void>(a[0], at::kBFloat16, {T, d}, "x"), *const res = typed<void>(a[5], at::kBFloat16, {T, d}, "residual");
+    void* const out = typed<void>(a[6], at::kBFloat16, {T, d}, "out");
+    const float* const gates = typed<float>(o_gates, at::kFloat, {T, k}, "gates");
+    const int32_t *const offsets = typed<int32_t>(o_offsets, at::kInt, {E + 1}, "offsets"), *const perm = typed<int32_t>(o_perm, at::kInt, {T * k}, "perm"),
+                  *const inv = typed<int32_t>(o_inv, at::kInt, {T, k}, "inv_pos");
+    void* const stream = reinterpret_cast<void*>(integer(a[8]));
+    return with_workspace(a[7], lib.forward_mx4_bytes((int)T, (int)d, (int)f, (int)E, (int)k), [&](void* ws, size_t bytes) {
+      return lib.forward_mx4(from, W1.codes, W1.scales, W3.codes, W3.scales, W2.codes, W2.scales, (int)T, (int)d, (int)f, (int)E, (int)k, gates,
+                             offsets, perm, inv, res, out, ws, bytes, stream);
+    });
+  });
+}
+
 // path of the library, which is loaded already
 PyObject* bind(PyObject*, PyObject* path) {
   const char* p = PyUnicode_AsUTF8(path);
@@ -246,7 +399,11 @@ PyObject* bind(PyObject*, PyObject* path) {
   };
   if (!find(l.route_bytes, "btx_moe_route_workspace_bytes") || !find(l.route, "btx_moe_route") || !find(l.norm_route, "btx_moe_norm_route") ||
       !find(l.forward_bytes, "btx_moe_ff_forward_workspace_bytes") || !find(l.forward, "btx_moe_ff_forward") ||
-      !find(l.backward_bytes, "btx_moe_ff_backward_workspace_bytes") || !find(l.backward, "btx_moe_ff_backward")) {
+      !find(l.backward_bytes, "btx_moe_ff_backward_workspace_bytes") || !find(l.backward, "btx_moe_ff_backward") ||
+      !find(l.group_route_bytes, "btx_moe_group_route_workspace_bytes") || !find(l.group_route, "btx_moe_group_route") ||
+      !find(l.group_route_backward, "btx_moe_group_route_backward") || !find(l.mx4_pitch, "btx_mx4_scale_pitch") ||
+      !find(l.mx4_quantize, "btx_mx4_quantize") || !find(l.mx4_dequantize, "btx_mx4_dequantize") ||
+      !find(l.forward_mx4_bytes, "btx_moe_ff_forward_mx4_workspace_bytes") || !find(l.forward_mx4, "btx_moe_ff_forward_mx4")) {
     PyErr_Format(PyExc_RuntimeError, "%s does not have the library's entry points", p);
     return nullptr;
   }
@@ -255,7 +412,8 @@ PyObject* bind(PyObject*, PyObject* path) {
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, FAST(route), FAST(norm_route), FAST(forward), FAST(backward), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, FAST(route), FAST(norm_route), FAST(forward), FAST(backward), FAST(group_route),
+                         FAST(group_route_backward), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(forward_mx4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
