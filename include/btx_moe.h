@@ -463,7 +463,8 @@ int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, con
  *           0: blocks down the columns: K = rows, n = cols; codes and scales are [batch, cols, ..].  So are the
  *              experts' weights quantised whose products sum over their rows: W1, W3 [E,d,f] and W2 [E,f,d].
  * Requirements: K a multiple of 32, n >= 0, batch >= 0 (nothing to do where one of them is 0); x, out, codes, scales on
- * 16-byte boundaries.  batch * rows * cols < 2^40.  axis 0: batch <= 65535 and cols <= 4194240 (BTX_ERR_UNSUPPORTED).
+ * 16-byte boundaries.  batch * rows * cols < 2^40.  axis 0: batch <= 65535, cols <= 4194240 and
+ * ceil(rows / 256) * ceil(cols / 64) < 2^24 (BTX_ERR_UNSUPPORTED).
  */
 int64_t btx_mx4_scale_pitch(int64_t K);
 int btx_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, uint8_t* codes,

@@ -2,8 +2,12 @@
 // of an element on one side, 17/32 on the other.
 //   axis 1: blocks lie along the rows.  A thread has 8 consecutive elements, four threads a block: its largest magnitude by two DPP steps.
 //   axis 0: blocks run down the columns, as the expert weights [K, N] are quantised, whose products sum over K; rows of the result
-//           are the columns of the tensor.  A thread has the 32 elements of a block in two neighbouring columns, so the magnitude needs no other
-//           lane; 64 columns x 256 rows go through LDS, so that 128 consecutive bytes of a row of codes are written at once.
+//           are the columns of the tensor.  A thread has 8 rows of 8 neighbouring columns (16 bytes a load or store of bf16), the four
+//           threads of a quad a block of 32 rows in each of them; 64 columns x 256 rows go through LDS, so that 128 consecutive bytes of a
+//           row of codes are moved at once.  Workgroups of neighbouring columns follow each other.  Four matrices [4096, 11008] of bf16
+//           (361 MB, 96 MB of codes and scales): 87 us to 4 bits, 5.2 TB/s, and 68 us back, 6.7 TB/s.  With two columns a thread and
+//           4 bytes a row of them it took 184 and 109 us, the latter also with 16 bytes a row as long as the values were put together
+//           from the codes' bits and not by the conversion.
 #include "mx4.h"
 
 namespace btx {
@@ -70,17 +74,15 @@ __global__ __launch_bounds__(kThreads) void layer_begin_kernel(const bf16_t* __r
   if (e == kThreads - 1) tiles[0] = TileInfo{0, at + n - 1, 0, 0};
 }
 
-// the value of code c
-__device__ __forceinline__ float code_value(uint32_t c) {
-  const uint32_t m = c & 7u;                            // 0 .5 1 1.5 2 3 4 6: an exponent of two bits and one of the mantissa
-  const float mag = m < 2u ? 0.5f * (float)m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
-  return (c & 8u) ? -mag : mag;
-}
 __device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte); }
-// the eight values of a word of codes; bf16: past its range (6 * 2^127 ...) or precision (below 2^-126) rounded once
+// The eight values of a word of codes; bf16: past its range (6 * 2^127 ...) or precision (below 2^-126) rounded once.  The hardware's
+// conversion: exact for every code and every scale, 2^-127 and NaN among them (a test goes through all of them).
 __device__ __forceinline__ void decode8(uint32_t w, float scale, float* v) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3)};
 #pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = code_value(w >> (4 * q) & 15u) * scale;
+  for (int q = 0; q < 8; ++q) v[q] = p[q / 2][q % 2];
 }
 
 template <typename XT>
@@ -97,37 +99,48 @@ __global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const uint32_
 
 // ---- axis 0: [batch, K, N] -> rows [batch, N] of K ------------------------------------------------------------
 constexpr int kCols = 64, kBlocks = 8;                  // columns, blocks of 32 rows of a workgroup: 32 threads x 8
-// grid: (pieces of 256 rows, pieces of 64 columns, batch)
-template <typename XT>
+// Column c's codes of block b, in LDS: the threads that write or read at once, of eight columns' distance or of the same column, are
+// on different banks
+__device__ __forceinline__ int col_piece(int c, int b) { return b ^ (c >> 3 & 7); }
+// Eight neighbouring elements of which n are there
+template <typename XT, bool VEC> __device__ __forceinline__ void load8(const XT* p, int64_t n, float* v) {
+  if constexpr (VEC) {
+    RowVec<XT, 8>::ld_stream(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? Elem<XT>::ld(p + i) : 0.f;
+  }
+}
+// grid: (pieces of 64 columns of 256 rows, the rows' pieces one after another, batch).  VEC: rows of whole 16 bytes.  A thread has 8 rows of 8 neighbouring columns,
+// the four lanes of a quad the 32 rows of a block.
+template <typename XT, bool VEC>
 __global__ __launch_bounds__(kThreads) void quantize_cols_kernel(const XT* __restrict__ x, int64_t K, int64_t N, u32x4* __restrict__ codes,
-                                                                 uint8_t* __restrict__ scales, int64_t pitch) {
-  __shared__ u32x4 s_codes[kCols][kBlocks + 1];
+                                                                 uint8_t* __restrict__ scales, int64_t pitch, unsigned col_pieces) {
+  __shared__ u32x4 s_codes[kCols][kBlocks];
   __shared__ uint8_t s_scales[kCols][kBlocks];
-  const int c = (threadIdx.x & 31) * 2, b = threadIdx.x / 32;
-  const int64_t col = (int64_t)blockIdx.y * kCols + c, blk = (int64_t)blockIdx.x * kBlocks + b, n_blk = K / kMxBlock;
-  const int64_t batch = blockIdx.z;
+  const int quarter = threadIdx.x & 3, c = (threadIdx.x >> 2 & 7) * 8, b = threadIdx.x / 32;
+  const int64_t piece = blockIdx.x / col_pieces, col0 = (int64_t)(blockIdx.x - piece * col_pieces) * kCols, blk0 = piece * kBlocks;
+  const int64_t col = col0 + c, blk = blk0 + b, n_blk = K / kMxBlock, batch = blockIdx.y;
   x += batch * K * N;
-  if (blk < n_blk && col < N) {
-    const XT* from = x + blk * kMxBlock * N + col;
-    const bool both = col + 1 < N;
-    float v[2][kMxBlock];
+  if (blk < n_blk && col < N) {                         // (whole quads)
+    const XT* const from = x + (blk * kMxBlock + quarter * 8) * N + col;
+    float v[8][8];
 #pragma unroll
-    for (int q = 0; q < kMxBlock; ++q) {
-      v[0][q] = Elem<XT>::ld(from + (int64_t)q * N);
-      v[1][q] = both ? Elem<XT>::ld(from + (int64_t)q * N + 1) : 0.f;
-    }
+    for (int q = 0; q < 8; ++q) load8<XT, VEC>(from + (int64_t)q * N, N - col, v[q]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 8; ++h) {
+      float w[8];
       uint32_t amax = 0;
 #pragma unroll
-      for (int q = 0; q < kMxBlock; ++q) amax = max(amax, magnitude(v[h][q]));
+      for (int q = 0; q < 8; ++q) {
+        w[q] = v[q][h];
+        amax = max(amax, magnitude(w[q]));
+      }
+      amax = max(amax, (uint32_t)dpp_i32<kDppXor1>((int)amax));
+      amax = max(amax, (uint32_t)dpp_i32<kDppXor2>((int)amax));
       const uint32_t byte = mx4_scale_byte(amax);
-      const float scale = mx4_scale(byte);
-      u32x4 w;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = byte == 255u ? 0u : mx4_codes8(v[h] + 8 * q, scale);
-      s_codes[c + h][b] = w;
-      s_scales[c + h][b] = (uint8_t)byte;
+      reinterpret_cast<uint32_t*>(&s_codes[c + h][col_piece(c + h, b)])[quarter] = byte == 255u ? 0u : mx4_codes8(w, mx4_scale(byte));
+      if (quarter == 0) s_scales[c + h][b] = (uint8_t)byte;
     }
   }
   __syncthreads();
@@ -136,46 +149,52 @@ __global__ __launch_bounds__(kThreads) void quantize_cols_kernel(const XT* __res
 #pragma unroll
   for (int i = threadIdx.x; i < kCols * kBlocks; i += kThreads) {
     const int q = i % kBlocks;
-    const int64_t n = (int64_t)blockIdx.y * kCols + i / kBlocks, k = (int64_t)blockIdx.x * kBlocks + q;
+    const int64_t n = col0 + i / kBlocks, k = blk0 + q;
     if (n >= N) continue;
-    if (k < n_blk) codes[n * n_blk + k] = s_codes[i / kBlocks][q];
+    if (k < n_blk) codes[n * n_blk + k] = s_codes[i / kBlocks][col_piece(i / kBlocks, q)];
     if (k < pitch) scales[n * pitch + k] = k < n_blk ? s_scales[i / kBlocks][q] : 0;
   }
 }
 
-template <typename XT>
+template <typename XT, bool VEC>
 __global__ __launch_bounds__(kThreads) void dequantize_cols_kernel(const u32x4* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t K, int64_t N,
-                                                                   int64_t pitch, XT* __restrict__ out) {
-  __shared__ u32x4 s_codes[kCols][kBlocks + 1];
+                                                                   int64_t pitch, XT* __restrict__ out, unsigned col_pieces) {
+  __shared__ u32x4 s_codes[kCols][kBlocks];
   __shared__ uint8_t s_scales[kCols][kBlocks];
-  const int64_t n_blk = K / kMxBlock, batch = blockIdx.z;
+  const int64_t n_blk = K / kMxBlock, batch = blockIdx.y;
+  const int64_t piece = blockIdx.x / col_pieces, col0 = (int64_t)(blockIdx.x - piece * col_pieces) * kCols, blk0 = piece * kBlocks;
   codes += batch * N * n_blk;
   scales += batch * N * pitch;
 #pragma unroll
   for (int i = threadIdx.x; i < kCols * kBlocks; i += kThreads) {
     const int q = i % kBlocks;
-    const int64_t n = (int64_t)blockIdx.y * kCols + i / kBlocks, k = (int64_t)blockIdx.x * kBlocks + q;
+    const int64_t n = col0 + i / kBlocks, k = blk0 + q;
     if (n < N && k < n_blk) {
-      s_codes[i / kBlocks][q] = codes[n * n_blk + k];
+      s_codes[i / kBlocks][col_piece(i / kBlocks, q)] = codes[n * n_blk + k];
       s_scales[i / kBlocks][q] = scales[n * pitch + k];
     }
   }
   __syncthreads();
-  const int c = (threadIdx.x & 31) * 2, b = threadIdx.x / 32;
-  const int64_t col = (int64_t)blockIdx.y * kCols + c, blk = (int64_t)blockIdx.x * kBlocks + b;
+  const int quarter = threadIdx.x & 3, c = (threadIdx.x >> 2 & 7) * 8, b = threadIdx.x / 32;
+  const int64_t col = col0 + c, blk = blk0 + b;
   if (blk >= n_blk || col >= N) return;
-  const bool both = col + 1 < N;
-  XT* to = out + batch * K * N + blk * kMxBlock * N + col;
-  const float sc[2] = {scale_value(s_scales[c][b]), both ? scale_value(s_scales[c + 1][b]) : 0.f};
+  XT* const to = out + batch * K * N + (blk * kMxBlock + quarter * 8) * N + col;
+  float v[8][8];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    float v[2][8];
-    decode8(s_codes[c][b][q], sc[0], v[0]);
-    decode8(both ? s_codes[c + 1][b][q] : 0u, sc[1], v[1]);
+  for (int h = 0; h < 8; ++h) {
+    float w[8];                                         // (of columns behind the last one: whatever is there, and not written)
+    decode8(reinterpret_cast<const uint32_t*>(&s_codes[c + h][col_piece(c + h, b)])[quarter], scale_value(s_scales[c + h][b]), w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      Elem<XT>::st(to + (int64_t)(8 * q + j) * N, v[0][j]);
-      if (both) Elem<XT>::st(to + (int64_t)(8 * q + j) * N + 1, v[1][j]);
+    for (int q = 0; q < 8; ++q) v[q][h] = w[q];
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    if constexpr (VEC) {
+      RowVec<XT, 8>::st_stream(to + (int64_t)q * N, v[q]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 8; ++h)
+        if (col + h < N) Elem<XT>::st(to + (int64_t)q * N + h, v[q][h]);
     }
   }
 }
@@ -193,13 +212,18 @@ int launch_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, i
     else
       quantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(static_cast<const float*>(x), n, K, reinterpret_cast<uint32_t*>(codes), scales, pitch);
   } else {
-    const int64_t gx = (pitch + kBlocks - 1) / kBlocks, gy = (cols + kCols - 1) / kCols;
-    if (!grid_fits(gx, kThreads) || gy > 65535 || batch > 65535) return BTX_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)gx, (unsigned)gy, (unsigned)batch);
-    if (dtype == BTX_BF16)
-      quantize_cols_kernel<<<grid, kThreads, 0, s>>>(static_cast<const bf16_t*>(x), K, cols, reinterpret_cast<u32x4*>(codes), scales, pitch);
-    else
-      quantize_cols_kernel<<<grid, kThreads, 0, s>>>(static_cast<const float*>(x), K, cols, reinterpret_cast<u32x4*>(codes), scales, pitch);
+    const int64_t gx = (cols + kCols - 1) / kCols, gy = (pitch + kBlocks - 1) / kBlocks;
+    if (gx > 65535 || !grid_fits(gx * gy, kThreads) || batch > 65535) return BTX_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)(gx * gy), (unsigned)batch);
+    const bool vec = cols % 8 == 0;
+    u32x4* const c = reinterpret_cast<u32x4*>(codes);
+    auto go = [&](auto tag) {
+      using XT = decltype(tag);
+      if (vec) quantize_cols_kernel<XT, true><<<grid, kThreads, 0, s>>>(static_cast<const XT*>(x), K, cols, c, scales, pitch, (unsigned)gx);
+      else quantize_cols_kernel<XT, false><<<grid, kThreads, 0, s>>>(static_cast<const XT*>(x), K, cols, c, scales, pitch, (unsigned)gx);
+    };
+    if (dtype == BTX_BF16) go(bf16_t{});
+    else go(float{});
   }
   BTX_LAUNCH_CHECK();
   return BTX_OK;
@@ -234,12 +258,18 @@ int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype
     if (dtype == BTX_BF16) dequantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(c, scales, n, K, pitch, static_cast<bf16_t*>(out));
     else dequantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(c, scales, n, K, pitch, static_cast<float*>(out));
   } else {
-    const int64_t gx = (K / kMxBlock + kBlocks - 1) / kBlocks, gy = (cols + kCols - 1) / kCols;
-    if (!grid_fits(gx, kThreads) || gy > 65535 || batch > 65535) return BTX_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)gx, (unsigned)gy, (unsigned)batch);
+    const int64_t gx = (cols + kCols - 1) / kCols, gy = (K / kMxBlock + kBlocks - 1) / kBlocks;
+    if (gx > 65535 || !grid_fits(gx * gy, kThreads) || batch > 65535) return BTX_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)(gx * gy), (unsigned)batch);
     const u32x4* const c = reinterpret_cast<const u32x4*>(codes);
-    if (dtype == BTX_BF16) dequantize_cols_kernel<<<grid, kThreads, 0, s>>>(c, scales, K, cols, pitch, static_cast<bf16_t*>(out));
-    else dequantize_cols_kernel<<<grid, kThreads, 0, s>>>(c, scales, K, cols, pitch, static_cast<float*>(out));
+    const bool vec = cols % 8 == 0;
+    auto go = [&](auto tag) {
+      using XT = decltype(tag);
+      if (vec) dequantize_cols_kernel<XT, true><<<grid, kThreads, 0, s>>>(c, scales, K, cols, pitch, static_cast<XT*>(out), (unsigned)gx);
+      else dequantize_cols_kernel<XT, false><<<grid, kThreads, 0, s>>>(c, scales, K, cols, pitch, static_cast<XT*>(out), (unsigned)gx);
+    };
+    if (dtype == BTX_BF16) go(bf16_t{});
+    else go(float{});
   }
   BTX_LAUNCH_CHECK();
   return BTX_OK;

@@ -82,6 +82,7 @@ def test_refusals():
                     dict(batch=1 << 62)):
             assert tensor(fn, **bad) == 1, (fn, bad)
         assert tensor(fn, axis=0, batch=65536) == 2 and tensor(fn, axis=0, batch=1, cols=64 * 65535 + 1) == 2
+        assert tensor(fn, axis=0, batch=1, rows=1 << 26, cols=64 * 64) == 2
     assert [lib.btx_mx4_scale_pitch(K) for K in (32, 512, 544, 1376, 11008, 0, 48, -32)] == [16, 16, 32, 48, 352, 0, 0, 0]
 
     def layer(x=p, W=(p, p, p, p, p, p), T=8, d=64, f=96, E=4, k=2, gates=p, off=p, out=p, res=null, ws=p, nbytes=1 << 30):
@@ -96,6 +97,13 @@ def test_refusals():
     sizes = [lib.btx_moe_ff_forward_mx4_workspace_bytes(T, 4096, 11008, 4, 2) for T in (0, 1, 16, 17, 300, 4096, 16384)]
     assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[1] > 0
     assert lib.btx_moe_ff_forward_mx4_workspace_bytes(8, 48, 64, 4, 2) == 0
+
+
+def test_workspace_never_falls():
+    lib = B.load_library()
+    for d, f, E, k in ((32, 32, 1, 1), (64, 6144, 4, 1), (4096, 1376, 32, 8), (256, 160, 256, 16), (2080, 96, 8, 4)):
+        sizes = [lib.btx_moe_ff_forward_mx4_workspace_bytes(T, d, f, E, k) for T in range(0, 3000)]
+        assert sizes == sorted(sizes) and sizes[1] > 0, (d, f, E, k)
 
 
 def test_binding_refuses_what_does_not_fit():
@@ -178,6 +186,38 @@ def test_quantise_extremes(axis):
 
 
 @gpu
+@pytest.mark.parametrize("shape", [(64, 8), (96, 72), (512, 64), (544, 136), (288, 200), (2, 320, 1376), (3, 32, 8)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantise_columns_of_whole_pieces(shape, dtype):
+    """Blocks down the columns of rows of whole 16 bytes."""
+    rng = rng_of(shape, dtype)
+    x = torch.from_numpy(rng.standard_normal(shape) * np.exp(rng.uniform(-6, 6, (*shape[:-1], 1)))).to(dtype)
+    q, codes, scale = quantise_both(x, -2)
+    same_bytes(q, codes, scale)
+    for to in (torch.bfloat16, torch.float32):
+        back = torch.full(x.shape, float("nan"), dtype=to, device=DEV)
+        B.btx_mx4_dequantize(q, to, -2, out=back)
+        assert np.array_equal(back.cpu().double().numpy(), np.swapaxes(O.mx4_values(codes, scale), -1, -2)), to
+
+
+@gpu
+@pytest.mark.parametrize("axis", [-1, -2])
+@pytest.mark.parametrize("n", [1, 8])
+def test_every_code_under_every_scale(axis, n):
+    K = 32 * 256
+    code = np.tile(np.arange(32) % 16, 256)
+    packed = np.repeat((code[0::2] | code[1::2] << 4)[None], n, 0).astype(np.uint8)
+    scales = np.repeat(np.arange(256, dtype=np.uint8)[None], n, 0)
+    q = B.Mx4(torch.from_numpy(packed).to(DEV), torch.from_numpy(scales).to(DEV), K)
+    value = O.mx4_values(code[None], np.arange(256)[None])[0]
+    for dtype in (torch.float32, torch.bfloat16):
+        want = torch.from_numpy(value).float().to(dtype)    # rounded (and past the range) as every conversion does
+        got = B.btx_mx4_dequantize(q, dtype, axis).cpu()
+        for i in range(n):
+            assert np.array_equal((got[i] if axis == -1 else got[:, i]).double().numpy(), want.double().numpy(), equal_nan=True), (dtype, i)
+
+
+@gpu
 @pytest.mark.parametrize("shape", [(0, 64), (5, 0), (0, 3, 32)])
 def test_quantise_nothing(shape):
     q = B.btx_mx4_quantize(torch.zeros(shape, device=DEV))
@@ -256,6 +296,61 @@ def test_layer(T, d, f, E, k):
 def test_layer_uneven_experts_and_dropped_pairs(T, E, favour, cap):
     """An expert with most of the rows, experts without any, and pairs that a capacity limit has dropped."""
     check_layer(T, 256, 288, E, 2, residual=True, favour=favour, cap=cap, tokens=60)
+
+
+@gpu
+@pytest.mark.parametrize("T,d,f,E,k", [
+    (260, 1024, 1280, 2, 1), (257, 1536, 2048, 3, 2), (200, 1312, 1824, 2, 1), (130, 2336, 768, 2, 1),      # of one to nine k tiles
+    (5, 8224, 64, 2, 1), (50, 8224, 32, 1, 1),                                                              # few rows, long sums
+    (140, 288, 4384, 2, 1), (150, 96, 8224, 2, 1), (257, 64, 6144, 1, 1),                                   # DOWN cut along its sums
+    (4096, 2080, 96, 8, 4), (4096, 64, 2080, 8, 4)])                                                        # more than two rounds of tiles
+def test_layer_of_many_tiles(T, d, f, E, k):
+    check_layer(T, d, f, E, k, residual=T % 2 == 0, tokens=40)
+
+
+@gpu
+@pytest.mark.parametrize("T,d,f,E,k,favour,cap", [(330, 96, 4384, 4, 1, 1, 0), (330, 96, 4384, 4, 2, 3, 90), (2300, 1056, 64, 32, 8, 5, 0),
+                                                  (2300, 64, 1056, 32, 8, 30, 700)])
+def test_layer_of_many_tiles_uneven(T, d, f, E, k, favour, cap):
+    check_layer(T, d, f, E, k, residual=True, favour=favour, cap=cap, tokens=60)
+
+
+@gpu
+@pytest.mark.parametrize("T,d,f,E,k", [(2, 256, 160, 8, 2), (300, 96, 4384, 4, 1), (2048, 1056, 1056, 8, 4)])
+def test_layers_in_graphs_and_on_two_streams(T, d, f, E, k):
+    """Two layers in flight, and each captured, with workspaces of their own; replays on other tokens."""
+    rng = rng_of("two", T, d, f)
+    lib = B.load_library()
+    nbytes = lib.btx_moe_ff_forward_mx4_workspace_bytes(T, d, f, E, k)
+    layers = []
+    for _ in range(2):
+        W = [experts(rng, E, d, f)[0], experts(rng, E, d, f)[0], experts(rng, E, f, d)[0]]
+        x = torch.from_numpy(rng.standard_normal((T, d))).bfloat16().to(DEV)
+        layers.append((x, W, routing_of(rng, T, E, k)[0], torch.empty(nbytes, dtype=torch.uint8, device=DEV), torch.empty_like(x)))
+    want = [B.btx_moe_ff_forward_mx4(x, *W, r) for x, W, r, _, _ in layers]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for (x, W, r, ws, out), s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                B.btx_moe_ff_forward_mx4(x, *W, r, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    for (_, _, _, _, out), w in zip(layers, want):
+        assert torch.equal(out, w)
+    graphs = []
+    for x, W, r, ws, out in layers:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            B.btx_moe_ff_forward_mx4(x, *W, r, out=out, workspace=ws)
+    first = [x.clone() for x, *_ in layers]
+    for i in range(3):
+        for (x, *_), x0 in zip(layers, first):
+            x.copy_(torch.roll(x0, i, 1))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for x, W, r, _, out in layers:
+            assert torch.equal(out, B.btx_moe_ff_forward_mx4(x, *W, r)), i
 
 
 @gpu
