@@ -503,7 +503,7 @@ Mx4Ws carve_mx4(void* ws, int T, int d, int f, int E, int k) {
   w.act_codes = static_cast<uint8_t*>(c.take(R * (f / 2)));
   w.act_scales = static_cast<uint8_t*>(c.take(R * mx4_pitch(f)));
   w.tokens = static_cast<int32_t*>(c.take(R * sizeof(int32_t)));
-  w.tiles = static_cast<TileInfo*>(c.take((1 + (size_t)mx4_most_tiles((int)R, E, 16)) * sizeof(TileInfo)));
+  w.tiles = static_cast<TileInfo*>(c.take((1 + (size_t)mx4_most_tiles((int)R, E, 32)) * sizeof(TileInfo)));
   w.y = c.take(mx4_y_bytes((int64_t)R, d));
   w.bytes = c.used;
   return w;

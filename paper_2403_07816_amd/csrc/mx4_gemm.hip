@@ -34,15 +34,17 @@ struct Mx4Args {
 // ---- few rows: up to 64 rows x 32 columns a workgroup, whose wavefronts share K ---------------------------------
 // Bound by reading the weights.  They go from memory to the registers that the products take, 512 elements of 16 rows a wavefront at a time: in
 // step s lane group g has chunk 4s + g, so that a load covers 64 bytes of a row; of the row's 16 scales a lane picks every fourth.  RB blocks of
-// 16 rows meet each fragment of the weights.  With 4 wavefronts and at most 128 registers three workgroups are on a compute unit and begin and end beside
-// each other (one token, 2 experts of 4096 x 11008: UP with 8 wavefronts, one workgroup at a time, 29 us).
+// 16 rows meet each fragment of the weights.  With 4 wavefronts two or three workgroups are on a compute unit and begin and end beside each
+// other (one token, 2 experts of 4096 x 11008: UP with 8 wavefronts, one workgroup at a time, 29 us).  All loads of a step are under way
+// before its first product: with a block's rows loaded as its turn came, 64 tokens of 32 experts of 4096 x 1376 took 71 us, now 68, and 96
+// tokens of 4 of 4096 x 11008 114 us, now 111.
 constexpr int kFewCols = 32;
 // byte g of each of four words; pick: g | (4 + g) << 8
 __device__ __forceinline__ uint32_t every_fourth(const u32x4& v, uint32_t pick) {
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[3], v[2], pick), __builtin_amdgcn_perm(v[1], v[0], pick), 0x05040100u);
 }
 template <bool UP, int RB, int NW>
-__global__ __launch_bounds__(NW* kWave, RB == 4 ? 2 : 3) void mx4_few_kernel(Mx4Args g) {
+__global__ __launch_bounds__(NW* kWave, UP || RB == 4 ? 2 : 3) void mx4_few_kernel(Mx4Args g) {
   constexpr int PANELS = UP ? 2 : 1;
   __shared__ f32x4 s_sum[NW][RB][PANELS * 2][kWave];
   if ((int)blockIdx.x >= g.tiles[0].row0) return;
@@ -74,28 +76,34 @@ __global__ __launch_bounds__(NW* kWave, RB == 4 ? 2 : 3) void mx4_few_kernel(Mx4
 #pragma unroll 1
   for (int b0 = 16 * wave; b0 < n_blk; b0 += 16 * NW) {
     const int at = b0 + grp;                           // (scale rows are whole 16 bytes; behind K / 32 they are zero)
-    u32x4 wv[PANELS * 2][4];
-    uint32_t ws[PANELS * 2];
+    // all loads before the first product, those of x, which are not memory's, first
+    u32x4 xv[RB][4], x_sc[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      if (rb > 0 && tile.row0 + rb * 16 >= tile.row_end) break;
+      x_sc[rb] = *reinterpret_cast<const u32x4*>(g.a.scales + row[rb] * pitch + b0);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) xv[rb][s] = at + 4 * s < n_blk ? a[(int64_t)row[rb] * n_blk + at + 4 * s] : u32x4{0u, 0u, 0u, 0u};
+    }
+    u32x4 wv[PANELS * 2][4], w_s[PANELS * 2];
 #pragma unroll
     for (int p = 0; p < PANELS * 2; ++p) {
-      ws[p] = every_fourth(*reinterpret_cast<const u32x4*>(w_sc[p] + (sc_row + b0)), pick);
+      w_s[p] = *reinterpret_cast<const u32x4*>(w_sc[p] + (sc_row + b0));
 #pragma unroll
       for (int s = 0; s < 4; ++s)
         wv[p][s] = at + 4 * s < n_blk ? *reinterpret_cast<const u32x4*>(w[p] + (w_row + (at + 4 * s) * 16u)) : u32x4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      if (rb > 0 && tile.row0 + rb * 16 >= tile.row_end) break;
-      const uint32_t xs = every_fourth(*reinterpret_cast<const u32x4*>(g.a.scales + row[rb] * pitch + b0), pick);
-      u32x4 xv[4];
+    for (int p = 0; p < PANELS * 2; ++p) {
+      const uint32_t ws = every_fourth(w_s[p], pick);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) xv[s] = at + 4 * s < n_blk ? a[(int64_t)row[rb] * n_blk + at + 4 * s] : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int p = 0; p < PANELS * 2; ++p) {
-        acc[rb][p] = mfma_mx4<0>(wv[p][0], xv[0], acc[rb][p], ws[p], xs);
-        acc[rb][p] = mfma_mx4<1>(wv[p][1], xv[1], acc[rb][p], ws[p], xs);
-        acc[rb][p] = mfma_mx4<2>(wv[p][2], xv[2], acc[rb][p], ws[p], xs);
-        acc[rb][p] = mfma_mx4<3>(wv[p][3], xv[3], acc[rb][p], ws[p], xs);
+      for (int rb = 0; rb < RB; ++rb) {
+        if (rb > 0 && tile.row0 + rb * 16 >= tile.row_end) break;
+        const uint32_t xs = every_fourth(x_sc[rb], pick);
+        acc[rb][p] = mfma_mx4<0>(wv[p][0], xv[rb][0], acc[rb][p], ws, xs);
+        acc[rb][p] = mfma_mx4<1>(wv[p][1], xv[rb][1], acc[rb][p], ws, xs);
+        acc[rb][p] = mfma_mx4<2>(wv[p][2], xv[rb][2], acc[rb][p], ws, xs);
+        acc[rb][p] = mfma_mx4<3>(wv[p][3], xv[rb][3], acc[rb][p], ws, xs);
       }
     }
   }
@@ -150,8 +158,7 @@ template <bool UP> int launch_few(const Mx4Args& g, int tile_rows, int E, hipStr
     mx4_few_kernel<UP, decltype(rb)::value, decltype(nw)::value><<<dim3((unsigned)tiles, (unsigned)cols), decltype(nw)::value * kWave, 0, s>>>(g);
   };
   auto rows = [&](auto nw) {
-    if (tile_rows == 16) go(std::integral_constant<int, 1>{}, nw);
-    else if (tile_rows == 32) go(std::integral_constant<int, 2>{}, nw);
+    if (tile_rows == 32) go(std::integral_constant<int, 2>{}, nw);
     else go(std::integral_constant<int, 4>{}, nw);
   };
   // 8 wavefronts where each has two pieces of 512 elements or more
@@ -652,14 +659,21 @@ int mx4_prepare() {
   return raise_lds<mx4_tile_kernel<false>>();
 }
 
-// How many rows a row tile has: 256 from 64 rows an expert on average on (rows of x, a tile's rows and their scales are found with 32-bit offsets there).
-// Below, 16, 32 or 64, so that few experts have more rows than the average and a tile's: those read their weights twice.
+// How many rows a row tile has, by the rows an expert has on average and by what there is to multiply.
+//   * 32 or 64, so that few experts have more rows than the average and a tile's: those read their weights twice.  At 24 rows both take the same
+//     (96 tokens, 32 experts of 4096 x 1376, 8 a token: 79 us with 32, 81 with 64), at 16 68 and 74, at 32 125 and 90.  (16 take what 32 do,
+//     down to one token.)
+//   * 256, whose products bound it and not the weights' reading, from 44 (4 experts of 4096 x 11008: 115 us with 64, 102 with 256; at 32
+//     95 and 99), where there is enough for all compute units: one tile of the result there takes as long as 256 of them.  12000 rows by 128
+//     columns of UP or 256 of DOWN: 2 experts of 1024 x 1024 take 31 and 32 us at 1024 rows, 24 and 31 at 768; 4 of 512 x 512 27 and 26
+//     at 2048; 8 of 4096 x 1376 40 and 52 us at 384 rows, 58 and 53 at 512; one of 4096 x 11008 58 and 60 at 96, 82 and 62 at 128.
+//     (Rows of x, a tile's rows and their scales are found with 32-bit offsets there.)
 int mx4_tile_rows(const Mx4Shapes& sh) {
   const int64_t R = (int64_t)sh.T * sh.k, avg = R / sh.E;
-  if (avg >= 64 && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 && (R + 256) * 16 < (int64_t)1 << 32 && sh.d <= 1 << 21 &&
-      sh.f <= 1 << 21)
+  if (avg >= 44 && R * (ceil_div(sh.f, 128) + ceil_div(sh.d, 256)) >= 12000 && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 &&
+      (R + 256) * 16 < (int64_t)1 << 32 && sh.d <= 1 << 21 && sh.f <= 1 << 21)
     return kTileRows;
-  return avg <= 8 ? 16 : avg <= 22 ? 32 : 64;
+  return avg <= 24 ? 32 : 64;
 }
 
 int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const Mx4Shapes& sh, hipStream_t s) {

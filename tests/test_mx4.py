@@ -309,14 +309,29 @@ def test_layer_of_many_tiles(T, d, f, E, k):
 
 
 @gpu
-@pytest.mark.parametrize("T,d,f,E,k,favour,cap", [(330, 96, 4384, 4, 1, 1, 0), (330, 96, 4384, 4, 2, 3, 90), (2300, 1056, 64, 32, 8, 5, 0),
+@pytest.mark.parametrize("T,d,f,E,k", [
+    (870, 1024, 1280, 2, 1), (520, 1536, 2048, 3, 2), (600, 1312, 1824, 2, 1), (840, 2336, 768, 2, 1), (3100, 288, 160, 3, 2), (4100, 32, 32, 2, 2),
+    (350, 288, 4384, 2, 1), (300, 96, 8224, 2, 1), (257, 64, 6144, 1, 1), (1300, 512, 1056, 6, 2)])
+def test_layer_of_tall_tiles(T, d, f, E, k):
+    """Enough rows for the tallest tiles, of one to nine k tiles; sums cut into ranges, and not."""
+    check_layer(T, d, f, E, k, residual=T % 3 == 1, tokens=40)
+
+
+@gpu
+@pytest.mark.parametrize("T,E,k,favour,cap", [(1500, 4, 2, 0, 0), (1500, 8, 2, 7, 0), (1500, 4, 2, 1, 500), (3000, 64, 1, 5, 0), (1200, 4, 3, 2, 257)])
+def test_layer_of_tall_tiles_uneven(T, E, k, favour, cap):
+    check_layer(T, 416, 544, E, k, residual=True, favour=favour, cap=cap, tokens=60)
+
+
+@gpu
+@pytest.mark.parametrize("T,d,f,E,k,favour,cap", [(900, 96, 4384, 4, 1, 1, 0), (900, 96, 4384, 4, 2, 3, 300), (330, 96, 4384, 4, 1, 1, 0), (330, 96, 4384, 4, 2, 3, 90), (2300, 1056, 64, 32, 8, 5, 0),
                                                   (2300, 64, 1056, 32, 8, 30, 700)])
 def test_layer_of_many_tiles_uneven(T, d, f, E, k, favour, cap):
     check_layer(T, d, f, E, k, residual=True, favour=favour, cap=cap, tokens=60)
 
 
 @gpu
-@pytest.mark.parametrize("T,d,f,E,k", [(2, 256, 160, 8, 2), (300, 96, 4384, 4, 1), (2048, 1056, 1056, 8, 4)])
+@pytest.mark.parametrize("T,d,f,E,k", [(2, 256, 160, 8, 2), (400, 96, 4384, 4, 1), (2048, 1056, 1056, 8, 4)])
 def test_layers_in_graphs_and_on_two_streams(T, d, f, E, k):
     """Two layers in flight, and each captured, with workspaces of their own; replays on other tokens."""
     rng = rng_of("two", T, d, f)
