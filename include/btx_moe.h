@@ -409,7 +409,7 @@ int btx_adamw_step(float* master, float* m, float* v, const void* grad, int grad
  *   scores     [T,E]   fp32 s, may be NULL
  *   counts, offsets, perm, inv_pos: as btx_moe_route's (without a capacity limit)
  * Requirements: E <= 256, n_groups <= 16, n_groups divides E, 1 <= k <= min(16, topk_groups * E / n_groups);
- * T*k < 2^31; scale finite.  workspace >= btx_moe_group_route_workspace_bytes(T,E,k) (16-byte aligned; may be NULL
+ * T*k < 2^30; scale finite.  workspace >= btx_moe_group_route_workspace_bytes(T,E,k) (16-byte aligned; may be NULL
  * where that is 0, which it is up to 64 tokens).
  */
 typedef enum { BTX_SCORE_SOFTMAX = 0, BTX_SCORE_SIGMOID = 1 } btx_score_fn;
@@ -428,7 +428,7 @@ int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias,
  *   dscores  [T,E]  fp32, may be NULL: gradient that reaches the scores directly (an auxiliary loss)
  *   dlogits  [T,E]  logits_dtype, out; may alias logits
  * A masked expert's gradient is 0.  Entries of topk_idx outside 0..E-1 are passed over.
- * Requirements: as btx_moe_group_route; no workspace.
+ * Requirements: as btx_moe_group_route, T < 2^28 (BTX_ERR_UNSUPPORTED); no workspace.
  */
 int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int32_t* topk_idx, const float* dgates,
                                  const float* dscores, int T, int E, int k, int score_fn, int renorm, float scale,
@@ -476,12 +476,14 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  * btx_moe_ff_forward_mx4 - the layer of 4-bit experts, for serving (forward only): btx_moe_ff_forward with both
  * operands of every product in microscaled 4-bit floats.  Token rows are quantised along d once each; per expert
  *     act = silu(xq W1_e) * (xq W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
+ *     (but for sums that are cut into ranges, which stay in fp32)
  *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
  *   x [T,d] bf16;  residual [T,d] bf16, may be NULL;  out [T,d] bf16; aliasing as in btx_moe_ff_forward
  *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
  *   btx_mx4_quantize (axis 0) writes them
  *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
- * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, everything on 16-byte boundaries.
+ * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T*k < 2^30, T*k*max(d,f) < 2^40, E*d*f < 2^40; x, residual, out, the weights
+ * and the workspace on 16-byte boundaries.  d and f <= 2097120 (BTX_ERR_UNSUPPORTED).
  */
 size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k);
 int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t* W1_scales, const uint8_t* W3_codes,

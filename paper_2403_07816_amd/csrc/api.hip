@@ -418,6 +418,11 @@ int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, con
                        save_h3, dX, dW1, dW3, dW2, dW_dtype, workspace, workspace_bytes, stream, nullptr, dgates);
 }
 
+namespace {
+// a count of pairs, and the next multiple of what a launch takes at a time, in 32 bits
+bool pairs_ok(int T, int k) { return (int64_t)T * k < (int64_t)1 << 30; }
+}  // namespace
+
 size_t btx_moe_group_route_workspace_bytes(int T, int E, int k) {
   if (T <= 0 || E < 1 || E > kGroupMaxExperts || k < 1 || k > E || k > kGroupMaxK) return 0;
   return group_route_workspace_bytes(T, E);
@@ -429,7 +434,7 @@ int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias,
                         void* stream) {
   if (!dtype_ok(logits_dtype) || T < 0 || E < 1 || E > kGroupMaxExperts || k < 1 || k > kGroupMaxK) return BTX_ERR_INVALID_ARG;
   if (n_groups < 1 || n_groups > kGroupMaxGroups || E % n_groups != 0 || topk_groups < 1 || topk_groups > n_groups) return BTX_ERR_INVALID_ARG;
-  if (k > topk_groups * (E / n_groups) || (int64_t)T * k >= (int64_t)1 << 31) return BTX_ERR_INVALID_ARG;
+  if (k > topk_groups * (E / n_groups) || !pairs_ok(T, k)) return BTX_ERR_INVALID_ARG;
   if (score_fn != BTX_SCORE_SOFTMAX && score_fn != BTX_SCORE_SIGMOID) return BTX_ERR_INVALID_ARG;
   if (group_score != BTX_GROUP_MAX && group_score != BTX_GROUP_TOP2) return BTX_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return BTX_ERR_INVALID_ARG;
@@ -448,7 +453,7 @@ int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias,
 int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int32_t* topk_idx, const float* dgates, const float* dscores,
                                  int T, int E, int k, int score_fn, int renorm, float scale, void* dlogits, void* stream) {
   if (!dtype_ok(logits_dtype) || T < 0 || E < 1 || E > kGroupMaxExperts || k < 1 || k > kGroupMaxK || k > E) return BTX_ERR_INVALID_ARG;
-  if ((int64_t)T * k >= (int64_t)1 << 31) return BTX_ERR_INVALID_ARG;
+  if (!pairs_ok(T, k)) return BTX_ERR_INVALID_ARG;
   if (score_fn != BTX_SCORE_SOFTMAX && score_fn != BTX_SCORE_SIGMOID) return BTX_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return BTX_ERR_INVALID_ARG;
   if (T == 0) return BTX_OK;
@@ -490,7 +495,7 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
 namespace {
 bool mx4_shapes_ok(int T, int d, int f, int E, int k) {
   return T >= 0 && d > 0 && f > 0 && E >= 1 && E <= kMx4MaxExperts && k >= 1 && k <= E && d % kMxBlock == 0 && f % kMxBlock == 0 &&
-         (int64_t)T * k < (int64_t)1 << 31 && (int64_t)T * k * (int64_t)(d > f ? d : f) < (int64_t)1 << 40 &&
+         pairs_ok(T, k) && (int64_t)T * k * (int64_t)(d > f ? d : f) < (int64_t)1 << 40 &&
          (int64_t)E * d * f < (int64_t)1 << 40;
 }
 struct Mx4Ws { uint8_t *x_codes, *x_scales, *act_codes, *act_scales; int32_t* tokens; TileInfo* tiles; void* y; size_t bytes; };
@@ -525,6 +530,7 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
       !workspace)
     return BTX_ERR_INVALID_ARG;
   if (!aligned16(x, W1_codes, W1_scales, W3_codes, W3_scales, W2_codes, W2_scales, residual, out, workspace)) return BTX_ERR_INVALID_ARG;
+  if (std::max(d, f) > kMx4MostColumns) return BTX_ERR_UNSUPPORTED;
   const Mx4Ws w = carve_mx4(workspace, T, d, f, E, k);
   if (workspace_bytes < w.bytes) return BTX_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);

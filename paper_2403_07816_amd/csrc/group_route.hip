@@ -615,7 +615,9 @@ __global__ __launch_bounds__(kBwdThreads) void gate_grads_kernel(const float* __
 }  // namespace
 
 int launch_gate_grads(const float* dg_part, int n_part, const int32_t* inv_pos, int R, float* dgates, hipStream_t s) {
-  gate_grads_kernel<<<ceil_div(R, kBwdTokens), kBwdThreads, 0, s>>>(dg_part, n_part, inv_pos, R, dgates);
+  const int64_t blocks = ((int64_t)R + kBwdTokens - 1) / kBwdTokens;
+  if (!grid_fits(blocks, kBwdThreads)) return BTX_ERR_UNSUPPORTED;
+  gate_grads_kernel<<<(unsigned)blocks, kBwdThreads, 0, s>>>(dg_part, n_part, inv_pos, R, dgates);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
@@ -668,6 +670,7 @@ int launch_group_route(GroupRouteArgs a, hipStream_t s) {
 
 int launch_group_route_bwd(const GroupRouteBwdArgs& a, hipStream_t s) {
   const int lsize = a.dtype == BTX_BF16 ? 2 : 4, blocks = ceil_div(a.T, kBwdTokens);
+  if (!grid_fits(blocks, kBwdThreads)) return BTX_ERR_UNSUPPORTED;
   const bool vec = a.E % 4 == 0 && (((uintptr_t)a.logits | (uintptr_t)a.dlogits) % (4 * lsize)) == 0 && ((uintptr_t)a.dscores & 15) == 0;
   auto go = [&](auto tag, auto score) {
     using XT = decltype(tag);

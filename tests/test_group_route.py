@@ -79,6 +79,7 @@ def test_refusals():
                 dict(l=null), dict(idx=null), dict(gates=null), dict(perm=null), dict(ws=null), dict(l=q), dict(scores=q), dict(ws=q),
                 dict(T=1 << 28, k=8)):
         assert fwd(**bad) == 1, bad
+    assert fwd(T=1 << 30, E=8, k=1, G=1, keep=1) == 1
     assert fwd(nbytes=16) == 3
 
     def bwd(l=p, dt=0, idx=p, dg=p, ds=null, T=100, E=64, k=8, score=0, scale=1.0, dl=p):
@@ -88,6 +89,7 @@ def test_refusals():
     for bad in (dict(dt=2), dict(T=-1), dict(E=257), dict(k=0), dict(k=17), dict(E=4, k=5), dict(score=2), dict(scale=float("nan")), dict(l=null),
                 dict(idx=null), dict(dg=null), dict(dl=null), dict(l=q), dict(ds=q), dict(dl=q), dict(T=1 << 28)):
         assert bwd(**bad) == 1, bad
+    assert bwd(T=(1 << 30) - 1, k=1) == 2 and bwd(T=1 << 30, k=1) == 1
 
     def gates(dt=1, dwt=1, dY=p, dg=p, dW=(p, p, p), s13=64 * 64, T=8, ws=p, nbytes=1 << 30, f=64):
         return lib.btx_moe_ff_backward_gates(dY, p, p, p, p, dt, s13, 64 * 64, T, 64, f, 4, 2, p, p, p, p, p, p, p, dg, *dW, dwt, ws, nbytes, null)
