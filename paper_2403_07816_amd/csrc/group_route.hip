@@ -1,7 +1,7 @@
 // Routing from logits for mixtures of many experts: softmax or sigmoid scores, a bias that only the selection sees, groups of
 // which the best are kept, top-k, renormalised and scaled gates, and the stable grouping of the (token, slot) pairs by expert.
 // Up to 64 tokens one launch, else two:
-//   1. group_select   16 lanes (one DPP row) take a token, four tokens a wavefront, 64 a workgroup at a time: scores, the groups'
+//   1. group_select   16 lanes (one DPP row) take a token, four tokens a wavefront, up to 64 a workgroup at a time: scores, the groups'
 //                     values and ranks, the k largest one after another; then the workgroup ranks its pairs among those of the same
 //                     expert and leaves how many of each it has.
 //   2. group_scatter  every workgroup adds those counts up (of the workgroups before it, and of all) and writes its pairs' places.
@@ -201,6 +201,7 @@ __device__ __forceinline__ void group_pick_f64(const GroupRouteArgs& a, const XT
 // grid: blocks of `tokens` tokens.  LDS: slots of the tokens of a pass; counts of [64 pairs][expert].
 template <typename XT, int P, int SCORE>
 __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteArgs a) {
+  __shared__ u32x4 s_key[kThreadsMost * (P / 4)];                       // of the lanes: [wavefront][four][lane]
   __shared__ int s_slot[kTokPass][kSlots];
   __shared__ int s_idx[kTokPass * kGroupMaxK];                          // of the pass' pairs
   __shared__ uint16_t s_count[kTokPass * kGroupMaxK / kWave][kGroupMaxExperts];
@@ -304,31 +305,45 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
         unsure = mine.group < a.G && !in && above < a.keep;
       }
       // ---- the k largest, and the next ----
-      uint32_t key[P];
+      // A lane's values lie in LDS in fours, whose largest it keeps; only the four that the winner was in is looked at again.  (With all of them
+      // in registers and looked at, 128 instructions a slot and not 50, 16384 tokens of 256 experts took 25 us here, now 22.)
+      u32x4* const fours = s_key + wave * (P / 4) * kWave + lane;
+      uint32_t most[P / 4];
 #pragma unroll
-      for (int i = 0; i < P; ++i) key[i] = i < mine.n ? ordered(v[i]) : 0u;
+      for (int q = 0; q < P / 4; ++q) {
+        u32x4 w;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) w[x] = in && 4 * q + x < mine.n ? ordered(v[4 * q + x]) : 0u;
+        fours[q * kWave] = w;
+        most[q] = max(max(w[0], w[1]), max(w[2], w[3]));
+      }
       int* const slot = s_slot[in_pass];
       for (int j = 0; j <= a.k; ++j) {
-        uint32_t best = key[0];
+        uint32_t best = most[0];
 #pragma unroll
-        for (int i = 1; i < P; ++i) best = max(best, key[i]);
-        best = in ? best : 0u;
+        for (int q = 1; q < P / 4; ++q) best = max(best, most[q]);
         const uint32_t top = row_max_u32(best);
         const uint32_t have = (uint32_t)(__ballot(best == top) >> row_base) & 0xffffu;
         if (sub == __ffs(have) - 1) {                                   // the first lane of those that have it
-          uint32_t hits = 0u;
+          int at = -1;                                                  // none is left
+          if (top) {
+            int q = 0;
 #pragma unroll
-          for (int i = P - 1; i >= 0; --i) {
-            const bool hit = key[i] == top;
-            hits = hits + hits + hit;
-            key[i] = hit ? 0u : key[i];
-          }
-          const uint32_t more = hits & (hits - 1u);                     // equal values: the first one only
-          if (more) {
+            for (int z = P / 4 - 1; z > 0; --z) q = most[z] == top ? z : q;
+            q = most[0] == top ? 0 : q;
+            u32x4 w = fours[q * kWave];
+            int x = 3;
 #pragma unroll
-            for (int i = 0; i < P; ++i) key[i] = more >> i & 1 ? top : key[i];
+            for (int z = 2; z >= 0; --z) x = w[z] == top ? z : x;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) w[z] = z == x ? 0u : w[z];      // of equal ones the first
+            reinterpret_cast<uint32_t*>(&fours[q * kWave])[x] = 0u;
+            const uint32_t next = max(max(w[0], w[1]), max(w[2], w[3]));
+#pragma unroll
+            for (int z = 0; z < P / 4; ++z) most[z] = z == q ? next : most[z];
+            at = mine.first + 4 * q + x;
           }
-          slot[j] = top ? mine.first + __ffs(hits) - 1 : -1;            // -1: none is left
+          slot[j] = at;
         }
       }
       wave_lds_fence();
@@ -365,7 +380,7 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
         const float l_last = __shfl(ls, at, kWave), least = __shfl(ve - room, at, kWave);
         const bool here = in && __shfl((int)tied, at, kWave);
 #pragma unroll
-        for (int i = 0; i < P; ++i) if (here && key[i]) unsure |= load_logit(from + i) != l_last && !(v[i] < least);
+        for (int i = 0; i < P; ++i) if (here && reinterpret_cast<const uint32_t*>(&fours[i / 4 * kWave])[i % 4]) unsure |= load_logit(from + i) != l_last && !(v[i] < least);
       }
       unsigned long long again = __ballot(unsure && live);
       if (again) {
@@ -445,6 +460,9 @@ __global__ __launch_bounds__(kScatterThreads) void group_scatter_kernel(GroupRou
   __shared__ __attribute__((aligned(16))) int s_part[kSegs][kGroupMaxExperts], s_upto[kSegs][kGroupMaxExperts];
   __shared__ int s_base[kGroupMaxExperts], s_off[kGroupMaxExperts], s_wave[kGroupMaxExperts / kWave];
   const int e4 = threadIdx.x % kFours * 4, seg = threadIdx.x / kFours;
+  const size_t p1 = min((size_t)(blockIdx.x + 1) * a.tokens * a.k, (size_t)a.T * a.k);
+  size_t p = (size_t)blockIdx.x * a.tokens * a.k + threadIdx.x;
+  int pair_e = p < p1 ? a.topk_idx[p] : 0, rank = p < p1 ? a.inv_pos[p] : 0;   // (under way while the counts are added up)
   u32x4 all{0, 0, 0, 0}, upto{0, 0, 0, 0};
   if (e4 < a.E) {
 #pragma unroll 16
@@ -472,11 +490,15 @@ __global__ __launch_bounds__(kScatterThreads) void group_scatter_kernel(GroupRou
     s_off[x] = n;
   }
   __syncthreads();
-  const size_t p0 = (size_t)blockIdx.x * a.tokens * a.k, p1 = min(p0 + (size_t)a.tokens * a.k, (size_t)a.T * a.k);
-  for (size_t p = p0 + threadIdx.x; p < p1; p += blockDim.x) {
-    const int pos = s_off[a.topk_idx[p]] + a.inv_pos[p];
+  while (p < p1) {
+    const int pos = s_off[pair_e] + rank;
     a.inv_pos[p] = pos;
     a.perm[pos] = (int32_t)p;
+    p += blockDim.x;
+    if (p < p1) {
+      pair_e = a.topk_idx[p];
+      rank = a.inv_pos[p];
+    }
   }
 }
 
@@ -622,14 +644,23 @@ int launch_gate_grads(const float* dg_part, int n_part, const int32_t* inv_pos, 
   return BTX_OK;
 }
 
-// tokens of a workgroup: 64, or more where that would be over 512 workgroups, whose counts every workgroup of the second launch adds up
-static int block_tokens(int T) { return T <= 512 * kTokPass ? kTokPass : ceil_div(ceil_div(T, 512), kTokPass) * kTokPass; }
-
-static int hist_pitch(int E) { return (E + 3) & ~3; }            // (whole pieces of 16 bytes)
+// Tokens of a workgroup: up to 64 tokens one workgroup does without the second launch.  Then 16, one wavefront a SIMD, as long as there are compute
+// units for them (301 tokens of 60 experts: 9.5 us with 16, 11.3 with 64; 1024 of 256 13.9 and 17.6), 32 and 64, and more where that would be over
+// 512 workgroups, whose counts every workgroup of the second launch adds up.
+constexpr int kFullChip = 256, kMostBlocks = 512;
+static int block_tokens(int T) {
+  if (T <= kTokPass) return kTokPass;
+  for (int n = 16; n < kTokPass; n *= 2)
+    if (T <= kFullChip * n) return n;
+  return T <= kMostBlocks * kTokPass ? kTokPass : ceil_div(ceil_div(T, kMostBlocks), kTokPass) * kTokPass;
+}
+static int hist_pitch(int E) { return (E + 3) & ~3; }    // (whole pieces of 16 bytes)
 
 size_t group_route_workspace_bytes(int T, int E) {
+  if (T <= kTokPass) return 0;
   // (of the most workgroups that fewer tokens have: never less for more tokens)
-  return T > kTokPass ? (size_t)std::min(512, ceil_div(T, kTokPass)) * hist_pitch(E) * sizeof(int) : 0;
+  const int blocks = std::max(std::min(kFullChip, ceil_div(T, 16)), std::min(kMostBlocks, ceil_div(T, kTokPass)));
+  return (size_t)blocks * hist_pitch(E) * sizeof(int);
 }
 
 int launch_group_route(GroupRouteArgs a, hipStream_t s) {
