@@ -42,7 +42,7 @@ struct Mx4Shapes { int T, d, f, E, k; };
 struct Mx4Matrix { const uint8_t* codes; const uint8_t* scales; };
 struct TileInfo { int e, row0, row_end, unused; };      // of an expert's rows the tile has those from row0 on, row_end is the expert's end
 inline int mx4_most_tiles(int R, int E, int tile_rows) { return (int)std::min<int64_t>((int64_t)R / tile_rows + std::min(E, R), R); }
-// Rows of a row tile: 256 (the products take tiles of them; x and act have their scales in another order then, mx4_scale_at()), 64, 32 or 16
+// Rows of a row tile: 256 (the products take tiles of them; x and act have their scales in another order then, mx4_scale_at()), 64 or 32
 int mx4_tile_rows(const Mx4Shapes& sh);
 // Where the scale of block b of a row is in that order: 16 bytes of every row for 16 blocks (two k tiles), in them those of blocks 2g, 2g + 1,
 // 8 + 2g and 9 + 2g together, which lane group g takes.

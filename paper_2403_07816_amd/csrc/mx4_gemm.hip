@@ -182,6 +182,8 @@ template <bool UP> int launch_few(const Mx4Args& g, int tile_rows, int E, hipStr
 //     (mx4_scale_at()) in which the four of two k tiles are one word, and 16 bytes of every row for two k tiles beside each other.  (With
 //     A's like B's, 12 words a lane and two k tiles dealt out by v_permlane32_swap and v_perm, the products of a k tile waited 260 cycles for it.)
 //   * Tiles are dealt so that the ones an XCD runs at a time share row and column panels in its L2.
+//   * Of a tile's rows that an expert does not have, 64 of a wavefront's are passed over, their reads and their products; the other wavefront of the SIMD
+//     goes on sooner (96 tokens of 4 experts of 4096 x 11008 108 us -> 92, 192 of 32 of 4096 x 1376 117 -> 95, 301 of the former 121 -> 116).
 __device__ __forceinline__ void copy16(uint64_t base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory");
 }
@@ -410,10 +412,15 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       // ---- memory phase
-      read_a(odd, h);
+      const bool live = row0 + wm * 128 + h * 64 < row_end;    // (of this half of its rows any: a phase without products is short)
+      if (live) {
+        read_a(odd, h);
+        if (h == 0) {
+          read_b(odd);
+          read_scales(kt, !odd);
+        }
+      }
       if (h == 0) {
-        read_b(odd);
-        read_scales(kt, !odd);
         if (kt + 1 < nk) copy_a1(kt + 1, a_from - kTileK / 2);
       } else {
         if (kt + 2 < nk) {
@@ -450,6 +457,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
       // ---- compute phase
+      if (live) {
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -460,6 +468,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
             c = st == 0 ? mfma_mx4<0, 2 * odd>(fb[j][0], fa[i][0], c, xb[j], xa[h * 4 + i])
                         : mfma_mx4<1, 2 * odd + 1>(fb[j][1], fa[i][1], c, xb[j], xa[h * 4 + i]);
           }
+      }
 #pragma unroll
       for (int i = 0; i < TM / 2; ++i)                   // here, and not where the sums are needed next: behind the next phases' barriers
 #pragma unroll
@@ -664,16 +673,16 @@ int mx4_prepare() {
 //   * 32 or 64, so that few experts have more rows than the average and a tile's: those read their weights twice.  At 24 rows both take the same
 //     (96 tokens, 32 experts of 4096 x 1376, 8 a token: 79 us with 32, 81 with 64), at 16 68 and 74, at 32 125 and 90.  (16 take what 32 do,
 //     down to one token.)
-//   * 256, whose products bound it and not the weights' reading, from 44 (4 experts of 4096 x 11008: 115 us with 64, 102 with 256; at 32
-//     95 and 99), where there is enough for all compute units: one tile of the result there takes as long as 256 of them.  12000 rows by 128
-//     columns of UP or 256 of DOWN: 2 experts of 1024 x 1024 take 31 and 32 us at 1024 rows, 24 and 31 at 768; 4 of 512 x 512 27 and 26
-//     at 2048; 8 of 4096 x 1376 40 and 52 us at 384 rows, 58 and 53 at 512; one of 4096 x 11008 58 and 60 at 96, 82 and 62 at 128.
+//   * 256 from 32 (4 experts of 4096 x 11008: 95 us with 64, 89 with 256; at 24 86 and 89; 32 of 4096 x 1376 90 and 94, at 48 102 and 96; 64 of
+//     1024 x 2048 80 and 68), where there is enough to multiply: a tile of the result takes as long alone as 256 of them beside each other.
+//     Either 12000 rows by 128 columns of UP or 256 of DOWN, or 2.3 10^9 products, as fewer tiles of long sums have:  2 experts of 1024 x 1024 at 768
+//     rows 24 and 32 us, at 1024 31 and 32; 4 of 512 x 512 at 1024 rows 20 and 26, at 2048 27 and 26; 8 of 4096 x 1376 at 384 rows 40
+//     and 45, at 512 57 and 47; one of 4096 x 11008 at 44 42 and 47, at 64 59 and 49; 2 at 88 70 and 52.
 //     (Rows of x, a tile's rows and their scales are found with 32-bit offsets there.)
 int mx4_tile_rows(const Mx4Shapes& sh) {
   const int64_t R = (int64_t)sh.T * sh.k, avg = R / sh.E;
-  if (avg >= 44 && R * (ceil_div(sh.f, 128) + ceil_div(sh.d, 256)) >= 12000 && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 &&
-      (R + 256) * 16 < (int64_t)1 << 32)
-    return kTileRows;
+  const bool enough = R * (ceil_div(sh.f, 128) + ceil_div(sh.d, 256)) >= 12000 || R * sh.d * (int64_t)sh.f >= (int64_t)2300000000;
+  if (avg >= 32 && enough && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 && (R + 256) * 16 < (int64_t)1 << 32) return kTileRows;
   return avg <= 24 ? 32 : 64;
 }
 

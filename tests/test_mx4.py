@@ -313,7 +313,8 @@ def test_layer_of_many_tiles(T, d, f, E, k):
 @gpu
 @pytest.mark.parametrize("T,d,f,E,k", [
     (870, 1024, 1280, 2, 1), (520, 1536, 2048, 3, 2), (600, 1312, 1824, 2, 1), (840, 2336, 768, 2, 1), (3100, 288, 160, 3, 2), (4100, 32, 32, 2, 2),
-    (350, 288, 4384, 2, 1), (300, 96, 8224, 2, 1), (257, 64, 6144, 1, 1), (1300, 512, 1056, 6, 2)])
+    (350, 288, 4384, 2, 1), (300, 96, 8224, 2, 1), (257, 64, 6144, 1, 1), (1300, 512, 1056, 6, 2),
+    (1300, 512, 1056, 32, 1), (4000, 64, 224, 64, 2), (2500, 96, 1824, 14, 1)])        # tiles of which an expert has a quarter, half, three quarters
 def test_layer_of_tall_tiles(T, d, f, E, k):
     """Enough rows for the tallest tiles, of one to nine k tiles; sums cut into ranges, and not."""
     check_layer(T, d, f, E, k, residual=T % 3 == 1, tokens=40)
