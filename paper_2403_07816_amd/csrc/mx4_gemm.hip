@@ -534,6 +534,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
     if constexpr (UP) {
       // a wavefront's 32 columns are one block; codes [256 rows][64 bytes] and scales [256][4] are put together in LDS
       char* const s_scales = out + 256 * 64;
+      if (more) start();                                 // (behind the activations: 301 tokens of 4 experts of 4096 x 11008 70 us, now 66)
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         const int row = wm * 128 + i * 16 + r;
@@ -559,7 +560,6 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void mx4_tile_kernel(Mx4Args 
         }
         if (lg == 0) s_scales[row * 4 + wn] = out_col0 + wn * 32 < g.N ? (char)byte : 0;
       }
-      if (more) start();
       __syncthreads();
       const int64_t out_row = g.N / 2, out_pitch = mx4_pitch(g.N);
 #pragma unroll
