@@ -93,8 +93,8 @@ int btx_version(void);
 
 /* One-time set-up on the CURRENT device: raises the dynamic-LDS limit of every expert-GEMM
  * kernel (they use all 160 KB of a compute unit's LDS).  Optional: the first bf16 call of
- * btx_moe_ff_forward / btx_moe_ff_backward on a device does the same by itself, but that
- * set-up cannot be recorded into a HIP graph, so a caller that captures its very first step
+ * btx_moe_ff_forward / btx_moe_ff_backward, and btx_moe_ff_forward_mx4's first, on a device does
+ * the same by itself, but that set-up cannot be recorded into a HIP graph, so a caller that captures its very first step
  * calls btx_init() before beginning the capture (once per device that it uses).  It also
  * looks up the device address of btx_moe_route_noalloc's fixed workspace.
  * Idempotent.  Errors: BTX_ERR_HIP. */
@@ -106,9 +106,11 @@ int btx_init(void);
  * kernels on the caller's stream, so that single kernels can be timed inside the real
  * sequence.  n_pairs = 0 switches it off.  Stage ids: */
 enum {
-  BTX_STAGE_ROUTE = 0,        /* btx_moe_route: its two or four kernels            */
+  BTX_STAGE_ROUTE = 0,        /* btx_moe_route: its two or four kernels;
+                                 btx_moe_group_route: its one or two              */
   BTX_STAGE_GATHER_X = 1,     /* forward: x -> expert-grouped rows (bf16, only when
-                                  x has 2^32 bytes or more: else UP reads x itself)  */
+                                  x has 2^32 bytes or more: else UP reads x itself);
+                                  4-bit experts: x quantised                         */
   BTX_STAGE_UP = 2,           /* forward: xs W1, xs W3, SwiGLU; small fp32 layers:
                                   and the work of DOWN, which is then empty          */
   BTX_STAGE_DOWN = 3,         /* forward: act W2                                   */
@@ -125,7 +127,8 @@ enum {
   BTX_STAGE_DW2 = 10,         /* backward: dW2                                     */
   BTX_STAGE_ROUTER_BWD = 11,  /* backward: router gradients and final dX (small
                                   batches: its first part runs beside the weight
-                                  gradients)                                        */
+                                  gradients); for gates of another router dgates
+                                  (dX: COMBINE); btx_moe_group_route_backward        */
   BTX_STAGE_NORM_BWD = 12,    /* btx_rmsnorm_backward: both kernels                */
   BTX_STAGE_COUNT = 13
 };
@@ -440,7 +443,7 @@ int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int
  * x's gradient is the caller's (for btx_moe_group_route: dlogits W_router^T).
  *   dX     [T,d]  dtype  out: through the experts alone
  *   dgates [T,k]  fp32   out: <dY[t], FF_{idx[t,j]}(x[t])>; 0 for a dropped pair
- * The other arguments, limits and the workspace's size as btx_moe_ff_backward's.
+ * The other arguments, limits and the workspace's size as btx_moe_ff_backward's; T < 2^26 (BTX_ERR_UNSUPPORTED).
  */
 int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype,
                               int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d, int f, int E, int k,
@@ -482,7 +485,7 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
  *   btx_mx4_quantize (axis 0) writes them
  *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
- * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T*k < 2^30, T*k*max(d,f) < 2^40, E*d*f < 2^40; x, residual, out, the weights
+ * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T < 2^26, T*k < 2^28 - 256, T*k*max(d,f) < 2^40, E*d*f < 2^40; x, residual, out, the weights
  * and the workspace on 16-byte boundaries.  d and f <= 2097120 (BTX_ERR_UNSUPPORTED).
  */
 size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k);

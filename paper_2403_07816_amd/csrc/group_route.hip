@@ -624,21 +624,20 @@ __global__ __launch_bounds__(kBwdThreads) void group_route_bwd_kernel(GroupRoute
 __global__ __launch_bounds__(kBwdThreads) void gate_grads_kernel(const float* __restrict__ part, int n_part, const int32_t* __restrict__ inv_pos, int R,
                                                                  float* __restrict__ dgates) {
   const int sub = threadIdx.x & (kLanes - 1);
-  const int64_t p = (int64_t)blockIdx.x * kBwdTokens + threadIdx.x / kLanes;
-  if (p >= R) return;
-  const int r = inv_pos[p];
-  float sum = 0.f;
-  if (r >= 0)
-    for (int i = sub; i < n_part; i += kLanes) sum += part[(size_t)r * n_part + i];
-  sum = row_sum_f32(sum);
-  if (sub == 0) dgates[p] = sum;
+  for (int64_t p = (int64_t)blockIdx.x * kBwdTokens + threadIdx.x / kLanes; p < R; p += (int64_t)gridDim.x * kBwdTokens) {
+    const int r = inv_pos[p];
+    float sum = 0.f;
+    if (r >= 0)
+      for (int i = sub; i < n_part; i += kLanes) sum += part[(size_t)r * n_part + i];
+    sum = row_sum_f32(sum);
+    if (sub == 0) dgates[p] = sum;
+  }
 }
 
 }  // namespace
 
 int launch_gate_grads(const float* dg_part, int n_part, const int32_t* inv_pos, int R, float* dgates, hipStream_t s) {
-  const int64_t blocks = ((int64_t)R + kBwdTokens - 1) / kBwdTokens;
-  if (!grid_fits(blocks, kBwdThreads)) return BTX_ERR_UNSUPPORTED;
+  const int64_t blocks = std::min<int64_t>(((int64_t)R + kBwdTokens - 1) / kBwdTokens, 1 << 20);
   gate_grads_kernel<<<(unsigned)blocks, kBwdThreads, 0, s>>>(dg_part, n_part, inv_pos, R, dgates);
   BTX_LAUNCH_CHECK();
   return BTX_OK;

@@ -38,8 +38,9 @@ struct Mx4Args {
 // other (one token, 2 experts of 4096 x 11008: UP with 8 wavefronts, one workgroup at a time, 29 us).  All loads of a step are under way
 // before its first product: with a block's rows loaded as its turn came, 64 tokens of 32 experts of 4096 x 1376 took 71 us, now 68, and 96
 // tokens of 4 of 4096 x 11008 114 us, now 111.
-constexpr int kFewCols = 32, kFewMostThreads = 8 * kWave;
-static_assert(kMx4MostColumns / kFewCols <= 65535, "rows of the grid");
+constexpr int kFewCols = 32, kFewMostWaves = 8;
+// (tiles of 32 rows only where R < 25 E)
+static_assert(kMx4MostColumns / kFewCols <= 65535 && (kMx4MostRows / 64 + kMx4MaxExperts + 0ll) * kFewMostWaves * kWave < 1ll << 32, "the grid");
 // byte g of each of four words; pick: g | (4 + g) << 8
 __device__ __forceinline__ uint32_t every_fourth(const u32x4& v, uint32_t pick) {
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[3], v[2], pick), __builtin_amdgcn_perm(v[1], v[0], pick), 0x05040100u);
@@ -154,7 +155,6 @@ __global__ __launch_bounds__(NW* kWave, UP || RB == 4 ? 2 : 3) void mx4_few_kern
 
 template <bool UP> int launch_few(const Mx4Args& g, int tile_rows, int E, hipStream_t s) {
   const int tiles = mx4_most_tiles(g.R, E, tile_rows), cols = g.N / kFewCols;
-  if (!grid_fits(tiles, kFewMostThreads)) return BTX_ERR_UNSUPPORTED;
   auto go = [&](auto rb, auto nw) {
     mx4_few_kernel<UP, decltype(rb)::value, decltype(nw)::value><<<dim3((unsigned)tiles, (unsigned)cols), decltype(nw)::value * kWave, 0, s>>>(g);
   };
@@ -647,8 +647,7 @@ int down_slices(const Mx4Args& g, const Mx4Shapes& sh) {
 template <bool UP> int launch_tiles(const Mx4Args& g, int E, hipStream_t s) {
   if (int rc = raise_lds<mx4_tile_kernel<UP>>()) return rc;
   const int n_ct = ceil_div(g.N, UP ? 128 : 256);
-  const int64_t tiles = ((int64_t)mx4_most_tiles(g.R, E, kTileRows) * n_ct + kXcds) * g.slices;
-  if (tiles >= (int64_t)1 << 30) return BTX_ERR_UNSUPPORTED;
+  const int64_t tiles = ((int64_t)mx4_most_tiles(g.R, E, kTileRows) * n_ct + kXcds) * g.slices;      // (R N < 2^40: fewer than 2^26)
   // A workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end.  Of less than two
   // rounds each has its own: a few ids name no tile, and their compute units take the ones behind the 256th.
   const int64_t grid = tiles <= 2 * kTileGrid ? tiles : kTileGrid;
@@ -682,7 +681,7 @@ int mx4_prepare() {
 int mx4_tile_rows(const Mx4Shapes& sh) {
   const int64_t R = (int64_t)sh.T * sh.k, avg = R / sh.E;
   const bool enough = R * (ceil_div(sh.f, 128) + ceil_div(sh.d, 256)) >= 12000 || R * sh.d * (int64_t)sh.f >= (int64_t)2300000000;
-  if (avg >= 32 && enough && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32 && (R + 256) * 16 < (int64_t)1 << 32) return kTileRows;
+  if (avg >= 32 && enough && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32) return kTileRows;
   return avg <= 24 ? 32 : 64;
 }
 

@@ -97,7 +97,7 @@ def test_refusals():
     assert gates(T=0) == 0
     for bad in (dict(dt=3), dict(dt=0, dwt=1), dict(dY=null), dict(dg=null), dict(dW=(p, null, p)), dict(s13=8), dict(ws=null), dict(f=60), dict(dY=q)):
         assert gates(**bad) == 1, bad
-    assert gates(nbytes=0) == 3
+    assert gates(nbytes=0) == 3 and gates(T=1 << 26) == 2
 
 
 def test_workspace_never_falls():

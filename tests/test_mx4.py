@@ -94,7 +94,8 @@ def test_refusals():
                 dict(W=(p, p, q, p, p, p))):
         assert layer(**bad) == 1, bad
     assert layer(nbytes=64) == 3
-    assert layer(T=1 << 30, k=1, d=32, f=32) == 1
+    assert layer(T=1 << 30, k=1, d=32, f=32) == 1 and layer(T=1 << 26, k=1, d=32, f=32) == 1
+    assert layer(T=(1 << 24) + 1, k=16, E=16, d=32, f=32) == 1
     assert layer(d=2097152, E=1, k=1) == 2 and layer(f=2097152, E=1, k=1) == 2
     sizes = [lib.btx_moe_ff_forward_mx4_workspace_bytes(T, 4096, 11008, 4, 2) for T in (0, 1, 16, 17, 300, 4096, 16384)]
     assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[1] > 0
