@@ -431,7 +431,7 @@ int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias,
  *   dscores  [T,E]  fp32, may be NULL: gradient that reaches the scores directly (an auxiliary loss)
  *   dlogits  [T,E]  logits_dtype, out; may alias logits
  * A masked expert's gradient is 0.  Entries of topk_idx outside 0..E-1 are passed over.
- * Requirements: as btx_moe_group_route, T < 2^28 (BTX_ERR_UNSUPPORTED); no workspace.
+ * Requirements: as btx_moe_group_route, T <= 2^28 - 16 (BTX_ERR_UNSUPPORTED); no workspace.
  */
 int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int32_t* topk_idx, const float* dgates,
                                  const float* dscores, int T, int E, int k, int score_fn, int renorm, float scale,
@@ -486,7 +486,8 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  *   btx_mx4_quantize (axis 0) writes them
  *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
  * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T < 2^26, T*k < 2^28 - 256, T*k*max(d,f) < 2^40, E*d*f < 2^40; x, residual, out, the weights
- * and the workspace on 16-byte boundaries.  d and f <= 2097120 (BTX_ERR_UNSUPPORTED).
+ * and the workspace on 16-byte boundaries.  d and f <= 2097120, T * btx_mx4_scale_pitch(d) < 2^30
+ * (BTX_ERR_UNSUPPORTED).
  */
 size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k);
 int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t* W1_scales, const uint8_t* W3_codes,

@@ -14,6 +14,7 @@ namespace btx {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kMostBlocks = 1 << 22;                // (a launch has fewer than 2^32 threads)
 
 // ---- axis 1: [rows, K] --------------------------------------------------------------------------------------
 // TILES: scales in mx4_scale_at()'s order
@@ -43,7 +44,7 @@ __device__ __forceinline__ void quantize_rows(int64_t block, const XT* __restric
 template <typename XT>
 __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const XT* __restrict__ x, int64_t rows, int64_t K, uint32_t* __restrict__ codes,
                                                                  uint8_t* __restrict__ scales, int64_t pitch) {
-  quantize_rows<XT, false>(blockIdx.x, x, rows, K, codes, scales, pitch);
+  for (int64_t b = blockIdx.x; b * kThreads < rows * pitch * 4; b += gridDim.x) quantize_rows<XT, false>(b, x, rows, K, codes, scales, pitch);
 }
 
 // The layer's first launch: its rows quantised, and beside them (the first blocks) the token of every grouped row and the row tiles
@@ -88,13 +89,13 @@ __device__ __forceinline__ void decode8(uint32_t w, float scale, float* v) {
 template <typename XT>
 __global__ __launch_bounds__(kThreads) void dequantize_rows_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows,
                                                                    int64_t K, int64_t pitch, XT* __restrict__ out) {
-  const int64_t per_row = K / 8, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t r = i / per_row;
-  if (r >= rows) return;
-  const int64_t p = i - r * per_row;
-  float v[8];
-  decode8(codes[i], scale_value(scales[r * pitch + p / 4]), v);
-  RowVec<XT, 8>::st_stream(out + r * K + p * 8, v);
+  const int64_t per_row = K / 8;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * per_row; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t r = i / per_row, p = i - r * per_row;
+    float v[8];
+    decode8(codes[i], scale_value(scales[r * pitch + p / 4]), v);
+    RowVec<XT, 8>::st_stream(out + r * K + p * 8, v);
+  }
 }
 
 // ---- axis 0: [batch, K, N] -> rows [batch, N] of K ------------------------------------------------------------
@@ -205,8 +206,7 @@ int launch_mx4_quantize(const void* x, int dtype, int64_t batch, int64_t rows, i
                         hipStream_t s) {
   const int64_t K = axis == 1 ? cols : rows, pitch = mx4_pitch(K);
   if (axis == 1) {
-    const int64_t n = batch * rows, blocks = (n * pitch * 4 + kThreads - 1) / kThreads;
-    if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
+    const int64_t n = batch * rows, blocks = std::min((n * pitch * 4 + kThreads - 1) / kThreads, kMostBlocks);
     if (dtype == BTX_BF16)
       quantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(static_cast<const bf16_t*>(x), n, K, reinterpret_cast<uint32_t*>(codes), scales, pitch);
     else
@@ -252,8 +252,7 @@ int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype
                           hipStream_t s) {
   const int64_t K = axis == 1 ? cols : rows, pitch = mx4_pitch(K);
   if (axis == 1) {
-    const int64_t n = batch * rows, blocks = (n * (K / 8) + kThreads - 1) / kThreads;
-    if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
+    const int64_t n = batch * rows, blocks = std::min((n * (K / 8) + kThreads - 1) / kThreads, kMostBlocks);
     const uint32_t* const c = reinterpret_cast<const uint32_t*>(codes);
     if (dtype == BTX_BF16) dequantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(c, scales, n, K, pitch, static_cast<bf16_t*>(out));
     else dequantize_rows_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(c, scales, n, K, pitch, static_cast<float*>(out));
