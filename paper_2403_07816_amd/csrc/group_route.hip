@@ -19,6 +19,7 @@ constexpr int kThreadsMost = 1024, kTokPass = kThreadsMost / kLanes;
 constexpr int kSlots = kGroupMaxK + 1;         // the k chosen and the one behind them
 constexpr float kMaskedF = -1e30f;             // value of a masked expert in float
 constexpr float kUlp = 1.1920929e-7f;          // 2^-23
+constexpr float kTiny = 1.1754944e-38f;        // 2^-126: a score below it may be 0 in float
 
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) { return (uint32_t)dpp_i32<CTRL>((int)v); }
 // over the 16 lanes of a row
@@ -88,12 +89,13 @@ template <int SCORE> __device__ __forceinline__ float score_f(float l, const Row
   if (SCORE == BTX_SCORE_SIGMOID) return sigmoid_f(l);
   return l == -INFINITY ? 0.f : __expf(l - st.m) * st.inv;
 }
-// bound of the error, in 2^-23, of a score in float: the argument of exp is rounded (|l| 2^-24 log2(e) of its value, at most), the
-// hardware's exp2 and reciprocal add an ulp each, softmax's sum one for every addition in line (36 at most)
+// bound of the error, in 2^-23 (and kTiny on top of it), of a score in float: the argument of exp is rounded as a product, softmax's also as
+// a difference (half of |l| each, an eighth for the factor), the hardware's exp2 and reciprocal add an ulp each, softmax's sum half a one for every
+// addition in line (36 at most)
 template <int SCORE> __device__ __forceinline__ float score_err(float l, float s) {
   if (l == -INFINITY) return 0.f;
   if (SCORE == BTX_SCORE_SIGMOID) return s * ((1.f - s) * (fabsf(l) + 2.f) + 3.f);
-  return s * (fabsf(l) + 26.f);                                         // l: less the row's largest
+  return s * (1.25f * fabsf(l) + 26.f);                                         // l: less the row's largest
 }
 template <int SCORE> __device__ __forceinline__ float score_err(float l, float s, const RowStat& st) {
   return score_err<SCORE>(SCORE == BTX_SCORE_SOFTMAX && l != -INFINITY ? l - st.m : l, s);
@@ -290,7 +292,7 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
         // errors of the difference of two groups' values: four of scores, the roundings of v (of a lower v than the group's best: what it
         // is lower by makes up for it), of two sums and of the difference
         const float most = row_max_f32(fmaxf(b1 > kMaskedF ? fabsf(b1) : 0.f, b2 > kMaskedF ? fabsf(b2) : 0.f));
-        const float e2 = kUlp * (4.f * all_err + 8.f * most);
+        const float e2 = kUlp * (4.f * all_err + 8.f * most) + 4.f * kTiny;
         const bool two = a.group_score == BTX_GROUP_TOP2 && b2 > kMaskedF;
         const float value = two ? b1 + b2 : b1;
         int above = 0, maybe = 0;                                       // groups that are better, or may be
@@ -368,7 +370,7 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
           const bool last = sub == a.k - 1;                             // behind it any that is left may be the next
           float err = score_err<SCORE>(ls, ss, st) + (last ? all_err : score_err<SCORE>(ln, sn, st));
           err += (ve > kMaskedF ? fabsf(ve) : 0.f) + (vn > kMaskedF ? fabsf(vn) : 0.f);
-          room = kUlp * err;
+          room = kUlp * err + 2.f * kTiny;
           const bool near = !(ve - vn > room), same = ls == ln && be == bn;
           tied = near && same && last && !a.bias;
           unsure |= near && !(same && (!last || tied));                 // (the same value: the lower index, which came first)
@@ -378,7 +380,8 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
         // The last slot's logit once more, left out: of all that are left, only that very logit may be so near.
         const int at = row_base + a.k - 1;
         const float l_last = __shfl(ls, at, kWave), least = __shfl(ve - room, at, kWave);
-        const bool here = in && __shfl((int)tied, at, kWave);
+        const int any = __shfl((int)tied, at, kWave);                   // (of all lanes, those of groups that are out too)
+        const bool here = in && any;
 #pragma unroll
         for (int i = 0; i < P; ++i) if (here && reinterpret_cast<const uint32_t*>(&fours[i / 4 * kWave])[i % 4]) unsure |= load_logit(from + i) != l_last && !(v[i] < least);
       }

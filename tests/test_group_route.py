@@ -183,6 +183,80 @@ def test_route_ties_go_to_the_lower_index(score, G, keep):
 
 @gpu
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("E,k", [(256, 8), (60, 16)])
+def test_route_ties_at_the_last_slot(score, E, k):
+    """Equal logits for the last slot and behind it, and some that differ from them by a step of float."""
+    rng = rng_of("last", score, E)
+    one = np.float32(1.0)
+    values = np.array([one, np.nextafter(one, np.float32(2)), np.nextafter(one, np.float32(0)), 2.0, -1.0], dtype=np.float32)
+    rare = min(k / E, 0.2)                                  # so that the k-th largest is now the one value, now the other
+    for p in ([rare, rare / 2, rare, rare / 4], [rare / 2, rare / 3, rare / 2, rare / 2], [rare / 4, rare, 3 * rare, 0.0]):
+        l = torch.from_numpy(rng.choice(values, (130, E), p=[*p, 1 - sum(p)]))
+        check_route(*route_both(l, k, score, None))
+        check_route(*route_both(l, k, score, None, 4, 3, "max"))
+    check_route(*route_both(torch.from_numpy(rng.standard_normal((130, E))).bfloat16(), k, score, None))
+
+
+@gpu
+@pytest.mark.parametrize("G,keep,gs", [(1, 1, "max"), (4, 2, "max"), (4, 2, "top2")])
+def test_route_of_scores_about_the_least_normal_float(G, keep, gs):
+    """Logits a few steps of float apart whose scores are 0 in float, or nearly: the order of double still."""
+    rng = rng_of("least", G, gs)
+    for base in (-87.33655, -80.0, -95.0, -103.0):
+        step = np.spacing(np.float32(abs(base)))
+        l = base + step * rng.integers(-6, 7, (150, 64))
+        r, o = route_both(torch.from_numpy(l).float(), 8, "sigmoid", None, G, keep, gs, renorm=False)
+        assert np.array_equal(r.topk_idx.cpu().numpy(), o["topk_idx"]), base
+        l[:, 5] = 0.0                                      # the row's largest, and far below it the others
+        r, o = route_both(torch.from_numpy(l).float(), 8, "softmax", None, G, keep, gs, renorm=False)
+        assert np.array_equal(r.topk_idx.cpu().numpy(), o["topk_idx"]), base
+
+
+@gpu
+@pytest.mark.parametrize("gs", ["top2", "max"])
+def test_route_under_a_bias_that_outweighs_the_scores(gs):
+    """Values near 1 of scores near 1 and of scores near 0: what is behind the last slot may be the less exact one."""
+    rng = rng_of("outweighs", gs)
+    one = rng.random(64) < 0.5
+    l = rng.uniform(9, 12, (200, 64)) * np.where(one, -1, 1)
+    bias = torch.from_numpy(np.where(one, 1.0, 0.0)).float()
+    check_route(*route_both(torch.from_numpy(l).float(), 9, "sigmoid", bias))
+    check_route(*route_both(torch.from_numpy(l).float(), 9, "sigmoid", bias, 8, 3, gs))
+    inf = torch.zeros(64)
+    inf[[3, 5, 20, 21, 50]] = float("inf")                 # more groups of an infinite value than are kept
+    check_route(*route_both(torch.from_numpy(l).float(), 4, "sigmoid", inf, 4, 1, gs))
+
+
+@gpu
+def test_route_with_a_bias_on_any_boundary():
+    l = torch.randn(70, 64, generator=torch.Generator().manual_seed(8)).to(DEV)
+    wide = 0.1 * torch.randn(67, generator=torch.Generator().manual_seed(9)).to(DEV)
+    for at in range(4):
+        want = B.btx_moe_group_route(l, 6, bias=wide[at:at + 64].clone(), n_groups=4, topk_groups=2)
+        got = B.btx_moe_group_route(l, 6, bias=wide[at:at + 64], n_groups=4, topk_groups=2)
+        assert all(torch.equal(getattr(got, n), getattr(want, n)) for n in vars(want)), at
+
+
+@gpu
+def test_routes_on_two_streams_at_once():
+    """Two calls in flight, each with its own workspace and outputs."""
+    T, E, k = 5000, 128, 6
+    ls = [torch.randn(T, E, generator=torch.Generator().manual_seed(i)).to(DEV) for i in (1, 2)]
+    want = [B.btx_moe_group_route(l, k, n_groups=4, topk_groups=2) for l in ls]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for l, s in zip(ls, streams):
+            with torch.cuda.stream(s):
+                got.append(B.btx_moe_group_route(l, k, n_groups=4, topk_groups=2))
+    torch.cuda.synchronize()
+    for i, r in enumerate(got):
+        assert all(torch.equal(getattr(r, n), getattr(want[i % 2], n)) for n in vars(r)), i
+
+
+@gpu
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
 @pytest.mark.parametrize("gs", ["top2", "max"])
 def test_route_masked_experts(score, gs):
     rng = rng_of("masked", score, gs)
