@@ -401,8 +401,8 @@ int btx_adamw_step(float* master, float* m, float* v, const void* grad, int grad
  *   n_groups           groups of E / n_groups consecutive experts; 1: no groups
  *   topk_groups        groups kept, 1 <= topk_groups <= n_groups
  *   group_score        btx_group_score (ignored with one group)
- * The selection is that of v and of the groups' values in double precision; ties go to the lower
- * index; topk_idx lists the chosen experts by descending v.  A logit of -inf masks its expert: its
+ * The selection is that of v and of the groups' values in double precision (what differs by no more than its
+ * own rounding may go either way); ties go to the lower index; topk_idx lists the chosen experts by descending v.  A logit of -inf masks its expert: its
  * score is 0 and it is chosen only where the kept groups have fewer than k others (TOP2 adds nothing for a
  * masked one; a group of masked experts only is behind all others).  A NaN logit counts as -inf, +inf as the
  * largest float; whatever the logits hold, a token's experts are in range and distinct.

@@ -17,7 +17,7 @@ constexpr int kLanes = 16;                     // of a token
 constexpr int kTokWave = kWave / kLanes;
 constexpr int kThreadsMost = 1024, kTokPass = kThreadsMost / kLanes;
 constexpr int kSlots = kGroupMaxK + 1;         // the k chosen and the one behind them
-constexpr float kMaskedF = -1e30f;             // value of a masked expert in float
+constexpr float kMaskedF = -INFINITY;          // value of a masked expert
 constexpr float kUlp = 1.1920929e-7f;          // 2^-23
 constexpr float kTiny = 1.1754944e-38f;        // 2^-126: a score below it may be 0 in float
 
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(kThreadsMost) void group_select_kernel(GroupRouteAr
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           s[x] = score_f<SCORE>(l[i + x], st);
-          const float y = fmaxf(s[x] + v[i + x], kMaskedF);             // (also of a NaN)
+          const float y = fmaxf(s[x] + v[i + x], kMaskedF);             // (of a NaN, too)
           v[i + x] = l[i + x] == -INFINITY ? kMaskedF : y;
           b2 = fmaxf(b2, fminf(b1, v[i + x]));
           b1 = fmaxf(b1, v[i + x]);

@@ -222,6 +222,9 @@ def test_route_under_a_bias_that_outweighs_the_scores(gs):
     bias = torch.from_numpy(np.where(one, 1.0, 0.0)).float()
     check_route(*route_both(torch.from_numpy(l).float(), 9, "sigmoid", bias))
     check_route(*route_both(torch.from_numpy(l).float(), 9, "sigmoid", bias, 8, 3, gs))
+    least = torch.from_numpy(rng.choice([0.0, 0.1, -1e30, -1e35, np.finfo(np.float32).min, -np.inf], 64)).float()
+    for k in (4, 14):                                      # experts that a bias all but masks, and the sums with theirs
+        check_route(*route_both(torch.from_numpy(l).float(), k, "sigmoid", least, 16, 6, gs))
     inf = torch.zeros(64)
     inf[[3, 5, 20, 21, 50]] = float("inf")                 # more groups of an infinite value than are kept
     check_route(*route_both(torch.from_numpy(l).float(), 4, "sigmoid", inf, 4, 1, gs))
