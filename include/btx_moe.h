@@ -402,10 +402,11 @@ int btx_adamw_step(float* master, float* m, float* v, const void* grad, int grad
  *   topk_groups        groups kept, 1 <= topk_groups <= n_groups
  *   group_score        btx_group_score (ignored with one group)
  * The selection is that of v and of the groups' values in double precision (what differs by no more than its
- * own rounding may go either way); ties go to the lower index; topk_idx lists the chosen experts by descending v.  A logit of -inf masks its expert: its
- * score is 0 and it is chosen only where the kept groups have fewer than k others (TOP2 adds nothing for a
- * masked one; a group of masked experts only is behind all others).  A NaN logit counts as -inf, +inf as the
- * largest float; whatever the logits hold, a token's experts are in range and distinct.
+ * own rounding may go either way); ties go to the lower index; topk_idx lists the chosen experts by descending
+ * v. A logit of -inf masks its expert: its score is 0 and it is chosen only where the kept groups have fewer
+ * than k others (TOP2 adds nothing for a masked one; a group of masked experts only is behind all others). A
+ * NaN logit counts as -inf, +inf as the largest float; whatever the logits hold, a token's experts are in
+ * range and distinct.
  * Outputs
  *   topk_idx   [T,k]   int32 expert ids
  *   gates      [T,k]   fp32
@@ -485,9 +486,9 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
  *   btx_mx4_quantize (axis 0) writes them
  *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
- * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T < 2^26, T*k < 2^28 - 256, T*k*max(d,f) < 2^40, E*d*f < 2^40; x, residual, out, the weights
- * and the workspace on 16-byte boundaries.  d and f <= 2097120, T * btx_mx4_scale_pitch(d) < 2^30
- * (BTX_ERR_UNSUPPORTED).
+ * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T < 2^26, T*k < 2^28 - 256, T*k*max(d,f) < 2^40,
+ * E*d*f < 2^40; x, residual, out, the weights and the workspace on 16-byte boundaries. d and f <= 2097120, T *
+ * btx_mx4_scale_pitch(d) < 2^30 (BTX_ERR_UNSUPPORTED).
  */
 size_t btx_moe_ff_forward_mx4_workspace_bytes(int T, int d, int f, int E, int k);
 int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t* W1_scales, const uint8_t* W3_codes,
