@@ -677,11 +677,12 @@ int mx4_prepare() {
 //     Either 12000 rows by 128 columns of UP or 256 of DOWN, or 2.3 10^9 products, as fewer tiles of long sums have:  2 experts of 1024 x 1024 at 768
 //     rows 24 and 32 us, at 1024 31 and 32; 4 of 512 x 512 at 1024 rows 20 and 26, at 2048 27 and 26; 8 of 4096 x 1376 at 384 rows 40
 //     and 45, at 512 57 and 47; one of 4096 x 11008 at 44 42 and 47, at 64 59 and 49; 2 at 88 70 and 52.
-//     (Rows of x, a tile's rows and their scales are found with 32-bit offsets there.)
+//     (Rows of x, a tile's rows and their scales are found with 32-bit offsets there: of x, set_sources()'s a_off, the last token's row, 112 bytes
+//     of a chunk and kCopyBias2.)
 int mx4_tile_rows(const Mx4Shapes& sh) {
   const int64_t R = (int64_t)sh.T * sh.k, avg = R / sh.E;
   const bool enough = R * (ceil_div(sh.f, 128) + ceil_div(sh.d, 256)) >= 12000 || R * sh.d * (int64_t)sh.f >= (int64_t)2300000000;
-  if (avg >= 32 && enough && (int64_t)sh.T * (sh.d / 2) + kTileK < (int64_t)1 << 32) return kTileRows;
+  if (avg >= 32 && enough && (int64_t)sh.T * (sh.d / 2) + kTileK / 2 + kCopyBias2 < (int64_t)1 << 32) return kTileRows;
   return avg <= 24 ? 32 : 64;
 }
 

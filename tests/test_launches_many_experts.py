@@ -123,3 +123,15 @@ def test_layer_limits(record):
              (4, 2097120, 2097120, 1, 1), (4, 32, 2097152, 1, 1), (4, 2097152, 32, 1, 1), (1 << 18, 2097120, 64, 2, 2), (1 << 19, 32, 2097120, 1, 1)]
     for case, (rc, found) in zip(cases, record(*[layer(*c) for c in cases])):
         assert (rc == 0 and len(found) == 4 and all(fits(x) for x in found)) or (rc in (1, 2) and not found), (case, rc, found)
+
+
+@pytest.mark.parametrize("T,d,rows", [
+    ((1 << 23) - 3, 1024, 256), ((1 << 23) - 2, 1024, 64), ((1 << 23) - 1, 1024, 64),
+    ((1 << 24) - 8, 512, 256), ((1 << 24) - 2, 512, 64), ((1 << 25) - 16, 256, 256), ((1 << 25) - 3, 256, 64), ((1 << 20) - 1, 8192, 256), (1 << 20, 8192, 64)])
+def test_token_rows_of_tall_tiles_have_offsets_of_32_bits(record, T, d, rows):
+    """A tall tile's lane finds 16 bytes of a token row at row * d/2 + chunk (112 at most) + 1024 from its base."""
+    (rc, found), = record(layer(T, d, 32, 2, 1))
+    assert rc == 0 and len(found) == 4 and all(fits(x) for x in found)
+    assert tile_rows(found) == rows
+    if rows == 256:
+        assert (T - 1) * (d // 2) + 112 + 1024 < 1 << 32
