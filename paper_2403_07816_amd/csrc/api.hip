@@ -295,7 +295,7 @@ int btx_moe_ff_forward(const void* x, const void* W1, const void* W3, const void
     BTX_STAGE(BTX_STAGE_UP, launch_up_swiglu(dtype, xs, W1, W3, offsets, sh, save_h1, save_h3, w.act, w.partial, s));
     BTX_STAGE(BTX_STAGE_DOWN, launch_down(dtype, w.act, W2, offsets, sh, w.y, w.partial, &y_slices, s));
   }
-  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(y, static_cast<const float*>(y_sums), y_slices, gates, inv_pos, residual, out, T, k, d, dtype, s));
+  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(y, static_cast<const float*>(y_sums), y_slices, true, gates, inv_pos, residual, out, T, k, d, dtype, s));
   return BTX_OK;
 }
 
@@ -368,7 +368,7 @@ int backward_impl(const void* dY, const void* x, const void* W1, const void* W3,
     BTX_STAGE(BTX_STAGE_ROUTER_BWD, launch_router_bwd(*router, ds_rides, s));
   } else {
     BTX_STAGE(BTX_STAGE_ROUTER_BWD, launch_gate_grads(w.dg_part, n_part, inv_pos, R, dgates, s));
-    BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.dxs, nullptr, 1, nullptr, inv_pos, nullptr, dX, T, k, d, dtype, s));
+    BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.dxs, nullptr, 1, true, nullptr, inv_pos, nullptr, dX, T, k, d, dtype, s));
   }
   return BTX_OK;
 }
@@ -543,7 +543,7 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
   BTX_STAGE(BTX_STAGE_UP, launch_mx4_up(l, {W1_codes, W1_scales}, {W3_codes, W3_scales}, sh, s));
   int slices = 1;
   BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down(l, {W2_codes, W2_scales}, sh, &slices, s));
-  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, static_cast<const float*>(w.y), slices, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
+  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, static_cast<const float*>(w.y), slices, false, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
   return BTX_OK;
 }
 

@@ -263,9 +263,10 @@ int launch_gather_rows_t(const void* src0, void* dst0, const void* src1, void* d
                          const int32_t* offsets, int R, int k, int d, int E, int pitch, hipStream_t s);
 // out[t] = sum_j gates[t,j] * y[inv_pos[t,j]]   (gates NULL => unit weights; inv_pos < 0: dropped pair, skipped)
 // residual (may be NULL): [T,d] added to the sum in fp32 before the one rounding
-// slices > 1: y is not there yet, y_sums [slices][T*k, d] are to be added first (see launch_down); at most combine_most_slices()
+// slices > 1: y is not there yet, y_sums [slices][T*k, d] are to be added first (see launch_down) and, round_sums, rounded to dtype, as y would
+// be; at most combine_most_slices()
 int combine_most_slices(int T, int k, int dtype);
-int launch_combine(const void* y, const float* y_sums, int slices, const float* gates, const int32_t* inv_pos,
+int launch_combine(const void* y, const float* y_sums, int slices, bool round_sums, const float* gates, const int32_t* inv_pos,
                    const void* residual, void* out, int T, int k, int d, int dtype, hipStream_t s);
 
 // Expert GEMM stages.  `offsets` = E+1 grouped-row offsets on the device.

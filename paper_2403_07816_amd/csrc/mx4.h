@@ -56,7 +56,8 @@ int launch_mx4_begin(const void* x, const int32_t* perm, const int32_t* offsets,
                      int32_t* tokens, TileInfo* tiles, hipStream_t s);
 // act = silu(xq W1) * (xq W3), quantised along f: rows in grouped order
 int launch_mx4_up(const Mx4Layer& l, const Mx4Matrix& W1, const Mx4Matrix& W3, const Mx4Shapes& sh, hipStream_t s);
-// y = act W2, [T*k, d] bf16; or *slices > 1 of its sums in fp32 instead, [slice][T*k, d], for launch_combine() to add.  l.y: mx4_y_bytes(R, d)
+// y = act W2, [T*k, d] bf16; or *slices > 1 of its sums in fp32 instead, [slice][T*k, d], for launch_combine() to add and weigh without
+// rounding them.  l.y: mx4_y_bytes(R, d)
 constexpr int64_t kMx4SumBytes = (int64_t)256 * 256 * 256 * 4;       // of 256 tiles
 inline size_t mx4_y_bytes(int64_t R, int d) { return (size_t)std::max(R * d * 2, std::min(R * d * 4 * 8, kMx4SumBytes)); }
 int launch_mx4_down(const Mx4Layer& l, const Mx4Matrix& W2, const Mx4Shapes& sh, int* slices, hipStream_t s);

@@ -116,10 +116,10 @@ template <> struct Chunk<float> {
 constexpr int kFewRows = 8192;
 // KMAX: slots whose grouped rows and gates a wavefront keeps in registers; the rows of those slots are
 // requested together for every 16-byte column chunk (k > KMAX: the remaining slots are looked up as they come).
-// SLICED: y is still the fp32 sums of a product cut along K, [slice][row][column]; they are added in slice order and rounded to
+// SLICED: y is still the fp32 sums of a product cut along K, [slice][row][column]; they are added in slice order and, ROUND, rounded to
 // ET as a finishing kernel of the product would have (forward pass, 16 tokens, 4 experts of 4096 x 11008 197.4 -> 195.7 us); no more
 // than combine_most_slices().
-template <typename ET, int KMAX, bool SLICED>
+template <typename ET, int KMAX, bool ROUND, bool SLICED>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const void* __restrict__ y_rows, int slices, int64_t slice_stride,
                                                            const float* __restrict__ gates,
                                                            const int32_t* __restrict__ inv_pos,
@@ -142,6 +142,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const void* __restric
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.f;
     u32x4 w[KMAX];
+    float sum[SLICED && !ROUND ? KMAX : 1][N];
 #pragma unroll
     for (int j = 0; j < KMAX; ++j) if (!SLICED) w[j] = BTX_LD(y + (size_t)max(row[j], 0) * chunks_per_row + c);   // all slots in flight
     if constexpr (SLICED) {                               // as many slices of all slots as the registers hold
@@ -166,13 +167,25 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const void* __restric
               v[j][i] = s0 + b == 0 ? u[b][j][i] : s0 + b < slices ? v[j][i] + u[b][j][i] : v[j][i];
       }
 #pragma unroll
-      for (int j = 0; j < KMAX; ++j) w[j] = Chunk<ET>::pack(v[j]);
+      for (int j = 0; j < KMAX; ++j) {
+        if constexpr (ROUND) {
+          w[j] = Chunk<ET>::pack(v[j]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) sum[j][i] = v[j][i];
+        }
+      }
     }
     if (residual) Chunk<ET>::unpack(residual[(size_t)t * chunks_per_row + c], acc);   // block input, added in fp32
 #pragma unroll
     for (int j = 0; j < KMAX; ++j) {          // ascending slot order, as the definition sums
       float v[N];
-      Chunk<ET>::unpack(w[j], v);
+      if constexpr (SLICED && !ROUND) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = sum[j][i];
+      } else {
+        Chunk<ET>::unpack(w[j], v);
+      }
       if (row[j] >= 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] = fmaf(gate[j], v[i], acc[i]);
@@ -223,7 +236,7 @@ int combine_most_slices(int T, int k, int dtype) {
   return (dtype == BTX_BF16 ? 32 : 64) / k;
 }
 
-int launch_combine(const void* y, const float* y_sums, int slices, const float* gates, const int32_t* inv_pos,
+int launch_combine(const void* y, const float* y_sums, int slices, bool round_sums, const float* gates, const int32_t* inv_pos,
                    const void* residual, void* out, int T, int k, int d, int dtype, hipStream_t s) {
   const int esz = dtype == BTX_BF16 ? 2 : 4;
   const int chunks = d * esz / 16;
@@ -231,8 +244,11 @@ int launch_combine(const void* y, const float* y_sums, int slices, const float* 
   const dim3 grid(ceil_div(T, kThreads / kWave), few ? std::min(ceil_div(kFewRows, T), ceil_div(chunks, kWave)) : 1);
   auto run = [&](auto tag, auto kmax) {
     using ET = decltype(tag);
+    constexpr int KMAX = decltype(kmax)::value;
     const bool sliced = slices > 1;
-    auto kernel = sliced ? combine_kernel<ET, decltype(kmax)::value, true> : combine_kernel<ET, decltype(kmax)::value, false>;
+    auto kernel = !sliced      ? combine_kernel<ET, KMAX, true, false>
+                  : round_sums ? combine_kernel<ET, KMAX, true, true>
+                               : combine_kernel<ET, KMAX, false, true>;
     kernel<<<grid, kThreads, 0, s>>>(
         sliced ? static_cast<const void*>(y_sums) : y, slices, (int64_t)T * k * d, gates, inv_pos,
         static_cast<const u32x4*>(residual), static_cast<u32x4*>(out), T, k, chunks);

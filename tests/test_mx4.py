@@ -439,3 +439,37 @@ def test_served_block_routed_from_logits_in_a_graph():
         want, bound = O.ff_forward_mx4(x.cpu().double().numpy(), *V, o["topk_idx"], r.gates.cpu().double().numpy(), None,
                                        x.cpu().double().numpy())
         assert np.all(np.abs(replayed.cpu().double().numpy() - want) <= bound)
+
+
+@gpu
+@pytest.mark.parametrize("T,d,f,E,k", [(257, 64, 6144, 1, 1), (350, 288, 4384, 2, 1), (400, 96, 4384, 4, 2), (300, 64, 4384, 5, 5)])
+def test_cut_sums_stay_in_fp32(T, d, f, E, k):
+    """DOWN cut along its sums: the residual takes away what the sum rounds to in bf16, and what is left has to be the rest of the fp32 sum."""
+    rng = rng_of("cut", T, d, f, E, k)
+    x = rng.choice([-2.0, -1.0, 0.0, 1.0, 2.0], (T, d))
+    x[:, ::32] = 4.0                                       # every block in the format as it is, scale 1
+    up = rng.integers(0, 16, (E, f, d))
+    w_bytes = np.full((E, f, d // 32), 127 - int(np.log2(4 * np.sqrt(d))))         # one scale: h1 is exact in fp32
+    down, down_bytes = rng.integers(1, 8, (E, d, f)), np.full((E, d, f // 32), 115)
+    W1, W2 = (B.Mx4(*(torch.from_numpy(a).to(DEV) for a in O.mx4_pack(c, s)), c.shape[2]) for c, s in ((up, w_bytes), (down, down_bytes)))
+    v1, v2 = O.mx4_values(up, w_bytes), O.mx4_values(down, down_bytes)
+    r, idx, _, _ = routing_of(rng, T, E, k)
+    r.gates.fill_(1.0)
+    y, near, size = np.zeros((T, d)), np.zeros((T, d)), np.zeros((T, d))
+    for t in range(T):
+        for e in idx[t]:
+            h = v1[e] @ x[t]
+            act = h / (1 + np.exp(-h)) * h                 # W3 = W1: nothing below 0, and W2 is positive: the sums do not cancel
+            # fp32: silu is 4 + |h| steps off, two more for the products
+            aq, far = O.mx4_round(act), O.mx4_near(act, (6 + np.abs(h)) * O.STEP * act)
+            y[t] += v2[e] @ aq
+            near[t] += v2[e] @ far
+            size[t] += v2[e] @ (aq + far)
+    res = torch.from_numpy(-y).bfloat16()
+    want = y + res.double().numpy()
+    # the fp32 sums: f / 128 products one after another, the ranges, the slots; the result's rounding to bf16
+    bound = near + (f / 128 + 24 + k) * O.STEP * size
+    bound = bound + 2.0 ** -8 * (np.abs(want) + bound)
+    assert (np.abs(want) > 4 * bound).mean() > 0.8         # of a y rounded to bf16 nothing would be left there (one slot), or other rests
+    out = B.btx_moe_ff_forward_mx4(torch.from_numpy(x).bfloat16().to(DEV), W1, W1, W2, r, residual=res.to(DEV))
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= bound)
