@@ -431,7 +431,8 @@ int btx_moe_group_route(const void* logits, int logits_dtype, const float* bias,
  *   dgates   [T,k]  fp32
  *   dscores  [T,E]  fp32, may be NULL: gradient that reaches the scores directly (an auxiliary loss)
  *   dlogits  [T,E]  logits_dtype, out; may alias logits
- * A masked expert's gradient is 0.  Entries of topk_idx outside 0..E-1 are passed over.
+ * A masked expert's gradient is 0, and its dgates and dscores go into no other one, whatever they hold.  Entries of
+ * topk_idx outside 0..E-1 are passed over.
  * Requirements: as btx_moe_group_route, T <= 2^28 - 16 (BTX_ERR_UNSUPPORTED); no workspace.
  */
 int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int32_t* topk_idx, const float* dgates,

@@ -509,6 +509,7 @@ __global__ __launch_bounds__(kScatterThreads) void group_scatter_kernel(GroupRou
 // dL/dlogits from dL/dgates (and dL/dscores), 16 lanes a token, four experts at a time a lane (vector) or one.  With
 //   w_j = s_{e_j},  g_j = scale w_j / Z,  Z = sum w + 1e-20:   dw_j = (scale dg_j - sum_i dg_i g_i) / Z      (or scale dg_j)
 //   ds = dscores + the dw at their experts;   sigmoid: dl = ds s (1 - s);   softmax: dl = s (ds - sum ds s)
+// A masked expert has dw = ds = 0, whatever its dgates and dscores are (0 times an infinity is not).
 // Bound by what it reads and writes; a sigmoid router without dscores reads only the chosen logits.
 constexpr int kBwdThreads = 256, kBwdTokens = kBwdThreads / kLanes;
 __device__ __forceinline__ void store_grad4(float* p, const float* v) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
@@ -570,8 +571,10 @@ __global__ __launch_bounds__(kBwdThreads) void group_route_bwd_kernel(GroupRoute
       w = score_f<SCORE>(x, st);
       const float z = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + z);
       slope = z * r * r;                                                // s (1 - s), also where s rounds to 1
+      if (x == -INFINITY) dg = 0.f;
     } else {
       e = -1;
+      dg = 0.f;
     }
   }
   float d = a.scale * dg;
@@ -593,8 +596,8 @@ __global__ __launch_bounds__(kBwdThreads) void group_route_bwd_kernel(GroupRoute
       if constexpr (VEC) {
         const f32x4 q = *reinterpret_cast<const f32x4*>(a.dscores + (size_t)t * a.E + x0);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) ds[i + x] += q[x];
-      } else {
+        for (int x = 0; x < 4; ++x) ds[i + x] += l[i + x] != -INFINITY ? q[x] : 0.f;
+      } else if (l[i] != -INFINITY) {
         ds[i] += a.dscores[(size_t)t * a.E + x0];
       }
     }

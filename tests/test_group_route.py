@@ -447,3 +447,33 @@ def test_route_on_another_stream_and_in_a_graph():
         assert torch.equal(dl, B.btx_moe_group_route_backward(inp, eager, dg)), i
         if i == 0:
             assert torch.equal(dl, want_dl)
+
+
+@gpu
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("E,renorm,dtype", [(12, True, torch.float32), (33, False, torch.bfloat16), (256, True, torch.float32)])
+def test_route_backward_takes_nothing_from_masked_experts(score, E, renorm, dtype):
+    """Whatever reaches the scores or gates of masked experts (a loss of log s has an infinite gradient there): their gradients are 0 and
+    the others' what they are without it."""
+    from types import SimpleNamespace
+    rng = rng_of("nothing", score, E)
+    T, k = 40, 6
+    l = rng.standard_normal((T, E))
+    l[rng.random((T, E)) < 0.4] = -np.inf
+    l[3] = -np.inf
+    l[4] = -np.inf
+    l[4, :2] = (0.5, np.nan)                               # fewer than k are left
+    l = torch.from_numpy(l).to(dtype)
+    masked = ~(l > -np.inf)
+    idx = torch.from_numpy(O.group_route(l.double().numpy(), k, score, renorm=renorm)["topk_idx"])
+    r = SimpleNamespace(topk_idx=idx.int().to(DEV))
+    dg, ds = torch.from_numpy(rng.standard_normal((T, k))).float(), torch.from_numpy(rng.standard_normal((T, E))).float()
+    at_gates = masked.gather(1, idx)
+    assert at_gates.any()
+    plain = [torch.where(at_gates, 0.0, dg), torch.where(masked, 0.0, ds)]
+    for junk in (float("inf"), -float("inf"), float("nan"), 3e38):
+        got = [torch.where(at_gates, junk, dg), torch.where(masked, junk, ds)]
+        for with_scores in (False, True):
+            want, have = (B.btx_moe_group_route_backward(l.to(DEV), r, a.to(DEV), SCORE[score], renorm, 2.5, b.to(DEV) if with_scores else None)
+                          for a, b in (plain, got))
+            assert torch.equal(have, want) and torch.isfinite(have).all() and (have.cpu()[masked] == 0).all(), (junk, with_scores)
