@@ -445,7 +445,7 @@ int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int
  * x's gradient is the caller's (for btx_moe_group_route: dlogits W_router^T).
  *   dX     [T,d]  dtype  out: through the experts alone
  *   dgates [T,k]  fp32   out: <dY[t], FF_{idx[t,j]}(x[t])>; 0 for a dropped pair
- * The other arguments, limits and the workspace's size as btx_moe_ff_backward's; T < 2^26 (BTX_ERR_UNSUPPORTED).
+ * The other arguments, limits and the workspace's size as btx_moe_ff_backward's; T <= 2^26 - 4 (BTX_ERR_UNSUPPORTED).
  */
 int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype,
                               int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d, int f, int E, int k,
@@ -487,7 +487,7 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
  *   btx_mx4_quantize (axis 0) writes them
  *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
- * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T < 2^26, T*k < 2^28 - 256, T*k*max(d,f) < 2^40,
+ * Requirements: d % 32 == 0, f % 32 == 0, 1 <= k <= E <= 256, T <= 2^26 - 4, T*k < 2^28 - 256, T*k*max(d,f) < 2^40,
  * E*d*f < 2^40; x, residual, out, the weights and the workspace on 16-byte boundaries. d and f <= 2097120, T *
  * btx_mx4_scale_pitch(d) < 2^30 (BTX_ERR_UNSUPPORTED).
  */

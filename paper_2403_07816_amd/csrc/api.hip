@@ -403,7 +403,7 @@ int btx_moe_ff_backward(const void* dY, const void* x, const float* W_router, co
                        save_h3, dX, dW1, dW3, dW2, dW_dtype, workspace, workspace_bytes, stream, &ra, nullptr);
 }
 
-constexpr int kCombineMostTokens = 1 << 26;             // launch_combine(): a wavefront each
+constexpr int kCombineMostTokens = (1 << 26) - 4;       // launch_combine(): a wavefront each, fewer than 2^32 threads
 
 int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype,
                               int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d, int f, int E, int k, const float* gates,
@@ -416,7 +416,7 @@ int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, con
   const int n_dw = (dW1 != nullptr) + (dW3 != nullptr) + (dW2 != nullptr);
   if (n_dw != 0 && n_dw != 3) return BTX_ERR_INVALID_ARG;
   if (T == 0) return BTX_OK;
-  if (T >= kCombineMostTokens) return BTX_ERR_UNSUPPORTED;
+  if (T > kCombineMostTokens) return BTX_ERR_UNSUPPORTED;
   return backward_impl(dY, x, W1, W3, W2, dtype, w13_expert_stride, w2_expert_stride, T, d, f, E, k, gates, offsets, perm, inv_pos, save_h1,
                        save_h3, dX, dW1, dW3, dW2, dW_dtype, workspace, workspace_bytes, stream, nullptr, dgates);
 }
@@ -498,7 +498,7 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
 namespace {
 bool mx4_shapes_ok(int T, int d, int f, int E, int k) {
   return T >= 0 && d > 0 && f > 0 && E >= 1 && E <= kMx4MaxExperts && k >= 1 && k <= E && d % kMxBlock == 0 && f % kMxBlock == 0 &&
-         (int64_t)T * k < kMx4MostRows && T < kCombineMostTokens && (int64_t)T * k * (int64_t)(d > f ? d : f) < (int64_t)1 << 40 &&
+         (int64_t)T * k < kMx4MostRows && T <= kCombineMostTokens && (int64_t)T * k * (int64_t)(d > f ? d : f) < (int64_t)1 << 40 &&
          (int64_t)E * d * f < (int64_t)1 << 40;
 }
 struct Mx4Ws { uint8_t *x_codes, *x_scales, *act_codes, *act_scales; int32_t* tokens; TileInfo* tiles; void* y; size_t bytes; };

@@ -9,6 +9,7 @@ namespace btx {
 constexpr int kMxBlock = 32;
 constexpr int kMx4MaxExperts = 256;
 constexpr int kMx4MostRows = (1 << 28) - 256;         // T k: 32-bit offsets of 16 bytes a row, grids of every tile's height
+constexpr int64_t kMx4MostScales = 1 << 30;           // bytes of x's scales; the layer takes fewer
 constexpr int kMx4MostColumns = 65535 * 32;           // d and f: rows of the grid of few rows, and 32-bit offsets in a row tile
 // bytes from a row of scales to the next: whole 16-byte pieces, which the products copy (one holds the scales of 512 elements)
 inline __host__ __device__ int64_t mx4_pitch(int64_t K) { return (K / kMxBlock + 15) / 16 * 16; }

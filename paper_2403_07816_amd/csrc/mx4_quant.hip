@@ -55,7 +55,8 @@ __global__ __launch_bounds__(kThreads) void layer_begin_kernel(const bf16_t* __r
                                                                const int32_t* __restrict__ offsets, int E, int tile_rows, TileInfo* __restrict__ tiles) {
   const int n_first = token_blocks + 1;
   if ((int)blockIdx.x >= n_first) {
-    quantize_rows<bf16_t, TILES>((int64_t)blockIdx.x - n_first, x, T, d, codes, scales, pitch);
+    for (int64_t b = (int64_t)blockIdx.x - n_first; b * kThreads < T * pitch * 4; b += gridDim.x - n_first)
+      quantize_rows<bf16_t, TILES>(b, x, T, d, codes, scales, pitch);
     return;
   }
   if ((int)blockIdx.x < token_blocks) {
@@ -233,8 +234,10 @@ int launch_mx4_begin(const void* x, const int32_t* perm, const int32_t* offsets,
                      int32_t* tokens, TileInfo* tiles, hipStream_t s) {
   static_assert(kMx4MaxExperts <= kThreads, "one thread an expert");
   const int R = sh.T * sh.k, token_blocks = ceil_div(R, kThreads);
-  const int64_t pitch = mx4_pitch(sh.d), blocks = token_blocks + 1 + ((int64_t)sh.T * pitch * 4 + kThreads - 1) / kThreads;
-  if (!grid_fits(blocks, kThreads)) return BTX_ERR_UNSUPPORTED;
+  static_assert((kMx4MostRows / kThreads + 2 + kMostBlocks) * kThreads < 1ll << 32, "the grid");
+  const int64_t pitch = mx4_pitch(sh.d);
+  if (sh.T * pitch >= kMx4MostScales) return BTX_ERR_UNSUPPORTED;
+  const int64_t blocks = token_blocks + 1 + std::min((sh.T * pitch * 4 + kThreads - 1) / kThreads, kMostBlocks);
   const bf16_t* const xp = static_cast<const bf16_t*>(x);
   uint32_t* const codes = reinterpret_cast<uint32_t*>(x_codes);
   const int tile_rows = mx4_tile_rows(sh);

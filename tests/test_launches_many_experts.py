@@ -135,3 +135,25 @@ def test_token_rows_of_tall_tiles_have_offsets_of_32_bits(record, T, d, rows):
     assert tile_rows(found) == rows
     if rows == 256:
         assert (T - 1) * (d // 2) + 112 + 1024 < 1 << 32
+
+
+MOST_TOKENS = (1 << 26) - 4     # the combining kernel has a wavefront for a token
+
+
+@pytest.mark.parametrize("T,d,f,E,k,status", [
+    (MOST_TOKENS, 32, 32, 1, 1, 0), (MOST_TOKENS, 32, 32, 256, 1, 0), ((1 << 26) - 65, 32, 32, 4, 4, 0), (MOST_TOKENS - 1, 512, 32, 1, 1, 0),
+    (MOST_TOKENS + 1, 32, 32, 1, 1, 1), ((1 << 26) - 1, 32, 32, 1, 1, 1), (MOST_TOKENS, 544, 32, 1, 1, 2),
+    ((1 << 14) - 1, 2097120, 32, 1, 1, 0), (1 << 14, 2097120, 32, 1, 1, 2), ((1 << 26) - 64, 32, 32, 4, 4, 1)])
+def test_layer_takes_what_its_limits_allow(record, T, d, f, E, k, status):
+    """T <= 2^26 - 4, T k < 2^28 - 256 (refused as arguments), T * scale pitch of d < 2^30 (not supported)."""
+    (rc, found), = record(layer(T, d, f, E, k))
+    assert rc == status and len(found) == (4 if status == 0 else 0) and all(fits(x) for x in found)
+
+
+def backward_gates(T, d, f, E, k, dtype=B.BTX_F32):
+    return ("btx_moe_ff_backward_gates", [P] * 5 + [dtype, d * f, d * f, T, d, f, E, k] + [P] * 11 + [dtype, P, PLENTY, 0])
+
+
+def test_backward_gates_limits(record):
+    (most, _), (more, found) = record(backward_gates(MOST_TOKENS, 8, 8, 1, 1), backward_gates(MOST_TOKENS + 1, 8, 8, 1, 1))
+    assert (most, more, found) == (2, 2, [])               # (the experts' products refuse the former)

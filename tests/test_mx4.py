@@ -473,3 +473,22 @@ def test_cut_sums_stay_in_fp32(T, d, f, E, k):
     assert (np.abs(want) > 4 * bound).mean() > 0.8         # of a y rounded to bf16 nothing would be left there (one slot), or other rests
     out = B.btx_moe_ff_forward_mx4(torch.from_numpy(x).bfloat16().to(DEV), W1, W1, W2, r, residual=res.to(DEV))
     assert np.all(np.abs(out.cpu().double().numpy() - want) <= bound)
+
+
+@gpu
+def test_layer_of_the_most_tokens():
+    """Every block of the first launch has several pieces of the rows then: each token as it is in a small batch."""
+    rng = rng_of("most")
+    T, d, n = (1 << 26) - 4, 32, 5000
+    W1, W3, W2 = (experts(rng, 1, 32, 32)[0] for _ in range(3))
+    few = torch.from_numpy(rng.standard_normal((n, d))).bfloat16().to(DEV)
+    pair = torch.arange(T, dtype=torch.int32, device=DEV)
+    r = SimpleNamespace(topk_idx=torch.zeros((T, 1), dtype=torch.int32, device=DEV), gates=torch.ones((T, 1), device=DEV),
+                        offsets=torch.tensor([0, T], dtype=torch.int32, device=DEV), perm=pair, inv_pos=pair.view(T, 1))
+    s = SimpleNamespace(topk_idx=r.topk_idx[:n], gates=r.gates[:n], offsets=torch.tensor([0, n], dtype=torch.int32, device=DEV), perm=pair[:n],
+                        inv_pos=r.inv_pos[:n])
+    want = B.btx_moe_ff_forward_mx4(few, W1, W3, W2, s)
+    x = few.repeat(-(-T // n), 1)[:T].contiguous()
+    out = B.btx_moe_ff_forward_mx4(x, W1, W3, W2, r)       # (32 elements deep: every sum is one product of the matrix cores)
+    whole = T // n * n
+    assert torch.equal(out[:whole].view(-1, n, d), want.expand(whole // n, n, d)) and torch.equal(out[whole:], want[:T - whole])
