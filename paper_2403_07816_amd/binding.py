@@ -229,7 +229,7 @@ def btx_rmsnorm_backward(dXn: torch.Tensor, h: torch.Tensor, gain: torch.Tensor,
     dgain = dgain if dgain is not None else torch.empty(d, dtype=torch.float32, device=h.device)
     ws = _workspace(lib.btx_rmsnorm_backward_workspace_bytes(T, d), h.device, workspace)
     st = lib.btx_rmsnorm_backward(_ptr(dXn), _ptr(h), _ptr(gain), _ptr(rstd), _ptr(dres), _dtype_code(h), T, d,
-                                  _ptr(dH), _ptr(dgain), _ptr(ws), ws.numel(), _stream())
+                                  _ptr(dH), _ptr(dgain), _ptr(ws), _nbytes(ws), _stream())
     _check(st, "btx_rmsnorm_backward")
     return dH, dgain
 

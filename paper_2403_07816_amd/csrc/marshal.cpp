@@ -166,12 +166,12 @@ template <typename Call> PyObject* called(Call call) {
 template <typename Call> PyObject* with_workspace(PyObject* workspace, size_t bytes, Call call) {
   if (workspace != Py_None) {
     const at::Tensor& w = tensor(workspace);
-    if ((size_t)w.numel() * w.element_size() >= bytes) {
+    const size_t has = (size_t)w.numel() * w.element_size();
+    if (has >= bytes) {
       void* const at = address(workspace);
-      const size_t numel = (size_t)w.numel();
       int status;
       Py_BEGIN_ALLOW_THREADS
-      status = call(at, numel);
+      status = call(at, has);
       Py_END_ALLOW_THREADS
       return PyLong_FromLong(status);
     }
