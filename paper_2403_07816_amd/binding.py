@@ -135,6 +135,12 @@ def _workspace(nbytes: int, device, workspace: Optional[torch.Tensor]) -> torch.
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+def _sizes32(*sizes: int) -> None:
+    """Sizes and options of a call through ctypes, which would pass on the low 32 bits of longer ones."""
+    if not -2 ** 31 <= min(sizes) <= max(sizes) < 2 ** 31:
+        raise ValueError("sizes and options have 32 bits")
+
+
 def _nbytes(t: Optional[torch.Tensor]) -> int:
     return t.numel() * t.element_size() if t is not None else 0
 
@@ -192,6 +198,7 @@ def btx_moe_route_noalloc(x: torch.Tensor, W_router: torch.Tensor, out: Routing,
     T, d = x.shape
     E = W_router.shape[1]
     assert W_router.shape[0] == d and W_router.dtype == torch.float32
+    _sizes32(T, d, E, k, route_mode, lb_mode)
     r = out
     st = lib.btx_moe_route_noalloc(_ptr(x), _dtype_code(x), _ptr(W_router), _ptr(b_router), _ptr(U), T, d, E, k,
                                    route_mode, lb_mode, lb_alpha, tau, capacity_factor, _ptr(r.topk_idx), _ptr(r.gates),
@@ -222,6 +229,7 @@ def btx_rmsnorm_backward(dXn: torch.Tensor, h: torch.Tensor, gain: torch.Tensor,
     """Returns (dH [T,d], dgain [d] fp32); dres (e.g. the layer's dY) is added to dH."""
     lib = load_library()
     T, d = h.shape
+    _sizes32(T, d)
     assert dXn.shape == h.shape and dXn.dtype == h.dtype and dXn.is_contiguous() and h.is_contiguous()
     assert gain.dtype == torch.float32 and rstd.dtype == torch.float32 and rstd.numel() == T
     assert dres is None or (dres.shape == h.shape and dres.dtype == h.dtype and dres.is_contiguous())
@@ -355,6 +363,7 @@ def btx_moe_ff_backward_gates(dY: torch.Tensor, x: torch.Tensor, W1: torch.Tenso
     lib = load_library()
     T, d = x.shape
     E, f, k, dt = W1.shape[0], W1.shape[2], routing.topk_idx.shape[1], x.dtype
+    _sizes32(T, d, f, E, k)
     dW_dtype = dt if dW_dtype is None else dW_dtype
     assert W1.shape == (E, d, f) and W3.shape == (E, d, f) and W2.shape == (E, f, d) and W1.dtype == W3.dtype == W2.dtype == dt
     assert E == 1 or W3.stride(0) == W1.stride(0), "W3 is stacked like W1"
@@ -483,6 +492,7 @@ def btx_mix_experts(W1: torch.Tensor, W3: torch.Tensor, W2: torch.Tensor, mode: 
     ([N,d,f], [N,f,d]) copies, made by the library's copy kernels."""
     lib = load_library()
     N, d, f = W1.shape
+    _sizes32(N, d, f, mode, C)
     assert W3.shape == W1.shape and W2.shape == (N, f, d) and W1.dtype == W3.dtype == W2.dtype
     n_out, fo = (N * C, f // max(C, 1)) if mode == BTX_MIX_SPLIT else (N, f)
     o1 = torch.empty((n_out, d, fo), dtype=W1.dtype, device=W1.device)

@@ -48,6 +48,11 @@ const at::Tensor& tensor(PyObject* o) {
   if (!THPVariable_Check(o)) fail(PyExc_TypeError, "a tensor is expected");
   return THPVariable_Unpack(o);
 }
+// a size or an option as the library takes it
+int size32(int64_t n) {
+  if (n != (int)n) fail(PyExc_ValueError, "sizes and options have 32 bits");
+  return (int)n;
+}
 // stacked expert matrices: each [rows, cols] matrix contiguous, the experts any distance apart
 bool is_stacked(const at::Tensor& w) {
   return w.dim() == 3 && w.stride(2) == 1 && w.stride(1) == w.size(2) && w.stride(0) >= w.size(1) * w.size(2);
@@ -93,6 +98,7 @@ struct Experts {
       : T(x.size(0)), d(x.size(1)), E(0), f(0), s13(stacked(W1)), s2(stacked(W2)) {
     E = W1.size(0);
     f = W1.size(2);
+    for (const int64_t n : {T, d, E, f}) size32(n);
     require(W1.size(1) == d && W3.sizes() == W1.sizes() && W2.size(0) == E && W2.size(1) == f && W2.size(2) == d &&
                 W1.scalar_type() == x.scalar_type() && W3.scalar_type() == x.scalar_type() && W2.scalar_type() == x.scalar_type(),
             "W1, W3 [E, d, f] and W2 [E, f, d] of x's dtype");
@@ -104,7 +110,7 @@ int64_t integer(PyObject* o) {
   if (v == -1 && PyErr_Occurred()) throw PyError{};
   return v;
 }
-int int32(PyObject* o) { return (int)integer(o); }
+int int32(PyObject* o) { return size32(integer(o)); }
 float real(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw PyError{};
@@ -120,7 +126,7 @@ struct RoutingPtrs {
       if (!o) throw PyError{};
       try {
         at[i] = address(o);
-        if (i == 0) k = (int)matrix(o).size(1);          // topk_idx
+        if (i == 0) k = size32(matrix(o).size(1));       // topk_idx
       } catch (...) {
         Py_DECREF(o);
         throw;
@@ -198,7 +204,7 @@ const char* const kRouting[10] = {"topk_idx", "gates", "probs", "counts", "offse
 PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 13, [&] {
     const at::Tensor &x = matrix(a[0]), &W = matrix(a[1]);
-    const int T = (int)x.size(0), d = (int)x.size(1), E = (int)W.size(1), k = int32(a[4]);
+    const int T = size32(x.size(0)), d = size32(x.size(1)), E = size32(W.size(1)), k = int32(a[4]);
     require(W.size(0) == d && W.scalar_type() == at::kFloat, "W_router is [d, E] fp32");
     const int dt = dtype_code(x), mode = int32(a[5]), lb_mode = int32(a[6]);
     const float alpha = real(a[7]), tau = real(a[8]), cf = real(a[9]);
@@ -218,7 +224,7 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* norm_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 17, [&] {
     const at::Tensor &h = matrix(a[0]), &gain = tensor(a[1]), &W = matrix(a[5]);
-    const int T = (int)h.size(0), d = (int)h.size(1), E = (int)W.size(1), k = int32(a[8]);
+    const int T = size32(h.size(0)), d = size32(h.size(1)), E = size32(W.size(1)), k = int32(a[8]);
     require(W.size(0) == d && W.scalar_type() == at::kFloat, "W_router is [d, E] fp32");
     require(gain.dim() == 1 && gain.size(0) == d && gain.scalar_type() == at::kFloat, "gain is [d] fp32");
     const int dt = dtype_code(h), mode = int32(a[9]), lb_mode = int32(a[10]);
@@ -272,7 +278,7 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const RoutingPtrs r(a[6], names, 9);
     const int dt = dtype_code(x), k = r.k, mode = int32(a[9]), lb_mode = int32(a[10]), dw_dt = dw_f32 ? BTX_F32 : BTX_BF16;
     const float alpha = real(a[11]), scale = real(a[12]), tau = real(a[15]);
-    const unsigned flags = (unsigned)integer(a[13]);
+    const unsigned flags = (unsigned)int32(a[13]);
     const void *dY = address(a[0]), *xp = address(a[1]), *w1 = address(a[3], true), *w3 = address(a[4], true), *w2 = address(a[5], true);
     const void *h1 = address(a[7]), *h3 = address(a[8]);
     const float *Wr = address_of<float>(a[2]), *noise = address_of<float>(a[14]);
@@ -292,7 +298,7 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* group_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 12, [&] {
     const at::Tensor& logits = matrix(a[0]);
-    const int64_t T = logits.size(0), E = logits.size(1);
+    const int T = size32(logits.size(0)), E = size32(logits.size(1));
     const int k = int32(a[1]), score_fn = int32(a[2]), groups = int32(a[4]), keep = int32(a[5]), group_score = int32(a[6]), renorm = int32(a[7]);
     const float scale = real(a[8]);
     const int dt = dtype_code(logits);
@@ -302,14 +308,14 @@ PyObject* group_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
         o_perm(a[9], "perm"), o_inv(a[9], "inv_pos");
     int32_t* const idx = typed<int32_t>(o_idx, at::kInt, {T, k}, "topk_idx");
     float *const gates = typed<float>(o_gates, at::kFloat, {T, k}, "gates"), *const scores = typed<float>(o_scores, at::kFloat, {T, E}, "scores");
-    int32_t *const counts = typed<int32_t>(o_counts, at::kInt, {E}, "counts"), *const offsets = typed<int32_t>(o_offsets, at::kInt, {E + 1}, "offsets");
-    int32_t *const perm = typed<int32_t>(o_perm, at::kInt, {T * k}, "perm"), *const inv = typed<int32_t>(o_inv, at::kInt, {T, k}, "inv_pos");
+    int32_t *const counts = typed<int32_t>(o_counts, at::kInt, {E}, "counts"), *const offsets = typed<int32_t>(o_offsets, at::kInt, {E + (int64_t)1}, "offsets");
+    int32_t *const perm = typed<int32_t>(o_perm, at::kInt, {(int64_t)T * k}, "perm"), *const inv = typed<int32_t>(o_inv, at::kInt, {T, k}, "inv_pos");
     void* const stream = reinterpret_cast<void*>(integer(a[11]));
     const auto call = [&](void* ws, size_t bytes) {
-      return lib.group_route(l, dt, bias, (int)T, (int)E, k, score_fn, groups, keep, group_score, renorm, scale, idx, gates, scores, counts, offsets,
+      return lib.group_route(l, dt, bias, T, E, k, score_fn, groups, keep, group_score, renorm, scale, idx, gates, scores, counts, offsets,
                              perm, inv, ws, bytes, stream);
     };
-    const size_t bytes = lib.group_route_bytes((int)T, (int)E, k);
+    const size_t bytes = lib.group_route_bytes(T, E, k);
     if (!bytes) return called([&] { return call(nullptr, 0); });
     return with_workspace(a[10], bytes, call);
   });
@@ -319,18 +325,18 @@ PyObject* group_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* group_route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
     const at::Tensor& logits = matrix(a[0]);
-    const int64_t T = logits.size(0), E = logits.size(1);
+    const int T = size32(logits.size(0)), E = size32(logits.size(1));
     const int dt = dtype_code(logits), score_fn = int32(a[3]), renorm = int32(a[4]);
     const float scale = real(a[5]);
     const Attr o_idx(a[1], "topk_idx");
-    const int64_t k = matrix(o_idx).size(1);
+    const int k = size32(matrix(o_idx).size(1));
     const void* const l = address(a[0]);
     const int32_t* const idx = typed<int32_t>(o_idx, at::kInt, {T, k}, "topk_idx");
     const float *const dgates = typed<float>(a[2], at::kFloat, {T, k}, "dgates"), *const dscores = typed<float>(a[6], at::kFloat, {T, E}, "dscores");
     void* const out = typed<void>(a[7], logits.scalar_type(), {T, E}, "dlogits");
     void* const stream = reinterpret_cast<void*>(integer(a[9]));
     return called([&] {
-      return lib.group_route_backward(l, dt, idx, dgates, dscores, (int)T, (int)E, (int)k, score_fn, renorm, scale, out, stream);
+      return lib.group_route_backward(l, dt, idx, dgates, dscores, T, E, k, score_fn, renorm, scale, out, stream);
     });
   });
 }
@@ -369,19 +375,20 @@ PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* forward_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&] {
     const at::Tensor& x = matrix(a[0]);
-    const int64_t T = x.size(0), d = x.size(1);
+    const int T = size32(x.size(0)), d = size32(x.size(1));
     const Attr w1_codes(a[1], "codes"), w2_K(a[3], "K"), o_idx(a[4], "topk_idx");
-    const int64_t E = tensor(w1_codes).dim() ? tensor(w1_codes).size(0) : 0, f = integer(w2_K), k = matrix(o_idx).size(1);
+    const int E = tensor(w1_codes).dim() ? size32(tensor(w1_codes).size(0)) : 0, f = int32(w2_K), k = size32(matrix(o_idx).size(1));
     const Mx4Ptrs W1(a[1], {E}, f, d, "W1"), W3(a[2], {E}, f, d, "W3"), W2(a[3], {E}, d, f, "W2");
     const Attr o_gates(a[4], "gates"), o_offsets(a[4], "offsets"), o_perm(a[4], "perm"), o_inv(a[4], "inv_pos");
     const void *const from = typed<void>(a[0], at::kBFloat16, {T, d}, "x"), *const res = typed<void>(a[5], at::kBFloat16, {T, d}, "residual");
     void* const out = typed<void>(a[6], at::kBFloat16, {T, d}, "out");
     const float* const gates = typed<float>(o_gates, at::kFloat, {T, k}, "gates");
-    const int32_t *const offsets = typed<int32_t>(o_offsets, at::kInt, {E + 1}, "offsets"), *const perm = typed<int32_t>(o_perm, at::kInt, {T * k}, "perm"),
+    const int32_t *const offsets = typed<int32_t>(o_offsets, at::kInt, {E + (int64_t)1}, "offsets"),
+                  *const perm = typed<int32_t>(o_perm, at::kInt, {(int64_t)T * k}, "perm"),
                   *const inv = typed<int32_t>(o_inv, at::kInt, {T, k}, "inv_pos");
     void* const stream = reinterpret_cast<void*>(integer(a[8]));
-    return with_workspace(a[7], lib.forward_mx4_bytes((int)T, (int)d, (int)f, (int)E, (int)k), [&](void* ws, size_t bytes) {
-      return lib.forward_mx4(from, W1.codes, W1.scales, W3.codes, W3.scales, W2.codes, W2.scales, (int)T, (int)d, (int)f, (int)E, (int)k, gates,
+    return with_workspace(a[7], lib.forward_mx4_bytes(T, d, f, E, k), [&](void* ws, size_t bytes) {
+      return lib.forward_mx4(from, W1.codes, W1.scales, W3.codes, W3.scales, W2.codes, W2.scales, T, d, f, E, k, gates,
                              offsets, perm, inv, res, out, ws, bytes, stream);
     });
   });

@@ -44,3 +44,55 @@ def test_workspace_of_any_dtype(dtype):
     Q = [B.btx_mx4_quantize(w, axis=-2) for w in (W1, W3, W2)]
     assert torch.equal(B.btx_moe_ff_forward_mx4(xb, *Q, r, workspace=ws(lib.btx_moe_ff_forward_mx4_workspace_bytes(T, d, f, E, k))),
                        B.btx_moe_ff_forward_mx4(xb, *Q, r))
+
+
+def shaped(*shape, dtype=torch.float32):
+    """Of any size, in no memory."""
+    return torch.zeros(1, dtype=dtype).expand(shape)
+
+
+def group_out(T, E, k):
+    i32 = torch.int32
+    return B.GroupRouting(shaped(T, k, dtype=i32), shaped(T, k), None, shaped(E, dtype=i32), shaped(E + 1, dtype=i32), shaped(T * k, dtype=i32),
+                          shaped(T, k, dtype=i32))
+
+
+def route_out(T, E, k):
+    i32 = torch.int32
+    return B.Routing(shaped(T, k, dtype=i32), shaped(T, k), shaped(T, E), shaped(E, dtype=i32), shaped(E + 1, dtype=i32), shaped(T * k, dtype=i32),
+                     shaped(T, k, dtype=i32), shaped(E), shaped(E), shaped(1))
+
+
+MANY = 2 ** 32 + 8         # rows: 8 in 32 bits
+EXPERTS = [torch.zeros(4, 16, 32), torch.zeros(4, 16, 32), torch.zeros(4, 32, 16)]
+H = shaped(2 * MANY, 32)
+
+
+def mx4(E, n, K):
+    return B.Mx4(shaped(E, n, K // 2, dtype=torch.uint8), shaped(E, n, 16, dtype=torch.uint8), K)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: B.btx_moe_group_route(shaped(MANY, 4), 2, out=group_out(MANY, 4, 2)),
+    lambda: B.btx_moe_group_route(shaped(8, 4), 2 ** 32 + 2, out=group_out(8, 4, 2)),
+    lambda: B.btx_moe_group_route(shaped(8, 4), 2, score_fn=2 ** 32, out=group_out(8, 4, 2)),
+    lambda: B.btx_moe_group_route(shaped(8, 4), 2, n_groups=2 ** 32 + 1, out=group_out(8, 4, 2)),
+    lambda: B.btx_moe_group_route(shaped(8, 4), 2, n_groups=1 - 2 ** 32, out=group_out(8, 4, 2)),
+    lambda: B.btx_moe_group_route_backward(shaped(MANY, 4), group_out(MANY, 4, 2), shaped(MANY, 2), out=shaped(MANY, 4)),
+    lambda: B.btx_moe_ff_forward_mx4(shaped(MANY, 32, dtype=torch.bfloat16), mx4(4, 64, 32), mx4(4, 64, 32), mx4(4, 32, 64), group_out(MANY, 4, 2),
+                                     out=shaped(MANY, 32, dtype=torch.bfloat16)),
+    lambda: B.btx_moe_ff_backward_gates(shaped(MANY, 16), shaped(MANY, 16), *EXPERTS, group_out(MANY, 4, 2), H, H,
+                                        out=B.ExpertGrads(shaped(MANY, 16), shaped(MANY, 2), None, None, None)),
+    lambda: B.btx_moe_route(shaped(MANY, 16), shaped(16, 4), out=route_out(MANY, 4, 2)),
+    lambda: B.btx_moe_route(shaped(8, 16), shaped(16, 4), k=2 ** 32 + 2, out=route_out(8, 4, 2)),
+    lambda: B.btx_moe_route_noalloc(shaped(MANY, 16), shaped(16, 4), route_out(MANY, 4, 2)),
+    lambda: B.btx_moe_norm_route(shaped(MANY, 16), shaped(16), 1e-5, shaped(16, 4), out=route_out(MANY, 4, 2), xn=shaped(MANY, 16), rstd=shaped(MANY)),
+    lambda: B.btx_rmsnorm_backward(shaped(MANY, 16), shaped(MANY, 16), shaped(16), shaped(MANY), dH=shaped(MANY, 16)),
+    lambda: B.btx_mix_experts(*EXPERTS, B.BTX_MIX_SPLIT, C=2 ** 32 + 2),
+    lambda: B.btx_moe_ff_forward(shaped(MANY, 16), *EXPERTS, route_out(MANY, 4, 2), out=shaped(MANY, 16), save=False),
+    lambda: B.btx_moe_ff_backward(shaped(MANY, 16), shaped(MANY, 16), shaped(16, 4), *EXPERTS, route_out(MANY, 4, 2), H, H, frozen_experts=True,
+                                  out=B.Grads(shaped(MANY, 16), shaped(16, 4), shaped(4), None, None, None))])
+def test_sizes_past_32_bits_are_refused(call):
+    """The library's sizes are ints: what does not fit one would be another size there."""
+    with pytest.raises(ValueError, match="32 bits"):
+        call()
