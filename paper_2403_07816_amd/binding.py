@@ -306,8 +306,9 @@ class GroupRouting:
 
 def alloc_group_routing(T: int, E: int, k: int, device, scores: bool = True) -> GroupRouting:
     i32, f32 = dict(dtype=torch.int32, device=device), dict(dtype=torch.float32, device=device)
+    by_expert = torch.empty if T else torch.zeros        # (without tokens nothing is written)
     return GroupRouting(torch.empty((T, k), **i32), torch.empty((T, k), **f32), torch.empty((T, E), **f32) if scores else None,
-                        torch.zeros(E, **i32), torch.zeros(E + 1, **i32), torch.empty(T * k, **i32), torch.empty((T, k), **i32))
+                        by_expert(E, **i32), by_expert(E + 1, **i32), torch.empty(T * k, **i32), torch.empty((T, k), **i32))
 
 
 def _typed(t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str):

@@ -96,3 +96,20 @@ def test_sizes_past_32_bits_are_refused(call):
     """The library's sizes are ints: what does not fit one would be another size there."""
     with pytest.raises(ValueError, match="32 bits"):
         call()
+
+
+def test_outputs_of_routing_from_logits_are_not_filled_first():
+    """The call writes every entry of them; only without tokens it writes none, and counts and offsets are 0 already."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Calls(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            names.append(func.overloadpacket.__name__)
+            return func(*args, **(kwargs or {}))
+
+    names = []
+    with Calls():
+        B.alloc_group_routing(5, 8, 2, "cpu")
+    assert set(names) == {"empty"}
+    r = B.alloc_group_routing(0, 8, 2, "cpu")
+    assert r.counts.tolist() == [0] * 8 and r.offsets.tolist() == [0] * 9 and r.topk_idx.shape == (0, 2)
