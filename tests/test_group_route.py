@@ -477,3 +477,50 @@ def test_route_backward_takes_nothing_from_masked_experts(score, E, renorm, dtyp
             want, have = (B.btx_moe_group_route_backward(l.to(DEV), r, a.to(DEV), SCORE[score], renorm, 2.5, b.to(DEV) if with_scores else None)
                           for a, b in (plain, got))
             assert torch.equal(have, want) and torch.isfinite(have).all() and (have.cpu()[masked] == 0).all(), (junk, with_scores)
+
+
+@gpu
+def test_route_past_32_bits():
+    """More than 2^31 logits: the tokens of a small batch again and again."""
+    T, n, E, k = (1 << 23) + 77, 1000, 256, 3
+    few = torch.randn(n, E, generator=torch.Generator().manual_seed(6)).to(DEV)
+    dg = torch.randn(n, k, generator=torch.Generator().manual_seed(7)).to(DEV)
+    kw = dict(score_fn=B.BTX_SCORE_SOFTMAX, n_groups=8, topk_groups=4)
+    want = B.btx_moe_group_route(few, k, **kw)
+    times, whole = -(-T // n), T // n * n
+    l = few.repeat(times, 1)[:T]
+    r = B.btx_moe_group_route(l, k, **kw)
+
+    def again(got, of):
+        return torch.equal(got[:whole].view(-1, n, got.shape[1]), of.expand(whole // n, n, got.shape[1])) and torch.equal(got[whole:], of[:T - whole])
+
+    for name in ("topk_idx", "gates", "scores"):
+        assert again(getattr(r, name), getattr(want, name)), name
+    flat = r.topk_idx.view(-1).long()
+    assert torch.equal(r.counts.long(), torch.bincount(flat, minlength=E))
+    perm = torch.sort(flat, stable=True).indices
+    assert torch.equal(r.perm.long(), perm) and torch.equal(r.perm[r.inv_pos.view(-1).long()].long(), torch.arange(T * k, device=DEV))
+    back = dict(score_fn=B.BTX_SCORE_SOFTMAX)
+    assert again(B.btx_moe_group_route_backward(l, r, dg.repeat(times, 1)[:T], **back), B.btx_moe_group_route_backward(few, want, dg, **back))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,d,f,E,k,cap", [(300, 128, 96, 64, 4, 0.5), (500, 64, 96, 4, 2, 0.7), (40, 64, 64, 5, 1, 1.0)])
+def test_backward_gates_of_dropped_pairs(T, d, f, E, k, cap, dtype):
+    """Pairs that a capacity limit has dropped have a gradient of 0, and the rest is as in the layer's own backward pass."""
+    from paper_2403_07816_amd import synth
+    L = synth.make_layer(T, d, f, E, dtype=dtype, seed=7, device=DEV, unit_rms=True, with_dY=True)
+    r = B.btx_moe_route(L["x"], L["W_router"], k=k, capacity_factor=cap)
+    dropped = r.inv_pos < 0
+    assert dropped.any() and not dropped.all()
+    _, h1, h3 = B.btx_moe_ff_forward(L["x"], L["W1"], L["W3"], L["W2"], r)
+    args = (L["W1"], L["W3"], L["W2"], r, h1, h3)
+    out = B.ExpertGrads(torch.empty_like(L["x"]), torch.full((T, k), float("nan"), device=DEV), *(torch.empty_like(w) for w in args[:3]))
+    b = B.btx_moe_ff_backward_gates(L["dY"], L["x"], *args, out=out)
+    a = B.btx_moe_ff_backward(L["dY"], L["x"], torch.zeros_like(L["W_router"]), *args)
+    assert (b.dgates[dropped] == 0).all() and torch.isfinite(b.dgates).all() and (b.dgates[~dropped] != 0).any()
+    for name in ("dW1", "dW3", "dW2"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+    eps = torch.finfo(dtype).eps
+    assert ((a.dX.float() - b.dX.float()).abs() <= eps * a.dX.float().abs() + k * 2.0 ** -22 * a.dX.float().abs().max()).all()
