@@ -267,7 +267,7 @@ int btx_rmsnorm_backward(const void* dXn, const void* h, const float* gain, cons
  * dtype BTX_BF16: bf16 storage, bf16 MFMA products, fp32 accumulation; the
  * activation silu(h1)*h3 and the expert output are rounded to bf16 once each.
  * dtype BTX_F32: fp32 matrix-instruction products (exact products, fp32 accumulation), fp32 storage.
- * Requirements: d % 8 == 0, f % 8 == 0, strides >= d*f and multiples of 8.
+ * Requirements: 1 <= k <= E <= 64, d % 8 == 0, f % 8 == 0, strides >= d*f and multiples of 8.
  * Limits (BTX_ERR_UNSUPPORTED beyond them; also for btx_moe_ff_backward): the bf16 kernels address the
  * padded grouped rows with 32-bit byte offsets, ceil(R/64)*64 + 64*E < 2^23 (about 8.3 M routed rows);
  * fp32, and bf16 with a d or f that is no multiple of 32 (or below 64), take R/64 + E <= 65535 row tiles
@@ -387,8 +387,9 @@ int btx_adamw_step(float* master, float* m, float* v, const void* grad, int grad
  * btx_moe_group_route - routing from logits, for mixtures of many experts: softmax or sigmoid
  * scores, a bias that balances the experts' loads and that only the selection sees, groups of
  * experts of which the best are kept, top-k, renormalised and scaled gates; then the same token ->
- * expert grouping as btx_moe_route's, so that btx_moe_ff_forward, btx_moe_ff_forward_mx4 and
- * btx_moe_ff_backward_gates take its outputs.
+ * expert grouping as btx_moe_route's, so that btx_moe_ff_forward_mx4 takes its outputs, and up to 64
+ * experts btx_moe_ff_forward and btx_moe_ff_backward_gates do (they refuse more: beyond that there
+ * is no layer to train).
  *     s = sigmoid(l) or softmax(l)                      (of a token's E logits l)
  *     v = s + bias                                      (bias NULL: s)
  *     a group's value = its largest v, or the sum of its two largest; the topk_groups groups of the
@@ -445,7 +446,8 @@ int btx_moe_group_route_backward(const void* logits, int logits_dtype, const int
  * x's gradient is the caller's (for btx_moe_group_route: dlogits W_router^T).
  *   dX     [T,d]  dtype  out: through the experts alone
  *   dgates [T,k]  fp32   out: <dY[t], FF_{idx[t,j]}(x[t])>; 0 for a dropped pair
- * The other arguments, limits and the workspace's size as btx_moe_ff_backward's; T <= 2^26 - 4 (BTX_ERR_UNSUPPORTED).
+ * The other arguments, limits (E <= 64 among them) and the workspace's size as btx_moe_ff_backward's;
+ * T <= 2^26 - 4 (BTX_ERR_UNSUPPORTED).
  */
 int btx_moe_ff_backward_gates(const void* dY, const void* x, const void* W1, const void* W3, const void* W2, int dtype,
                               int64_t w13_expert_stride, int64_t w2_expert_stride, int T, int d, int f, int E, int k,

@@ -157,3 +157,14 @@ def backward_gates(T, d, f, E, k, dtype=B.BTX_F32):
 def test_backward_gates_limits(record):
     (most, _), (more, found) = record(backward_gates(MOST_TOKENS, 8, 8, 1, 1), backward_gates(MOST_TOKENS + 1, 8, 8, 1, 1))
     assert (most, more, found) == (2, 2, [])               # (the experts' products refuse the former)
+
+
+def test_experts_that_a_layer_takes(record):
+    """Routing from logits and the layer of 4-bit experts: 256; the experts' gradients and the bf16 and fp32 layers: 64."""
+    def forward(E):
+        return ("btx_moe_ff_forward", [P] * 4 + [B.BTX_BF16, 4096, 4096, 100, 64, 64, E, 4] + [P] * 8 + [P, PLENTY, 0])
+
+    calls = [route(100, 256, 4), layer(100, 64, 64, 256, 4), forward(64), backward_gates(100, 64, 64, 64, 4),
+             route(100, 257, 4), layer(100, 64, 64, 257, 4), forward(65), backward_gates(100, 64, 64, 65, 4)]
+    for i, (rc, found) in enumerate(record(*calls)):
+        assert (rc, bool(found)) == ((0, True) if i < 4 else (1, False)), i
