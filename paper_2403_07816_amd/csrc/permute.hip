@@ -245,10 +245,11 @@ int launch_combine(const void* y, const float* y_sums, int slices, bool round_su
   auto run = [&](auto tag, auto kmax) {
     using ET = decltype(tag);
     constexpr int KMAX = decltype(kmax)::value;
+    constexpr bool AS_IS = std::is_same_v<ET, float>;     // fp32: nothing to round, one kernel for both
     const bool sliced = slices > 1;
     auto kernel = !sliced      ? combine_kernel<ET, KMAX, true, false>
                   : round_sums ? combine_kernel<ET, KMAX, true, true>
-                               : combine_kernel<ET, KMAX, false, true>;
+                               : combine_kernel<ET, KMAX, AS_IS, true>;
     kernel<<<grid, kThreads, 0, s>>>(
         sliced ? static_cast<const void*>(y_sums) : y, slices, (int64_t)T * k * d, gates, inv_pos,
         static_cast<const u32x4*>(residual), static_cast<u32x4*>(out), T, k, chunks);
