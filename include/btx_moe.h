@@ -93,8 +93,8 @@ int btx_version(void);
 
 /* One-time set-up on the CURRENT device: raises the dynamic-LDS limit of every expert-GEMM
  * kernel (they use all 160 KB of a compute unit's LDS).  Optional: the first bf16 call of
- * btx_moe_ff_forward / btx_moe_ff_backward, and btx_moe_ff_forward_mx4's first, on a device does
- * the same by itself, but that set-up cannot be recorded into a HIP graph, so a caller that captures its very first step
+ * btx_moe_ff_forward / btx_moe_ff_backward, and the first of btx_moe_ff_forward_mx4,
+ * btx_moe_ff_forward_fp8 and btx_fp8_matmul, on a device does the same by itself, but that set-up cannot be recorded into a HIP graph, so a caller that captures its very first step
  * calls btx_init() before beginning the capture (once per device that it uses).  It also
  * looks up the device address of btx_moe_route_noalloc's fixed workspace.
  * Idempotent.  Errors: BTX_ERR_HIP. */
@@ -499,6 +499,88 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
                            int E, int k, const float* gates, const int32_t* offsets, const int32_t* perm,
                            const int32_t* inv_pos, const void* residual, void* out, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Block-scaled 8-bit floats: e4m3 values (3 bits of fraction, largest 448, smallest 2^-9), of which 128 consecutive ones along the quantised axis
+ * (of length K) share a power of two (e8m0).  For serving: btx_rmsnorm_fp8 or btx_fp8_quantize makes the rows, btx_moe_ff_forward_fp8 and
+ * btx_fp8_matmul multiply them with weights that were quantised once.  For training a linear layer y = x W^T, all three products are
+ * btx_fp8_matmul's: y of x and W; dx of dy and W^T; dW of dy^T and x^T (quantised with axis 0).
+ *   codes   [.., n, btx_fp8_code_pitch(K)]    uint8, one an element, zeros from K up to a multiple of 128
+ *   scales  [.., n, btx_fp8_scale_pitch(K)]   uint8: byte b stands for 2^(b-127), 255 for NaN; the ceil(K/128) scales of a row, then zeros up
+ *           to a multiple of 16 bytes
+ * btx_fp8_quantize: a block's scale is the smallest power of two, at least 2^-127, of which its largest magnitude is at most 448 times; its values
+ * divided by that are rounded to the nearest e4m3 value, ties to the even one.  A block that holds an infinity or a NaN gets the scale
+ * 255: all its values are NaN.
+ * btx_fp8_dequantize: value of the code * scale, exact in fp32, and down to 2^-133 in bf16.
+ *   x, out      [batch, rows, cols]  dtype (BTX_F32 or BTX_BF16)
+ *   axis        1: blocks along the rows: K = cols, n = rows (activations: [T,d] with batch 1)
+ *               0: blocks down the columns: K = rows, n = cols; codes and scales are [batch, cols, ..].  So are the experts' weights
+ *                  quantised whose products sum over their rows: W1, W3 [E,d,f] and W2 [E,f,d].
+ *   block_rows  1: a block is 128 elements along K.  128: blocks of 128 x 128 elements, whose scale each of the 128 rows has: a matrix and its
+ *               transpose (the other axis) then have the same values.
+ * K, n and batch may be any sizes (nothing to do where one of them is 0); x, out, codes, scales on 16-byte boundaries.
+ * batch * n * btx_fp8_code_pitch(K) < 2^40.  axis 0 or block_rows 128: batch <= 65535, ceil(rows / 128) * ceil(cols / 128) < 2^24
+ * (BTX_ERR_UNSUPPORTED).
+ */
+int64_t btx_fp8_code_pitch(int64_t K);
+int64_t btx_fp8_scale_pitch(int64_t K);
+int btx_fp8_quantize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, int block_rows, uint8_t* codes,
+                     uint8_t* scales, void* stream);
+int btx_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, void* out,
+                       void* stream);
+
+/* ---------------------------------------------------------------------------
+ * btx_rmsnorm_fp8 - the residual's addition and the block's pre-normalisation, with the result in 8 bits:
+ *     sum[t,c] = h[t,c] + residual[t,c], rounded to dtype;   rstd[t] = 1 / sqrt(mean_c sum[t,c]^2 + eps);
+ *     xn[t,c] = gain[c] * sum[t,c] * rstd[t]
+ *   h         [T,d]  dtype
+ *   residual  [T,d]  dtype, may be NULL: sum is h
+ *   gain      [d]    fp32;   eps >= 0
+ *   sum       [T,d]  dtype  out, may be NULL; may be h or residual itself
+ *   xn        [T,d]  dtype  out, may be NULL (a router reads it); must not be h, residual or sum
+ *   rstd      [T]    fp32   out
+ *   codes [T,btx_fp8_code_pitch(d)], scales [T,btx_fp8_scale_pitch(d)]: out, xn as btx_fp8_quantize (axis 1, block_rows 1) writes fp32 values: of xn before it
+ *             is rounded to dtype.  Both NULL: xn alone.
+ * Mean square, rstd and the product are evaluated in fp64, as by btx_moe_norm_route.  The backward pass is btx_rmsnorm_backward with `sum` in h's
+ * place, rstd, and the gradient of sum as dres: its dH is that of h and of residual.
+ * Requirements: d % 8 == 0; d <= 16384 (BTX_ERR_UNSUPPORTED); all but rstd on 16-byte boundaries.
+ */
+int btx_rmsnorm_fp8(const void* h, const void* residual, int dtype, const float* gain, float eps, int T, int d, void* sum, void* xn, float* rstd,
+                    uint8_t* codes, uint8_t* scales, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * btx_fp8_matmul - out[m,n] = residual[m,n] + sum_k A[m,k] B[n,k] of two matrices in block-scaled 8-bit floats: exact products, sums in fp32
+ * (in an order that the sizes fix), rounded once.
+ *   A         codes [M,btx_fp8_code_pitch(K)], scales [M,btx_fp8_scale_pitch(K)];   B: the same with N rows
+ *   residual  [M,N]  dtype, may be NULL; may be out itself (a gradient that is added to)
+ *   out       [M,N]  dtype (BTX_F32 or BTX_BF16)
+ * What lies behind K in the codes' rows has to be zeros, as btx_fp8_quantize writes them.
+ * Requirements: N % 8 == 0, K >= 1, M * max(N, pitch) < 2^40, N * pitch < 2^40; M < 2^28 - 256, N and K <= 2097120 (BTX_ERR_UNSUPPORTED); everything on 16-byte
+ * boundaries; workspace >= btx_fp8_matmul_workspace_bytes(M,N,K) (may be NULL where that is 0).
+ */
+size_t btx_fp8_matmul_workspace_bytes(int M, int N, int K);
+int btx_fp8_matmul(const uint8_t* A_codes, const uint8_t* A_scales, const uint8_t* B_codes, const uint8_t* B_scales, int M, int N, int K,
+                   const void* residual, void* out, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * btx_moe_ff_forward_fp8 - the layer of 8-bit experts, for serving (forward only): btx_moe_ff_forward with both operands of every product in block-scaled
+ * 8-bit floats.  Per expert
+ *     act = silu(x W1_e) * (x W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
+ *     (but for sums that are cut into ranges, which stay in fp32)
+ *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
+ *   x         codes [T,btx_fp8_code_pitch(d)] and scales [T,btx_fp8_scale_pitch(d)], as btx_rmsnorm_fp8 or btx_fp8_quantize (axis 1) writes them
+ *   W1, W3    codes [E,f,btx_fp8_code_pitch(d)] and scales [E,f,btx_fp8_scale_pitch(d)];   W2: [E,d,btx_fp8_code_pitch(f)] and
+ *             [E,d,btx_fp8_scale_pitch(f)], as btx_fp8_quantize (axis 0; any block_rows) writes them
+ *   residual  [T,d] bf16, may be NULL;   out [T,d] bf16;   residual may be out
+ *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
+ * Requirements: d % 8 == 0, f % 8 == 0, 1 <= k <= E <= 256, T <= 2^26 - 4, T*k < 2^28 - 256, T*k*max(pitches) < 2^40,
+ * E*max(f*btx_fp8_code_pitch(d), d*btx_fp8_code_pitch(f)) < 2^40; codes, scales, residual, out and the workspace on 16-byte boundaries. d and f <= 2097120 (BTX_ERR_UNSUPPORTED).
+ */
+size_t btx_moe_ff_forward_fp8_workspace_bytes(int T, int d, int f, int E, int k);
+int btx_moe_ff_forward_fp8(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* W1_codes, const uint8_t* W1_scales,
+                           const uint8_t* W3_codes, const uint8_t* W3_scales, const uint8_t* W2_codes, const uint8_t* W2_scales, int T, int d, int f,
+                           int E, int k, const float* gates, const int32_t* offsets, const int32_t* perm, const int32_t* inv_pos, const void* residual,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

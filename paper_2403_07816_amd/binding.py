@@ -62,6 +62,15 @@ _SIGNATURES = {
     "btx_mx4_dequantize": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _i, _vp, _vp]),
     "btx_moe_ff_forward_mx4_workspace_bytes": (_sz, [_i] * 5),
     "btx_moe_ff_forward_mx4": (_i, [_vp] * 7 + [_i] * 5 + [_vp] * 7 + [_sz, _vp]),
+    "btx_fp8_code_pitch": (_i64, [_i64]),
+    "btx_fp8_scale_pitch": (_i64, [_i64]),
+    "btx_fp8_quantize": (_i, [_vp, _i, _i64, _i64, _i64, _i, _i, _vp, _vp, _vp]),
+    "btx_fp8_dequantize": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _i, _vp, _vp]),
+    "btx_rmsnorm_fp8": (_i, [_vp, _vp, _i, _vp, _f, _i, _i] + [_vp] * 6),
+    "btx_fp8_matmul_workspace_bytes": (_sz, [_i] * 3),
+    "btx_fp8_matmul": (_i, [_vp] * 4 + [_i] * 3 + [_vp, _vp, _i, _vp, _sz, _vp]),
+    "btx_moe_ff_forward_fp8_workspace_bytes": (_sz, [_i] * 5),
+    "btx_moe_ff_forward_fp8": (_i, [_vp] * 8 + [_i] * 5 + [_vp] * 7 + [_sz, _vp]),
     "btx_mix_experts": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
 }
 
@@ -438,6 +447,96 @@ def btx_moe_ff_forward_mx4(x: torch.Tensor, W1: Mx4, W3: Mx4, W2: Mx4, routing, 
     btx_moe_group_route."""
     out = out if out is not None else torch.empty_like(x)
     _run("forward_mx4", "btx_moe_ff_forward_mx4", x, workspace, (x, W1, W3, W2, routing, residual, out))
+    return out
+
+
+# ---- block-scaled 8-bit floats: the norm and the tensors in them, their products, and the layer of experts that are kept in them ------------
+
+
+@dataclass
+class Fp8:
+    codes: torch.Tensor      # [.., n, K padded to 128] uint8
+    scales: torch.Tensor     # [.., n, 16-byte rows] uint8
+    K: int                   # length of the quantised axis
+
+
+def alloc_fp8(shape, axis: int, device) -> Fp8:
+    """For a tensor of this shape ([.., rows, cols]), quantised along its last axis (-1) or the one before (-2)."""
+    *batch, rows, cols = shape
+    K, n = (cols, rows) if axis == -1 else (rows, cols)
+    lib, u8 = load_library(), dict(dtype=torch.uint8, device=device)
+    return Fp8(torch.empty((*batch, n, lib.btx_fp8_code_pitch(K)), **u8), torch.empty((*batch, n, lib.btx_fp8_scale_pitch(K)), **u8), K)
+
+
+def _on_current(t: torch.Tensor) -> None:
+    """The stream is the current device's; the other tensors of a call have to be where this one is."""
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on {t.device}, which is not the current device")
+
+
+def btx_fp8_quantize(x: torch.Tensor, axis: int = -1, block_rows: int = 1, out: Optional[Fp8] = None) -> Fp8:
+    """[.., rows, cols] in blocks of 128 along axis -1 (activations) or -2 (the experts' weights [E, K, N], a weight gradient's factors);
+    block_rows 128: blocks of 128 x 128, of which a matrix and its transpose have the same values."""
+    ax = _mx4_axis(axis)
+    _on_current(x)
+    out = out if out is not None else alloc_fp8(x.shape, axis, x.device)
+    _run("fp8_quantize", "btx_fp8_quantize", x, None, (x, ax, block_rows, out))
+    return out
+
+
+def btx_fp8_dequantize(q: Fp8, dtype: torch.dtype = torch.bfloat16, axis: int = -1, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of q as a tensor; axis: as given to btx_fp8_quantize."""
+    ax = _mx4_axis(axis)
+    _on_current(q.codes)
+    *batch, n, _ = q.codes.shape
+    shape = (*batch, n, q.K) if axis == -1 else (*batch, q.K, n)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.codes.device)
+    elif out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"out is {str(dtype)[6:]} {shape}")
+    _run("fp8_dequantize", "btx_fp8_dequantize", out, None, (q, ax, out))
+    return out
+
+
+@dataclass
+class Norm8:
+    q: Fp8                         # xn in 8 bits
+    rstd: torch.Tensor             # [T] fp32
+    sum: torch.Tensor              # [T,d]: h + residual (h itself without one)
+    xn: Optional[torch.Tensor]     # [T,d]
+
+
+def btx_rmsnorm_fp8(h: torch.Tensor, gain: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                    sum: Optional[torch.Tensor] = None, xn: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                    out: Optional[Fp8] = None) -> Norm8:
+    """RMS-normalise the rows of h + residual, in 8 bits and, where xn is given, into that.  sum may be h or residual.  The backward pass is
+    btx_rmsnorm_backward(dxn, n.sum, gain, n.rstd, dres=dsum)."""
+    _on_current(h)
+    out = out if out is not None else alloc_fp8(h.shape, -1, h.device)
+    rstd = rstd if rstd is not None else torch.empty(h.shape[0], dtype=torch.float32, device=h.device)
+    if sum is None and residual is not None:
+        sum = torch.empty_like(h)
+    _run("rmsnorm_fp8", "btx_rmsnorm_fp8", h, None, (h, gain, eps, residual, sum, xn, rstd, out))
+    return Norm8(out, rstd, sum if sum is not None else h, xn)
+
+
+def btx_fp8_matmul(a: Fp8, b: Fp8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out [M,N] = residual + a b^T of a [M,K] and b [N,K]; of `out`'s dtype where there is one.  residual may be out."""
+    _on_current(a.codes)
+    if out is None:
+        out = torch.empty((a.codes.shape[0], b.codes.shape[0]), dtype=dtype, device=a.codes.device)
+    _run("fp8_matmul", "btx_fp8_matmul", a.codes, workspace, (a, b, residual, out))
+    return out
+
+
+def btx_moe_ff_forward_fp8(x: Fp8, W1: Fp8, W3: Fp8, W2: Fp8, routing, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[T,d] of the layer of 8-bit experts: x of btx_rmsnorm_fp8 or btx_fp8_quantize(x); W1, W3, W2 as btx_fp8_quantize(W, axis=-2) returns
+    them; routing of btx_moe_route or btx_moe_group_route."""
+    _on_current(x.codes)
+    out = out if out is not None else torch.empty((x.codes.shape[0], x.K), dtype=torch.bfloat16, device=x.codes.device)
+    _run("forward_fp8", "btx_moe_ff_forward_fp8", x.codes, workspace, (x, W1, W3, W2, routing, residual, out))
     return out
 
 

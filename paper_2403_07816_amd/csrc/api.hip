@@ -4,6 +4,7 @@
 #include <cmath>
 
 #include "common.h"
+#include "fp8.h"
 #include "gemm_f32.h"
 #include "gemm_mfma.h"
 #include "group_route.h"
@@ -198,6 +199,7 @@ int btx_init(void) {
   void* p = nullptr;
   if (int rc = static_scratch(&p)) return rc;   // also looks up this device's copy of the fixed workspace
   if (int rc = mx4_prepare()) return rc;
+  if (int rc = f8_prepare()) return rc;
   return ff_prepare();
 }
 
@@ -543,6 +545,120 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
   BTX_STAGE(BTX_STAGE_UP, launch_mx4_up(l, {W1_codes, W1_scales}, {W3_codes, W3_scales}, sh, s));
   int slices = 1;
   BTX_STAGE(BTX_STAGE_DOWN, launch_mx4_down(l, {W2_codes, W2_scales}, sh, &slices, s));
+  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, static_cast<const float*>(w.y), slices, false, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
+  return BTX_OK;
+}
+
+int64_t btx_fp8_code_pitch(int64_t K) { return K > 0 && K < (int64_t)1 << 40 ? f8_pitch(K) : 0; }
+int64_t btx_fp8_scale_pitch(int64_t K) { return K > 0 && K < (int64_t)1 << 40 ? f8_scale_pitch(K) : 0; }
+
+namespace {
+int fp8_tensor_ok(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, const uint8_t* codes, const uint8_t* scales) {
+  if (!dtype_ok(dtype) || batch < 0 || rows < 0 || cols < 0 || (axis != 0 && axis != 1)) return BTX_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0 || cols == 0) return BTX_OK;
+  // (codes of one element are 128 bytes)
+  const int64_t n = axis == 1 ? rows : cols, K = f8_pitch(std::min<int64_t>(axis == 1 ? cols : rows, (int64_t)1 << 40));
+  if (n >= (int64_t)1 << 40 || K >= ((int64_t)1 << 40) / n || batch >= ((int64_t)1 << 40) / (n * K)) return BTX_ERR_INVALID_ARG;
+  if (!x || !codes || !scales || !aligned16(x, codes, scales)) return BTX_ERR_INVALID_ARG;
+  return BTX_OK;
+}
+}  // namespace
+
+int btx_fp8_quantize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, int block_rows, uint8_t* codes,
+                     uint8_t* scales, void* stream) {
+  if (block_rows != 1 && block_rows != kF8Block) return BTX_ERR_INVALID_ARG;
+  if (int rc = fp8_tensor_ok(x, dtype, batch, rows, cols, axis, codes, scales)) return rc;
+  if (batch == 0 || rows == 0 || cols == 0) return BTX_OK;
+  return launch_f8_quantize(x, dtype, batch, rows, cols, axis, block_rows, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+int btx_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int64_t batch, int64_t rows, int64_t cols, int axis, void* out,
+                       void* stream) {
+  if (int rc = fp8_tensor_ok(out, dtype, batch, rows, cols, axis, codes, scales)) return rc;
+  if (batch == 0 || rows == 0 || cols == 0) return BTX_OK;
+  return launch_f8_dequantize(codes, scales, dtype, batch, rows, cols, axis, out, static_cast<hipStream_t>(stream));
+}
+
+int btx_rmsnorm_fp8(const void* h, const void* residual, int dtype, const float* gain, float eps, int T, int d, void* sum, void* xn, float* rstd,
+                    uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!dtype_ok(dtype) || T < 0 || d <= 0 || d % 8 != 0 || !(eps >= 0.f)) return BTX_ERR_INVALID_ARG;
+  if (d > kF8NormMostColumns) return BTX_ERR_UNSUPPORTED;
+  if (T == 0) return BTX_OK;
+  if (!h || !gain || !rstd || (!codes != !scales) || (!codes && !xn)) return BTX_ERR_INVALID_ARG;
+  if (!aligned16(h, residual, gain, sum, xn, codes, scales)) return BTX_ERR_INVALID_ARG;
+  if (xn && (xn == h || xn == residual || xn == sum)) return BTX_ERR_INVALID_ARG;
+  return launch_f8_norm(F8NormArgs{h, residual, dtype, gain, eps, T, d, sum, xn, rstd, codes, scales}, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+bool fp8_matmul_ok(int M, int N, int K) {
+  return M >= 0 && N > 0 && K > 0 && N % 8 == 0 && (int64_t)M * std::max<int64_t>(N, f8_pitch(K)) < (int64_t)1 << 40 &&
+         (int64_t)N * f8_pitch(K) < (int64_t)1 << 40;
+}
+bool fp8_matmul_supported(int M, int N, int K) { return M < kF8MostRows && std::max(N, K) <= kF8MostColumns; }
+}  // namespace
+
+size_t btx_fp8_matmul_workspace_bytes(int M, int N, int K) {
+  if (!fp8_matmul_ok(M, N, K) || !fp8_matmul_supported(M, N, K) || M == 0) return 0;
+  return f8_matmul_workspace_bytes(M, N, K);
+}
+
+int btx_fp8_matmul(const uint8_t* A_codes, const uint8_t* A_scales, const uint8_t* B_codes, const uint8_t* B_scales, int M, int N, int K,
+                   const void* residual, void* out, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!fp8_matmul_ok(M, N, K) || !dtype_ok(dtype)) return BTX_ERR_INVALID_ARG;
+  if (M == 0) return BTX_OK;
+  if (!A_codes || !A_scales || !B_codes || !B_scales || !out) return BTX_ERR_INVALID_ARG;
+  if (!aligned16(A_codes, A_scales, B_codes, B_scales, residual, out, workspace)) return BTX_ERR_INVALID_ARG;
+  if (!fp8_matmul_supported(M, N, K)) return BTX_ERR_UNSUPPORTED;
+  const size_t bytes = f8_matmul_workspace_bytes(M, N, K);
+  if (bytes && !workspace) return BTX_ERR_INVALID_ARG;
+  if (workspace_bytes < bytes) return BTX_ERR_WORKSPACE;
+  return launch_f8_matmul(F8Matmul{{A_codes, A_scales}, {B_codes, B_scales}, M, N, K, residual, out, dtype, workspace}, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+bool fp8_layer_ok(int T, int d, int f, int E, int k) {
+  return T >= 0 && d > 0 && f > 0 && E >= 1 && E <= kF8MaxExperts && k >= 1 && k <= E && d % 8 == 0 && f % 8 == 0 &&
+         (int64_t)T * k < kF8MostRows && T <= kCombineMostTokens && (int64_t)T * k * std::max(f8_pitch(d), f8_pitch(f)) < (int64_t)1 << 40 &&
+         (int64_t)E * std::max(f * f8_pitch(d), d * f8_pitch(f)) < (int64_t)1 << 40;
+}
+struct Fp8Ws { uint8_t *act_codes, *act_scales; void* y; size_t bytes; };
+Fp8Ws carve_fp8(void* ws, int T, int d, int f, int E, int k) {
+  const size_t R = (size_t)T * k;
+  Carver c(ws);
+  Fp8Ws w;
+  w.act_codes = static_cast<uint8_t*>(c.take(R * f8_pitch(f)));
+  w.act_scales = static_cast<uint8_t*>(c.take(R * f8_scale_pitch(f)));
+  w.y = c.take(f8_y_bytes((int64_t)R, d));
+  w.bytes = c.used;
+  return w;
+}
+}  // namespace
+
+size_t btx_moe_ff_forward_fp8_workspace_bytes(int T, int d, int f, int E, int k) {
+  if (!fp8_layer_ok(T, d, f, E, k) || T == 0) return 0;
+  return carve_fp8(nullptr, T, d, f, E, k).bytes;
+}
+
+int btx_moe_ff_forward_fp8(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* W1_codes, const uint8_t* W1_scales,
+                           const uint8_t* W3_codes, const uint8_t* W3_scales, const uint8_t* W2_codes, const uint8_t* W2_scales, int T, int d, int f,
+                           int E, int k, const float* gates, const int32_t* offsets, const int32_t* perm, const int32_t* inv_pos, const void* residual,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!fp8_layer_ok(T, d, f, E, k)) return BTX_ERR_INVALID_ARG;
+  if (T == 0) return BTX_OK;
+  if (!x_codes || !x_scales || !W1_codes || !W1_scales || !W3_codes || !W3_scales || !W2_codes || !W2_scales || !gates || !offsets || !perm ||
+      !inv_pos || !out || !workspace)
+    return BTX_ERR_INVALID_ARG;
+  if (!aligned16(x_codes, x_scales, W1_codes, W1_scales, W3_codes, W3_scales, W2_codes, W2_scales, residual, out, workspace)) return BTX_ERR_INVALID_ARG;
+  if (std::max(d, f) > kF8MostColumns) return BTX_ERR_UNSUPPORTED;
+  const Fp8Ws w = carve_fp8(workspace, T, d, f, E, k);
+  if (workspace_bytes < w.bytes) return BTX_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const F8Layer l{{x_codes, x_scales}, {W1_codes, W1_scales}, {W3_codes, W3_scales}, {W2_codes, W2_scales}, T, d, f, E, k, offsets, perm,
+                  w.act_codes, w.act_scales, w.y};
+  BTX_STAGE(BTX_STAGE_UP, launch_f8_up(l, s));
+  int slices = 1;
+  BTX_STAGE(BTX_STAGE_DOWN, launch_f8_down(l, &slices, s));
   BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, static_cast<const float*>(w.y), slices, false, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
   return BTX_OK;
 }

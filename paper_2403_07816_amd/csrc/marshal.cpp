@@ -1,5 +1,5 @@
 // Argument marshalling of the entry points that a program calls once or more for every layer (routing with and without the
-// normalisation or from logits, forward, backward, those of 4-bit floats), for binding.py: the checks and addresses of up to thirty tensors and the call itself.  In
+// normalisation or from logits, forward, backward, those of 4-bit and of 8-bit floats), for binding.py: the checks and addresses of up to thirty tensors and the call itself.  In
 // Python these are 0.2 us a tensor and 0.1 us an argument (0.6 where its shape and dtype are checked), 7 us of a call that launches two
 // kernels.  Nothing is kept from one call
 // for the next but the addresses of the library's functions.
@@ -33,6 +33,15 @@ struct Library {
   decltype(&btx_mx4_dequantize) mx4_dequantize;
   decltype(&btx_moe_ff_forward_mx4_workspace_bytes) forward_mx4_bytes;
   decltype(&btx_moe_ff_forward_mx4) forward_mx4;
+  decltype(&btx_fp8_code_pitch) fp8_pitch;
+  decltype(&btx_fp8_scale_pitch) fp8_scale_pitch;
+  decltype(&btx_fp8_quantize) fp8_quantize;
+  decltype(&btx_fp8_dequantize) fp8_dequantize;
+  decltype(&btx_rmsnorm_fp8) rmsnorm_fp8;
+  decltype(&btx_fp8_matmul_workspace_bytes) matmul_bytes;
+  decltype(&btx_fp8_matmul) matmul;
+  decltype(&btx_moe_ff_forward_fp8_workspace_bytes) forward_fp8_bytes;
+  decltype(&btx_moe_ff_forward_fp8) forward_fp8;
 } lib{};
 
 struct PyError {};                       // a Python exception has been set
@@ -158,6 +167,30 @@ struct Mx4Ptrs {
     codes = typed<uint8_t>(c, at::kByte, shape, what + ".codes");
     shape.back() = lib.mx4_pitch(K);
     scales = typed<uint8_t>(s, at::kByte, shape, what + ".scales");
+  }
+};
+
+// Tensors of a call on one device, that of `first`
+struct Place {
+  int64_t device;
+  explicit Place(PyObject* first) : device(tensor(first).is_cuda() ? tensor(first).get_device() : -1) {}
+  template <typename T> T* operator()(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const std::string& what) const {
+    T* const p = typed<T>(o, type, shape, what);
+    if (o != Py_None && tensor(o).get_device() != device) fail(PyExc_ValueError, (what + " is on another device").c_str());
+    return p;
+  }
+};
+// codes [.., n, K padded] and scales of an Fp8
+struct Fp8Ptrs {
+  uint8_t *codes, *scales;
+  Fp8Ptrs(const Place& at, PyObject* q, at::IntArrayRef batch, int64_t n, int64_t K, const std::string& what) {
+    const Attr c(q, "codes"), s(q, "scales"), k(q, "K");
+    if (integer(k) != K) fail(PyExc_ValueError, (what + ".K is " + std::to_string(K)).c_str());
+    at::DimVector shape(batch.begin(), batch.end());
+    shape.append({n, lib.fp8_pitch(K)});
+    codes = at.operator()<uint8_t>(c, at::kByte, shape, what + ".codes");
+    shape.back() = lib.fp8_scale_pitch(K);
+    scales = at.operator()<uint8_t>(s, at::kByte, shape, what + ".scales");
   }
 };
 
@@ -394,6 +427,100 @@ PyObject* forward_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// x, axis (of the library), block_rows, out, workspace (none), stream
+PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&] {
+    const at::Tensor& x = tensor(a[0]);
+    if (x.dim() < 2) fail(PyExc_ValueError, "a matrix or a stack of them is expected");
+    const int axis = int32(a[1]), block_rows = int32(a[2]), dt = dtype_code(x);
+    const at::IntArrayRef batch = x.sizes().slice(0, x.dim() - 2);
+    const int64_t rows = x.size(-2), cols = x.size(-1);
+    const Place at(a[0]);
+    const Fp8Ptrs q(at, a[3], batch, axis ? rows : cols, axis ? cols : rows, "out");
+    const void* const from = address(a[0]);
+    void* const stream = reinterpret_cast<void*>(integer(a[5]));
+    return called([&] { return lib.fp8_quantize(from, dt, c10::multiply_integers(batch), rows, cols, axis, block_rows, q.codes, q.scales, stream); });
+  });
+}
+
+// q, axis, out, workspace (none), stream
+PyObject* fp8_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const at::Tensor& out = tensor(a[2]);
+    if (out.dim() < 2) fail(PyExc_ValueError, "a matrix or a stack of them is expected");
+    const int axis = int32(a[1]), dt = dtype_code(out);
+    const at::IntArrayRef batch = out.sizes().slice(0, out.dim() - 2);
+    const int64_t rows = out.size(-2), cols = out.size(-1);
+    const Place at(a[2]);
+    const Fp8Ptrs q(at, a[0], batch, axis ? rows : cols, axis ? cols : rows, "q");
+    void* const to = address(a[2]);
+    void* const stream = reinterpret_cast<void*>(integer(a[4]));
+    return called([&] { return lib.fp8_dequantize(q.codes, q.scales, dt, c10::multiply_integers(batch), rows, cols, axis, to, stream); });
+  });
+}
+
+// h, gain, eps, residual, sum, xn, rstd, out, workspace (none), stream
+PyObject* rmsnorm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    const at::Tensor& h = matrix(a[0]);
+    const int T = size32(h.size(0)), d = size32(h.size(1)), dt = dtype_code(h);
+    const at::ScalarType type = h.scalar_type();
+    const float eps = real(a[2]);
+    const Place at(a[0]);
+    const void* const from = address(a[0]);
+    const float* const gain = at.operator()<float>(a[1], at::kFloat, {d}, "gain");
+    const void* const res = at.operator()<void>(a[3], type, {T, d}, "residual");
+    void *const sum = at.operator()<void>(a[4], type, {T, d}, "sum"), *const xn = at.operator()<void>(a[5], type, {T, d}, "xn");
+    float* const rstd = at.operator()<float>(a[6], at::kFloat, {T}, "rstd");
+    const Fp8Ptrs q(at, a[7], {}, T, d, "out");
+    void* const stream = reinterpret_cast<void*>(integer(a[9]));
+    return called([&] { return lib.rmsnorm_fp8(from, res, dt, gain, eps, T, d, sum, xn, rstd, q.codes, q.scales, stream); });
+  });
+}
+
+// a, b, residual, out, workspace, stream
+PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&] {
+    const at::Tensor& out = matrix(a[3]);
+    const Attr a_K(a[0], "K");
+    const int M = size32(out.size(0)), N = size32(out.size(1)), K = int32(a_K), dt = dtype_code(out);
+    const Place at(a[3]);
+    const Fp8Ptrs A(at, a[0], {}, M, K, "a"), B(at, a[1], {}, N, K, "b");
+    const void* const res = at.operator()<void>(a[2], out.scalar_type(), {M, N}, "residual");
+    void* const to = address(a[3]);
+    void* const stream = reinterpret_cast<void*>(integer(a[5]));
+    const auto call = [&](void* ws, size_t bytes) {
+      return lib.matmul(A.codes, A.scales, B.codes, B.scales, M, N, K, res, to, dt, ws, bytes, stream);
+    };
+    const size_t bytes = lib.matmul_bytes(M, N, K);
+    if (!bytes) return called([&] { return call(nullptr, 0); });
+    return with_workspace(a[4], bytes, call);
+  });
+}
+
+// x, W1, W3, W2, routing, residual, out, workspace, stream
+PyObject* forward_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&] {
+    const Attr x_codes(a[0], "codes"), x_K(a[0], "K"), w1_codes(a[1], "codes"), w2_K(a[3], "K"), o_idx(a[4], "topk_idx");
+    const int T = size32(matrix(x_codes).size(0)), d = int32(x_K);
+    const int E = tensor(w1_codes).dim() ? size32(tensor(w1_codes).size(0)) : 0, f = int32(w2_K), k = size32(matrix(o_idx).size(1));
+    const Place at(x_codes);
+    const Fp8Ptrs x(at, a[0], {}, T, d, "x"), W1(at, a[1], {E}, f, d, "W1"), W3(at, a[2], {E}, f, d, "W3"), W2(at, a[3], {E}, d, f, "W2");
+    const Attr o_gates(a[4], "gates"), o_offsets(a[4], "offsets"), o_perm(a[4], "perm"), o_inv(a[4], "inv_pos");
+    const void* const res = at.operator()<void>(a[5], at::kBFloat16, {T, d}, "residual");
+    void* const out = at.operator()<void>(a[6], at::kBFloat16, {T, d}, "out");
+    const float* const gates = at.operator()<float>(o_gates, at::kFloat, {T, k}, "gates");
+    const int32_t *const offsets = at.operator()<int32_t>(o_offsets, at::kInt, {E + (int64_t)1}, "offsets"),
+                  *const perm = at.operator()<int32_t>(o_perm, at::kInt, {(int64_t)T * k}, "perm"),
+                  *const inv = at.operator()<int32_t>(o_inv, at::kInt, {T, k}, "inv_pos");
+    void* const stream = reinterpret_cast<void*>(integer(a[8]));
+    return with_workspace(a[7], lib.forward_fp8_bytes(T, d, f, E, k), [&](void* ws, size_t bytes) {
+      return lib.forward_fp8(x.codes, x.scales, W1.codes, W1.scales, W3.codes, W3.scales, W2.codes, W2.scales, T, d, f, E, k, gates, offsets, perm,
+                             inv, res, out, ws, bytes, stream);
+    });
+  });
+}
+
 // path of the library, which is loaded already
 PyObject* bind(PyObject*, PyObject* path) {
   const char* p = PyUnicode_AsUTF8(path);
@@ -410,7 +537,11 @@ PyObject* bind(PyObject*, PyObject* path) {
       !find(l.group_route_bytes, "btx_moe_group_route_workspace_bytes") || !find(l.group_route, "btx_moe_group_route") ||
       !find(l.group_route_backward, "btx_moe_group_route_backward") || !find(l.mx4_pitch, "btx_mx4_scale_pitch") ||
       !find(l.mx4_quantize, "btx_mx4_quantize") || !find(l.mx4_dequantize, "btx_mx4_dequantize") ||
-      !find(l.forward_mx4_bytes, "btx_moe_ff_forward_mx4_workspace_bytes") || !find(l.forward_mx4, "btx_moe_ff_forward_mx4")) {
+      !find(l.forward_mx4_bytes, "btx_moe_ff_forward_mx4_workspace_bytes") || !find(l.forward_mx4, "btx_moe_ff_forward_mx4") ||
+      !find(l.fp8_pitch, "btx_fp8_code_pitch") || !find(l.fp8_scale_pitch, "btx_fp8_scale_pitch") || !find(l.fp8_quantize, "btx_fp8_quantize") ||
+      !find(l.fp8_dequantize, "btx_fp8_dequantize") || !find(l.rmsnorm_fp8, "btx_rmsnorm_fp8") ||
+      !find(l.matmul_bytes, "btx_fp8_matmul_workspace_bytes") || !find(l.matmul, "btx_fp8_matmul") ||
+      !find(l.forward_fp8_bytes, "btx_moe_ff_forward_fp8_workspace_bytes") || !find(l.forward_fp8, "btx_moe_ff_forward_fp8")) {
     PyErr_Format(PyExc_RuntimeError, "%s does not have the library's entry points", p);
     return nullptr;
   }
@@ -420,7 +551,8 @@ PyObject* bind(PyObject*, PyObject* path) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, FAST(route), FAST(norm_route), FAST(forward), FAST(backward), FAST(group_route),
-                         FAST(group_route_backward), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(forward_mx4), {nullptr, nullptr, 0, nullptr}};
+                         FAST(group_route_backward), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(forward_mx4), FAST(fp8_quantize), FAST(fp8_dequantize),
+                         FAST(rmsnorm_fp8), FAST(fp8_matmul), FAST(forward_fp8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
