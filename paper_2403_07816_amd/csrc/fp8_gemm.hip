@@ -8,7 +8,9 @@
 //   * Results in fp32: the codes become bf16, exactly, with their scale (values under 2^-126: to bf16's precision there), and
 //     v_mfma_f32_16x16x32_bf16 multiplies those: exact products, sums in fp32, at half the rate.
 #include "fp8.h"
+#include "tile_lds.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace btx {
@@ -41,6 +43,7 @@ struct F8Args {
   int E, k, R, N, K;                    // N columns, depth K
   uint8_t* act_codes; uint8_t* act_scales;
   void* out; const void* residual;
+  int slices; float* sums;              // K ranges of a tile; more than one: their sums [slice][R][N] go there, and not to out
 };
 
 struct Tile { int e, row0, row_end; };
@@ -48,7 +51,7 @@ struct Tile { int e, row0, row_end; };
 // The row tiles of up to 256 experts, found by every wavefront for itself: lane l looks at experts 4l .. 4l + 3 (all 64 lanes active)
 struct ExpertTiles {
   int o[5], n, incl, rows;
-  __device__ __forceinline__ ExpertTiles(const int32_t* __restrict__ offsets, int E, int tile_rows, int lane) : n(0), rows(tile_rows) {
+  template <typename P> __device__ __forceinline__ ExpertTiles(P offsets, int E, int tile_rows, int lane) : n(0), rows(tile_rows) {
     static_assert(kF8MaxExperts <= 4 * kWave, "four experts a lane");
 #pragma unroll
     for (int i = 0; i < 5; ++i) o[i] = offsets[min(4 * lane + i, E)];
@@ -287,7 +290,435 @@ __global__ __launch_bounds__(kUpWaves* kWave, 2) void f8_few_up_kernel(F8Args g)
   }
 }
 
-int few_tile_rows(int64_t rows, int E) { return rows / E <= 24 ? 32 : 64; }
+// ---- many rows: 256 x 256 tiles ---------------------------------------------------------------------------------
+// Bound by the matrix cores and by what feeds them from LDS.  A k tile is a block: [row][128 bytes] of either operand, 8 wavefronts have 128 x 64 of the
+// result each (UP: 32 columns of either panel, 128 in all: a block of the activations), 128 accumulator registers.
+//   * global -> LDS copies are direct, 16 bytes a lane, two stages of both operands (128 KB); chunks are swizzled by row (tile_swz()).
+//   * The two wavefronts of a SIMD alternate between a memory phase and a compute phase (16 products), half a period apart, with a barrier at
+//     every boundary.  The first memory phase of a k tile reads all fragments of B and those of half of A's rows, the second the other half's: B's
+//     stage and half of A's are free half a k tile early, and the copies of the k tile after the next go there.
+//   * Scales: 16 bytes of every row are copied for 16 k tiles, a wavefront 64 rows with one instruction; a lane reads a word of each of its rows
+//     for 4 k tiles, and the products pick the byte.
+//   * Tiles are dealt so that the ones an XCD runs at a time share row and column panels in its L2; a workgroup takes tile after tile, the next
+//     one's first stage is under way beside the epilogue.
+//   * Of a tile's rows that are not there, 64 of a wavefront's are passed over.
+constexpr int kTileRows = 256, kTileWaves = 8;
+constexpr uint32_t kStage = 32768, kScaleStage = 8192;  // scales of 16 k tiles: 256 rows of A, 256 of B
+constexpr uint32_t kB0 = 2 * kStage, kScale0 = 4 * kStage, kOffsets0 = kScale0 + 2 * kScaleStage;
+constexpr int kTileLds = kOffsets0 + (kF8MaxExperts + 1) * 4;
+enum TileMode { kUp, kOut, kOutExact };                 // activations; bf16; fp32 by way of bf16
+
+template <TileMode MODE>
+__global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g, int n_ct) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr bool UP = MODE == kUp;
+  constexpr int TM = 8, TN = 4, TNH = UP ? 2 : 4, COLS = UP ? 128 : 256;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave >> 2, wn = wave & 3, grp = wm;     // the wavefronts of a SIMD are w and w + 4
+  const int64_t row_bytes = f8_pitch(g.K), sc_pitch = f8_scale_pitch(g.K);
+  const int nk_all = (int)(row_bytes / kF8Block), slices = UP ? 1 : g.slices;
+  const uint32_t base = (uint32_t)(uintptr_t)smem;
+  typedef const __attribute__((address_space(3))) int32_t* lds_int;
+
+  // ---- the tile
+  const lds_int s_offsets = (lds_int)(uintptr_t)(base + kOffsets0);
+  if (g.offsets) {
+    for (int i = threadIdx.x; i <= g.E; i += kTileWaves * kWave) reinterpret_cast<int32_t*>(smem + kOffsets0)[i] = g.offsets[i];
+    __syncthreads();
+  }
+  int e, row0, row_end, col0, slice, id = blockIdx.x;
+  int k_first, nk;                                       // its k tiles: k_first (a multiple of four, as words of scales are read) .. + nk - 1
+  auto find_tile = [&]() -> bool {                       // `id`, or the next one of this workgroup that names a tile
+    auto among = [&](int n_rt, auto rows_of) -> bool {
+      const int most = n_rt * n_ct + kXcds;
+      int tm, tn;
+      for (; id < most * slices; id += gridDim.x)
+        if (tile_of(id % most, n_rt, n_ct, tm, tn)) {
+          const int quads = (nk_all + 3) / 4;
+          slice = id / most;
+          k_first = slice * quads / slices * 4;
+          nk = min((slice + 1) * quads / slices * 4, nk_all) - k_first;
+          const Tile t = rows_of(tm);
+          e = t.e;
+          row0 = t.row0;
+          row_end = t.row_end;
+          col0 = tn * COLS;
+          return true;
+        }
+      return false;
+    };
+    if (!g.offsets) return among((g.R + kTileRows - 1) / kTileRows, [&](int tm) { return Tile{0, tm * kTileRows, g.R}; });
+    const ExpertTiles tiles(s_offsets, g.E, kTileRows, here(lane));
+    return among(tiles.count(), [&](int tm) { return tiles.at(tm); });
+  };
+
+  // ---- copies.  Rows 0-63 and 128-191 of A are its first half (A0), which the first memory phase reads, the others the second (A1): a
+  // wavefront has 16 rows of either and 32 rows of B, 8 lanes a row, 8 rows an instruction; 64 rows of A's scales, or of B's
+  auto chunk = [](int ln, int q) { return (ln & 7) ^ tile_swz(ln / 8 + 8 * (q & 1)); };
+  const int a_row = wm * 128 + wn * 16;
+  uint32_t a_off[4], b_off[4], s_off;                    // a_off: A0, A0, A1, A1
+  uint64_t a_from, b_from, s_from;                       // a, b: of the k tile behind the next (A1: the one before)
+  auto row_index = [&](int at) -> uint32_t {
+    const int gr = min(row0 + at, row_end - 1);
+    return g.perm ? (uint32_t)g.perm[gr] / (uint32_t)g.k : (uint32_t)(gr - row0);
+  };
+  auto set_rows = [&] {                                  // (as indexes of rows, for now)
+    const int ln = here(lane);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) a_off[q] = row_index(a_row + (q >> 1) * 64 + (q & 1) * 8 + ln / 8);
+    if (wm == 0) s_off = row_index(wn * 64 + ln);
+  };
+  auto set_sources = [&] {
+    const int ln = here(lane);
+    // (asm: one register for each of these for the whole loop, not the pair that their 64-bit products are in)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      a_off[q] = a_off[q] * (uint32_t)row_bytes + chunk(ln, q) * 16 + (kCopyBias2 - 1024 * (q & 1));
+      const int row = wave * 32 + q * 8 + ln / 8, col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
+      b_off[q] = (uint32_t)col * (uint32_t)row_bytes + chunk(ln, q) * 16 + (kCopyBias4 - 1024 * q);
+      asm volatile("" : "+v"(a_off[q]), "+v"(b_off[q]));
+    }
+    const F8Matrix& bm = UP && wave >= 4 ? g.b1 : g.b0;
+    const int64_t k0 = (int64_t)k_first * kF8Block;
+    a_from = uniform64(g.a.codes + (g.perm ? 0 : (int64_t)row0 * row_bytes) + k0) - kCopyBias2;
+    b_from = uniform64(bm.codes + ((int64_t)e * g.N + col0) * row_bytes + k0) - kCopyBias4;
+    if (wm == 0) {
+      s_off *= (uint32_t)sc_pitch;
+      s_from = uniform64(g.a.scales + (g.perm ? 0 : (int64_t)row0 * sc_pitch));
+    } else {
+      const int row = wn * 64 + ln, col = min(col0 + (UP ? row & 127 : row), g.N - 1) - col0;
+      s_off = (uint32_t)col * (uint32_t)sc_pitch;
+      s_from = uniform64((UP && wn >= 2 ? g.b1 : g.b0).scales + ((int64_t)e * g.N + col0) * sc_pitch);
+    }
+    asm volatile("" : "+v"(s_off));
+  };
+  const uint32_t to_a = base + a_row * 128, to_b = base + kB0 + wave * 4096, to_s = base + kScale0 + wave * 1024;
+  auto copy_a0b = [&](int stage) {
+    copy32(a_from, a_off[0], a_off[1], to_a + stage * kStage);
+    copy64(b_from, b_off, to_b + stage * kStage);
+  };
+  auto copy_a1 = [&](int stage, uint64_t from) { copy32(from, a_off[2], a_off[3], to_a + stage * kStage + 64 * 128); };
+  auto copy_scales = [&](int c) { copy16(s_from + (uint64_t)c * 16, s_off, to_s + (c & 1) * kScaleStage); };   // of k tiles 16 c ..
+
+  // ---- fragments: lane l has row l % 16, chunks 2g and 2g + 1 of lane group g = l / 16
+  const int r = lane & 15, lg = lane >> 4;
+  typedef const __attribute__((address_space(3))) u32x4* lds_frag;
+  typedef const __attribute__((address_space(3))) uint32_t* lds_word;
+  const uint32_t at_a = base + (wm * 128 + r) * 128 + ((2 * lg) ^ tile_swz(r)) * 16;
+  const uint32_t at_b = base + kB0 + (wn * (TNH * 16) + r) * 128 + ((2 * lg) ^ tile_swz(r)) * 16;
+  const uint32_t sc_a = base + kScale0 + (wm * 128 + r) * 16;
+  const uint32_t sc_b = base + kScale0 + 4096 + (wn * (TNH * 16) + r) * 16;
+  f32x4 acc[TM][TN];
+  u32x4 fa[TM / 2][2], fb[TN][2];                        // (of one half of A)
+  uint32_t xa[TM], xb[TN];
+  auto read_a = [&](int stage, int half) {
+#pragma unroll
+    for (int i = 0; i < TM / 2; ++i)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) fa[i][st] = *(lds_frag)(uintptr_t)((at_a ^ (st << 4)) + stage * kStage + (half * 4 + i) * 2048);
+  };
+  auto read_b = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+        fb[j][st] = *(lds_frag)(uintptr_t)((at_b ^ (st << 4)) + stage * kStage + (j / TNH) * (128 * 128) + (j % TNH) * 2048);
+  };
+  auto read_scales = [&](int k) {                        // of k tiles k .. k + 3
+    const uint32_t at = ((k >> 4) & 1) * kScaleStage + (k & 12);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) xa[i] = *(lds_word)(uintptr_t)(sc_a + at + i * 256);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) xb[j] = *(lds_word)(uintptr_t)(sc_b + at + (j / TNH) * 2048 + (j % TNH) * 256);
+  };
+  // the products of half h of A's rows
+  auto multiply = [&](auto q_tag, int h) {
+    constexpr int Q = decltype(q_tag)::value;
+    if constexpr (MODE == kOutExact) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {                      // 8 codes a lane
+        bf16x8 bb[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          bb[j] = to_bf16x8(fb[j][q / 2][2 * (q & 1)], fb[j][q / 2][2 * (q & 1) + 1], f8_scale_or_nan(xb[j] >> (8 * Q) & 255u));
+#pragma unroll
+        for (int i = 0; i < TM / 2; ++i) {
+          const bf16x8 aa = to_bf16x8(fa[i][q / 2][2 * (q & 1)], fa[i][q / 2][2 * (q & 1) + 1], f8_scale_or_nan(xa[h * 4 + i] >> (8 * Q) & 255u));
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[h * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[j], aa, acc[h * 4 + i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM / 2; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[h * 4 + i][j] = mfma_f8<Q>(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[h * 4 + i][j], xb[j], xa[h * 4 + i]);
+    }
+  };
+  // Copies: in the first memory phase of k tile kt A1 of kt + 1 (2 instructions), in the second A0 and B of kt + 2 (2 and 4), in front of them
+  // now and then one of scales.  What they overwrite was read last in the memory phases before, and they have four phases or more to land.
+  auto k_tile = [&](auto q_tag, int kt) {
+    constexpr int Q = decltype(q_tag)::value, stage = Q & 1;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // ---- memory phase
+      const bool live = row0 + wm * 128 + h * 64 < row_end;    // (of this half of its rows any: a phase without products is short)
+      if (Q == 0 && h == 0) read_scales(k_first + kt);
+      if (live) {
+        read_a(stage, h);
+        if (h == 0) read_b(stage);
+      }
+      if (h == 0) {
+        if (kt + 1 < nk) copy_a1(stage ^ 1, a_from - kF8Block);
+      } else {
+        // the scales of the next 16 k tiles, where those of the 16 before were (the first two are there from the start)
+        if (Q == 2) {
+          const int k = k_first + kt, c = k >> 4;
+          if ((k & 15) == 2 && c > k_first >> 4 && 16 * (c + 1) < k_first + nk) copy_scales(c + 1);
+        }
+        if (kt + 2 < nk) {
+          copy_a0b(stage);
+          a_from += kF8Block;
+          b_from += kF8Block;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(0xC07F);                // lgkmcnt(0)
+      // What the next memory phases read has landed: behind h == 0, A1 of this k tile; behind h == 1, A0 and B of the next.  What has been issued
+      // since may be outstanding (scales, which are needed much later, count as if they were not).
+      auto landed = [&] {
+        if (h == 0) {
+          if (kt + 1 < nk) wait_vmcnt<8>(); else wait_vmcnt<0>();
+        } else {
+          if (kt + 2 < nk) wait_vmcnt<8>(); else wait_vmcnt<2>();
+        }
+      };
+      if (grp == 1) landed();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      // ---- compute phase
+      if (live) multiply(q_tag, h);
+#pragma unroll
+      for (int i = 0; i < TM / 2; ++i)                   // here, and not where the sums are needed next: behind the next phases' barriers
+#pragma unroll
+        for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(acc[h * 4 + i][j]));
+      if (grp == 0) landed();
+      __builtin_amdgcn_sched_barrier(0);
+      if (!(grp == 1 && h == 1 && kt + 1 == nk)) __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (!find_tile()) return;
+  set_rows();
+  auto start = [&] {                                     // into the first stages: k tile 0; and scales
+    set_sources();
+    const int c = k_first >> 4;
+    copy_scales(c);
+    if (16 * (c + 1) < k_first + nk) copy_scales(c + 1);
+    copy_a0b(0);
+    copy_a1(0, a_from);
+    a_from += kF8Block;
+    b_from += kF8Block;
+  };
+  start();
+  for (;;) {
+    if (nk > 1) {                                        // into the second stages, as k tile -1 would have
+      copy_a0b(1);
+      a_from += kF8Block;
+      b_from += kF8Block;
+      wait_vmcnt<6>();
+    } else {
+      wait_vmcnt<0>();
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    if (grp == 1) __builtin_amdgcn_s_barrier();          // group 1 is a phase behind
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+    for (int kt = 0; kt < nk; kt += 4) {
+      k_tile(std::integral_constant<int, 0>{}, kt);
+      if (kt + 1 < nk) k_tile(std::integral_constant<int, 1>{}, kt + 1);
+      if (kt + 2 < nk) k_tile(std::integral_constant<int, 2>{}, kt + 2);
+      if (kt + 3 < nk) k_tile(std::integral_constant<int, 3>{}, kt + 3);
+    }
+
+    // ---- epilogue: acc[i][j][v] is row wm 128 + 16 i + l % 16, column 16 j + 4 (l / 16) + v of the wavefront's.  All of LDS is free (group
+    // 0's last barrier comes after group 1's last read); the result goes through the second stages, and the first stages are filled for
+    // the workgroup's next tile beside it.
+    const int out_row0 = row0, out_end = row_end, out_col0 = col0, out_slice = slice;
+    const int ln = here(lane), r = ln & 15, lg = ln >> 4, tid = wave * kWave + ln;
+    __syncthreads();
+    id += gridDim.x;
+    const bool more = find_tile();
+    if (more) set_rows();
+    char* const out = smem + kStage;
+    if constexpr (UP) {
+      // a workgroup's 128 columns are one block; its codes [256 rows][128 bytes] are put together in LDS, 16-byte chunks swizzled by row
+      uint32_t* const s_amax = reinterpret_cast<uint32_t*>(smem + kB0 + kStage);      // [256][4]
+      if (more) start();
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const bool there = out_col0 + wn * 32 + j * 16 + 4 * lg + x < g.N;
+            acc[i][j][x] = there ? silu_f(acc[i][j][x]) * acc[i][j + 2][x] : 0.f;
+            amax = max(amax, f8_magnitude(acc[i][j][x]));
+          }
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, kWave));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, kWave));
+        if (lg == 0) s_amax[(wm * 128 + i * 16 + r) * 4 + wn] = amax;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int row = wm * 128 + i * 16 + r;
+        const u32x4 four = *reinterpret_cast<const u32x4*>(s_amax + row * 4);
+        const uint32_t byte = f8_scale_byte(max(max(four[0], four[1]), max(four[2], four[3])));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+          *reinterpret_cast<uint32_t*>(out + row * 128 + (((wn * 2 + j) ^ (row >> 1 & 7)) << 4) + lg * 4) = f8_codes4(v, byte);
+        }
+        if (wn == 0 && lg == 0 && out_row0 + row < out_end) g.act_scales[(int64_t)(out_row0 + row) * f8_scale_pitch(g.N) + out_col0 / 128] = (uint8_t)byte;
+      }
+      __syncthreads();
+      const int64_t out_pitch = f8_pitch(g.N), out_sc_pitch = f8_scale_pitch(g.N);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int idx = q * 512 + tid, row = idx >> 3, c = idx & 7;
+        if (out_row0 + row < out_end)
+          *reinterpret_cast<u32x4*>(g.act_codes + (int64_t)(out_row0 + row) * out_pitch + out_col0 + c * 16) =
+              *reinterpret_cast<const u32x4*>(out + row * 128 + ((c ^ (row >> 1 & 7)) << 4));
+      }
+      if (out_col0 + COLS >= g.N && tid < 256 && out_row0 + tid < out_end)          // the zeros behind a row's scales
+        for (int64_t z = out_col0 / 128 + 1; z < out_sc_pitch; ++z) g.act_scales[(int64_t)(out_row0 + tid) * out_sc_pitch + z] = 0;
+    } else {
+      if (more) start();
+      if (slices > 1 || MODE == kOutExact) {             // four columns a lane, as they are
+        float* const to = slices > 1 ? g.sums + (int64_t)out_slice * g.R * g.N : static_cast<float*>(g.out);
+        const float* const residual = slices > 1 ? nullptr : static_cast<const float*>(g.residual);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const int m = wm * 128 + i * 16 + r, n = out_col0 + wn * 64 + j * 16 + 4 * lg;
+            if (out_row0 + m >= out_end || n >= g.N) continue;
+            const int64_t at = (int64_t)(out_row0 + m) * g.N + n;
+            if (MODE == kOutExact && residual) acc[i][j] += *reinterpret_cast<const f32x4*>(residual + at);
+            *reinterpret_cast<f32x4*>(to + at) = acc[i][j];
+          }
+        if (!more) return;
+        __syncthreads();
+        continue;
+      }
+      // 32 rows of the wavefront's 64 columns at a time (128 bytes a row) through its own piece of LDS, chunks swizzled by row
+      char* const band = out + wave * 4096;
+      const int n0 = out_col0 + wn * 64;
+      bf16_t* const to = static_cast<bf16_t*>(g.out);
+#pragma unroll
+      for (int ib = 0; ib < TM / 2; ++ib) {
+#pragma unroll
+        for (int i2 = 0; i2 < 2; ++i2)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            f32x4& v = acc[2 * ib + i2][j];
+            const int row = i2 * 16 + r, byte = (j * 16 + 4 * lg) * 2;
+            if (g.residual) {
+              const int m = out_row0 + wm * 128 + ib * 32 + row, n = n0 + j * 16 + 4 * lg;
+              if (m < out_end && n < g.N) {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const bf16_t*>(g.residual) + (int64_t)m * g.N + n);
+                v += f32x4{bf16lo(w[0]), bf16hi(w[0]), bf16lo(w[1]), bf16hi(w[1])};
+              }
+            }
+            *reinterpret_cast<u32x2*>(band + row * 128 + ((byte >> 4 ^ (row & 7)) << 4) + (byte & 15)) =
+                u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+          }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int row = q * 8 + ln / 8, c = ln & 7, m = out_row0 + wm * 128 + ib * 32 + row;
+          const u32x4 w = *reinterpret_cast<const u32x4*>(band + row * 128 + ((c ^ (row & 7)) << 4));
+          if (m < out_end && n0 + c * 8 < g.N) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(to + (int64_t)m * g.N + n0 + c * 8));
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+    if (!more) return;
+    __syncthreads();                                     // the second stages are free
+  }
+}
+
+// the dynamic-LDS limit, once per device (not while a stream is being captured; btx_init() does it too)
+template <auto KERNEL> int raise_lds() {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return BTX_ERR_HIP;
+  if (!(done.load(std::memory_order_relaxed) >> dev & 1)) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, kTileLds) != hipSuccess)
+      return BTX_ERR_HIP;
+    done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return BTX_OK;
+}
+
+template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
+  if (int rc = raise_lds<f8_tile_kernel<MODE>>()) return rc;
+  const int n_ct = ceil_div(g.N, MODE == kUp ? 128 : 256);
+  const int64_t n_rt = g.offsets ? most_tiles(g.R, g.E, kTileRows) : ceil_div(g.R, kTileRows);
+  const int64_t tiles = (n_rt * n_ct + kXcds) * g.slices;
+  // A workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end.  Of less than two
+  // rounds each has its own: a few ids name no tile, and their compute units take the ones behind the 256th.
+  const int64_t grid = tiles <= 2 * kTileGrid ? tiles : kTileGrid;
+  f8_tile_kernel<MODE><<<(unsigned)grid, kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+
+// K ranges of the tiles: as many as fill the chip where the tiles alone do not, of eight k tiles or more each; no more than whoever adds them takes, and
+// than there is room for
+constexpr int kMostSlices = 8;
+constexpr int64_t kSumBytes = (int64_t)kTileGrid * 256 * 256 * 4;        // of 256 tiles
+int64_t sum_bytes(int64_t R, int N) { return std::min(R * N * 4 * kMostSlices, kSumBytes); }
+int slices_of(int64_t tiles, int64_t R, int N, int K, int most) {
+  const int64_t fit = sum_bytes(R, N) / (R * N * 4);
+  return (int)std::max<int64_t>(std::min({kTileGrid / tiles, f8_pitch(K) / kF8Block / 8, fit, (int64_t)most, (int64_t)kMostSlices}), 1);
+}
+
+// out = residual + the sums of the slices, in order; four columns a thread
+constexpr int kAddThreads = 256;
+template <typename OT>
+__global__ __launch_bounds__(kAddThreads) void f8_add_slices_kernel(const f32x4* __restrict__ sums, int slices, int64_t n, const OT* residual, OT* out) {
+  for (int64_t i = (int64_t)blockIdx.x * kAddThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kAddThreads) {
+    f32x4 u[kMostSlices];
+#pragma unroll
+    for (int q = 0; q < kMostSlices; ++q) u[q] = sums[(int64_t)min(q, slices - 1) * n + i];
+    f32x4 v = u[0];
+#pragma unroll
+    for (int q = 1; q < kMostSlices; ++q)
+      if (q < slices) v += u[q];
+    if constexpr (std::is_same_v<OT, float>) {
+      if (residual) v += reinterpret_cast<const f32x4*>(residual)[i];
+      reinterpret_cast<f32x4*>(out)[i] = v;
+    } else {
+      if (residual) {
+        const u32x2 w = reinterpret_cast<const u32x2*>(residual)[i];
+        v += f32x4{bf16lo(w[0]), bf16hi(w[0]), bf16lo(w[1]), bf16hi(w[1])};
+      }
+      reinterpret_cast<u32x2*>(out)[i] = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    }
+  }
+}
 
 template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_t s) {
   const dim3 grid((unsigned)(g.offsets ? most_tiles(g.R, g.E, tile_rows) : ceil_div(g.R, tile_rows)), (unsigned)ceil_div(g.N, kFewCols));
@@ -307,29 +738,63 @@ int launch_few_up(const F8Args& g, int tile_rows, hipStream_t s) {
 // (tiles of 32 rows only where there are fewer than 25 an expert)
 static_assert(kF8MostColumns / kFewCols <= 65535 && (kF8MostRows / 64 + kF8MaxExperts + 0ll) * 8 * kWave < 1ll << 32, "the grid");
 
+// How many rows a row tile has: 32, 64 or 256, as mx4_tile_rows()
+int tile_rows_of(int64_t R, int E, int64_t tile_columns, int64_t depth, int64_t a_rows, int64_t a_pitch) {
+  const int64_t avg = R / E;
+  const bool enough = R * tile_columns >= 12000 || R * depth >= (int64_t)1150000000;
+  // (rows of a are found with 32-bit offsets in a tile: the last one's, 112 bytes of a chunk and kCopyBias2)
+  if (avg >= 32 && enough && a_rows * a_pitch + kF8Block + kCopyBias2 < (int64_t)1 << 32) return kTileRows;
+  return avg <= 24 ? 32 : 64;
+}
+int layer_rows(const F8Layer& l) {
+  return tile_rows_of((int64_t)l.T * l.k, l.E, ceil_div(l.f, 128) + ceil_div(l.d, 256), (int64_t)l.d * l.f, l.T, f8_pitch(l.d));
+}
+// (rows of a tile are neighbours)
+int matmul_rows(int M, int N, int K) { return tile_rows_of(M, 1, ceil_div(N, 256), (int64_t)N * K, kTileRows, f8_pitch(K)); }
+
 }  // namespace
 
-int f8_prepare() { return BTX_OK; }
+int f8_prepare() {
+  if (int rc = raise_lds<f8_tile_kernel<kUp>>()) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<kOut>>()) return rc;
+  return raise_lds<f8_tile_kernel<kOutExact>>();
+}
 
-size_t f8_matmul_workspace_bytes(int, int, int) { return 0; }
+// (never less for more rows, also where so many are not cut)
+size_t f8_matmul_workspace_bytes(int M, int N, int K) { return f8_pitch(K) / kF8Block >= 16 && M >= 32 ? (size_t)sum_bytes(M, N) : 0; }
 int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
-  const F8Args g{m.a, m.b, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.M, m.N, m.K, nullptr, nullptr, m.out, m.residual};
-  const int rows = few_tile_rows(m.M, 1);
-  return m.dtype == BTX_BF16 ? launch_few<bf16_t>(g, rows, s) : launch_few<float>(g, rows, s);
+  F8Args g{m.a, m.b, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.M, m.N, m.K, nullptr, nullptr, m.out, m.residual, 1, static_cast<float*>(m.workspace)};
+  const int rows = matmul_rows(m.M, m.N, m.K);
+  const bool bf16 = m.dtype == BTX_BF16;
+  if (rows != kTileRows) return bf16 ? launch_few<bf16_t>(g, rows, s) : launch_few<float>(g, rows, s);
+  g.slices = slices_of((int64_t)ceil_div(m.M, kTileRows) * ceil_div(m.N, 256), m.M, m.N, m.K, kMostSlices);
+  if (int rc = bf16 ? launch_tiles<kOut>(g, s) : launch_tiles<kOutExact>(g, s)) return rc;
+  if (g.slices > 1) {
+    const int64_t n = (int64_t)m.M * m.N / 4;
+    const unsigned blocks = (unsigned)std::min<int64_t>((n + kAddThreads - 1) / kAddThreads, 1 << 20);
+    const f32x4* const sums = reinterpret_cast<const f32x4*>(g.sums);
+    if (bf16) f8_add_slices_kernel<<<blocks, kAddThreads, 0, s>>>(sums, g.slices, n, static_cast<const bf16_t*>(m.residual), static_cast<bf16_t*>(m.out));
+    else f8_add_slices_kernel<<<blocks, kAddThreads, 0, s>>>(sums, g.slices, n, static_cast<const float*>(m.residual), static_cast<float*>(m.out));
+    BTX_LAUNCH_CHECK();
+  }
+  return BTX_OK;
 }
 
 int launch_f8_up(const F8Layer& l, hipStream_t s) {
-  const int R = l.T * l.k;
-  return launch_few_up(F8Args{l.x, l.W1, l.W3, l.offsets, l.perm, l.E, l.k, R, l.f, l.d, l.act_codes, l.act_scales, nullptr, nullptr},
-                       few_tile_rows(R, l.E), s);
+  const F8Args g{l.x, l.W1, l.W3, l.offsets, l.perm, l.E, l.k, l.T * l.k, l.f, l.d, l.act_codes, l.act_scales, nullptr, nullptr, 1, nullptr};
+  const int rows = layer_rows(l);
+  return rows == kTileRows ? launch_tiles<kUp>(g, s) : launch_few_up(g, rows, s);
 }
 
-size_t f8_y_bytes(int64_t R, int d) { return (size_t)R * d * 2; }
+size_t f8_y_bytes(int64_t R, int d) { return (size_t)std::max(R * d * 2, sum_bytes(R, d)); }
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s) {
-  const int R = l.T * l.k;
+  const int R = l.T * l.k, rows = layer_rows(l);
+  F8Args g{{l.act_codes, l.act_scales}, l.W2, {nullptr, nullptr}, l.offsets, nullptr, l.E, l.k, R, l.d, l.f, nullptr, nullptr, l.y, nullptr, 1, static_cast<float*>(l.y)};
   *slices = 1;
-  return launch_few<bf16_t>(F8Args{{l.act_codes, l.act_scales}, l.W2, {nullptr, nullptr}, l.offsets, nullptr, l.E, l.k, R, l.d, l.f, nullptr, nullptr, l.y, nullptr},
-                            few_tile_rows(R, l.E), s);
+  if (rows != kTileRows) return launch_few<bf16_t>(g, rows, s);
+  const int64_t busy = std::min<int64_t>(l.E, R), tiles = busy * ceil_div(ceil_div(R, busy), kTileRows) * ceil_div(l.d, 256);
+  *slices = g.slices = slices_of(tiles, R, l.d, l.f, combine_most_slices(l.T, l.k, BTX_BF16));
+  return launch_tiles<kOut>(g, s);
 }
 
 }  // namespace btx
