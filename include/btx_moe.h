@@ -574,7 +574,8 @@ int btx_fp8_matmul(const uint8_t* A_codes, const uint8_t* A_scales, const uint8_
  *   residual  [T,d] bf16, may be NULL;   out [T,d] bf16;   residual may be out
  *   gates, offsets, perm, inv_pos: as written by btx_moe_route or btx_moe_group_route
  * Requirements: d % 8 == 0, f % 8 == 0, 1 <= k <= E <= 256, T <= 2^26 - 4, T*k < 2^28 - 256, T*k*max(pitches) < 2^40,
- * E*max(f*btx_fp8_code_pitch(d), d*btx_fp8_code_pitch(f)) < 2^40; codes, scales, residual, out and the workspace on 16-byte boundaries. d and f <= 2097120 (BTX_ERR_UNSUPPORTED).
+ * E*max(f*btx_fp8_code_pitch(d), d*btx_fp8_code_pitch(f)) < 2^40; codes, scales, residual, out and the workspace on 16-byte boundaries.
+ * d and f <= 2097120, T*btx_fp8_code_pitch(d) <= 2^32 - 2048 (BTX_ERR_UNSUPPORTED).
  */
 size_t btx_moe_ff_forward_fp8_workspace_bytes(int T, int d, int f, int E, int k);
 int btx_moe_ff_forward_fp8(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* W1_codes, const uint8_t* W1_scales,

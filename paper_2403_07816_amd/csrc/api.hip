@@ -629,7 +629,7 @@ Fp8Ws carve_fp8(void* ws, int T, int d, int f, int E, int k) {
   Fp8Ws w;
   w.act_codes = static_cast<uint8_t*>(c.take(R * f8_pitch(f)));
   w.act_scales = static_cast<uint8_t*>(c.take(R * f8_scale_pitch(f)));
-  w.y = c.take(f8_y_bytes((int64_t)R, d));
+  w.y = c.take(f8_y_bytes((int64_t)R, d, f, E));
   w.bytes = c.used;
   return w;
 }
@@ -650,7 +650,7 @@ int btx_moe_ff_forward_fp8(const uint8_t* x_codes, const uint8_t* x_scales, cons
       !inv_pos || !out || !workspace)
     return BTX_ERR_INVALID_ARG;
   if (!aligned16(x_codes, x_scales, W1_codes, W1_scales, W3_codes, W3_scales, W2_codes, W2_scales, residual, out, workspace)) return BTX_ERR_INVALID_ARG;
-  if (std::max(d, f) > kF8MostColumns) return BTX_ERR_UNSUPPORTED;
+  if (std::max(d, f) > kF8MostColumns || T * f8_pitch(d) > kF8MostTokenBytes) return BTX_ERR_UNSUPPORTED;
   const Fp8Ws w = carve_fp8(workspace, T, d, f, E, k);
   if (workspace_bytes < w.bytes) return BTX_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -63,14 +63,15 @@ struct F8Matmul { F8Matrix a, b; int M, N, K; const void* residual; void* out; i
 size_t f8_matmul_workspace_bytes(int M, int N, int K);
 int launch_f8_matmul(const F8Matmul& m, hipStream_t s);
 
-// The layer of 8-bit experts
+// The layer of 8-bit experts.  Rows of x are found with 32-bit offsets in tiles of 256: the last one's, 112 bytes of a chunk and the copies' bias
+constexpr int64_t kF8MostTokenBytes = ((int64_t)1 << 32) - 2048;
 struct F8Layer {
   F8Matrix x, W1, W3, W2; int T, d, f, E, k; const int32_t* offsets; const int32_t* perm;
   uint8_t* act_codes; uint8_t* act_scales; void* y;
 };
 int launch_f8_up(const F8Layer& l, hipStream_t s);
 // y = act W2, [T*k, d] bf16; or *slices > 1 of its sums in fp32 instead, [slice][T*k, d], for launch_combine() to add and weigh without rounding them
-size_t f8_y_bytes(int64_t R, int d);
+size_t f8_y_bytes(int64_t R, int d, int f, int E);
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s);
 int f8_prepare();                      // one-time set-up on the current device (not capturable)
 

@@ -78,132 +78,165 @@ struct ExpertTiles {
 inline int most_tiles(int R, int E, int tile_rows) { return (int)std::min<int64_t>((int64_t)R / tile_rows + std::min(E, R), R); }
 
 // ---- few rows -------------------------------------------------------------------------------------------------
-// Bound by reading B.  It goes from memory to the registers that the products take, 256 elements of 16 rows a wavefront at a time: in load s lane group
-// g has 16-byte chunk 4s + g, so that a load covers 64 bytes of a row.  RB blocks of 16 rows meet each fragment of it.
-constexpr int kFewCols = 32;
-
-// acc += the products of RB x 16 rows of a and NF x 16 rows of b over blocks first, first + 1, first + step, first + step + 1, ..  live: how many
-// of the RB have rows.  EXACT: by way of bf16
-template <bool EXACT, int RB, int NF>
-__device__ __forceinline__ void few_products(f32x4 (&acc)[RB][NF], const char* const (&b)[NF], const char* const (&b_sc)[NF], const uint32_t (&b_off)[NF],
-                                             const uint32_t (&b_sc_off)[NF], const F8Matrix& a, const uint32_t (&row)[RB], int live, int n_blk,
-                                             int64_t a_pitch, int first, int step, int grp) {
-#pragma unroll 1
-  for (int b0 = first; b0 < n_blk; b0 += step) {
-    const bool two = b0 + 1 < n_blk;
-    auto chunk = [&](const uint8_t* base, int64_t r, int s) -> u32x4 {
-      return s < 2 || two ? *reinterpret_cast<const u32x4*>(base + (r * n_blk + b0) * kF8Block + (4 * s + grp) * 16) : u32x4{0u, 0u, 0u, 0u};
-    };
-    // all loads before the first product, those of a, which are not memory's, first
-    u32x4 av[RB][4];
-    uint32_t a_s[RB];
+// Bound by reading B.  It goes from memory to the registers that the products take, 256 elements (two blocks) of 16 rows a wavefront at a time: in load s
+// lane group g has 16-byte chunk 4s + g, so that a load covers 64 bytes of a row.  RB blocks of 16 rows of A meet each fragment of it.
+// NF x 16 rows of b: a base that the wavefront shares and a lane's offset of 32 bits, for codes and scales
+template <int NF> struct FewB { const char* codes[NF]; const char* scales[NF]; uint32_t at[NF], sc_at[NF]; };
+// N blocks' codes and scales of RB x 16 rows of a and NF x 16 rows of b
+template <int N, int RB, int NF> struct FewStep { u32x4 a[RB][2 * N], b[NF][2 * N]; uint32_t a_s[RB], b_s[NF]; };
+template <int N> __device__ __forceinline__ uint32_t few_scales(const void* p) {
+  static_assert(N == 1 || N == 2, "bytes");
+  if constexpr (N == 1) return *static_cast<const uint8_t*>(p);
+  else return *static_cast<const uint16_t*>(p);
+}
+template <int N, int RB, int NF>
+__device__ __forceinline__ void few_load(FewStep<N, RB, NF>& v, const FewB<NF>& b, const F8Matrix& a, const uint32_t (&row)[RB], int n_blk,
+                                         int64_t a_pitch, int b0, int grp) {
+  const uint32_t at = (uint32_t)b0 * kF8Block + grp * 16u;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      if (rb >= live) break;
-      a_s[rb] = *reinterpret_cast<const uint16_t*>(a.scales + row[rb] * a_pitch + b0);
+  for (int p = 0; p < NF; ++p) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) av[rb][s] = chunk(a.codes, row[rb], s);
-    }
-    u32x4 bv[NF][4];
-    uint32_t b_s[NF];
+    for (int s = 0; s < 2 * N; ++s) v.b[p][s] = *reinterpret_cast<const u32x4*>(b.codes[p] + (b.at[p] + at + s * 64u));
+    v.b_s[p] = few_scales<N>(b.scales[p] + (b.sc_at[p] + b0));
+  }
 #pragma unroll
-    for (int p = 0; p < NF; ++p) {
-      b_s[p] = *reinterpret_cast<const uint16_t*>(b_sc[p] + (b_sc_off[p] + b0));
+  for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        bv[p][s] = s < 2 || two ? *reinterpret_cast<const u32x4*>(b[p] + (b_off[p] + b0 * (uint32_t)kF8Block + (4 * s + grp) * 16u)) : u32x4{0u, 0u, 0u, 0u};
-    }
-    if constexpr (EXACT) {
+    for (int s = 0; s < 2 * N; ++s) v.a[rb][s] = *reinterpret_cast<const u32x4*>(a.codes + (int64_t)row[rb] * n_blk * kF8Block + (at + s * 64u));
+    v.a_s[rb] = few_scales<N>(a.scales + row[rb] * a_pitch + b0);
+  }
+}
+template <bool EXACT, int H, int N, int RB, int NF> __device__ __forceinline__ void few_multiply(f32x4 (*acc)[NF], const FewStep<N, RB, NF>& v) {
+  if constexpr (EXACT) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+    for (int q = 0; q < 4; ++q) {                        // 8 codes a lane
+      bf16x8 bb[NF];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {                    // 8 codes a lane
-          bf16x8 bb[NF];
-#pragma unroll
-          for (int p = 0; p < NF; ++p) {
-            const u32x4& v = bv[p][2 * h + q / 2];
-            bb[p] = to_bf16x8(v[2 * (q & 1)], v[2 * (q & 1) + 1], f8_scale_or_nan(b_s[p] >> (8 * h) & 255u));
-          }
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) {
-            if (rb >= live) break;
-            const u32x4& v = av[rb][2 * h + q / 2];
-            const bf16x8 aa = to_bf16x8(v[2 * (q & 1)], v[2 * (q & 1) + 1], f8_scale_or_nan(a_s[rb] >> (8 * h) & 255u));
-#pragma unroll
-            for (int p = 0; p < NF; ++p) acc[rb][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[p], aa, acc[rb][p], 0, 0, 0);
-          }
-        }
+      for (int p = 0; p < NF; ++p) {
+        const u32x4& w = v.b[p][2 * H + q / 2];
+        bb[p] = to_bf16x8(w[2 * (q & 1)], w[2 * (q & 1) + 1], f8_scale_or_nan(v.b_s[p] >> (8 * H) & 255u));
       }
-      continue;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const u32x4& w = v.a[rb][2 * H + q / 2];
+        const bf16x8 aa = to_bf16x8(w[2 * (q & 1)], w[2 * (q & 1) + 1], f8_scale_or_nan(v.a_s[rb] >> (8 * H) & 255u));
+#pragma unroll
+        for (int p = 0; p < NF; ++p) acc[rb][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[p], aa, acc[rb][p], 0, 0, 0);
+      }
     }
+  } else {
 #pragma unroll
     for (int p = 0; p < NF; ++p)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        if (rb >= live) break;
-        acc[rb][p] = mfma_f8<0>(bv[p][0], bv[p][1], av[rb][0], av[rb][1], acc[rb][p], b_s[p], a_s[rb]);
-        acc[rb][p] = mfma_f8<1>(bv[p][2], bv[p][3], av[rb][2], av[rb][3], acc[rb][p], b_s[p], a_s[rb]);
-      }
+      for (int rb = 0; rb < RB; ++rb)
+        acc[rb][p] = mfma_f8<H>(v.b[p][2 * H], v.b[p][2 * H + 1], v.a[rb][2 * H], v.a[rb][2 * H + 1], acc[rb][p], v.b_s[p], v.a_s[rb]);
   }
+}
+// acc += the products of RB x 16 rows of a and NF x 16 rows of b over pairs of blocks first, first + step, ..; who would have the next pair
+// has the block behind the last one.  EXACT: by way of bf16.  All loads of a step are under way before its first product; with the next step's
+// under way as well there were fewer wavefronts, and it was no faster.  turn: of the pairs `first` means, to have workgroups of neighbouring
+// columns at different places of their rows.
+template <bool EXACT, int RB, int NF>
+__device__ __forceinline__ void few_products(f32x4 (*acc)[NF], const FewB<NF>& b, const F8Matrix& a, const uint32_t (&row)[RB], int n_blk, int64_t a_pitch,
+                                             int first, int step, int turn, int grp) {
+  const int pairs = n_blk / 2;
+#pragma unroll 1
+  for (int i = first; i < pairs; i += step) {
+    FewStep<2, RB, NF> v;
+    const int at = i + turn;
+    few_load(v, b, a, row, n_blk, a_pitch, 2 * (at < pairs ? at : at - pairs), grp);
+    __builtin_amdgcn_sched_barrier(0);
+    few_multiply<EXACT, 0>(acc, v);
+    few_multiply<EXACT, 1>(acc, v);
+  }
+  if (n_blk % 2 && pairs % step == first) {
+    FewStep<1, RB, NF> v;
+    few_load(v, b, a, row, n_blk, a_pitch, n_blk - 1, grp);
+    few_multiply<EXACT, 0>(acc, v);
+  }
+}
+// the same, of the blocks of rows that have one
+template <bool EXACT, int RB, int NF>
+__device__ __forceinline__ void few_live_products(f32x4 (&acc)[RB][NF], const FewB<NF>& b, const F8Args& g, const Tile& t, int n_blk, int64_t a_pitch,
+                                                  int first, int step, int turn, int grp, int r) {
+  auto go = [&](auto n_tag) {
+    constexpr int N = decltype(n_tag)::value;
+    uint32_t row[N];
+#pragma unroll
+    for (int rb = 0; rb < N; ++rb) {
+      row[rb] = (uint32_t)min(t.row0 + rb * 16 + r, t.row_end - 1);
+      if (g.perm) row[rb] = (uint32_t)g.perm[row[rb]] / (uint32_t)g.k;
+    }
+    few_products<EXACT, N, NF>(acc, b, g.a, row, n_blk, a_pitch, first, step, turn, grp);
+  };
+  const int live = (t.row_end - t.row0 + 15) / 16;
+  if (live <= 1) go(std::integral_constant<int, 1>{});
+  else if (RB <= 2 || live <= 2) go(std::integral_constant<int, RB <= 2 ? RB : 2>{});
+  else go(std::integral_constant<int, RB>{});
 }
 
 // the workgroup's tile of rows; false: there is none
 template <int RB> __device__ __forceinline__ bool few_tile(const F8Args& g, int lane, Tile& t) {
   if (!g.offsets) {
-    t = Tile{0, (int)blockIdx.x * (RB * 16), g.R};
+    t = Tile{0, (int)blockIdx.y * (RB * 16), g.R};
     return true;
   }
   const ExpertTiles tiles(g.offsets, g.E, RB * 16, lane);
-  if ((int)blockIdx.x >= tiles.count()) return false;
-  t = tiles.at(blockIdx.x);
+  if ((int)blockIdx.y >= tiles.count()) return false;
+  t = tiles.at(blockIdx.y);
   return true;
 }
-template <int RB> __device__ __forceinline__ void few_rows(const F8Args& g, const Tile& t, int r, uint32_t (&row)[RB]) {
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    row[rb] = (uint32_t)min(t.row0 + rb * 16 + r, t.row_end - 1);
-    if (g.perm) row[rb] = (uint32_t)g.perm[row[rb]] / (uint32_t)g.k;
-  }
+// rows n0 .. of expert e's matrix, up to the last one
+template <int NF> __device__ __forceinline__ void few_b(FewB<NF>& b, int p, const F8Matrix& m, const F8Args& g, int e, int n0, int r) {
+  const int64_t pitch = f8_pitch(g.K), sc_pitch = f8_scale_pitch(g.K), n = (int64_t)e * g.N + min(n0, g.N - 1);
+  const uint32_t at = (uint32_t)max(min(r, g.N - 1 - n0), 0);
+  b.codes[p] = reinterpret_cast<const char*>(m.codes) + n * pitch;
+  b.scales[p] = reinterpret_cast<const char*>(m.scales) + n * sc_pitch;
+  b.at[p] = at * (uint32_t)pitch;
+  b.sc_at[p] = at * (uint32_t)sc_pitch;
 }
 
-// out, 32 columns a workgroup, whose NW wavefronts share K
-template <int RB, int NW, typename OT>
-__global__ __launch_bounds__(NW* kWave, 2) void f8_few_kernel(F8Args g) {
-  __shared__ f32x4 s_sum[NW][RB][2][kWave];
-  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = lane & 15, grp = lane >> 4;
+// FR x 16 columns, by KS wavefronts that share K.  UP: both panels, and the activations in fp32 (sums [R][N]): their blocks of 128 columns would make
+// workgroups too large to spread over the chip (one token, 2 experts of 4096 x 11008: 53 us), and another launch quantises them
+template <bool UP, int RB, int FR, int KS, typename OT>
+__global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
+  constexpr int NF = UP ? 2 * FR : FR;
+  __shared__ f32x4 s_sum[KS][RB][NF][kWave];
+  const int lane = threadIdx.x & (kWave - 1), ks = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = lane & 15, grp = lane >> 4;
   Tile t;
   if (!few_tile<RB>(g, lane, t)) return;
-  uint32_t row[RB];
-  few_rows<RB>(g, t, r, row);
-  const int n0 = blockIdx.y * kFewCols, live = min(RB, (t.row_end - t.row0 + 15) / 16);
-  const int64_t pitch = f8_pitch(g.K), sc_pitch = f8_scale_pitch(g.K);
-  const char* b[2];
-  const char* b_sc[2];
-  uint32_t b_off[2], b_sc_off[2];
+  const int n0 = blockIdx.x * (FR * 16), n_blk = (int)(f8_pitch(g.K) / kF8Block);
+  FewB<NF> b;
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int64_t n = (int64_t)t.e * g.N + n0;
-    const int at = min(16 * p + r, g.N - 1 - n0);
-    b[p] = reinterpret_cast<const char*>(g.b0.codes) + n * pitch;
-    b_sc[p] = reinterpret_cast<const char*>(g.b0.scales) + n * sc_pitch;
-    b_off[p] = (uint32_t)at * (uint32_t)pitch;
-    b_sc_off[p] = (uint32_t)at * (uint32_t)sc_pitch;
-  }
-  f32x4 acc[RB][2] = {};
-  few_products<std::is_same_v<OT, float>, RB, 2>(acc, b, b_sc, b_off, b_sc_off, g.a, row, live, (int)(pitch / kF8Block), sc_pitch, 2 * wave, 2 * NW, grp);
+  for (int p = 0; p < NF; ++p) few_b(b, p, p < FR ? g.b0 : g.b1, g, t.e, n0 + 16 * (p % FR), r);
+  f32x4 acc[RB][NF] = {};
+  // (one token, DOWN of 2 experts of 4096 x 11008: 22.8 us with all workgroups at the same place of their rows, 18.9 so; wider ones gained nothing)
+  const int turn = FR == 1 && n_blk > 1 ? 3 * blockIdx.x % (n_blk / 2) : 0;
+  few_live_products<std::is_same_v<OT, float> && !UP>(acc, b, g, t, n_blk, f8_scale_pitch(g.K), ks, KS, turn, grp, r);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int p = 0; p < 2; ++p) s_sum[wave][rb][p][lane] = acc[rb][p];
+    for (int p = 0; p < NF; ++p) s_sum[ks][rb][p][lane] = acc[rb][p];
   __syncthreads();
-  for (int i = wave; i < 2 * RB; i += NW) {
-    const int rb = i >> 1, p = i & 1, m = t.row0 + rb * 16 + r, n = n0 + 16 * p + 4 * grp;
-    if (m >= t.row_end || n >= g.N) continue;
-    f32x4 v = s_sum[0][rb][p][lane];
 #pragma unroll
-    for (int x = 1; x < NW; ++x) v += s_sum[x][rb][p][lane];
+  for (int i = 0; i < FR * RB; ++i) {
+    if (i % KS != ks) continue;
+    const int rb = i / FR, p = i % FR, m = t.row0 + rb * 16 + r, n = n0 + 16 * p + 4 * grp;
+    if (m >= t.row_end || n >= g.N) continue;
+    auto sum = [&](int q) {
+      f32x4 v = s_sum[0][rb][q][lane];
+#pragma unroll
+      for (int x = 1; x < KS; ++x) v += s_sum[x][rb][q][lane];
+      return v;
+    };
+    f32x4 v = sum(p);
     const int64_t at = (int64_t)m * g.N + n;
-    if constexpr (std::is_same_v<OT, float>) {
+    if constexpr (UP) {
+      const f32x4 h3 = sum(FR + p);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[x] = silu_f(v[x]) * h3[x];
+      *reinterpret_cast<f32x4*>(g.sums + at) = v;
+    } else if constexpr (std::is_same_v<OT, float>) {
       if (g.residual) v += *reinterpret_cast<const f32x4*>(static_cast<const float*>(g.residual) + at);
       *reinterpret_cast<f32x4*>(static_cast<float*>(g.out) + at) = v;
     } else {
@@ -216,79 +249,32 @@ __global__ __launch_bounds__(NW* kWave, 2) void f8_few_kernel(F8Args g) {
   }
 }
 
-// The activations of 128 columns, a block, by a workgroup: 4 wavefronts' columns x 2 halves of K
-constexpr int kUpWaves = 8;
-template <int RB>
-__global__ __launch_bounds__(kUpWaves* kWave, 2) void f8_few_up_kernel(F8Args g) {
-  __shared__ f32x4 s_sum[kUpWaves][4][kWave];
-  __shared__ uint32_t s_amax[2][4][16];
-  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = lane & 15, grp = lane >> 4;
-  const int cg = wave & 3, half = wave >> 2;
-  Tile t;
-  if (!few_tile<RB>(g, lane, t)) return;
-  uint32_t row[RB];
-  few_rows<RB>(g, t, r, row);
-  const int n0 = blockIdx.y * kF8Block + cg * 32, live = min(RB, (t.row_end - t.row0 + 15) / 16);
-  const int64_t pitch = f8_pitch(g.K), sc_pitch = f8_scale_pitch(g.K);
-  const char* b[4];
-  const char* b_sc[4];
-  uint32_t b_off[4], b_sc_off[4];
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const F8Matrix& m = p < 2 ? g.b0 : g.b1;
-    const int64_t n = (int64_t)t.e * g.N + min(n0, g.N - 1);
-    const int at = max(min(16 * (p & 1) + r, g.N - 1 - n0), 0);
-    b[p] = reinterpret_cast<const char*>(m.codes) + n * pitch;
-    b_sc[p] = reinterpret_cast<const char*>(m.scales) + n * sc_pitch;
-    b_off[p] = (uint32_t)at * (uint32_t)pitch;
-    b_sc_off[p] = (uint32_t)at * (uint32_t)sc_pitch;
-  }
-  f32x4 acc[RB][4] = {};
-  few_products<false, RB, 4>(acc, b, b_sc, b_off, b_sc_off, g.a, row, live, (int)(pitch / kF8Block), sc_pitch, 2 * half, 4, grp);
-  // Two blocks of rows at a time, one for either half's wavefronts, which give each other their sums
-  const int64_t act_pitch = f8_pitch(g.N), act_sc_pitch = f8_scale_pitch(g.N);
-#pragma unroll
-  for (int rb0 = 0; rb0 < RB; rb0 += 2) {
-    const bool mine = rb0 + half < RB, others = rb0 + 1 - half < RB;
-    __syncthreads();
-    if (others) {
-#pragma unroll
-      for (int p = 0; p < 4; ++p) s_sum[wave][p][lane] = half ? acc[rb0][p] : acc[rb0 + 1 < RB ? rb0 + 1 : rb0][p];
-    }
-    __syncthreads();
-    float v[2][4];
-    uint32_t amax = 0;
-    if (mine) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const f32x4 h1 = s_sum[wave ^ 4][j][lane] + (half ? acc[rb0 + 1 < RB ? rb0 + 1 : rb0][j] : acc[rb0][j]);
-        const f32x4 h3 = s_sum[wave ^ 4][2 + j][lane] + (half ? acc[rb0 + 1 < RB ? rb0 + 1 : rb0][2 + j] : acc[rb0][2 + j]);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          v[j][x] = n0 + 16 * j + 4 * grp + x < g.N ? silu_f(h1[x]) * h3[x] : 0.f;
-          amax = max(amax, f8_magnitude(v[j][x]));
-        }
-      }
-      amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, kWave));
-      amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, kWave));
-      if (grp == 0) s_amax[half][cg][r] = amax;
-    }
-    __syncthreads();
-    const int m = t.row0 + (rb0 + half) * 16 + r;
-    if (mine && m < t.row_end) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) amax = max(amax, s_amax[half][x][r]);
-      const uint32_t byte = f8_scale_byte(amax);
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        *reinterpret_cast<uint32_t*>(g.act_codes + (int64_t)m * act_pitch + n0 + 16 * j + 4 * grp) = f8_codes4(v[j], byte);
-      if (cg == 0 && grp == 0) g.act_scales[(int64_t)m * act_sc_pitch + blockIdx.y] = (uint8_t)byte;
-      // the zeros behind the scales of a row
-      if (cg == 0 && blockIdx.y + 1 == gridDim.y)
-        for (int64_t z = gridDim.y + grp; z < act_sc_pitch; z += 4) g.act_scales[(int64_t)m * act_sc_pitch + z] = 0;
-    }
-  }
+template <bool UP, int FR, int KS, typename OT> int launch_few_shape(const F8Args& g, int tile_rows, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(g.N, FR * 16), (unsigned)(g.offsets ? most_tiles(g.R, g.E, tile_rows) : ceil_div(g.R, tile_rows)));
+  if (tile_rows == 32) f8_few_kernel<UP, 2, FR, KS, OT><<<grid, KS * kWave, 0, s>>>(g);
+  else f8_few_kernel<UP, 4, FR, KS, OT><<<grid, KS * kWave, 0, s>>>(g);
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
 }
+// 16 columns a workgroup, whose 4 wavefronts share K, or, where there are 2048 such pieces, 64 and 2.  A compute unit reads 25 GB/s from memory, so all
+// of them are needed.  DOWN of one token, 2 experts of 4096 x 11008 (512 pieces): 18.9 us with 16 columns, 24 with 32, 31 with 64; of 64 tokens,
+// 32 experts of 4096 x 1376 (8192): 58, 46, 40; 2048 x 4096 (4096): 84, 66, 60; 16 experts of 1024 x 2048 (1024): 9.7, 9.0, 9.3.
+// (fp32 results: 16 always; bf16 values of 64 columns and 64 rows do not fit the registers)
+template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_t s) {
+  const int64_t tiles = g.offsets ? std::min(g.E, g.R) : ceil_div(g.R, tile_rows);
+  if constexpr (!std::is_same_v<OT, float>) {
+    if (tiles * ceil_div(g.N, 16) >= 2048) return launch_few_shape<false, 4, 2, OT>(g, tile_rows, s);
+  }
+  return launch_few_shape<false, 1, 4, OT>(g, tile_rows, s);
+}
+// (one token, 2 experts of 4096 x 11008, and 64 tokens, 32 of 4096 x 1376: 37 and 85 us; with 4 wavefronts 40 and 86, with 16 columns and 4 37 and 90)
+int launch_few_up(const F8Args& g, int tile_rows, hipStream_t s) {
+  if (int rc = launch_few_shape<true, 2, 2, float>(g, tile_rows, s)) return rc;
+  return launch_f8_quantize(g.sums, BTX_F32, 1, g.R, g.N, 1, 1, g.act_codes, g.act_scales, s);
+}
+
+// (tiles of 32 rows only where there are fewer than 25 an expert)
+static_assert(kF8MostColumns / 32 <= 65535 && (kF8MostRows / 64 + kF8MaxExperts + 0ll) * 8 * kWave < 1ll << 32, "the grid");
 
 // ---- many rows: 256 x 256 tiles ---------------------------------------------------------------------------------
 // Bound by the matrix cores and by what feeds them from LDS.  A k tile is a block: [row][128 bytes] of either operand, 8 wavefronts have 128 x 64 of the
@@ -720,37 +706,15 @@ __global__ __launch_bounds__(kAddThreads) void f8_add_slices_kernel(const f32x4*
   }
 }
 
-template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_t s) {
-  const dim3 grid((unsigned)(g.offsets ? most_tiles(g.R, g.E, tile_rows) : ceil_div(g.R, tile_rows)), (unsigned)ceil_div(g.N, kFewCols));
-  if (tile_rows == 32) f8_few_kernel<2, 8, OT><<<grid, 8 * kWave, 0, s>>>(g);
-  else f8_few_kernel<4, 8, OT><<<grid, 8 * kWave, 0, s>>>(g);
-  BTX_LAUNCH_CHECK();
-  return BTX_OK;
-}
-int launch_few_up(const F8Args& g, int tile_rows, hipStream_t s) {
-  const dim3 grid((unsigned)most_tiles(g.R, g.E, tile_rows), (unsigned)ceil_div(g.N, kF8Block));
-  if (tile_rows == 32) f8_few_up_kernel<2><<<grid, kUpWaves * kWave, 0, s>>>(g);
-  else f8_few_up_kernel<4><<<grid, kUpWaves * kWave, 0, s>>>(g);
-  BTX_LAUNCH_CHECK();
-  return BTX_OK;
-}
-
-// (tiles of 32 rows only where there are fewer than 25 an expert)
-static_assert(kF8MostColumns / kFewCols <= 65535 && (kF8MostRows / 64 + kF8MaxExperts + 0ll) * 8 * kWave < 1ll << 32, "the grid");
-
 // How many rows a row tile has: 32, 64 or 256, as mx4_tile_rows()
-int tile_rows_of(int64_t R, int E, int64_t tile_columns, int64_t depth, int64_t a_rows, int64_t a_pitch) {
+int tile_rows_of(int64_t R, int E, int64_t tile_columns, int64_t depth) {
   const int64_t avg = R / E;
   const bool enough = R * tile_columns >= 12000 || R * depth >= (int64_t)1150000000;
-  // (rows of a are found with 32-bit offsets in a tile: the last one's, 112 bytes of a chunk and kCopyBias2)
-  if (avg >= 32 && enough && a_rows * a_pitch + kF8Block + kCopyBias2 < (int64_t)1 << 32) return kTileRows;
+  if (avg >= 32 && enough) return kTileRows;
   return avg <= 24 ? 32 : 64;
 }
-int layer_rows(const F8Layer& l) {
-  return tile_rows_of((int64_t)l.T * l.k, l.E, ceil_div(l.f, 128) + ceil_div(l.d, 256), (int64_t)l.d * l.f, l.T, f8_pitch(l.d));
-}
-// (rows of a tile are neighbours)
-int matmul_rows(int M, int N, int K) { return tile_rows_of(M, 1, ceil_div(N, 256), (int64_t)N * K, kTileRows, f8_pitch(K)); }
+int layer_rows(int64_t R, int d, int f, int E) { return tile_rows_of(R, E, ceil_div(f, 128) + ceil_div(d, 256), (int64_t)d * f); }
+int matmul_rows(int M, int N, int K) { return tile_rows_of(M, 1, ceil_div(N, 256), (int64_t)N * K); }
 
 }  // namespace
 
@@ -781,14 +745,18 @@ int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
 }
 
 int launch_f8_up(const F8Layer& l, hipStream_t s) {
-  const F8Args g{l.x, l.W1, l.W3, l.offsets, l.perm, l.E, l.k, l.T * l.k, l.f, l.d, l.act_codes, l.act_scales, nullptr, nullptr, 1, nullptr};
-  const int rows = layer_rows(l);
+  const F8Args g{l.x, l.W1, l.W3, l.offsets, l.perm, l.E, l.k, l.T * l.k, l.f, l.d, l.act_codes, l.act_scales, nullptr, nullptr, 1, static_cast<float*>(l.y)};
+  const int rows = layer_rows(g.R, l.d, l.f, l.E);
   return rows == kTileRows ? launch_tiles<kUp>(g, s) : launch_few_up(g, rows, s);
 }
 
-size_t f8_y_bytes(int64_t R, int d) { return (size_t)std::max(R * d * 2, sum_bytes(R, d)); }
+// y or the sums of its slices; before these the activations of tiles of few rows in fp32: fewer than 32 rows an expert, or 12000 x 128 columns in all
+size_t f8_y_bytes(int64_t R, int d, int f, int E) {
+  const int64_t few = std::min(R, std::max<int64_t>(32 * E, 12000 / ceil_div(f, 128)));
+  return (size_t)std::max({R * d * 2, sum_bytes(R, d), few * f * 4});
+}
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s) {
-  const int R = l.T * l.k, rows = layer_rows(l);
+  const int R = l.T * l.k, rows = layer_rows(R, l.d, l.f, l.E);
   F8Args g{{l.act_codes, l.act_scales}, l.W2, {nullptr, nullptr}, l.offsets, nullptr, l.E, l.k, R, l.d, l.f, nullptr, nullptr, l.y, nullptr, 1, static_cast<float*>(l.y)};
   *slices = 1;
   if (rows != kTileRows) return launch_few<bf16_t>(g, rows, s);

@@ -155,6 +155,7 @@ def test_refusals_of_products():
         assert layer(**bad) == 1, bad
     assert layer(nbytes=64) == 3
     assert layer(d=2097128, E=1, k=1) == 2 and layer(f=2097128, E=1, k=1) == 2
+    assert layer(T=1 << 20, d=4096, E=1, k=1) == 2 and layer(T=(1 << 25), d=128, f=128, E=1, k=1) == 2
     assert lib.btx_moe_ff_forward_fp8_workspace_bytes(8, 60, 64, 4, 2) == 0
 
 
@@ -448,7 +449,8 @@ def check_product(out, a, b, residual=None):
 
 MATMULS = [(1, 8, 1), (1, 64, 128), (3, 40, 130), (16, 72, 256), (17, 128, 384), (24, 136, 1000), (25, 256, 640), (64, 512, 4096), (65, 264, 129),
            (130, 1376, 300), (256, 256, 2048), (257, 520, 1100), (301, 1032, 2177), (600, 768, 500), (1025, 264, 4001), (33, 2048, 11008), (2000, 1536, 384),
-           (300, 1032, 4100), (64, 2056, 11008), (513, 264, 18000), (16500, 2048, 130), (2100, 2048, 6500), (4200, 2048, 6500)]
+           (300, 1032, 4100), (64, 2056, 11008), (513, 264, 18000), (16500, 2048, 130), (2100, 2048, 6500), (4200, 2048, 6500),
+           (5, 33000, 136), (30, 32776, 264), (40, 33000, 520)]
 
 
 @gpu
