@@ -43,6 +43,13 @@ __device__ __forceinline__ uint32_t f8_row_max(uint32_t v) {
   v = max(v, (uint32_t)dpp_i32<kDppRor4>((int)v));
   return max(v, (uint32_t)dpp_i32<kDppRor8>((int)v));
 }
+// the largest of the four lanes that are 16 apart (the halves, then the odd and even rows of 16 change places: no trip through LDS)
+__device__ __forceinline__ uint32_t f8_across_max(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max(b[0], b[1]);
+}
 
 struct F8Matrix { const uint8_t* codes; const uint8_t* scales; };
 

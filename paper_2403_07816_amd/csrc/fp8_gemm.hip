@@ -561,8 +561,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
             acc[i][j][x] = there ? silu_f(acc[i][j][x]) * acc[i][j + 2][x] : 0.f;
             amax = max(amax, f8_magnitude(acc[i][j][x]));
           }
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, kWave));
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, kWave));
+        amax = f8_across_max(amax);
         if (lg == 0) s_amax[(wm * 128 + i * 16 + r) * 4 + wn] = amax;
       }
       __syncthreads();
@@ -673,7 +672,7 @@ template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
 
 // K ranges of the tiles: as many as fill the chip where the tiles alone do not, of eight k tiles or more each; no more than whoever adds them takes, and
 // than there is room for
-constexpr int kMostSlices = 8;
+constexpr int kMostSlices = 16;
 constexpr int64_t kSumBytes = (int64_t)kTileGrid * 256 * 256 * 4;        // of 256 tiles
 int64_t sum_bytes(int64_t R, int N) { return std::min(R * N * 4 * kMostSlices, kSumBytes); }
 int slices_of(int64_t tiles, int64_t R, int N, int K, int most) {
@@ -686,13 +685,15 @@ constexpr int kAddThreads = 256;
 template <typename OT>
 __global__ __launch_bounds__(kAddThreads) void f8_add_slices_kernel(const f32x4* __restrict__ sums, int slices, int64_t n, const OT* residual, OT* out) {
   for (int64_t i = (int64_t)blockIdx.x * kAddThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kAddThreads) {
-    f32x4 u[kMostSlices];
+    f32x4 v = sums[i];
+    for (int s0 = 1; s0 < slices; s0 += 4) {             // four loads at a time
+      f32x4 u[4];
 #pragma unroll
-    for (int q = 0; q < kMostSlices; ++q) u[q] = sums[(int64_t)min(q, slices - 1) * n + i];
-    f32x4 v = u[0];
+      for (int q = 0; q < 4; ++q) u[q] = s0 + q < slices ? sums[(int64_t)(s0 + q) * n + i] : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int q = 1; q < kMostSlices; ++q)
-      if (q < slices) v += u[q];
+      for (int q = 0; q < 4; ++q)
+        if (s0 + q < slices) v += u[q];
+    }
     if constexpr (std::is_same_v<OT, float>) {
       if (residual) v += reinterpret_cast<const f32x4*>(residual)[i];
       reinterpret_cast<f32x4*>(out)[i] = v;

@@ -135,8 +135,9 @@ template <typename XT, bool VEC, bool SHARED>
 __global__ __launch_bounds__(kThreads) void f8_quantize_cols_kernel(const XT* __restrict__ x, int64_t K, int64_t N, uint8_t* __restrict__ codes,
                                                                     uint8_t* __restrict__ scales, unsigned col_pieces) {
   __shared__ __attribute__((aligned(16))) uint8_t s_codes[kTile * kTile];
-  __shared__ uint32_t s_amax[kWaves][kTile];
+  __shared__ u32x4 s_amax[kTile];                       // of a column, or in the first of all: the four wavefronts'
   __shared__ uint8_t s_scale[kTile];
+  static_assert(kWaves == 4, "u32x4");
   const int64_t b = blockIdx.x / col_pieces, col0 = (int64_t)(blockIdx.x - b * col_pieces) * kTile, batch = blockIdx.y;
   const int64_t n_blk = f8_pitch(K) / kF8Block, pitch = f8_scale_pitch(K);
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, cq = lane & 15, kq = wave * 4 + lane / 16;
@@ -151,27 +152,24 @@ __global__ __launch_bounds__(kThreads) void f8_quantize_cols_kernel(const XT* __
     amax[h] = 0;
 #pragma unroll
     for (int q = 0; q < 8; ++q) amax[h] = max(amax[h], f8_magnitude(v[q][h]));
-    amax[h] = max(amax[h], (uint32_t)__shfl_xor((int)amax[h], 16, kWave));
-    amax[h] = max(amax[h], (uint32_t)__shfl_xor((int)amax[h], 32, kWave));
+    amax[h] = f8_across_max(amax[h]);
   }
   if constexpr (SHARED) {
     uint32_t all = 0;
 #pragma unroll
     for (int h = 0; h < 8; ++h) all = max(all, amax[h]);
     all = f8_row_max(all);
-    if (lane == 0) s_amax[wave][0] = all;
+    if (lane == 0) reinterpret_cast<uint32_t*>(s_amax)[wave] = all;
   } else if (lane < 16) {
 #pragma unroll
-    for (int h = 0; h < 8; ++h) s_amax[wave][cq * 8 + h] = amax[h];
+    for (int h = 0; h < 8; ++h) reinterpret_cast<uint32_t*>(s_amax + cq * 8 + h)[wave] = amax[h];
   }
   __syncthreads();
 #pragma unroll
   for (int h = 0; h < 8; ++h) {
     const int c = cq * 8 + h;
-    uint32_t most = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) most = max(most, s_amax[w][SHARED ? 0 : c]);
-    const uint32_t byte = f8_scale_byte(most);
+    const u32x4 four = s_amax[SHARED ? 0 : c];
+    const uint32_t byte = f8_scale_byte(max(max(four[0], four[1]), max(four[2], four[3])));
     float w[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) w[q] = v[q][h];

@@ -24,6 +24,20 @@ __device__ __forceinline__ void store_norm(bf16_t* p, const double* v) {
   for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f64_to_bf16(v[2 * i]) | (uint32_t)f64_to_bf16(v[2 * i + 1]) << 16;
   *reinterpret_cast<u32x4*>(p) = w;
 }
+// v and that of the lane that a DPP step names
+template <int CTRL> __device__ __forceinline__ double dpp_add_f64(double v) {
+  return v + __hiloint2double(dpp_i32<CTRL>(__double2hiint(v)), dpp_i32<CTRL>(__double2loint(v)));
+}
+__device__ __forceinline__ double lane_f64(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+  v = dpp_add_f64<kDppXor1>(v);
+  v = dpp_add_f64<kDppXor2>(v);
+  v = dpp_add_f64<kDppRor4>(v);
+  v = dpp_add_f64<kDppRor8>(v);
+  return (lane_f64(v, 0) + lane_f64(v, 16)) + (lane_f64(v, 32) + lane_f64(v, 48));
+}
 // the sum as it is kept, in eight floats
 __device__ __forceinline__ void round_sum(const float*, float*) {}
 __device__ __forceinline__ void round_sum(const bf16_t*, float* v) {
@@ -79,8 +93,7 @@ __global__ __launch_bounds__(kThreads) void f8_norm_kernel(const XT* h, const XT
       if (c < d) RowVec<XT, 8>::st(sum + t * d + c, v[m]);
     }
   }
-#pragma unroll
-  for (int x = 1; x < kWave; x *= 2) square += __shfl_xor(square, x, kWave);
+  square = wave_sum_f64(square);
   if constexpr (TPR > kWave) {
     if (lane == 0) s_part[threadIdx.x / kWave] = square;
     __syncthreads();
