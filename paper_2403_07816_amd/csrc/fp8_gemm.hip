@@ -77,6 +77,20 @@ struct ExpertTiles {
 };
 inline int most_tiles(int R, int E, int tile_rows) { return (int)std::min<int64_t>((int64_t)R / tile_rows + std::min(E, R), R); }
 
+// four columns of the result, from element `at` on
+template <bool F32> __device__ __forceinline__ void store_out(const F8Args& g, int64_t at, f32x4 v) {
+  if constexpr (F32) {
+    if (g.residual) v += *reinterpret_cast<const f32x4*>(static_cast<const float*>(g.residual) + at);
+    *reinterpret_cast<f32x4*>(static_cast<float*>(g.out) + at) = v;
+  } else {
+    if (g.residual) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const bf16_t*>(g.residual) + at);
+      v += f32x4{bf16lo(w[0]), bf16hi(w[0]), bf16lo(w[1]), bf16hi(w[1])};
+    }
+    *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(g.out) + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  }
+}
+
 // ---- few rows -------------------------------------------------------------------------------------------------
 // Bound by reading B.  It goes from memory to the registers that the products take, 256 elements (two blocks) of 16 rows a wavefront at a time: in load s
 // lane group g has 16-byte chunk 4s + g, so that a load covers 64 bytes of a row.  RB blocks of 16 rows of A meet each fragment of it.
@@ -236,15 +250,8 @@ __global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) v[x] = silu_f(v[x]) * h3[x];
       *reinterpret_cast<f32x4*>(g.sums + at) = v;
-    } else if constexpr (std::is_same_v<OT, float>) {
-      if (g.residual) v += *reinterpret_cast<const f32x4*>(static_cast<const float*>(g.residual) + at);
-      *reinterpret_cast<f32x4*>(static_cast<float*>(g.out) + at) = v;
     } else {
-      if (g.residual) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const bf16_t*>(g.residual) + at);
-        v += f32x4{bf16lo(w[0]), bf16hi(w[0]), bf16lo(w[1]), bf16hi(w[1])};
-      }
-      *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(g.out) + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      store_out<std::is_same_v<OT, float>>(g, at, v);
     }
   }
 }
@@ -269,12 +276,204 @@ template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_
 }
 // (one token, 2 experts of 4096 x 11008, and 64 tokens, 32 of 4096 x 1376: 37 and 85 us; with 4 wavefronts 40 and 86, with 16 columns and 4 37 and 90)
 int launch_few_up(const F8Args& g, int tile_rows, hipStream_t s) {
-  if (int rc = launch_few_shape<true, 2, 2, float>(g, tile_rows, s)) return rc;
-  return launch_f8_quantize(g.sums, BTX_F32, 1, g.R, g.N, 1, 1, g.act_codes, g.act_scales, s);
+  return launch_few_shape<true, 2, 2, float>(g, tile_rows, s);
 }
 
 // (tiles of 32 rows only where there are fewer than 25 an expert)
 static_assert(kF8MostColumns / 32 <= 65535 && (kF8MostRows / 64 + kF8MaxExperts + 0ll) * 8 * kWave < 1ll << 32, "the grid");
+
+// ---- a middling number of rows: BM x 128 tiles, BM 64 or 128 -----------------------------------------------------
+// Bound by reading B where rows are few, by LDS where they are many.  A k tile is a block: [row][128 bytes] of either operand, in a ring of NS stages that
+// direct copies fill; 4 wavefronts have BM/2 x 64 of the result each (UP: 32 columns of either panel).  Two workgroups are on a compute unit
+// and overlap what each waits for, the conversions to bf16 of fp32 results among it.  Rows of A that are not there are not copied.
+constexpr int kMidWaves = 4, kMidCols = 128;
+enum MidMode { kMidUp, kMidOut, kMidExact };           // activations in fp32 (sums), bf16, fp32 by way of bf16
+template <int BM> struct Mid {
+  static constexpr int NS = BM == 128 ? 2 : 3;
+  static constexpr uint32_t stage = (BM + kMidCols) * 128, scale_stage = (BM + kMidCols) * 16, scales0 = NS * stage;
+  static constexpr int lds = scales0 + 2 * scale_stage;
+};
+
+template <MidMode MODE, int BM>
+__global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, int n_ct) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  using M = Mid<BM>;
+  constexpr bool UP = MODE == kMidUp;
+  constexpr int NA = BM / 32, TM = BM / 32, TN = 4, COLS = UP ? 64 : 128, PER_K = NA + 4;      // a wavefront's copies of a k tile
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wm = wave >> 1, wn = wave & 1;
+  const int64_t row_bytes = f8_pitch(g.K), sc_pitch = f8_scale_pitch(g.K);
+  const int nk_all = (int)(row_bytes / kF8Block), slices = UP ? 1 : g.slices;
+  const uint32_t base = (uint32_t)(uintptr_t)smem;
+
+  // ---- the tile.  Workgroups that are a multiple of 8 apart are on one XCD: those of an expert's row tiles, which read the same columns, follow
+  // each other there
+  Tile t;
+  const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
+  int c;
+  if (g.offsets) {
+    const ExpertTiles tiles(g.offsets, g.E, BM, lane);
+    const int n_rt = tiles.count();
+    if (n_rt == 0) return;
+    c = local / n_rt * kXcds + xcd;
+    if (c >= n_ct * slices) return;
+    t = tiles.at(local % n_rt);
+  } else {
+    const int n_rt = (g.R + BM - 1) / BM;
+    c = local / n_rt * kXcds + xcd;
+    if (c >= n_ct * slices) return;
+    t = Tile{0, local % n_rt * BM, g.R};
+  }
+  const int slice = c / n_ct, col0 = (c - slice * n_ct) * COLS, quads = (nk_all + 3) / 4;
+  const int k_first = slice * quads / slices * 4, nk = min((slice + 1) * quads / slices * 4, nk_all) - k_first;
+
+  // ---- copies: a wavefront has BM / 4 rows of A and 32 of B, 8 lanes a row, 8 rows an instruction; 64 rows of A's scales, or of B's
+  auto chunk = [&](int q) { return (lane & 7) ^ tile_swz(lane / 8 + 8 * (q & 1)); };
+  auto row_index = [&](int at) -> uint32_t {
+    const int gr = min(t.row0 + at, t.row_end - 1);
+    return g.perm ? (uint32_t)g.perm[gr] / (uint32_t)g.k : (uint32_t)(gr - t.row0);
+  };
+  auto column = [&](int row) { return min(col0 + (UP ? row & 63 : row), g.N - 1) - col0; };
+  const F8Matrix& bm = UP && wave >= 2 ? g.b1 : g.b0;
+  uint32_t a_off[NA], b_off[4], s_off;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) b_off[q] = (uint32_t)column(wave * 32 + q * 8 + lane / 8) * (uint32_t)row_bytes + chunk(q) * 16 + (kCopyBias4 - 1024 * q);
+#pragma unroll
+  for (int q = 0; q < NA; ++q) a_off[q] = row_index(wave * (BM / 4) + q * 8 + lane / 8) * (uint32_t)row_bytes + chunk(q) * 16;
+  const int64_t k0 = (int64_t)k_first * kF8Block;
+  uint64_t a_from = uniform64(g.a.codes + (g.perm ? 0 : (int64_t)t.row0 * row_bytes) + k0);
+  uint64_t b_from = uniform64(bm.codes + ((int64_t)t.e * g.N + col0) * row_bytes + k0) - kCopyBias4;
+  uint64_t s_from;
+  const bool a_scales = wave < 2, has_scales = !a_scales || wave < BM / 64;
+  if (a_scales) {
+    s_off = row_index(min(wave * 64, BM - 64) + lane) * (uint32_t)sc_pitch;
+    s_from = uniform64(g.a.scales + (g.perm ? 0 : (int64_t)t.row0 * sc_pitch));
+  } else {
+    s_off = (uint32_t)column((wave - 2) * 64 + lane) * (uint32_t)sc_pitch;
+    s_from = uniform64((UP && wave == 3 ? g.b1 : g.b0).scales + ((int64_t)t.e * g.N + col0) * sc_pitch);
+  }
+  const int a_live = min(max((t.row_end - t.row0 - wave * (BM / 4) + 7) / 8, 0), NA);            // of its copies of A, those that have a row
+  const uint32_t to_a = base + wave * (BM / 4) * 128, to_b = base + BM * 128 + wave * 4096, to_s = base + M::scales0 + (a_scales ? wave * 1024 : BM * 16 + (wave - 2) * 1024);
+  auto copy_scales = [&](int c) {                        // of k tiles 16 c ..
+    if (has_scales) copy16(s_from + (uint64_t)c * 16, s_off, to_s + (c & 1) * M::scale_stage);
+  };
+  auto copy = [&](uint32_t stage) {
+    copy64(b_from, b_off, to_b + stage);
+#pragma unroll
+    for (int q = 0; q < NA; ++q)
+      if (q < a_live) copy16(a_from, a_off[q], to_a + stage + q * 1024);
+    a_from += kF8Block;
+    b_from += kF8Block;
+  };
+
+  // ---- fragments: lane l has row l % 16, chunks 2g and 2g + 1 of lane group g = l / 16
+  const int r = lane & 15, lg = lane >> 4;
+  typedef const __attribute__((address_space(3))) u32x4* lds_frag;
+  typedef const __attribute__((address_space(3))) uint32_t* lds_word;
+  const uint32_t at_a = base + (wm * (BM / 2) + r) * 128 + ((2 * lg) ^ tile_swz(r)) * 16;
+  const uint32_t at_b = base + (BM + wn * (UP ? 32 : 64) + r) * 128 + ((2 * lg) ^ tile_swz(r)) * 16;
+  auto b_row = [](int j) { return UP ? (j >> 1) * 64 + (j & 1) * 16 : j * 16; };
+  const uint32_t sc_a = base + M::scales0 + (wm * (BM / 2) + r) * 16, sc_b = base + M::scales0 + (BM + wn * (UP ? 32 : 64) + r) * 16;
+  f32x4 acc[TM][TN] = {};
+  uint32_t xa[TM], xb[TN];
+  const bool live = t.row0 + wm * (BM / 2) < t.row_end;
+  auto multiply = [&](auto q_tag, uint32_t stage) {
+    constexpr int Q = decltype(q_tag)::value;
+    u32x4 fa[TM][2], fb[TN][2];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) fb[j][st] = *(lds_frag)(uintptr_t)((at_b ^ (st << 4)) + stage + b_row(j) * 128);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) fa[i][st] = *(lds_frag)(uintptr_t)((at_a ^ (st << 4)) + stage + i * 2048);
+    if constexpr (MODE == kMidExact) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {                      // 8 codes a lane
+        bf16x8 bb[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          bb[j] = to_bf16x8(fb[j][q / 2][2 * (q & 1)], fb[j][q / 2][2 * (q & 1) + 1], f8_scale_or_nan(xb[j] >> (8 * Q) & 255u));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const bf16x8 aa = to_bf16x8(fa[i][q / 2][2 * (q & 1)], fa[i][q / 2][2 * (q & 1) + 1], f8_scale_or_nan(xa[i] >> (8 * Q) & 255u));
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[j], aa, acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma_f8<Q>(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[i][j], xb[j], xa[i]);
+    }
+  };
+
+  // ---- k tiles.  Whoever passes the barrier of k tile kt has read all of k tile kt - 1, whose stage the copies behind it fill
+  copy_scales(k_first >> 4);
+  if (16 * ((k_first >> 4) + 1) < k_first + nk) copy_scales((k_first >> 4) + 1);
+  uint32_t stage = 0, next = (M::NS - 1) * M::stage;     // of k tile kt, and of the one that is copied beside it
+#pragma unroll
+  for (int p = 0; p < M::NS - 1; ++p)
+    if (p < nk) copy(p * M::stage);
+  auto k_tile = [&](auto q_tag, int kt) {
+    constexpr int Q = decltype(q_tag)::value;
+    if (M::NS > 2 && kt + 1 < nk) {                      // the next k tile's copies may be outstanding
+      if (a_live == NA) wait_vmcnt<PER_K>(); else wait_vmcnt<4>();
+    } else {
+      wait_vmcnt<0>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (Q == 2) {                                        // the scales of the next 16 k tiles, where those of the 16 before were (the first two are there)
+      const int k = k_first + kt, c = k >> 4;
+      if ((k & 15) == 2 && c > k_first >> 4 && 16 * (c + 1) < k_first + nk) copy_scales(c + 1);
+    }
+    if (kt + M::NS - 1 < nk) copy(next);
+    __builtin_amdgcn_sched_barrier(0);
+    if (live) {
+      if (Q == 0) {                                      // of k tiles k .. k + 3
+        const int k = k_first + kt;
+        const uint32_t at = ((k >> 4) & 1) * M::scale_stage + (k & 12);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) xa[i] = *(lds_word)(uintptr_t)(sc_a + at + i * 256);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) xb[j] = *(lds_word)(uintptr_t)(sc_b + at + b_row(j) * 16);
+      }
+      multiply(q_tag, stage);
+    }
+    next = stage;
+    stage = stage + M::stage == M::scales0 ? 0 : stage + M::stage;
+  };
+#pragma unroll 1
+  for (int kt = 0; kt < nk; kt += 4) {
+    k_tile(std::integral_constant<int, 0>{}, kt);
+    if (kt + 1 < nk) k_tile(std::integral_constant<int, 1>{}, kt + 1);
+    if (kt + 2 < nk) k_tile(std::integral_constant<int, 2>{}, kt + 2);
+    if (kt + 3 < nk) k_tile(std::integral_constant<int, 3>{}, kt + 3);
+  }
+
+  // ---- acc[i][j][v] is row 16 i + l % 16, column 16 j + 4 (l / 16) + v of the wavefront's
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < (UP ? 2 : TN); ++j) {
+      const int m = t.row0 + wm * (BM / 2) + i * 16 + r, n = col0 + wn * (COLS / 2) + j * 16 + 4 * lg;
+      if (m >= t.row_end || n >= g.N) continue;
+      const int64_t at = (int64_t)m * g.N + n;
+      f32x4 v = acc[i][j];
+      if constexpr (UP) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = silu_f(v[x]) * acc[i][j + 2][x];
+        *reinterpret_cast<f32x4*>(g.sums + at) = v;
+      } else if (slices > 1) {
+        *reinterpret_cast<f32x4*>(g.sums + (int64_t)slice * g.R * g.N + at) = v;
+      } else {
+        store_out<MODE == kMidExact>(g, at, v);
+      }
+    }
+}
 
 // ---- many rows: 256 x 256 tiles ---------------------------------------------------------------------------------
 // Bound by the matrix cores and by what feeds them from LDS.  A k tile is a block: [row][128 bytes] of either operand, 8 wavefronts have 128 x 64 of the
@@ -292,7 +491,7 @@ constexpr int kTileRows = 256, kTileWaves = 8;
 constexpr uint32_t kStage = 32768, kScaleStage = 8192;  // scales of 16 k tiles: 256 rows of A, 256 of B
 constexpr uint32_t kB0 = 2 * kStage, kScale0 = 4 * kStage, kOffsets0 = kScale0 + 2 * kScaleStage;
 constexpr int kTileLds = kOffsets0 + (kF8MaxExperts + 1) * 4;
-enum TileMode { kUp, kOut, kOutExact };                 // activations; bf16; fp32 by way of bf16
+enum TileMode { kUp, kOut };                            // activations in 8 bits; bf16
 
 template <TileMode MODE>
 __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g, int n_ct) {
@@ -421,27 +620,11 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
   // the products of half h of A's rows
   auto multiply = [&](auto q_tag, int h) {
     constexpr int Q = decltype(q_tag)::value;
-    if constexpr (MODE == kOutExact) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {                      // 8 codes a lane
-        bf16x8 bb[TN];
+    for (int i = 0; i < TM / 2; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-          bb[j] = to_bf16x8(fb[j][q / 2][2 * (q & 1)], fb[j][q / 2][2 * (q & 1) + 1], f8_scale_or_nan(xb[j] >> (8 * Q) & 255u));
-#pragma unroll
-        for (int i = 0; i < TM / 2; ++i) {
-          const bf16x8 aa = to_bf16x8(fa[i][q / 2][2 * (q & 1)], fa[i][q / 2][2 * (q & 1) + 1], f8_scale_or_nan(xa[h * 4 + i] >> (8 * Q) & 255u));
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[h * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bb[j], aa, acc[h * 4 + i][j], 0, 0, 0);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < TM / 2; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[h * 4 + i][j] = mfma_f8<Q>(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[h * 4 + i][j], xb[j], xa[h * 4 + i]);
-    }
+      for (int j = 0; j < TN; ++j)
+        acc[h * 4 + i][j] = mfma_f8<Q>(fb[j][0], fb[j][1], fa[i][0], fa[i][1], acc[h * 4 + i][j], xb[j], xa[h * 4 + i]);
   };
   // Copies: in the first memory phase of k tile kt A1 of kt + 1 (2 instructions), in the second A0 and B of kt + 2 (2 and 4), in front of them
   // now and then one of scales.  What they overwrite was read last in the memory phases before, and they have four phases or more to land.
@@ -590,18 +773,14 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
         for (int64_t z = out_col0 / 128 + 1; z < out_sc_pitch; ++z) g.act_scales[(int64_t)(out_row0 + tid) * out_sc_pitch + z] = 0;
     } else {
       if (more) start();
-      if (slices > 1 || MODE == kOutExact) {             // four columns a lane, as they are
-        float* const to = slices > 1 ? g.sums + (int64_t)out_slice * g.R * g.N : static_cast<float*>(g.out);
-        const float* const residual = slices > 1 ? nullptr : static_cast<const float*>(g.residual);
+      if (slices > 1) {                                  // four columns a lane, as they are
+        float* const to = g.sums + (int64_t)out_slice * g.R * g.N;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int j = 0; j < TN; ++j) {
             const int m = wm * 128 + i * 16 + r, n = out_col0 + wn * 64 + j * 16 + 4 * lg;
-            if (out_row0 + m >= out_end || n >= g.N) continue;
-            const int64_t at = (int64_t)(out_row0 + m) * g.N + n;
-            if (MODE == kOutExact && residual) acc[i][j] += *reinterpret_cast<const f32x4*>(residual + at);
-            *reinterpret_cast<f32x4*>(to + at) = acc[i][j];
+            if (out_row0 + m < out_end && n < g.N) *reinterpret_cast<f32x4*>(to + (int64_t)(out_row0 + m) * g.N + n) = acc[i][j];
           }
         if (!more) return;
         __syncthreads();
@@ -645,20 +824,33 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
 }
 
 // the dynamic-LDS limit, once per device (not while a stream is being captured; btx_init() does it too)
-template <auto KERNEL> int raise_lds() {
+template <auto KERNEL> int raise_lds(int bytes) {
   static std::atomic<uint64_t> done{0};
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return BTX_ERR_HIP;
   if (!(done.load(std::memory_order_relaxed) >> dev & 1)) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, kTileLds) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
       return BTX_ERR_HIP;
     done.fetch_or(1ull << dev, std::memory_order_relaxed);
   }
   return BTX_OK;
 }
 
+template <MidMode MODE, int BM> int launch_mid_tiles(const F8Args& g, hipStream_t s) {
+  if (int rc = raise_lds<f8_mid_kernel<MODE, BM>>(Mid<BM>::lds)) return rc;
+  const int n_ct = ceil_div(g.N, MODE == kMidUp ? 64 : kMidCols);
+  const int64_t n_rt = g.offsets ? most_tiles(g.R, g.E, BM) : ceil_div(g.R, BM), grid = ceil_div((int64_t)n_ct * g.slices, kXcds) * kXcds * n_rt;
+  if (!grid_fits(grid, kMidWaves * kWave)) return BTX_ERR_UNSUPPORTED;
+  f8_mid_kernel<MODE, BM><<<(unsigned)grid, kMidWaves * kWave, Mid<BM>::lds, s>>>(g, n_ct);
+  BTX_LAUNCH_CHECK();
+  return BTX_OK;
+}
+template <MidMode MODE> int launch_mid(const F8Args& g, int tile_rows, hipStream_t s) {
+  return tile_rows == 64 ? launch_mid_tiles<MODE, 64>(g, s) : launch_mid_tiles<MODE, 128>(g, s);
+}
+
 template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
-  if (int rc = raise_lds<f8_tile_kernel<MODE>>()) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<MODE>>(kTileLds)) return rc;
   const int n_ct = ceil_div(g.N, MODE == kUp ? 128 : 256);
   const int64_t n_rt = g.offsets ? most_tiles(g.R, g.E, kTileRows) : ceil_div(g.R, kTileRows);
   const int64_t tiles = (n_rt * n_ct + kXcds) * g.slices;
@@ -670,14 +862,14 @@ template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
   return BTX_OK;
 }
 
-// K ranges of the tiles: as many as fill the chip where the tiles alone do not, of eight k tiles or more each; no more than whoever adds them takes, and
-// than there is room for
+// K ranges of the tiles: as many as fill the chip (`places` workgroups at once) where the tiles alone do not, of `shortest` k tiles or more each; no more
+// than whoever adds them takes, and than there is room for
 constexpr int kMostSlices = 16;
 constexpr int64_t kSumBytes = (int64_t)kTileGrid * 256 * 256 * 4;        // of 256 tiles
 int64_t sum_bytes(int64_t R, int N) { return std::min(R * N * 4 * kMostSlices, kSumBytes); }
-int slices_of(int64_t tiles, int64_t R, int N, int K, int most) {
+int slices_of(int64_t tiles, int places, int shortest, int64_t R, int N, int K, int most) {
   const int64_t fit = sum_bytes(R, N) / (R * N * 4);
-  return (int)std::max<int64_t>(std::min({kTileGrid / tiles, f8_pitch(K) / kF8Block / 8, fit, (int64_t)most, (int64_t)kMostSlices}), 1);
+  return (int)std::max<int64_t>(std::min({places / tiles, f8_pitch(K) / kF8Block / shortest, fit, (int64_t)most, (int64_t)kMostSlices}), 1);
 }
 
 // out = residual + the sums of the slices, in order; four columns a thread
@@ -707,33 +899,86 @@ __global__ __launch_bounds__(kAddThreads) void f8_add_slices_kernel(const f32x4*
   }
 }
 
-// How many rows a row tile has: 32, 64 or 256, as mx4_tile_rows()
-int tile_rows_of(int64_t R, int E, int64_t tile_columns, int64_t depth) {
-  const int64_t avg = R / E;
-  const bool enough = R * tile_columns >= 12000 || R * depth >= (int64_t)1150000000;
-  if (avg >= 32 && enough) return kTileRows;
-  return avg <= 24 ? 32 : 64;
+// Which kernel, and the rows of its tiles
+enum Path { kFew32, kFew64, kMid64, kMid128, kTall };
+constexpr int kPathRows[] = {32, 64, 64, 128, kTileRows};
+// Rows of E experts (those that have a row: about as many each), in tiles
+struct Rows {
+  int64_t busy, each;
+  Rows(int64_t R, int E) : busy(std::min<int64_t>(E, R)), each((R + busy - 1) / busy) {}
+  int64_t tiles(int rows) const { return busy * ((each + rows - 1) / rows); }
+};
+// The activations.  Tiles of 64 columns; the middling ones' activations are quantised by another launch (2.5 us and more).  us, few / 64 / 128 / tall:
+//   2 of 4 experts of 4096 x 11008, rows each:  4  87 89 94 104;  16  97 91 89 103;  32  108 87 93 103;  64  161 93 96 106;  150  275 131 120 110
+//   8 of 32 of 4096 x 1376:  4  84 93 97 100;  16  93 99 102 102;  32  110 100 104 102;  100  208 112 115 106
+//   2 of 8 of 1024 x 2048:  4  14 13 13 20;  32  18 15 15 20;  64  24 17 16 21;  128  35 24 21 22;  256  54 31 31 25
+constexpr int kUpFewRows = 12, kUpMidRows = 64, kUpMidTiles = kTileGrid;
+Path up_path(int64_t R, int E, int f) {
+  const Rows n(R, E);
+  if (n.each <= kUpFewRows) return kFew32;
+  if (n.each <= kUpMidRows) return kMid64;
+  return n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
 }
-int layer_rows(int64_t R, int d, int f, int E) { return tile_rows_of(R, E, ceil_div(f, 128) + ceil_div(d, 256), (int64_t)d * f); }
-int matmul_rows(int M, int N, int K) { return tile_rows_of(M, 1, ceil_div(N, 256), (int64_t)N * K); }
+// Other products.  Of one matrix (sums of tiles that are cut along K are added by another launch), rows, us:
+//   1024 x 1024: 64  5.3 6.7 7.8 12;  256  5.3 6.7 9.1 16;  1024  13 7.0 9.5 16        4096 x 1376:  32  5.3 7.8 9.0 15;  96  8.6 8.1 11 17;  1024  27 12 13 20
+//   4096 x 4096: 24  9.3 10 11 15;  32  10 10 11 15;  64  15 11 13 17;  256  47 17 18 29;  1024  75 26 28 42;  2048  156 48 39 53
+//   4096 x 11008: 16  15 - - 20;  24  19 16 16 21;  64  33 16 19 24;  256  120 28 31 44;  1024  192 71 67 65;  2048  401 144 104 91
+//   11008 x 4096: 24  21 17 18 17;  256  58 29 31 35;  512  120 45 38 44;  1024  217 75 68 45          512 x 8192: 16  11 - - 14;  24  14 9 10 15
+// Of experts (the sums of tiles that are cut are added where the rows are combined), rows each:
+//   4 of 11008 x 4096 (K x N): 4  42 44 46 43;  16  56 46 46 44;  32  86 47 48 45;  64  132 58 50 49;  150  297 86 79 59
+//   32 of 1376 x 4096: 4  37 36 37 41;  16  44 41 41 43;  32  52 43 43 44;  100  99 61 53 47       8 of 2048 x 1024: 4  8 9 10 15;  16  11 9 10 15;
+//   64  20 11 12 18;  256  51 16 19 27;  1024  166 38 38 45;      64 of 1024 x 2048: 4  29 31 31 36;  32  40 37 36 38;  64  57 42 41 39;  256  155 89 86 62
+Path out_path(int64_t R, int E, int N, int K) {
+  const Rows n(R, E);
+  const int columns = ceil_div(N, kMidCols), n_blk = (int)(f8_pitch(K) / kF8Block);
+  const int64_t tiles = n.tiles(64) * columns;
+  if (E == 1) {
+    // (a few long columns: only cut along K do they fill the chip)
+    if ((n.each <= 16 || n.each * n_blk <= 1024) && (tiles >= 8 || n_blk < 48)) return n.each <= 24 ? kFew32 : kFew64;
+    if (tiles <= 2 * kTileGrid) return kMid64;
+  } else {
+    if (n.each <= 8) return kFew32;
+    if (n.each <= 48 || tiles * n_blk <= 8192) return kMid64;
+  }
+  return n.tiles(128) * columns <= 2 * kTileGrid && n_blk <= 64 ? kMid128 : kTall;
+}
+
+// out, or the sums of g.slices ranges of K, which are set here
+template <bool F32> int launch_out(F8Args& g, Path path, int most_slices, hipStream_t s) {
+  using OT = std::conditional_t<F32, float, bf16_t>;
+  if (path <= kFew64) return launch_few<OT>(g, kPathRows[path], s);
+  const int64_t row_tiles = Rows(g.R, g.E).tiles(kPathRows[path]);
+  if (path <= kMid128) {
+    g.slices = slices_of(row_tiles * ceil_div(g.N, kMidCols), kTileGrid, 8, g.R, g.N, g.K, most_slices);
+    return launch_mid<F32 ? kMidExact : kMidOut>(g, kPathRows[path], s);
+  }
+  g.slices = slices_of(row_tiles * ceil_div(g.N, 256), kTileGrid, 8, g.R, g.N, g.K, most_slices);
+  if constexpr (F32) return BTX_ERR_UNSUPPORTED;
+  else return launch_tiles<kOut>(g, s);
+}
 
 }  // namespace
 
 int f8_prepare() {
-  if (int rc = raise_lds<f8_tile_kernel<kUp>>()) return rc;
-  if (int rc = raise_lds<f8_tile_kernel<kOut>>()) return rc;
-  return raise_lds<f8_tile_kernel<kOutExact>>();
+  if (int rc = raise_lds<f8_tile_kernel<kUp>>(kTileLds)) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<kOut>>(kTileLds)) return rc;
+  if (int rc = raise_lds<f8_mid_kernel<kMidUp, 64>>(Mid<64>::lds)) return rc;
+  if (int rc = raise_lds<f8_mid_kernel<kMidUp, 128>>(Mid<128>::lds)) return rc;
+  if (int rc = raise_lds<f8_mid_kernel<kMidOut, 64>>(Mid<64>::lds)) return rc;
+  if (int rc = raise_lds<f8_mid_kernel<kMidOut, 128>>(Mid<128>::lds)) return rc;
+  if (int rc = raise_lds<f8_mid_kernel<kMidExact, 64>>(Mid<64>::lds)) return rc;
+  return raise_lds<f8_mid_kernel<kMidExact, 128>>(Mid<128>::lds);
 }
 
 // (never less for more rows, also where so many are not cut)
-size_t f8_matmul_workspace_bytes(int M, int N, int K) { return f8_pitch(K) / kF8Block >= 16 && M >= 32 ? (size_t)sum_bytes(M, N) : 0; }
+size_t f8_matmul_workspace_bytes(int M, int N, int K) { return f8_pitch(K) / kF8Block >= 16 ? (size_t)sum_bytes(M, N) : 0; }
 int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
   F8Args g{m.a, m.b, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.M, m.N, m.K, nullptr, nullptr, m.out, m.residual, 1, static_cast<float*>(m.workspace)};
-  const int rows = matmul_rows(m.M, m.N, m.K);
   const bool bf16 = m.dtype == BTX_BF16;
-  if (rows != kTileRows) return bf16 ? launch_few<bf16_t>(g, rows, s) : launch_few<float>(g, rows, s);
-  g.slices = slices_of((int64_t)ceil_div(m.M, kTileRows) * ceil_div(m.N, 256), m.M, m.N, m.K, kMostSlices);
-  if (int rc = bf16 ? launch_tiles<kOut>(g, s) : launch_tiles<kOutExact>(g, s)) return rc;
+  Path path = out_path(m.M, 1, m.N, m.K);
+  if (path == kTall && !bf16) path = kMid128;
+  const int most = f8_matmul_workspace_bytes(m.M, m.N, m.K) ? kMostSlices : 1;
+  if (int rc = bf16 ? launch_out<false>(g, path, most, s) : launch_out<true>(g, path, most, s)) return rc;
   if (g.slices > 1) {
     const int64_t n = (int64_t)m.M * m.N / 4;
     const unsigned blocks = (unsigned)std::min<int64_t>((n + kAddThreads - 1) / kAddThreads, 1 << 20);
@@ -747,23 +992,23 @@ int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
 
 int launch_f8_up(const F8Layer& l, hipStream_t s) {
   const F8Args g{l.x, l.W1, l.W3, l.offsets, l.perm, l.E, l.k, l.T * l.k, l.f, l.d, l.act_codes, l.act_scales, nullptr, nullptr, 1, static_cast<float*>(l.y)};
-  const int rows = layer_rows(g.R, l.d, l.f, l.E);
-  return rows == kTileRows ? launch_tiles<kUp>(g, s) : launch_few_up(g, rows, s);
+  const Path path = up_path(g.R, l.E, l.f);
+  if (path == kTall) return launch_tiles<kUp>(g, s);
+  if (int rc = path <= kFew64 ? launch_few_up(g, kPathRows[path], s) : launch_mid<kMidUp>(g, kPathRows[path], s)) return rc;
+  return launch_f8_quantize(g.sums, BTX_F32, 1, g.R, g.N, 1, 1, g.act_codes, g.act_scales, s);
 }
 
-// y or the sums of its slices; before these the activations of tiles of few rows in fp32: fewer than 32 rows an expert, or 12000 x 128 columns in all
+// y or the sums of its slices; before these the activations of all but the tall tiles in fp32
 size_t f8_y_bytes(int64_t R, int d, int f, int E) {
-  const int64_t few = std::min(R, std::max<int64_t>(32 * E, 12000 / ceil_div(f, 128)));
-  return (size_t)std::max({R * d * 2, sum_bytes(R, d), few * f * 4});
+  const int64_t rows = std::min(R, std::max<int64_t>(kUpMidRows * E, kUpMidTiles * 128 / ceil_div(f, 64)));
+  return (size_t)std::max({R * d * 2, sum_bytes(R, d), rows * f * 4});
 }
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s) {
-  const int R = l.T * l.k, rows = layer_rows(R, l.d, l.f, l.E);
+  const int R = l.T * l.k;
   F8Args g{{l.act_codes, l.act_scales}, l.W2, {nullptr, nullptr}, l.offsets, nullptr, l.E, l.k, R, l.d, l.f, nullptr, nullptr, l.y, nullptr, 1, static_cast<float*>(l.y)};
-  *slices = 1;
-  if (rows != kTileRows) return launch_few<bf16_t>(g, rows, s);
-  const int64_t busy = std::min<int64_t>(l.E, R), tiles = busy * ceil_div(ceil_div(R, busy), kTileRows) * ceil_div(l.d, 256);
-  *slices = g.slices = slices_of(tiles, R, l.d, l.f, combine_most_slices(l.T, l.k, BTX_BF16));
-  return launch_tiles<kOut>(g, s);
+  if (int rc = launch_out<false>(g, out_path(R, l.E, l.d, l.f), combine_most_slices(l.T, l.k, BTX_BF16), s)) return rc;
+  *slices = g.slices;
+  return BTX_OK;
 }
 
 }  // namespace btx
