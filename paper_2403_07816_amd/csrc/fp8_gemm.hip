@@ -259,7 +259,7 @@ __global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
 template <bool UP, int FR, int KS, typename OT> int launch_few_shape(const F8Args& g, int tile_rows, hipStream_t s) {
   const dim3 grid((unsigned)ceil_div(g.N, FR * 16), (unsigned)(g.offsets ? most_tiles(g.R, g.E, tile_rows) : ceil_div(g.R, tile_rows)));
   if (tile_rows == 32) f8_few_kernel<UP, 2, FR, KS, OT><<<grid, KS * kWave, 0, s>>>(g);
-  else f8_few_kernel<UP, 4, FR, KS, OT><<<grid, KS * kWave, 0, s>>>(g);
+  else if constexpr (!UP) f8_few_kernel<UP, 4, FR, KS, OT><<<grid, KS * kWave, 0, s>>>(g);    // (of one matrix)
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
@@ -275,9 +275,7 @@ template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_
   return launch_few_shape<false, 1, 4, OT>(g, tile_rows, s);
 }
 // (one token, 2 experts of 4096 x 11008, and 64 tokens, 32 of 4096 x 1376: 37 and 85 us; with 4 wavefronts 40 and 86, with 16 columns and 4 37 and 90)
-int launch_few_up(const F8Args& g, int tile_rows, hipStream_t s) {
-  return launch_few_shape<true, 2, 2, float>(g, tile_rows, s);
-}
+int launch_few_up(const F8Args& g, hipStream_t s) { return launch_few_shape<true, 2, 2, float>(g, 32, s); }
 
 // (tiles of 32 rows only where there are fewer than 25 an expert)
 static_assert(kF8MostColumns / 32 <= 65535 && (kF8MostRows / 64 + kF8MaxExperts + 0ll) * 8 * kWave < 1ll << 32, "the grid");
@@ -994,7 +992,7 @@ int launch_f8_up(const F8Layer& l, hipStream_t s) {
   const F8Args g{l.x, l.W1, l.W3, l.offsets, l.perm, l.E, l.k, l.T * l.k, l.f, l.d, l.act_codes, l.act_scales, nullptr, nullptr, 1, static_cast<float*>(l.y)};
   const Path path = up_path(g.R, l.E, l.f);
   if (path == kTall) return launch_tiles<kUp>(g, s);
-  if (int rc = path <= kFew64 ? launch_few_up(g, kPathRows[path], s) : launch_mid<kMidUp>(g, kPathRows[path], s)) return rc;
+  if (int rc = path == kFew32 ? launch_few_up(g, s) : launch_mid<kMidUp>(g, kPathRows[path], s)) return rc;
   return launch_f8_quantize(g.sums, BTX_F32, 1, g.R, g.N, 1, 1, g.act_codes, g.act_scales, s);
 }
 

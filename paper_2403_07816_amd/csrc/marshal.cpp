@@ -202,9 +202,10 @@ template <typename Call> PyObject* called(Call call) {
   return PyLong_FromLong(status);
 }
 // The call with this workspace, or, where it is too small or there is none, minus the bytes that one has to have
-template <typename Call> PyObject* with_workspace(PyObject* workspace, size_t bytes, Call call) {
+template <typename Call> PyObject* with_workspace(PyObject* workspace, size_t bytes, Call call, const Place* place = nullptr) {
   if (workspace != Py_None) {
     const at::Tensor& w = tensor(workspace);
+    if (place && w.get_device() != place->device) fail(PyExc_ValueError, "workspace is on another device");
     const size_t has = (size_t)w.numel() * w.element_size();
     if (has >= bytes) {
       void* const at = address(workspace);
@@ -494,7 +495,7 @@ PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
     };
     const size_t bytes = lib.matmul_bytes(M, N, K);
     if (!bytes) return called([&] { return call(nullptr, 0); });
-    return with_workspace(a[4], bytes, call);
+    return with_workspace(a[4], bytes, call, &at);
   });
 }
 
@@ -517,7 +518,7 @@ PyObject* forward_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return with_workspace(a[7], lib.forward_fp8_bytes(T, d, f, E, k), [&](void* ws, size_t bytes) {
       return lib.forward_fp8(x.codes, x.scales, W1.codes, W1.scales, W3.codes, W3.scales, W2.codes, W2.scales, T, d, f, E, k, gates, offsets, perm,
                              inv, res, out, ws, bytes, stream);
-    });
+    }, &at);
   });
 }
 

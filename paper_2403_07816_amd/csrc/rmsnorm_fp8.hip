@@ -137,10 +137,14 @@ __global__ __launch_bounds__(kThreads) void f8_norm_kernel(const XT* h, const XT
 template <typename XT> int launch_typed(const F8NormArgs& a, hipStream_t s) {
   auto run = [&](auto tpr, auto maxc) {
     constexpr int TPR = decltype(tpr)::value;
-    const int rows = kThreads / TPR;
-    f8_norm_kernel<XT, TPR, decltype(maxc)::value><<<ceil_div(a.T, rows), kThreads, 0, s>>>(
-        static_cast<const XT*>(a.h), static_cast<const XT*>(a.residual), a.gain, a.eps, a.T, a.d, static_cast<XT*>(a.sum), static_cast<XT*>(a.xn),
-        a.rstd, reinterpret_cast<u32x2*>(a.codes), a.scales);
+    constexpr int ROWS = kThreads / TPR, MOST = (1 << 22) * ROWS;       // (a launch has fewer than 2^32 threads)
+    for (int t0 = 0; t0 < a.T; t0 += std::min(MOST, a.T - t0)) {
+      auto at = [&](auto* p, int64_t pitch) { return p ? p + t0 * pitch : p; };
+      const int n = std::min(MOST, a.T - t0);
+      f8_norm_kernel<XT, TPR, decltype(maxc)::value><<<ceil_div(n, ROWS), kThreads, 0, s>>>(
+          at(static_cast<const XT*>(a.h), a.d), at(static_cast<const XT*>(a.residual), a.d), a.gain, a.eps, n, a.d, at(static_cast<XT*>(a.sum), a.d),
+          at(static_cast<XT*>(a.xn), a.d), a.rstd + t0, reinterpret_cast<u32x2*>(at(a.codes, f8_pitch(a.d))), at(a.scales, f8_scale_pitch(a.d)));
+    }
   };
   auto by_columns = [&](auto tpr) {
     const int per = decltype(tpr)::value * 8;

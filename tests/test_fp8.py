@@ -450,7 +450,8 @@ def check_product(out, a, b, residual=None):
 MATMULS = [(1, 8, 1), (1, 64, 128), (3, 40, 130), (16, 72, 256), (17, 128, 384), (24, 136, 1000), (25, 256, 640), (64, 512, 4096), (65, 264, 129),
            (130, 1376, 300), (256, 256, 2048), (257, 520, 1100), (301, 1032, 2177), (600, 768, 500), (1025, 264, 4001), (33, 2048, 11008), (2000, 1536, 384),
            (300, 1032, 4100), (64, 2056, 11008), (513, 264, 18000), (16500, 2048, 130), (2100, 2048, 6500), (4200, 2048, 6500),
-           (5, 33000, 136), (30, 32776, 264), (40, 33000, 520)]
+           (5, 33000, 136), (30, 32776, 264), (40, 33000, 520), (17, 264, 7000), (16, 520, 8000),
+           (700, 1032, 3000), (1100, 4104, 264), (2048, 4096, 8300)]
 
 
 @gpu
@@ -512,20 +513,36 @@ def test_products_of_wide_scales():
         assert np.all(np.abs(out.double().cpu().numpy() - want) <= err + 2.0 ** -24 * np.abs(want))
 
 
+LONG, LONG_K, MARKED = 540000, 8200, (0, 255, 516222, 539999)
+
+
+def long_operand():
+    """A matrix of more than 4 GiB whose rows are zero but for a few."""
+    q = B.Fp8(torch.zeros((LONG, 8320), dtype=torch.uint8, device=DEV), torch.full((LONG, 80), 127, dtype=torch.uint8, device=DEV), LONG_K)
+    for i in MARKED:
+        row, _ = operand(1, LONG_K, 100 + i)
+        q.codes[i], q.scales[i] = row.codes[0], row.scales[0]
+    return q
+
+
 @gpu
-def test_products_past_32_bit_offsets():
-    """A of more than 4 GiB, and a result of more than 2^32 elements."""
-    M, K, N = 540000, 8200, 8
-    a = B.Fp8(torch.zeros((M, 8320), dtype=torch.uint8, device=DEV), torch.full((M, 80), 127, dtype=torch.uint8, device=DEV), K)
-    b, bv = operand(N, K, 5)
-    for i in (0, 255, 516222, M - 1):
-        (row, rv) = operand(1, K, 100 + i)
-        a.codes[i], a.scales[i] = row.codes[0], row.scales[0]
-    out = B.btx_fp8_matmul(a, b, dtype=F32)
-    for i in (0, 255, 516222, M - 1):
-        check_product(out[i:i + 1], operand(1, K, 100 + i)[1], bv)
-    assert int(out.count_nonzero()) == 4 * N
-    del out, a
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("other", [8, 40, 3000])
+def test_products_of_long_operands(other, dtype):
+    q, (b, bv) = long_operand(), operand(other, LONG_K, 5)
+    if other == 8:                                         # as rows, and as columns below
+        out = B.btx_fp8_matmul(q, b, dtype=dtype)
+        for i in MARKED:
+            check_product(out[i:i + 1], operand(1, LONG_K, 100 + i)[1], bv)
+        assert int(out.count_nonzero()) == len(MARKED) * other
+    out = B.btx_fp8_matmul(b, q, dtype=dtype)
+    for i in MARKED:
+        check_product(out[:, i:i + 1], bv, operand(1, LONG_K, 100 + i)[1])
+    assert int(out.count_nonzero()) == len(MARKED) * other
+
+
+@gpu
+def test_results_past_32_bit_offsets():
     M, N, K = 66000, 65600, 40
     (a, av), (b, bv) = operand(M, K, 6), operand(N, K, 7)
     out = B.btx_fp8_matmul(a, b)
@@ -602,6 +619,10 @@ def make_layer(T, d, f, E, k, seed=0, skew=False, drop=0.0):
 
 
 def check_layer(out, xv, W, idx, gates, inv, residual=None):
+    T, f, d = out.shape[0], *W[0][1].shape[1:]
+    if T * d * f > 2e8 and T > 200:                        # some tokens of many: they do not depend on each other
+        some = np.unique(np.concatenate([np.arange(40), np.arange(T - 40, T), rng_of("some", T).integers(0, T, 80)]))
+        out, xv, idx, gates, inv, residual = out[some], xv[some], idx[some], gates[some], inv[some], None if residual is None else residual[some]
     want, bound = O.ff_forward(xv, W[0][1], W[1][1], W[2][1], idx, gates, inv, None if residual is None else residual.double().cpu().numpy())
     off = np.abs(out.double().cpu().numpy() - want)
     assert np.all(off <= bound), float((off / bound).max())
@@ -617,7 +638,7 @@ def parts(xv, W, idx, gates, inv):
 
 
 LAYERS = [(1, 8, 8, 1, 1), (1, 256, 384, 4, 2), (3, 136, 264, 4, 4), (7, 520, 128, 3, 1), (40, 256, 200, 8, 3), (64, 264, 1376, 5, 2), (130, 128, 136, 256, 8),
-          (300, 384, 640, 2, 1), (513, 256, 520, 1, 1), (700, 512, 392, 6, 2), (2000, 128, 256, 3, 2), (900, 768, 904, 3, 2), (1500, 264, 1160, 2, 1), (4100, 136, 128, 256, 4), (600, 256, 8200, 2, 1)]
+          (300, 384, 640, 2, 1), (513, 256, 520, 1, 1), (700, 512, 392, 6, 2), (2000, 128, 256, 3, 2), (900, 768, 904, 3, 2), (1500, 264, 1160, 2, 1), (4100, 136, 128, 256, 4), (600, 256, 8200, 2, 1), (24, 264, 200, 1, 1), (90, 136, 520, 4, 2), (1750, 1032, 2104, 2, 2), (500, 1032, 8200, 2, 2)]
 
 
 @gpu
@@ -640,6 +661,65 @@ def test_layer_of_a_favoured_expert_and_dropped_pairs(T, d, f, E, k):
         x, xv, W, routing, idx, gates, inv = make_layer(T, d, f, E, k, 3, skew, drop)
         residual = torch.tensor(rng_of("dres", T).standard_normal((T, d))).to(BF).to(DEV)
         check_layer(B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing, residual=residual), xv, W, idx, gates, inv, residual)
+
+
+@gpu
+@pytest.mark.parametrize("T", [5, 200, 1500])
+def test_layer_of_one_expert_twice(T):
+    """A routing that names an expert in both of a token's slots, and a workspace that holds NaN."""
+    x, xv, W, routing, _, gates, _ = make_layer(T, 264, 392, 4, 2, 6)
+    idx = np.repeat(rng_of("twice", T).integers(0, 4, (T, 1)), 2, 1)
+    perm = np.argsort(idx.reshape(-1), kind="stable")
+    inv = np.argsort(perm).reshape(T, 2)
+    offsets = np.concatenate([[0], np.cumsum(np.bincount(idx.reshape(-1), minlength=4))])
+    for name, v in (("topk_idx", idx), ("perm", perm), ("inv_pos", inv), ("offsets", offsets)):
+        setattr(routing, name, torch.tensor(v, dtype=torch.int32, device=DEV))
+    ws = torch.full((B.load_library().btx_moe_ff_forward_fp8_workspace_bytes(T, 264, 392, 4, 2),), 255, dtype=torch.uint8, device=DEV)
+    out = B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing, workspace=ws)
+    check_layer(out, xv, W, idx, gates, inv)
+    assert torch.equal(B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing, workspace=ws), out)
+
+
+@gpu
+@pytest.mark.parametrize("T", [3, 40, 400])
+def test_layer_of_weights_past_32_bit_offsets(T):
+    """The last of experts of more than 4 GiB in all; the others are zero."""
+    d, f, E = 8192, 16400, 33
+    codes = lambda n, K: torch.zeros((E, n, B.load_library().btx_fp8_code_pitch(K)), dtype=torch.uint8, device=DEV)  # noqa: E731
+    scales = lambda n, K: torch.full((E, n, B.load_library().btx_fp8_scale_pitch(K)), 127, dtype=torch.uint8, device=DEV)  # noqa: E731
+    q = [B.Fp8(codes(n, K), scales(n, K), K) for n, K in ((f, d), (f, d), (d, f))]
+    last = []
+    for w, (n, K) in zip(q, ((f, d), (f, d), (d, f))):
+        v = torch.randn((n, K), generator=torch.Generator(device=DEV).manual_seed(n + K), device=DEV) * K ** -0.5
+        part = B.btx_fp8_quantize(v)
+        w.codes[E - 1], w.scales[E - 1] = part.codes, part.scales
+        last.append(B.btx_fp8_dequantize(part, F32).double())
+    xq = B.btx_fp8_quantize(torch.randn((T, d), generator=torch.Generator(device=DEV).manual_seed(T), device=DEV))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    half = T // 2                                          # tokens of expert 0, and of the last
+    routing = SimpleNamespace(topk_idx=i32([[0]] * half + [[E - 1]] * (T - half)), gates=torch.ones((T, 1), device=DEV), perm=i32(range(T)),
+                              offsets=i32([0] + [half] * (E - 1) + [T]), inv_pos=i32([[t] for t in range(T)]))
+    out = B.btx_moe_ff_forward_fp8(xq, *q, routing).double()
+    assert not out[:half].any()
+    x = B.btx_fp8_dequantize(xq, F32).double()[half:]
+    h1, h3 = x @ last[0].T, x @ last[1].T
+    act = B.btx_fp8_dequantize(B.btx_fp8_quantize((h1 * torch.sigmoid(h1) * h3).float()), F32).double()
+    want = act @ last[2].T
+    # codes on the other side of a rounding, and two roundings to bf16: 2^-8 of the norm each at most
+    assert (out[half:] - want).norm() <= 2 * 2.0 ** -8 * want.norm()
+
+
+@gpu
+def test_norm_past_32_bit_offsets():
+    T, d = 530000, 4104
+    h = torch.zeros((T, d), dtype=BF, device=DEV)
+    rows = [0, 1, 523265, T - 1]
+    v, r, gain = norm_inputs(4, d, BF, 9)
+    h[rows] = v.to(DEV)
+    n = B.btx_rmsnorm_fp8(h, gain.to(DEV), 1e-5, xn=torch.empty_like(h))
+    part = SimpleNamespace(rstd=n.rstd[rows], xn=n.xn[rows], q=B.Fp8(n.q.codes[rows], n.q.scales[rows], d))
+    check_norm(part, v, gain, 1e-5, BF)
+    assert int(n.xn.count_nonzero()) == int(n.xn[rows].count_nonzero())
 
 
 @gpu
