@@ -332,14 +332,23 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   };
   auto column = [&](int row) { return min(col0 + (UP ? row & 63 : row), g.N - 1) - col0; };
   const F8Matrix& bm = UP && wave >= 2 ? g.b1 : g.b0;
+  const uint32_t to_a = base + wave * (BM / 4) * 128, to_b = base + BM * 128 + wave * 4096;
+  const int64_t k0 = (int64_t)k_first * kF8Block;
   uint32_t a_off[NA], b_off[4], s_off;
 #pragma unroll
   for (int q = 0; q < 4; ++q) b_off[q] = (uint32_t)column(wave * 32 + q * 8 + lane / 8) * (uint32_t)row_bytes + chunk(q) * 16 + (kCopyBias4 - 1024 * q);
+  uint64_t b_from = uniform64(bm.codes + ((int64_t)t.e * g.N + col0) * row_bytes + k0) - kCopyBias4;
+  auto copy_b = [&](uint32_t stage) {
+    copy64(b_from, b_off, to_b + stage);
+    b_from += kF8Block;
+  };
+  // (the first ones, while the rows of A are looked up)
+#pragma unroll
+  for (int p = 0; p < M::NS - 1; ++p)
+    if (p < nk) copy_b(p * M::stage);
 #pragma unroll
   for (int q = 0; q < NA; ++q) a_off[q] = row_index(wave * (BM / 4) + q * 8 + lane / 8) * (uint32_t)row_bytes + chunk(q) * 16;
-  const int64_t k0 = (int64_t)k_first * kF8Block;
   uint64_t a_from = uniform64(g.a.codes + (g.perm ? 0 : (int64_t)t.row0 * row_bytes) + k0);
-  uint64_t b_from = uniform64(bm.codes + ((int64_t)t.e * g.N + col0) * row_bytes + k0) - kCopyBias4;
   uint64_t s_from;
   const bool a_scales = wave < 2, has_scales = !a_scales || wave < BM / 64;
   if (a_scales) {
@@ -350,17 +359,15 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
     s_from = uniform64((UP && wave == 3 ? g.b1 : g.b0).scales + ((int64_t)t.e * g.N + col0) * sc_pitch);
   }
   const int a_live = min(max((t.row_end - t.row0 - wave * (BM / 4) + 7) / 8, 0), NA);            // of its copies of A, those that have a row
-  const uint32_t to_a = base + wave * (BM / 4) * 128, to_b = base + BM * 128 + wave * 4096, to_s = base + M::scales0 + (a_scales ? wave * 1024 : BM * 16 + (wave - 2) * 1024);
+  const uint32_t to_s = base + M::scales0 + (a_scales ? wave * 1024 : BM * 16 + (wave - 2) * 1024);
   auto copy_scales = [&](int c) {                        // of k tiles 16 c ..
     if (has_scales) copy16(s_from + (uint64_t)c * 16, s_off, to_s + (c & 1) * M::scale_stage);
   };
-  auto copy = [&](uint32_t stage) {
-    copy64(b_from, b_off, to_b + stage);
+  auto copy_a = [&](uint32_t stage) {
 #pragma unroll
     for (int q = 0; q < NA; ++q)
       if (q < a_live) copy16(a_from, a_off[q], to_a + stage + q * 1024);
     a_from += kF8Block;
-    b_from += kF8Block;
   };
 
   // ---- fragments: lane l has row l % 16, chunks 2g and 2g + 1 of lane group g = l / 16
@@ -413,10 +420,10 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   uint32_t stage = 0, next = (M::NS - 1) * M::stage;     // of k tile kt, and of the one that is copied beside it
 #pragma unroll
   for (int p = 0; p < M::NS - 1; ++p)
-    if (p < nk) copy(p * M::stage);
+    if (p < nk) copy_a(p * M::stage);
   auto k_tile = [&](auto q_tag, int kt) {
     constexpr int Q = decltype(q_tag)::value;
-    if (M::NS > 2 && kt + 1 < nk) {                      // the next k tile's copies may be outstanding
+    if (M::NS > 2 && kt > 0 && kt + 1 < nk) {            // the next k tile's copies may be outstanding (but for those from before the first)
       if (a_live == NA) wait_vmcnt<PER_K>(); else wait_vmcnt<4>();
     } else {
       wait_vmcnt<0>();
@@ -428,7 +435,10 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
       const int k = k_first + kt, c = k >> 4;
       if ((k & 15) == 2 && c > k_first >> 4 && 16 * (c + 1) < k_first + nk) copy_scales(c + 1);
     }
-    if (kt + M::NS - 1 < nk) copy(next);
+    if (kt + M::NS - 1 < nk) {
+      copy_b(next);
+      copy_a(next);
+    }
     __builtin_amdgcn_sched_barrier(0);
     if (live) {
       if (Q == 0) {                                      // of k tiles k .. k + 3
@@ -730,7 +740,6 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
     if constexpr (UP) {
       // a workgroup's 128 columns are one block; its codes [256 rows][128 bytes] are put together in LDS, 16-byte chunks swizzled by row
       uint32_t* const s_amax = reinterpret_cast<uint32_t*>(smem + kB0 + kStage);      // [256][4]
-      if (more) start();
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         uint32_t amax = 0;
@@ -745,6 +754,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
         amax = f8_across_max(amax);
         if (lg == 0) s_amax[(wm * 128 + i * 16 + r) * 4 + wn] = amax;
       }
+      if (more) start();                                 // (behind the activations, beside which its rows were looked up)
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < TM; ++i) {

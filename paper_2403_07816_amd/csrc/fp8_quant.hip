@@ -16,13 +16,21 @@ constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int64_t kMostBlocks = 1 << 22;                // (a launch has fewer than 2^32 threads)
 constexpr int kTile = kF8Block;
 
-// Eight neighbouring elements of which n are there
-template <typename XT, bool VEC> __device__ __forceinline__ void load8(const XT* p, int64_t n, float* v) {
-  if (VEC && n >= 8) {
-    RowVec<XT, 8>::ld_stream(p, v);
+// Elements at, at + 1, .. + 7 of a row of `cols`, zeros where there is none; VEC: rows of whole 8.  (Without a branch around a load: behind one, the
+// next waits for it.)
+template <typename XT, bool VEC> __device__ __forceinline__ void load8(const XT* row, int64_t at, int64_t cols, bool there, float* v) {
+  if constexpr (VEC) {
+    if (there && at < cols) {
+      RowVec<XT, 8>::ld_stream(row + at, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? Elem<XT>::ld(p + i) : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = Elem<XT>::ld(row + min(at + i, cols - 1));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = there && at + i < cols ? v[i] : 0.f;
   }
 }
 template <typename XT, bool VEC> __device__ __forceinline__ void store8(XT* p, int64_t n, const float* v) {
@@ -48,7 +56,7 @@ __global__ __launch_bounds__(kThreads) void f8_quantize_rows_kernel(const XT* __
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * per_row; i += (int64_t)gridDim.x * kThreads) {
     const int64_t r = i / per_row, p = i - r * per_row, b = p / 16;
     float v[8];
-    load8<XT, VEC>(x + r * K + p * 8, K - p * 8, v);
+    load8<XT, VEC>(x + r * K, p * 8, K, true, v);
     uint32_t amax = 0;
 #pragma unroll
     for (int q = 0; q < 8; ++q) amax = max(amax, f8_magnitude(v[q]));
@@ -75,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void f8_quantize_tile_rows_kernel(const X
 #pragma unroll
   for (int q = 0; q < N; ++q) {
     const int64_t r = piece * kTile + q * STEP + threadIdx.x / 16;
-    load8<XT, VEC>(x + (batch * rows + min(r, rows - 1)) * K + k0, r < rows ? K - k0 : 0, v[q]);
+    load8<XT, VEC>(x + (batch * rows + min(r, rows - 1)) * K, k0, K, r < rows, v[q]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) amax = max(amax, f8_magnitude(v[q][i]));
   }
@@ -145,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void f8_quantize_cols_kernel(const XT* __
   const XT* const from = x + batch * K * N;
   float v[8][8];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) load8<XT, VEC>(from + min(k0 + q, K - 1) * N + min(col, N - 1), k0 + q < K ? N - col : 0, v[q]);
+  for (int q = 0; q < 8; ++q) load8<XT, VEC>(from + min(k0 + q, K - 1) * N, col, N, k0 + q < K, v[q]);
   uint32_t amax[8];
 #pragma unroll
   for (int h = 0; h < 8; ++h) {
