@@ -44,6 +44,7 @@ struct F8Args {
   uint8_t* act_codes; uint8_t* act_scales;
   void* out; const void* residual;
   int slices; float* sums;              // K ranges of a tile; more than one: their sums [slice][R][N] go there, and not to out
+  bool turned;                          // few rows: these are the result's columns, and it is written [N][R]
 };
 
 struct Tile { int e, row0, row_end; };
@@ -224,8 +225,9 @@ __global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
 #pragma unroll
   for (int p = 0; p < NF; ++p) few_b(b, p, p < FR ? g.b0 : g.b1, g, t.e, n0 + 16 * (p % FR), r);
   f32x4 acc[RB][NF] = {};
-  // (one token, DOWN of 2 experts of 4096 x 11008: 22.8 us with all workgroups at the same place of their rows, 18.9 so; wider ones gained nothing)
-  const int turn = FR == 1 && n_blk > 1 ? 3 * blockIdx.x % (n_blk / 2) : 0;
+  // (DOWN of one token, 2 experts of 4096 x 11008: 22.8 us with all workgroups at the same place of their rows, 18.9 so; UP of two to 16, 4 experts: 87-90,
+  // 75-78; of 64 columns nothing was gained)
+  const int turn = (UP || FR == 1) && n_blk > 1 ? 3 * blockIdx.x % (n_blk / 2) : 0;
   few_live_products<std::is_same_v<OT, float> && !UP>(acc, b, g, t, n_blk, f8_scale_pitch(g.K), ks, KS, turn, grp, r);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
@@ -250,6 +252,12 @@ __global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) v[x] = silu_f(v[x]) * h3[x];
       *reinterpret_cast<f32x4*>(g.sums + at) = v;
+    } else if (g.turned) {
+      const OT* const residual = static_cast<const OT*>(g.residual);
+      for (int x = 0; x < 4 && n + x < g.N; ++x) {
+        const int64_t to = (int64_t)(n + x) * g.R + m;
+        Elem<OT>::st(static_cast<OT*>(g.out) + to, v[x] + (residual ? Elem<OT>::ld(residual + to) : 0.f));
+      }
     } else {
       store_out<std::is_same_v<OT, float>>(g, at, v);
     }
@@ -266,11 +274,12 @@ template <bool UP, int FR, int KS, typename OT> int launch_few_shape(const F8Arg
 // 16 columns a workgroup, whose 4 wavefronts share K, or, where there are 2048 such pieces, 64 and 2.  A compute unit reads 25 GB/s from memory, so all
 // of them are needed.  DOWN of one token, 2 experts of 4096 x 11008 (512 pieces): 18.9 us with 16 columns, 24 with 32, 31 with 64; of 64 tokens,
 // 32 experts of 4096 x 1376 (8192): 58, 46, 40; 2048 x 4096 (4096): 84, 66, 60; 16 experts of 1024 x 2048 (1024): 9.7, 9.0, 9.3.
+// A turned product's "columns" are its many rows: 16384 (1024 pieces) x 16, K 8192, 39 us with 16 of them a workgroup, 31 with 64; 6400 20 and 25.
 // (fp32 results: 16 always; bf16 values of 64 columns and 64 rows do not fit the registers)
 template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_t s) {
-  const int64_t tiles = g.offsets ? std::min(g.E, g.R) : ceil_div(g.R, tile_rows);
+  const int64_t tiles = g.offsets ? std::min(g.E, g.R) : ceil_div(g.R, tile_rows), pieces = tiles * ceil_div(g.N, 16);
   if constexpr (!std::is_same_v<OT, float>) {
-    if (tiles * ceil_div(g.N, 16) >= 2048) return launch_few_shape<false, 4, 2, OT>(g, tile_rows, s);
+    if (pieces >= (g.turned ? 1024 : 2048)) return launch_few_shape<false, 4, 2, OT>(g, tile_rows, s);
   }
   return launch_few_shape<false, 1, 4, OT>(g, tile_rows, s);
 }
@@ -303,26 +312,46 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   const int nk_all = (int)(row_bytes / kF8Block), slices = UP ? 1 : g.slices;
   const uint32_t base = (uint32_t)(uintptr_t)smem;
 
-  // ---- the tile.  Workgroups that are a multiple of 8 apart are on one XCD: those of an expert's row tiles, which read the same columns, follow
-  // each other there
+  // ---- the tile.  Workgroups that are a multiple of 8 apart are on one XCD: those that read the same columns, or, of one matrix with more tiles of rows than
+  // of columns, the same rows, follow each other there.  Every XCD has as many: with columns dealt to the XCDs in turn, 16384 x 128 x 8192 was one XCD's
+  // work, 147 us for 32, and 16384 x 512 x 8192 149 for 72.  (Experts' columns are, where that is even: UP of 2 of 4 experts of 4096 x 11008 then
+  // reads them in order, 95 us and 97.)
   Tile t;
   const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
-  int c;
+  int c, n_c = n_ct * slices;
+  auto place = [&](int n_rt) {                           // the 8 XCDs' equal runs; past the last tile: none
+    const int tiles = n_rt * n_c, each = (tiles + kXcds - 1) / kXcds;
+    return local < each ? min(xcd * each + local, tiles) : tiles;
+  };
   if (g.offsets) {
     const ExpertTiles tiles(g.offsets, g.E, BM, lane);
     const int n_rt = tiles.count();
     if (n_rt == 0) return;
-    c = local / n_rt * kXcds + xcd;
-    if (c >= n_ct * slices) return;
-    t = tiles.at(local % n_rt);
+    int rt;
+    if (n_c % kXcds == 0 || n_c >= 64) {
+      c = local / n_rt * kXcds + xcd;
+      rt = local % n_rt;
+    } else {
+      const int id = place(n_rt);
+      c = id / n_rt;
+      rt = id % n_rt;
+    }
+    if (c >= n_c) return;
+    t = tiles.at(rt);
   } else {
-    const int n_rt = (g.R + BM - 1) / BM;
-    c = local / n_rt * kXcds + xcd;
-    if (c >= n_ct * slices) return;
-    t = Tile{0, local % n_rt * BM, g.R};
+    const int n_rt = (g.R + BM - 1) / BM, id = place(n_rt);
+    if (id >= n_rt * n_c) return;
+    const bool rows_first = n_rt > n_ct;
+    c = rows_first ? id % n_c : id / n_rt;
+    t = Tile{0, (rows_first ? id / n_c : id % n_rt) * BM, g.R};
   }
   const int slice = c / n_ct, col0 = (c - slice * n_ct) * COLS, quads = (nk_all + 3) / 4;
   const int k_first = slice * quads / slices * 4, nk = min((slice + 1) * quads / slices * 4, nk_all) - k_first;
+  // Columns begin at different places of their rows, four k tiles apart, and go round (where the scales' 16 k tiles come out even): rows that lie 4096 bytes
+  // apart, of which all workgroups read the same block, use part of the memory's channels.  2 of 8 experts of 4096 x 4096, 64 tokens: 107 us and 86 so;
+  // of 4 of 4096 x 11008: 140, 130
+  const int turn = slices == 1 && nk % 16 == 0 ? 4 * c % nk : 0, start = k_first + turn;
+  int a_left = nk - turn, b_left = a_left;               // copies up to the end of a row
 
   // ---- copies: a wavefront has BM / 4 rows of A and 32 of B, 8 lanes a row, 8 rows an instruction; 64 rows of A's scales, or of B's
   auto chunk = [&](int q) { return (lane & 7) ^ tile_swz(lane / 8 + 8 * (q & 1)); };
@@ -333,7 +362,7 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   auto column = [&](int row) { return min(col0 + (UP ? row & 63 : row), g.N - 1) - col0; };
   const F8Matrix& bm = UP && wave >= 2 ? g.b1 : g.b0;
   const uint32_t to_a = base + wave * (BM / 4) * 128, to_b = base + BM * 128 + wave * 4096;
-  const int64_t k0 = (int64_t)k_first * kF8Block;
+  const int64_t k0 = (int64_t)start * kF8Block;
   uint32_t a_off[NA], b_off[4], s_off;
 #pragma unroll
   for (int q = 0; q < 4; ++q) b_off[q] = (uint32_t)column(wave * 32 + q * 8 + lane / 8) * (uint32_t)row_bytes + chunk(q) * 16 + (kCopyBias4 - 1024 * q);
@@ -341,6 +370,7 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   auto copy_b = [&](uint32_t stage) {
     copy64(b_from, b_off, to_b + stage);
     b_from += kF8Block;
+    if (--b_left == 0) b_from -= (int64_t)nk * kF8Block;
   };
   // (the first ones, while the rows of A are looked up)
 #pragma unroll
@@ -361,13 +391,14 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   const int a_live = min(max((t.row_end - t.row0 - wave * (BM / 4) + 7) / 8, 0), NA);            // of its copies of A, those that have a row
   const uint32_t to_s = base + M::scales0 + (a_scales ? wave * 1024 : BM * 16 + (wave - 2) * 1024);
   auto copy_scales = [&](int c) {                        // of k tiles 16 c ..
-    if (has_scales) copy16(s_from + (uint64_t)c * 16, s_off, to_s + (c & 1) * M::scale_stage);
+    if (has_scales) copy16(s_from + (uint64_t)(16 * c < k_first + nk ? c : c - nk / 16) * 16, s_off, to_s + (c & 1) * M::scale_stage);
   };
   auto copy_a = [&](uint32_t stage) {
 #pragma unroll
     for (int q = 0; q < NA; ++q)
       if (q < a_live) copy16(a_from, a_off[q], to_a + stage + q * 1024);
     a_from += kF8Block;
+    if (--a_left == 0) a_from -= (int64_t)nk * kF8Block;
   };
 
   // ---- fragments: lane l has row l % 16, chunks 2g and 2g + 1 of lane group g = l / 16
@@ -415,8 +446,8 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   };
 
   // ---- k tiles.  Whoever passes the barrier of k tile kt has read all of k tile kt - 1, whose stage the copies behind it fill
-  copy_scales(k_first >> 4);
-  if (16 * ((k_first >> 4) + 1) < k_first + nk) copy_scales((k_first >> 4) + 1);
+  copy_scales(start >> 4);
+  if (16 * ((start >> 4) + 1) < start + nk) copy_scales((start >> 4) + 1);
   uint32_t stage = 0, next = (M::NS - 1) * M::stage;     // of k tile kt, and of the one that is copied beside it
 #pragma unroll
   for (int p = 0; p < M::NS - 1; ++p)
@@ -432,8 +463,8 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     if (Q == 2) {                                        // the scales of the next 16 k tiles, where those of the 16 before were (the first two are there)
-      const int k = k_first + kt, c = k >> 4;
-      if ((k & 15) == 2 && c > k_first >> 4 && 16 * (c + 1) < k_first + nk) copy_scales(c + 1);
+      const int k = start + kt, c = k >> 4;
+      if ((k & 15) == 2 && c > start >> 4 && 16 * (c + 1) < start + nk) copy_scales(c + 1);
     }
     if (kt + M::NS - 1 < nk) {
       copy_b(next);
@@ -442,7 +473,7 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
     __builtin_amdgcn_sched_barrier(0);
     if (live) {
       if (Q == 0) {                                      // of k tiles k .. k + 3
-        const int k = k_first + kt;
+        const int k = start + kt;
         const uint32_t at = ((k >> 4) & 1) * M::scale_stage + (k & 12);
 #pragma unroll
         for (int i = 0; i < TM; ++i) xa[i] = *(lds_word)(uintptr_t)(sc_a + at + i * 256);
@@ -916,33 +947,41 @@ struct Rows {
   Rows(int64_t R, int E) : busy(std::min<int64_t>(E, R)), each((R + busy - 1) / busy) {}
   int64_t tiles(int rows) const { return busy * ((each + rows - 1) / rows); }
 };
-// The activations.  Tiles of 64 columns; the middling ones' activations are quantised by another launch (2.5 us and more).  us, few / 64 / 128 / tall:
-//   2 of 4 experts of 4096 x 11008, rows each:  4  87 89 94 104;  16  97 91 89 103;  32  108 87 93 103;  64  161 93 96 106;  150  275 131 120 110
-//   8 of 32 of 4096 x 1376:  4  84 93 97 100;  16  93 99 102 102;  32  110 100 104 102;  100  208 112 115 106
-//   2 of 8 of 1024 x 2048:  4  14 13 13 20;  32  18 15 15 20;  64  24 17 16 21;  128  35 24 21 22;  256  54 31 31 25
-constexpr int kUpFewRows = 12, kUpMidRows = 64, kUpMidTiles = kTileGrid;
+// The activations.  Tiles of 64 columns; the middling ones' activations are quantised by another launch (2.5 us and more).  A layer's time, us, with
+// few / 64 / 128 / tall for all its products:
+//   2 of 4 experts of 4096 x 11008, rows each:  4  116 125 129 149;  16  140 130 131 150;  32  220 132 136 152;  64  334 145 144 160;  95  485 162 153 164;
+//     150  715 219 197 178         8 of 32 of 4096 x 1376:  4  116 118 122 132;  16  133 127 129 136;  32  190 132 135 137;  95  384 169 158 147
+//   2 of 8 of 1024 x 2048:  4  21 21 22 33;  32  31 24 25 34;  64  44 28 29 37;  128  73 37 34 43;  256  123 47 51 51
+//   2 of 8 of 2048 x 8192:  1  59 74 77 80;  32  157 99 100 103;  88  328 129 111 112;  125  436 153 143 118
+constexpr int kUpFewRows = 12, kUpMid64Rows = 64, kUpMidRows = 96, kUpMidTiles = kTileGrid;
 Path up_path(int64_t R, int E, int f) {
   const Rows n(R, E);
   if (n.each <= kUpFewRows) return kFew32;
-  if (n.each <= kUpMidRows) return kMid64;
-  return n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
+  if (n.each <= kUpMid64Rows) return kMid64;
+  return n.each <= kUpMidRows || n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
 }
-// Other products.  Of one matrix (sums of tiles that are cut along K are added by another launch), rows, us:
-//   1024 x 1024: 64  5.3 6.7 7.8 12;  256  5.3 6.7 9.1 16;  1024  13 7.0 9.5 16        4096 x 1376:  32  5.3 7.8 9.0 15;  96  8.6 8.1 11 17;  1024  27 12 13 20
-//   4096 x 4096: 24  9.3 10 11 15;  32  10 10 11 15;  64  15 11 13 17;  256  47 17 18 29;  1024  75 26 28 42;  2048  156 48 39 53
-//   4096 x 11008: 16  15 - - 20;  24  19 16 16 21;  64  33 16 19 24;  256  120 28 31 44;  1024  192 71 67 65;  2048  401 144 104 91
-//   11008 x 4096: 24  21 17 18 17;  256  58 29 31 35;  512  120 45 38 44;  1024  217 75 68 45          512 x 8192: 16  11 - - 14;  24  14 9 10 15
+// Other products.  Of one matrix (sums of tiles that are cut along K are added by another launch), columns x K, rows, us:
+//   1024 x 1024: 64  5.1 7.3 8.3 13;  256  5.6 7.1 9.5 16;  1024  13 7.5 9.8 16;  16384  75 36 29 22
+//   4096 x 1376: 32  5.4 8.0 9.5 15;  96  8.5 8.4 11 17;  1024  27 12 13 20;  16384  366 207 143 97
+//   4096 x 4096: 16  7.4 9.6 11 15;  32  9.5 10 12 16;  64  15 12 13 17;  256  47 16 21 29;  1024  74 27 29 43;  2048  157 52 41 53;  16384  - 591 333 211
+//   4096 x 11008: 16  15 15 17 21;  64  33 18 20 24;  256  120 30 33 44;  1024  193 73 74 65;  2048  402 146 105 94
+//   512 x 8192: 16  11 9.3 10 15;  256  25 12 14 25;  2048  91 23 22 31        256 x 2048: 64  7.4 9.4 10 15;  1024  8.1 10 13 23;  16384  37 16 17 32
+//   11008 x 4096: 1  12 16 - -;  8  14 17 - -;  16  16 13 18 17;  32  23 14 18 19;  256  59 29 32 35;  512  118 45 40 44;  1024  216 76 70 46
+//   11008 x 2048: 16  8.8 9.6 - -;  32  12 11 - -        8192 x 8192: 4  16 19 - -;  12  19 17 - -        33000 x 512: 8  7.0 6.5;  48  11 7.7;
+//   33000 x 4096: 1  40 32 - -;  32  46 37 - -
 // Of experts (the sums of tiles that are cut are added where the rows are combined), rows each:
 //   4 of 11008 x 4096 (K x N): 4  42 44 46 43;  16  56 46 46 44;  32  86 47 48 45;  64  132 58 50 49;  150  297 86 79 59
 //   32 of 1376 x 4096: 4  37 36 37 41;  16  44 41 41 43;  32  52 43 43 44;  100  99 61 53 47       8 of 2048 x 1024: 4  8 9 10 15;  16  11 9 10 15;
 //   64  20 11 12 18;  256  51 16 19 27;  1024  166 38 38 45;      64 of 1024 x 2048: 4  29 31 31 36;  32  40 37 36 38;  64  57 42 41 39;  256  155 89 86 62
-Path out_path(int64_t R, int E, int N, int K) {
+Path out_path(int64_t R, int E, int N, int K, bool exact) {
   const Rows n(R, E);
   const int columns = ceil_div(N, kMidCols), n_blk = (int)(f8_pitch(K) / kF8Block);
   const int64_t tiles = n.tiles(64) * columns;
   if (E == 1) {
-    // (a few long columns: only cut along K do they fill the chip)
-    if ((n.each <= 16 || n.each * n_blk <= 1024) && (tiles >= 8 || n_blk < 48)) return n.each <= 24 ? kFew32 : kFew64;
+    // (a few long columns: only cut along K do they fill the chip; exact: conversions of rows that are not there)
+    const bool wide = columns >= 64 && !exact, few = wide ? n.each * n_blk <= 384 && (columns < 256 || n_blk < 4)
+                                                          : (n.each <= 16 || n.each * n_blk <= 1024) && (tiles >= 8 || n_blk < 48);
+    if (few) return n.each <= 24 ? kFew32 : kFew64;
     if (tiles <= 2 * kTileGrid) return kMid64;
   } else {
     if (n.each <= 8) return kFew32;
@@ -983,7 +1022,14 @@ size_t f8_matmul_workspace_bytes(int M, int N, int K) { return f8_pitch(K) / kF8
 int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
   F8Args g{m.a, m.b, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.M, m.N, m.K, nullptr, nullptr, m.out, m.residual, 1, static_cast<float*>(m.workspace)};
   const bool bf16 = m.dtype == BTX_BF16;
-  Path path = out_path(m.M, 1, m.N, m.K);
+  // A result of few columns, turned: few rows of b, with the many of a for weights.  Tiles of 64 rows and 128 columns are cut along K for these, and have
+  // most of their columns empty.  us, turned / not, rows x columns, K:  800 x 8  2048 4.6 7.7, 8192 9.3 8.6;  800 x 64  2048 7.6 8.6, 4096 13 8.5;
+  // 3000 x 16  2048 4.9 8.3, 4096 7.2 8.8, 8192 12 12;  16384 x 16  520 5.7 5.6, 4096 15 18, 8192 31 35 (fp32 40 55);  16384 x 64  2048 15 11, 8192 46 36
+  if (m.M > 64 && (m.M < 4096 ? m.N <= 64 && (int64_t)m.K * (m.N + 16) <= 180000 : m.N <= 16)) {
+    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true};
+    return bf16 ? launch_few<bf16_t>(t, m.N <= 32 ? 32 : 64, s) : launch_few<float>(t, m.N <= 32 ? 32 : 64, s);
+  }
+  Path path = out_path(m.M, 1, m.N, m.K, !bf16);
   if (path == kTall && !bf16) path = kMid128;
   const int most = f8_matmul_workspace_bytes(m.M, m.N, m.K) ? kMostSlices : 1;
   if (int rc = bf16 ? launch_out<false>(g, path, most, s) : launch_out<true>(g, path, most, s)) return rc;
@@ -1014,7 +1060,7 @@ size_t f8_y_bytes(int64_t R, int d, int f, int E) {
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s) {
   const int R = l.T * l.k;
   F8Args g{{l.act_codes, l.act_scales}, l.W2, {nullptr, nullptr}, l.offsets, nullptr, l.E, l.k, R, l.d, l.f, nullptr, nullptr, l.y, nullptr, 1, static_cast<float*>(l.y)};
-  if (int rc = launch_out<false>(g, out_path(R, l.E, l.d, l.f), combine_most_slices(l.T, l.k, BTX_BF16), s)) return rc;
+  if (int rc = launch_out<false>(g, out_path(R, l.E, l.d, l.f, false), combine_most_slices(l.T, l.k, BTX_BF16), s)) return rc;
   *slices = g.slices;
   return BTX_OK;
 }

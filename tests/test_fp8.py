@@ -451,7 +451,10 @@ MATMULS = [(1, 8, 1), (1, 64, 128), (3, 40, 130), (16, 72, 256), (17, 128, 384),
            (130, 1376, 300), (256, 256, 2048), (257, 520, 1100), (301, 1032, 2177), (600, 768, 500), (1025, 264, 4001), (33, 2048, 11008), (2000, 1536, 384),
            (300, 1032, 4100), (64, 2056, 11008), (513, 264, 18000), (16500, 2048, 130), (2100, 2048, 6500), (4200, 2048, 6500),
            (5, 33000, 136), (30, 32776, 264), (40, 33000, 520), (17, 264, 7000), (16, 520, 8000),
-           (700, 1032, 3000), (1100, 4104, 264), (2048, 4096, 8300)]
+           (700, 1032, 3000), (1100, 4104, 264), (2048, 4096, 8300),
+           # of few columns and many rows
+           (301, 8, 2048), (1001, 40, 500), (3001, 64, 1024), (5003, 16, 8192), (16411, 16, 300), (9001, 256, 2304), (4100, 72, 2600), (20003, 136, 384),
+           (6007, 512, 1300)]
 
 
 @gpu
