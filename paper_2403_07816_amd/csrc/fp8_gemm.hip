@@ -2,10 +2,10 @@
 // quantised along f, and DOWN, y = act W2_e).  Both operands have K contiguous.  Lane l holds row l % 16; which chunks of K the lane groups
 // l / 16 hold is free, as long as both operands agree.  B is the first operand: each lane then ends up with four consecutive columns of one
 // row of the result.
-//   * Results in bf16 and activations: v_mfma_scale_f32_16x16x128_f8f6f4 takes 128 codes of a row with their scale as they are.  Of every 8
+//   * Results in bf16 and the activations of tall tiles: v_mfma_scale_f32_16x16x128_f8f6f4 takes 128 codes of a row with their scale as they are.  Of every 8
 //     neighbouring products it drops what lies 13 bits or more below the exponent of the largest before it adds them up, and then sums in
 //     fp32: normally distributed rows and columns give a result 2e-5 of its norm off, where rounding it to bf16 puts it 1.7e-3 off.
-//   * Results in fp32: the codes become bf16, exactly, with their scale (values under 2^-126: to bf16's precision there), and
+//   * Results in fp32 and all other activations: the codes become bf16, exactly, with their scale (values under 2^-126: to bf16's precision there), and
 //     v_mfma_f32_16x16x32_bf16 multiplies those: exact products, sums in fp32, at half the rate.
 #include "fp8.h"
 #include "tile_lds.h"
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
   // (DOWN of one token, 2 experts of 4096 x 11008: 22.8 us with all workgroups at the same place of their rows, 18.9 so; UP of two to 16, 4 experts: 87-90,
   // 75-78; of 64 columns nothing was gained)
   const int turn = (UP || FR == 1) && n_blk > 1 ? 3 * blockIdx.x % (n_blk / 2) : 0;
-  few_live_products<std::is_same_v<OT, float> && !UP>(acc, b, g, t, n_blk, f8_scale_pitch(g.K), ks, KS, turn, grp, r);
+  few_live_products<std::is_same_v<OT, float>>(acc, b, g, t, n_blk, f8_scale_pitch(g.K), ks, KS, turn, grp, r);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -294,7 +294,7 @@ static_assert(kF8MostColumns / 32 <= 65535 && (kF8MostRows / 64 + kF8MaxExperts 
 // direct copies fill; 4 wavefronts have BM/2 x 64 of the result each (UP: 32 columns of either panel).  Two workgroups are on a compute unit
 // and overlap what each waits for, the conversions to bf16 of fp32 results among it.  Rows of A that are not there are not copied.
 constexpr int kMidWaves = 4, kMidCols = 128;
-enum MidMode { kMidUp, kMidOut, kMidExact };           // activations in fp32 (sums), bf16, fp32 by way of bf16
+enum MidMode { kMidUp, kMidOut, kMidExact };           // activations in fp32 (sums) and fp32 results, both by way of bf16; bf16 results
 template <int BM> struct Mid {
   static constexpr int NS = BM == 128 ? 2 : 3;
   static constexpr uint32_t stage = (BM + kMidCols) * 128, scale_stage = (BM + kMidCols) * 16, scales0 = NS * stage;
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int st = 0; st < 2; ++st) fa[i][st] = *(lds_frag)(uintptr_t)((at_a ^ (st << 4)) + stage + i * 2048);
-    if constexpr (MODE == kMidExact) {
+    if constexpr (MODE != kMidOut) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {                      // 8 codes a lane
         bf16x8 bb[TN];
@@ -947,18 +947,21 @@ struct Rows {
   Rows(int64_t R, int E) : busy(std::min<int64_t>(E, R)), each((R + busy - 1) / busy) {}
   int64_t tiles(int rows) const { return busy * ((each + rows - 1) / rows); }
 };
-// The activations.  Tiles of 64 columns; the middling ones' activations are quantised by another launch (2.5 us and more).  A layer's time, us, with
-// few / 64 / 128 / tall for all its products:
-//   2 of 4 experts of 4096 x 11008, rows each:  4  116 125 129 149;  16  140 130 131 150;  32  220 132 136 152;  64  334 145 144 160;  95  485 162 153 164;
-//     150  715 219 197 178         8 of 32 of 4096 x 1376:  4  116 118 122 132;  16  133 127 129 136;  32  190 132 135 137;  95  384 169 158 147
-//   2 of 8 of 1024 x 2048:  4  21 21 22 33;  32  31 24 25 34;  64  44 28 29 37;  128  73 37 34 43;  256  123 47 51 51
-//   2 of 8 of 2048 x 8192:  1  59 74 77 80;  32  157 99 100 103;  88  328 129 111 112;  125  436 153 143 118
-constexpr int kUpFewRows = 12, kUpMid64Rows = 64, kUpMidRows = 96, kUpMidTiles = kTileGrid;
+// The activations.  Few and middling rows: products by way of bf16, whose sums are exact to fp32, and fp32 activations that another launch quantises
+// (2.5 us and more): a sum that is 2e-5 off is on the other side of a code's border now and then, or its block of a scale's, and over few tokens one such
+// block shows (3 tokens of 4 experts of 168 x 88: 0.0053 of the result's norm, and 0.0017).  That costs little where reading the weights bounds it:
+// 16 tokens of 2 of 4 experts of 4096 x 11008 122 -> 132 us, 64 131 -> 135.  Tall tiles' are on the matrix cores' own 8-bit products: 16384 tokens would
+// take twice as long, and the sums' errors average out over those.  A layer's time, us, with few / 64 / 128 / tall for UP:
+//   2 of 4 experts of 4096 x 11008, rows each:  1  66 66 80 73;  4  134 126 128 145;  16  152 133 139 153;  64  236 142 149 159;  95  316 179 162 164
+//   8 of 32 of 4096 x 1376:  4  124 129 142 137;  16  142 136 144 142;  50  216 147 153 149;  95  315 180 165 156
+//   2 of 8 of 2048 x 8192:  1  63 68 73 78;  16  108 98 104 106;  32  130 101 108 107;  63  188 127 122 115
+//   2 of 8 of 1024 x 2048:  1  15 18 21 23;  16  26 24 26 27;  64  39 31 32 30;  128  56 42 40 35
+constexpr int kUpFewRows = 3, kUpMidRows = 64, kUpMidTiles = kTileGrid;
 Path up_path(int64_t R, int E, int f) {
   const Rows n(R, E);
   if (n.each <= kUpFewRows) return kFew32;
-  if (n.each <= kUpMid64Rows) return kMid64;
-  return n.each <= kUpMidRows || n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
+  if (n.each <= kUpMidRows) return kMid64;
+  return n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
 }
 // Other products.  Of one matrix (sums of tiles that are cut along K are added by another launch), columns x K, rows, us:
 //   1024 x 1024: 64  5.1 7.3 8.3 13;  256  5.6 7.1 9.5 16;  1024  13 7.5 9.8 16;  16384  75 36 29 22
