@@ -313,37 +313,35 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
   const uint32_t base = (uint32_t)(uintptr_t)smem;
 
   // ---- the tile.  Workgroups that are a multiple of 8 apart are on one XCD: those that read the same columns, or, of one matrix with more tiles of rows than
-  // of columns, the same rows, follow each other there.  Every XCD has as many: with columns dealt to the XCDs in turn, 16384 x 128 x 8192 was one XCD's
-  // work, 147 us for 32, and 16384 x 512 x 8192 149 for 72.  (Experts' columns are, where that is even: UP of 2 of 4 experts of 4096 x 11008 then
-  // reads them in order, 95 us and 97.)
+  // of columns, the same rows, follow each other there.  Every XCD has as many: with columns always in turn, 16384 x 128 x 8192 was one XCD's work,
+  // 147 us for 32, and 16384 x 512 x 8192 149 for 72.  (In turn, where that is even: neighbouring columns are read at a time.  UP of 2 of 4 experts of
+  // 4096 x 11008 95 us and 97; 64 x 4096 x 11008 16.8 and 17.7; but 256 x 4096 x 4096 17.8 and 16.0)
   Tile t;
   const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
-  int c, n_c = n_ct * slices;
-  auto place = [&](int n_rt) {                           // the 8 XCDs' equal runs; past the last tile: none
-    const int tiles = n_rt * n_c, each = (tiles + kXcds - 1) / kXcds;
-    return local < each ? min(xcd * each + local, tiles) : tiles;
+  const int n_c = n_ct * slices;
+  int c, rt;
+  // columns in turn, rows of them one after another; or 8 equal runs of the tiles (past the last one: no tile), columns or rows first
+  auto in_turn = [&](int n_rt) {
+    c = local / n_rt * kXcds + xcd;
+    rt = local % n_rt;
+    return c < n_c;
   };
+  auto in_runs = [&](int n_rt, bool rows_first) {
+    const int tiles = n_rt * n_c, each = (tiles + kXcds - 1) / kXcds, id = xcd * each + local;
+    c = rows_first ? id % n_c : id / n_rt;
+    rt = rows_first ? id / n_c : id % n_rt;
+    return local < each && id < tiles;
+  };
+  const bool even = n_c % kXcds == 0 || n_c >= 64;
   if (g.offsets) {
     const ExpertTiles tiles(g.offsets, g.E, BM, lane);
     const int n_rt = tiles.count();
-    if (n_rt == 0) return;
-    int rt;
-    if (n_c % kXcds == 0 || n_c >= 64) {
-      c = local / n_rt * kXcds + xcd;
-      rt = local % n_rt;
-    } else {
-      const int id = place(n_rt);
-      c = id / n_rt;
-      rt = id % n_rt;
-    }
-    if (c >= n_c) return;
+    if (n_rt == 0 || !(even ? in_turn(n_rt) : in_runs(n_rt, false))) return;
     t = tiles.at(rt);
   } else {
-    const int n_rt = (g.R + BM - 1) / BM, id = place(n_rt);
-    if (id >= n_rt * n_c) return;
-    const bool rows_first = n_rt > n_ct;
-    c = rows_first ? id % n_c : id / n_rt;
-    t = Tile{0, (rows_first ? id / n_c : id % n_rt) * BM, g.R};
+    const int n_rt = (g.R + BM - 1) / BM;
+    if (!(even && n_rt <= 2 ? in_turn(n_rt) : in_runs(n_rt, n_rt > n_ct))) return;
+    t = Tile{0, rt * BM, g.R};
   }
   const int slice = c / n_ct, col0 = (c - slice * n_ct) * COLS, quads = (nk_all + 3) / 4;
   const int k_first = slice * quads / slices * 4, nk = min((slice + 1) * quads / slices * 4, nk_all) - k_first;
