@@ -143,7 +143,7 @@ template <typename XT, bool VEC, bool SHARED>
 __global__ __launch_bounds__(kThreads) void f8_quantize_cols_kernel(const XT* __restrict__ x, int64_t K, int64_t N, uint8_t* __restrict__ codes,
                                                                     uint8_t* __restrict__ scales, unsigned col_pieces) {
   __shared__ __attribute__((aligned(16))) uint8_t s_codes[kTile * kTile];
-  __shared__ u32x4 s_amax[kTile];                       // of a column, or in the first of all: the four wavefronts'
+  __shared__ u32x4 s_amax[8][kTile / 8];                // of column 8 cq + h at [h][cq], or in the first of all: the four wavefronts'
   __shared__ uint8_t s_scale[kTile];
   static_assert(kWaves == 4, "u32x4");
   const int64_t b = blockIdx.x / col_pieces, col0 = (int64_t)(blockIdx.x - b * col_pieces) * kTile, batch = blockIdx.y;
@@ -167,16 +167,16 @@ __global__ __launch_bounds__(kThreads) void f8_quantize_cols_kernel(const XT* __
 #pragma unroll
     for (int h = 0; h < 8; ++h) all = max(all, amax[h]);
     all = f8_row_max(all);
-    if (lane == 0) reinterpret_cast<uint32_t*>(s_amax)[wave] = all;
+    if (lane == 0) reinterpret_cast<uint32_t*>(&s_amax[0][0])[wave] = all;
   } else if (lane < 16) {
 #pragma unroll
-    for (int h = 0; h < 8; ++h) reinterpret_cast<uint32_t*>(s_amax + cq * 8 + h)[wave] = amax[h];
+    for (int h = 0; h < 8; ++h) reinterpret_cast<uint32_t*>(&s_amax[h][cq])[wave] = amax[h];
   }
   __syncthreads();
 #pragma unroll
   for (int h = 0; h < 8; ++h) {
     const int c = cq * 8 + h;
-    const u32x4 four = s_amax[SHARED ? 0 : c];
+    const u32x4 four = SHARED ? s_amax[0][0] : s_amax[h][cq];
     const uint32_t byte = f8_scale_byte(max(max(four[0], four[1]), max(four[2], four[3])));
     float w[8];
 #pragma unroll
