@@ -61,19 +61,15 @@ __global__ __launch_bounds__(kThreads) void f8_norm_kernel(const XT* h, const XT
   const int64_t t = TPR == kWave ? (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave : blockIdx.x;
   if (t >= T) return;                                    // (whole wavefronts; with TPR the workgroup none)
   const XT* const hr = h + t * d;
-  float v[MAXC][8] = {};
+  // (without a branch around a load: behind one, the next waits for it)
+  auto at = [&](int m) { return min((m * TPR + tid) * 8, d - 8); };
+  float v[MAXC][8];
 #pragma unroll
-  for (int m = 0; m < MAXC; ++m) {
-    const int c = (m * TPR + tid) * 8;
-    if (c < d) RowVec<XT, 8>::ld(hr + c, v[m]);
-  }
+  for (int m = 0; m < MAXC; ++m) RowVec<XT, 8>::ld(hr + at(m), v[m]);
   if (residual) {
-    float r[MAXC][8] = {};
+    float r[MAXC][8];
 #pragma unroll
-    for (int m = 0; m < MAXC; ++m) {
-      const int c = (m * TPR + tid) * 8;
-      if (c < d) RowVec<XT, 8>::ld(residual + t * d + c, r[m]);
-    }
+    for (int m = 0; m < MAXC; ++m) RowVec<XT, 8>::ld(residual + t * d + at(m), r[m]);
 #pragma unroll
     for (int m = 0; m < MAXC; ++m) {
 #pragma unroll
@@ -81,6 +77,10 @@ __global__ __launch_bounds__(kThreads) void f8_norm_kernel(const XT* h, const XT
       round_sum(hr, v[m]);
     }
   }
+#pragma unroll
+  for (int m = 0; m < MAXC; ++m)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[m][i] = (m * TPR + tid) * 8 < d ? v[m][i] : 0.f;
   double square = 0.0;
 #pragma unroll
   for (int m = 0; m < MAXC; ++m)
