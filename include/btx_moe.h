@@ -483,7 +483,7 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  * btx_moe_ff_forward_mx4 - the layer of 4-bit experts, for serving (forward only): btx_moe_ff_forward with both
  * operands of every product in microscaled 4-bit floats.  Token rows are quantised along d once each; per expert
  *     act = silu(xq W1_e) * (xq W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
- *     (but for sums that are cut into ranges, which stay in fp32)
+ *     (but for up to 2^22 values and for sums that are cut into ranges, which stay in fp32; not with more than 8 experts a token, 4 of many tokens)
  *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
  *   x [T,d] bf16;  residual [T,d] bf16, may be NULL;  out [T,d] bf16; aliasing as in btx_moe_ff_forward
  *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
@@ -549,14 +549,17 @@ int btx_rmsnorm_fp8(const void* h, const void* residual, int dtype, const float*
                     uint8_t* codes, uint8_t* scales, void* stream);
 
 /* ---------------------------------------------------------------------------
- * btx_fp8_matmul - out[m,n] = residual[m,n] + sum_k A[m,k] B[n,k] of two matrices in block-scaled 8-bit floats: exact products, sums in fp32
- * (in an order that the sizes fix), rounded once.
+ * btx_fp8_matmul - out[m,n] = residual[m,n] + sum_k A[m,k] B[n,k] of two matrices in block-scaled 8-bit floats: sums in fp32 in an order that the sizes
+ * fix (the same bits every time), rounded once.  fp32 results: exact products (of values under 2^-126, those to bf16's precision there).  bf16 results: of
+ * every 8 neighbouring products what lies 13 bits or more below the largest is dropped before they are added up (2e-5 of the result's norm, where rounding
+ * it to bf16 is 1.7e-3), in up to twice the rate.
  *   A         codes [M,btx_fp8_code_pitch(K)], scales [M,btx_fp8_scale_pitch(K)];   B: the same with N rows
  *   residual  [M,N]  dtype, may be NULL; may be out itself (a gradient that is added to)
  *   out       [M,N]  dtype (BTX_F32 or BTX_BF16)
  * What lies behind K in the codes' rows has to be zeros, as btx_fp8_quantize writes them.
- * Requirements: N % 8 == 0, K >= 1, M * max(N, pitch) < 2^40, N * pitch < 2^40; M < 2^28 - 256, N and K <= 2097120 (BTX_ERR_UNSUPPORTED); everything on 16-byte
- * boundaries; workspace >= btx_fp8_matmul_workspace_bytes(M,N,K) (may be NULL where that is 0).
+ * Requirements: N % 8 == 0, K >= 1, M * max(N, pitch) < 2^40, N * pitch < 2^40; M < 2^28 - 256, N and K <= 2097120, in fp32
+ * ceil(M/128) * ceil(N/128) < 2^24 (BTX_ERR_UNSUPPORTED); everything on 16-byte boundaries; workspace >= btx_fp8_matmul_workspace_bytes(M,N,K) (may be NULL
+ * where that is 0).
  */
 size_t btx_fp8_matmul_workspace_bytes(int M, int N, int K);
 int btx_fp8_matmul(const uint8_t* A_codes, const uint8_t* A_scales, const uint8_t* B_codes, const uint8_t* B_scales, int M, int N, int K,
@@ -567,7 +570,8 @@ int btx_fp8_matmul(const uint8_t* A_codes, const uint8_t* A_scales, const uint8_
  * 8-bit floats.  Per expert
  *     act = silu(x W1_e) * (x W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
  *     (but for sums that are cut into ranges, which stay in fp32)
- *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
+ * Products as btx_fp8_matmul's: for act as its fp32 results' up to 64 rows an expert on average and in small layers, else as its bf16 ones', with which one
+ * code in a few thousand is the neighbour of the one that exact sums have (out 2.1e-3 of its norm from the formula instead of 1.7e-3); for y as its bf16 ones'.
  *   x         codes [T,btx_fp8_code_pitch(d)] and scales [T,btx_fp8_scale_pitch(d)], as btx_rmsnorm_fp8 or btx_fp8_quantize (axis 1) writes them
  *   W1, W3    codes [E,f,btx_fp8_code_pitch(d)] and scales [E,f,btx_fp8_scale_pitch(d)];   W2: [E,d,btx_fp8_code_pitch(f)] and
  *             [E,d,btx_fp8_scale_pitch(f)], as btx_fp8_quantize (axis 0; any block_rows) writes them

@@ -657,9 +657,9 @@ int btx_moe_ff_forward_fp8(const uint8_t* x_codes, const uint8_t* x_scales, cons
   const F8Layer l{{x_codes, x_scales}, {W1_codes, W1_scales}, {W3_codes, W3_scales}, {W2_codes, W2_scales}, T, d, f, E, k, offsets, perm,
                   w.act_codes, w.act_scales, w.y};
   BTX_STAGE(BTX_STAGE_UP, launch_f8_up(l, s));
-  int slices = 1;
+  int slices = 0;
   BTX_STAGE(BTX_STAGE_DOWN, launch_f8_down(l, &slices, s));
-  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(w.y, static_cast<const float*>(w.y), slices, false, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
+  BTX_STAGE(BTX_STAGE_COMBINE, launch_combine(slices ? nullptr : w.y, static_cast<const float*>(w.y), std::max(slices, 1), false, gates, inv_pos, residual, out, T, k, d, BTX_BF16, s));
   return BTX_OK;
 }
 

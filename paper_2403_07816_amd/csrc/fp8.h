@@ -77,7 +77,7 @@ struct F8Layer {
   uint8_t* act_codes; uint8_t* act_scales; void* y;
 };
 int launch_f8_up(const F8Layer& l, hipStream_t s);
-// y = act W2, [T*k, d] bf16; or *slices > 1 of its sums in fp32 instead, [slice][T*k, d], for launch_combine() to add and weigh without rounding them
+// y = act W2, [T*k, d] bf16; or *slices > 0 sums of it in fp32 instead, [slice][T*k, d], for launch_combine() to add and weigh without rounding them
 size_t f8_y_bytes(int64_t R, int d, int f, int E);
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s);
 int f8_prepare();                      // one-time set-up on the current device (not capturable)

@@ -43,8 +43,9 @@ struct F8Args {
   int E, k, R, N, K;                    // N columns, depth K
   uint8_t* act_codes; uint8_t* act_scales;
   void* out; const void* residual;
-  int slices; float* sums;              // K ranges of a tile; more than one: their sums [slice][R][N] go there, and not to out
+  int slices; float* sums;              // K ranges of a tile; more than one, or in32: their sums [slice][R][N] go there, and not to out
   bool turned;                          // few rows: these are the result's columns, and it is written [N][R]
+  bool in32;
 };
 
 struct Tile { int e, row0, row_end; };
@@ -251,6 +252,8 @@ __global__ __launch_bounds__(KS* kWave, 2) void f8_few_kernel(F8Args g) {
       const f32x4 h3 = sum(FR + p);
 #pragma unroll
       for (int x = 0; x < 4; ++x) v[x] = silu_f(v[x]) * h3[x];
+      *reinterpret_cast<f32x4*>(g.sums + at) = v;
+    } else if (g.in32) {
       *reinterpret_cast<f32x4*>(g.sums + at) = v;
     } else if (g.turned) {
       const OT* const residual = static_cast<const OT*>(g.residual);
@@ -504,7 +507,7 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
 #pragma unroll
         for (int x = 0; x < 4; ++x) v[x] = silu_f(v[x]) * acc[i][j + 2][x];
         *reinterpret_cast<f32x4*>(g.sums + at) = v;
-      } else if (slices > 1) {
+      } else if (slices > 1 || g.in32) {
         *reinterpret_cast<f32x4*>(g.sums + (int64_t)slice * g.R * g.N + at) = v;
       } else {
         store_out<MODE == kMidExact>(g, at, v);
@@ -810,7 +813,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
         for (int64_t z = out_col0 / 128 + 1; z < out_sc_pitch; ++z) g.act_scales[(int64_t)(out_row0 + tid) * out_sc_pitch + z] = 0;
     } else {
       if (more) start();
-      if (slices > 1) {                                  // four columns a lane, as they are
+      if (slices > 1 || g.in32) {                        // four columns a lane, as they are
         float* const to = g.sums + (int64_t)out_slice * g.R * g.N;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -1027,7 +1030,7 @@ int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
   // most of their columns empty.  us, turned / not, rows x columns, K:  800 x 8  2048 4.6 7.7, 8192 9.3 8.6;  800 x 64  2048 7.6 8.6, 4096 13 8.5;
   // 3000 x 16  2048 4.9 8.3, 4096 7.2 8.8, 8192 12 12;  16384 x 16  520 5.7 5.6, 4096 15 18, 8192 31 35 (fp32 40 55);  16384 x 64  2048 15 11, 8192 46 36
   if (m.M > 64 && (m.M < 4096 ? m.N <= 64 && (int64_t)m.K * (m.N + 16) <= 180000 : m.N <= 16)) {
-    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true};
+    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true, false};
     return bf16 ? launch_few<bf16_t>(t, m.N <= 32 ? 32 : 64, s) : launch_few<float>(t, m.N <= 32 ? 32 : 64, s);
   }
   Path path = out_path(m.M, 1, m.N, m.K, !bf16);
@@ -1058,11 +1061,16 @@ size_t f8_y_bytes(int64_t R, int d, int f, int E) {
   const int64_t rows = std::min(R, std::max<int64_t>(kUpMidRows * E, kUpMidTiles * 128 / ceil_div(f, 64)));
   return (size_t)std::max({R * d * 2, sum_bytes(R, d), rows * f * 4});
 }
+// y in fp32 where it is this small (1 us at most of 64 tokens, 2 of 256 with top-4).  Rounded to bf16, as it is where writing and reading it counts, two
+// experts' rows put out 2.3e-3 of its norm off, and not the 1.7e-3 that rounding out itself costs
+constexpr int64_t kMost32Bytes = 16 << 20;
+static_assert(kMost32Bytes <= kSumBytes, "room in y");
 int launch_f8_down(const F8Layer& l, int* slices, hipStream_t s) {
-  const int R = l.T * l.k;
+  const int R = l.T * l.k, most = combine_most_slices(l.T, l.k, BTX_BF16);
   F8Args g{{l.act_codes, l.act_scales}, l.W2, {nullptr, nullptr}, l.offsets, nullptr, l.E, l.k, R, l.d, l.f, nullptr, nullptr, l.y, nullptr, 1, static_cast<float*>(l.y)};
-  if (int rc = launch_out<false>(g, out_path(R, l.E, l.d, l.f, false), combine_most_slices(l.T, l.k, BTX_BF16), s)) return rc;
-  *slices = g.slices;
+  g.in32 = most > 1 && (int64_t)R * l.d * 4 <= kMost32Bytes;
+  if (int rc = launch_out<false>(g, out_path(R, l.E, l.d, l.f, false), most, s)) return rc;
+  *slices = g.in32 || g.slices > 1 ? g.slices : 0;
   return BTX_OK;
 }
 

@@ -246,7 +246,7 @@ int launch_combine(const void* y, const float* y_sums, int slices, bool round_su
     using ET = decltype(tag);
     constexpr int KMAX = decltype(kmax)::value;
     constexpr bool AS_IS = std::is_same_v<ET, float>;     // fp32: nothing to round, one kernel for both
-    const bool sliced = slices > 1;
+    const bool sliced = slices > 1 || !y;
     auto kernel = !sliced      ? combine_kernel<ET, KMAX, true, false>
                   : round_sums ? combine_kernel<ET, KMAX, true, true>
                                : combine_kernel<ET, KMAX, AS_IS, true>;
