@@ -98,10 +98,10 @@ def sums_error(a, b, exact=False):
     return err
 
 
-def ff_forward(x, W1, W3, W2, topk_idx, gates, inv_pos=None, residual=None):
+def ff_forward(x, W1, W3, W2, topk_idx, gates, inv_pos=None, residual=None, small=False):
     """(out, bound) of the layer.  x [T,d], W1, W3 [E,f,d] and W2 [E,d,f]: the values that the 8 bits stand for.  bound: how far the layer may
     be off whose products sum in fp32, whose activations may therefore fall on the other side of a rounding, and which rounds an
-    expert's output and the result to bf16."""
+    expert's output and the result to bf16; small: whose activations are of exact products and whose experts' outputs stay in fp32."""
     T, d = x.shape
     out = np.zeros((T, d)) if residual is None else np.asarray(residual, dtype=np.float64).copy()
     bound, mag = np.zeros((T, d)), np.abs(out)
@@ -110,7 +110,7 @@ def ff_forward(x, W1, W3, W2, topk_idx, gates, inv_pos=None, residual=None):
         if t.size == 0:
             continue
         g, xs = np.asarray(gates, dtype=np.float64)[t, j][:, None], x[t]
-        h1, h3, e1, e3 = xs @ W1[e].T, xs @ W3[e].T, sums_error(xs, W1[e]), sums_error(xs, W3[e])
+        h1, h3, e1, e3 = xs @ W1[e].T, xs @ W3[e].T, sums_error(xs, W1[e], small), sums_error(xs, W3[e], small)
         with np.errstate(over="ignore"):
             silu = h1 / (1.0 + np.exp(-h1))
         act = silu * h3
@@ -119,7 +119,8 @@ def ff_forward(x, W1, W3, W2, topk_idx, gates, inv_pos=None, residual=None):
         aq, far = rounded(act), near(act, ea)
         y = aq @ W2[e].T
         ey = far @ np.abs(W2[e]).T + sums_error(np.abs(aq) + far, W2[e])
-        ey += 2.0 ** -8 * (np.abs(y) + ey)
+        if not small:
+            ey += 2.0 ** -8 * (np.abs(y) + ey)
         np.add.at(out, t, g * y)
         np.add.at(bound, t, np.abs(g) * ey)
         np.add.at(mag, t, np.abs(g) * (np.abs(y) + ey))

@@ -658,6 +658,20 @@ def test_layer(T, d, f, E, k):
 
 
 @gpu
+@pytest.mark.parametrize("T,d,f,E,k", [(1, 256, 384, 4, 2), (3, 168, 88, 4, 2), (8, 440, 72, 16, 6), (10, 128, 136, 16, 8), (40, 256, 200, 8, 3), (16, 512, 392, 2, 2),
+                                       (64, 264, 1376, 5, 2), (71, 1600, 944, 4, 3), (125, 488, 168, 1, 1), (200, 1032, 520, 8, 2), (300, 264, 2056, 2, 2)])
+def test_small_layers_round_only_what_the_formula_does(T, d, f, E, k):
+    """Up to 64 rows an expert, or 256 tiles of 128 rows and 64 columns, and 2^22 values of y: exact products in front of the activations' codes, and
+    nothing but them and the result is rounded to fewer bits than fp32."""
+    assert T * k * d <= 1 << 22
+    x, xv, W, routing, idx, gates, inv = make_layer(T, d, f, E, k, 9)
+    out = B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing)
+    want, bound = O.ff_forward(xv, W[0][1], W[1][1], W[2][1], idx, gates, inv, small=True)
+    off = np.abs(out.double().cpu().numpy() - want)
+    assert np.all(off <= bound), float((off / bound).max())
+
+
+@gpu
 @pytest.mark.parametrize("T,d,f,E,k", [(50, 256, 264, 6, 2), (900, 256, 264, 6, 2), (3000, 256, 264, 6, 2)])
 def test_layer_of_a_favoured_expert_and_dropped_pairs(T, d, f, E, k):
     for skew, drop in ((True, 0.0), (False, 0.4), (True, 0.9), (False, 1.0)):
