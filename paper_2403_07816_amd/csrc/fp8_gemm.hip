@@ -973,6 +973,8 @@ Path up_path(int64_t R, int E, int f) {
 //   11008 x 4096: 1  12 16 - -;  8  14 17 - -;  16  16 13 18 17;  32  23 14 18 19;  256  59 29 32 35;  512  118 45 40 44;  1024  216 76 70 46
 //   11008 x 2048: 16  8.8 9.6 - -;  32  12 11 - -        8192 x 8192: 4  16 19 - -;  12  19 17 - -        33000 x 512: 8  7.0 6.5;  48  11 7.7;
 //   33000 x 4096: 1  40 32 - -;  32  46 37 - -
+// In fp32:  1024 x 2048: 64  7.9 12 14;  200  8.4 12 15        4096 x 4001: 64  15 14 16;  400  - 29 29;  1376  - 63 59;  4096  - 171 128
+//   4096 x 16384: 40  38 20 23;  100  79 33 28;  400  - 104 81;  1024  - 156 147        512 x 8192: 400  - 15 19;  2048  - 34 29
 // Of experts (the sums of tiles that are cut are added where the rows are combined), rows each:
 //   4 of 11008 x 4096 (K x N): 4  42 44 46 43;  16  56 46 46 44;  32  86 47 48 45;  64  132 58 50 49;  150  297 86 79 59
 //   32 of 1376 x 4096: 4  37 36 37 41;  16  44 41 41 43;  32  52 43 43 44;  100  99 61 53 47       8 of 2048 x 1024: 4  8 9 10 15;  16  11 9 10 15;
@@ -982,10 +984,13 @@ Path out_path(int64_t R, int E, int N, int K, bool exact) {
   const int columns = ceil_div(N, kMidCols), n_blk = (int)(f8_pitch(K) / kF8Block);
   const int64_t tiles = n.tiles(64) * columns;
   if (E == 1) {
-    // (a few long columns: only cut along K do they fill the chip; exact: conversions of rows that are not there)
+    // (a few long columns: only cut along K do they fill the chip; short ones do as long as a compute unit has one workgroup; exact: conversions of rows
+    // that are not there, and of columns twice where tiles have 64 rows)
+    const bool one_round = n_blk <= 16 && ceil_div(R, 64) * ceil_div(N, 16) <= kTileGrid;
     const bool wide = columns >= 64 && !exact, few = wide ? n.each * n_blk <= 384 && (columns < 256 || n_blk < 4)
-                                                          : (n.each <= 16 || n.each * n_blk <= 1024) && (tiles >= 8 || n_blk < 48);
+                                                          : one_round || ((n.each <= 16 || n.each * n_blk <= 1024) && (tiles >= 8 || n_blk < 48));
     if (few) return n.each <= 24 ? kFew32 : kFew64;
+    if (exact && n.each > 64 && n_blk > 64 && tiles >= 64) return kMid128;
     if (tiles <= 2 * kTileGrid) return kMid64;
   } else {
     if (n.each <= 8) return kFew32;

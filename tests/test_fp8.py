@@ -454,7 +454,9 @@ MATMULS = [(1, 8, 1), (1, 64, 128), (3, 40, 130), (16, 72, 256), (17, 128, 384),
            (700, 1032, 3000), (1100, 4104, 264), (2048, 4096, 8300),
            # of few columns and many rows
            (301, 8, 2048), (1001, 40, 500), (3001, 64, 1024), (5003, 16, 8192), (16411, 16, 300), (9001, 256, 2304), (4100, 72, 2600), (20003, 136, 384),
-           (6007, 512, 1300)]
+           (6007, 512, 1300),
+           # few workgroups of few rows; fp32 results over long sums
+           (250, 1000, 2048), (1500, 136, 700), (200, 2080, 8300)]
 
 
 @gpu

@@ -75,13 +75,14 @@ PATHS = [
     (33, 11008, 1024, "few16", "few16", False), (16, 4096, 11008, "few16", "few16", False), (17, 4096, 11008, "mid64", "mid64", True),
     (24, 4096, 4096, "few16", "few16", False), (32, 4096, 4096, "few16", "few16", False), (33, 4096, 4096, "mid64", "mid64", True),
     (16, 512, 8192, "mid64", "mid64", True), (16, 1024, 8192, "few16", "few16", False), (5, 33000, 136, "few64", "few16", False),
-    (30, 33000, 300, "few64", "few16", False), (40, 33000, 520, "mid64", "few16", False), (128, 1024, 1024, "few16", "few16", False), (129, 1024, 1024, "mid64", "mid64", False),
+    (30, 33000, 300, "few64", "few16", False), (40, 33000, 520, "mid64", "few16", False), (128, 1024, 1024, "few16", "few16", False), (129, 1024, 1024, "few16", "few16", False), (256, 1024, 2048, "few16", "few16", False),
+    (257, 1024, 2048, "mid64", "mid64", True), (256, 1024, 2056, "mid64", "mid64", True), (700, 4096, 8300, "mid64", "mid128", False),
     (64, 4096, 11008, "mid64", "mid64", True), (1024, 4096, 4096, "mid64", "mid64", False), (1025, 4096, 4096, "mid128", "mid128", False),
     (2049, 4096, 4096, "tall", "mid128", False), (1376, 4096, 4001, "mid128", "mid128", False), (16384, 11008, 4096, "tall", "mid128", False),
     (2048, 4096, 11008, "tall", "mid128", True),
     # of few columns and many rows
     (65, 16, 2048, "few16", "few16", False), (4095, 64, 2048, "few16", "few16", False), (4095, 64, 2304, "mid64", "mid64", True),
-    (4096, 64, 2048, "mid64", "mid64", True), (5000, 16, 8192, "few16", "few16", False), (16384, 8, 520, "few64", "few16", False),
+    (4096, 64, 2048, "few16", "few16", False), (4097, 64, 2048, "mid64", "mid64", True), (5000, 16, 8192, "few16", "few16", False), (16384, 8, 520, "few64", "few16", False),
     (64, 8, 8192, "mid64", "mid64", True), (65, 8, 8192, "mid64", "mid64", True)]
 
 
