@@ -14,7 +14,7 @@ constexpr uint32_t kCopyBias4 = 3 * 1024;
 __device__ __forceinline__ void copy64(uint64_t base, const uint32_t (&off)[4], uint32_t lds) {
   asm volatile(
       "s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-      "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072"
+      "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3*1024"
       :
       : "s"(lds), "s"(base), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3])
       : "memory");
