@@ -286,7 +286,8 @@ template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_
   }
   return launch_few_shape<false, 1, 4, OT>(g, tile_rows, s);
 }
-// (one token, 2 experts of 4096 x 11008, and 64 tokens, 32 of 4096 x 1376: 37 and 85 us; with 4 wavefronts 40 and 86, with 16 columns and 4 37 and 90)
+// (one token, 2 experts of 4096 x 11008: 37-40 us (4.7 TB/s); before products were by way of bf16, with 2 wavefronts, 4, or 16 columns and 4: 37, 40, 37;
+// 64 tokens, 32 of 4096 x 1376: 85, 86, 90)
 int launch_few_up(const F8Args& g, hipStream_t s) { return launch_few_shape<true, 2, 2, float>(g, 32, s); }
 
 // (tiles of 32 rows only where there are fewer than 25 an expert)
@@ -295,7 +296,9 @@ static_assert(kF8MostColumns / 32 <= 65535 && (kF8MostRows / 64 + kF8MaxExperts 
 // ---- a middling number of rows: BM x 128 tiles, BM 64 or 128 -----------------------------------------------------
 // Bound by reading B where rows are few, by LDS where they are many.  A k tile is a block: [row][128 bytes] of either operand, in a ring of NS stages that
 // direct copies fill; 4 wavefronts have BM/2 x 64 of the result each (UP: 32 columns of either panel).  Two workgroups are on a compute unit
-// and overlap what each waits for, the conversions to bf16 of fp32 results among it.  Rows of A that are not there are not copied.
+// and overlap what each waits for, the conversions to bf16 among it.  Rows of A that are not there are not copied.
+// 64 tokens of 32 experts of 4096 x 1376, top-8: UP 89 us (4.1 TB/s), DOWN 38 (4.8); 1024 x 4096 x 4096 27 us (1.3 PFLOP/s); in fp32 4096 x 4096 x 4001 128 us
+// (1.05 PFLOP/s; the conversions run at a quarter of the vector rate).
 constexpr int kMidWaves = 4, kMidCols = 128;
 enum MidMode { kMidUp, kMidOut, kMidExact };           // activations in fp32 (sums) and fp32 results, both by way of bf16; bf16 results
 template <int BM> struct Mid {
@@ -527,6 +530,8 @@ __global__ __launch_bounds__(kMidWaves* kWave, 2) void f8_mid_kernel(F8Args g, i
 //   * Tiles are dealt so that the ones an XCD runs at a time share row and column panels in its L2; a workgroup takes tile after tile, the next
 //     one's first stage is under way beside the epilogue.
 //   * Of a tile's rows that are not there, 64 of a wavefront's are passed over.
+// 16384 x 11008 x 4096 543 us (2.72 PFLOP/s; with codes of zero 431: the power budget), matrix cores busy 67 % of the time at 1.7 GHz; UP and DOWN of 16384 tokens,
+// top-2, 2.2-2.4 and 1.1 ms.
 constexpr int kTileRows = 256, kTileWaves = 8;
 constexpr uint32_t kStage = 32768, kScaleStage = 8192;  // scales of 16 k tiles: 256 rows of A, 256 of B
 constexpr uint32_t kB0 = 2 * kStage, kScale0 = 4 * kStage, kOffsets0 = kScale0 + 2 * kScaleStage;

@@ -5,6 +5,8 @@
 //           8 neighbouring columns (16 bytes a load or store of bf16, 256 a row of the workgroup's), and whole 128 bytes of every row of
 //           codes go through LDS.
 // block_rows 128: the 128 rows of the result that share a scale are one workgroup's.
+// bf16, there and back: 2^30 elements along rows 5.9 and 5.8 TB/s, down columns 5.2 and 5.3; 4 x 4096 x 11008 down columns in 128 x 128 blocks 91 us each way;
+// 4001 x 4096 down columns 11.8 us (992 workgroups, one round of the chip) and 7.5.
 #include "fp8.h"
 
 #include <type_traits>
