@@ -46,6 +46,7 @@ struct F8Args {
   int slices; float* sums;              // K ranges of a tile; more than one, or in32: their sums [slice][R][N] go there, and not to out
   bool turned;                          // few rows: these are the result's columns, and it is written [N][R]
   bool in32;
+  bool apart;                           // tall tiles of neighbouring columns begin at different places of K
 };
 
 struct Tile { int e, row0, row_end; };
@@ -559,6 +560,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
   }
   int e, row0, row_end, col0, slice, id = blockIdx.x;
   int k_first, nk;                                       // its k tiles: k_first (a multiple of four, as words of scales are read) .. + nk - 1
+  int first, left;                                       // the one that it begins at, to go round, and copies up to the last one
   auto find_tile = [&]() -> bool {                       // `id`, or the next one of this workgroup that names a tile
     auto among = [&](int n_rt, auto rows_of) -> bool {
       const int most = n_rt * n_ct + kXcds;
@@ -574,6 +576,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
           row0 = t.row0;
           row_end = t.row_end;
           col0 = tn * COLS;
+          first = k_first + (g.apart && slices == 1 && nk % 16 == 0 ? 4 * tn % nk : 0);
           return true;
         }
       return false;
@@ -588,7 +591,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
   auto chunk = [](int ln, int q) { return (ln & 7) ^ tile_swz(ln / 8 + 8 * (q & 1)); };
   const int a_row = wm * 128 + wn * 16;
   uint32_t a_off[4], b_off[4], s_off;                    // a_off: A0, A0, A1, A1
-  uint64_t a_from, b_from, s_from;                       // a, b: of the k tile behind the next (A1: the one before)
+  uint64_t a_from, a1_from, b_from, s_from;              // a, b: of the k tile behind the next (A1: the one before)
   auto row_index = [&](int at) -> uint32_t {
     const int gr = min(row0 + at, row_end - 1);
     return g.perm ? (uint32_t)g.perm[gr] / (uint32_t)g.k : (uint32_t)(gr - row0);
@@ -610,7 +613,8 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
       asm volatile("" : "+v"(a_off[q]), "+v"(b_off[q]));
     }
     const F8Matrix& bm = UP && wave >= 4 ? g.b1 : g.b0;
-    const int64_t k0 = (int64_t)k_first * kF8Block;
+    const int64_t k0 = (int64_t)first * kF8Block;
+    left = k_first + nk - first;
     a_from = uniform64(g.a.codes + (g.perm ? 0 : (int64_t)row0 * row_bytes) + k0) - kCopyBias2;
     b_from = uniform64(bm.codes + ((int64_t)e * g.N + col0) * row_bytes + k0) - kCopyBias4;
     if (wm == 0) {
@@ -628,8 +632,16 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
     copy32(a_from, a_off[0], a_off[1], to_a + stage * kStage);
     copy64(b_from, b_off, to_b + stage * kStage);
   };
+  auto advance = [&] {
+    a1_from = a_from;
+    const int64_t to = --left == 0 ? (int64_t)(1 - nk) * kF8Block : (int64_t)kF8Block;
+    a_from += to;
+    b_from += to;
+  };
   auto copy_a1 = [&](int stage, uint64_t from) { copy32(from, a_off[2], a_off[3], to_a + stage * kStage + 64 * 128); };
-  auto copy_scales = [&](int c) { copy16(s_from + (uint64_t)c * 16, s_off, to_s + (c & 1) * kScaleStage); };   // of k tiles 16 c ..
+  auto copy_scales = [&](int c) {                        // of k tiles 16 c ..
+    copy16(s_from + (uint64_t)(16 * c < k_first + nk ? c : c - nk / 16) * 16, s_off, to_s + (c & 1) * kScaleStage);
+  };
 
   // ---- fragments: lane l has row l % 16, chunks 2g and 2g + 1 of lane group g = l / 16
   const int r = lane & 15, lg = lane >> 4;
@@ -679,23 +691,22 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
     for (int h = 0; h < 2; ++h) {
       // ---- memory phase
       const bool live = row0 + wm * 128 + h * 64 < row_end;    // (of this half of its rows any: a phase without products is short)
-      if (Q == 0 && h == 0) read_scales(k_first + kt);
+      if (Q == 0 && h == 0) read_scales(first + kt);
       if (live) {
         read_a(stage, h);
         if (h == 0) read_b(stage);
       }
       if (h == 0) {
-        if (kt + 1 < nk) copy_a1(stage ^ 1, a_from - kF8Block);
+        if (kt + 1 < nk) copy_a1(stage ^ 1, a1_from);
       } else {
         // the scales of the next 16 k tiles, where those of the 16 before were (the first two are there from the start)
         if (Q == 2) {
-          const int k = k_first + kt, c = k >> 4;
-          if ((k & 15) == 2 && c > k_first >> 4 && 16 * (c + 1) < k_first + nk) copy_scales(c + 1);
+          const int k = first + kt, c = k >> 4;
+          if ((k & 15) == 2 && c > first >> 4 && 16 * (c + 1) < first + nk) copy_scales(c + 1);
         }
         if (kt + 2 < nk) {
           copy_a0b(stage);
-          a_from += kF8Block;
-          b_from += kF8Block;
+          advance();
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -730,20 +741,18 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
   set_rows();
   auto start = [&] {                                     // into the first stages: k tile 0; and scales
     set_sources();
-    const int c = k_first >> 4;
+    const int c = first >> 4;
     copy_scales(c);
-    if (16 * (c + 1) < k_first + nk) copy_scales(c + 1);
+    if (16 * (c + 1) < first + nk) copy_scales(c + 1);
     copy_a0b(0);
     copy_a1(0, a_from);
-    a_from += kF8Block;
-    b_from += kF8Block;
+    advance();
   };
   start();
   for (;;) {
     if (nk > 1) {                                        // into the second stages, as k tile -1 would have
       copy_a0b(1);
-      a_from += kF8Block;
-      b_from += kF8Block;
+      advance();
       wait_vmcnt<6>();
     } else {
       wait_vmcnt<0>();
@@ -894,15 +903,21 @@ template <MidMode MODE> int launch_mid(const F8Args& g, int tile_rows, hipStream
   return tile_rows == 64 ? launch_mid_tiles<MODE, 64>(g, s) : launch_mid_tiles<MODE, 128>(g, s);
 }
 
+// Of so few rows, which an XCD's L2 keeps, neighbouring columns begin at different places of K, as the middling tiles' do: 301 tokens, 2 of 4 experts of 4096 x
+// 11008, 177 us and 168; 500, 2 of 8 of 4096 x 4096, 133 and 118.  Of more the tiles beside each other would read them from memory again: 16384 tokens of the
+// former 3.41 and 3.58 ms, 8 MB of rows as fast as together.
+constexpr int64_t kApartBytes = 2 << 20;
 template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
   if (int rc = raise_lds<f8_tile_kernel<MODE>>(kTileLds)) return rc;
   const int n_ct = ceil_div(g.N, MODE == kUp ? 128 : 256);
   const int64_t n_rt = g.offsets ? most_tiles(g.R, g.E, kTileRows) : ceil_div(g.R, kTileRows);
   const int64_t tiles = (n_rt * n_ct + kXcds) * g.slices;
+  F8Args h = g;
+  h.apart = (int64_t)(g.perm ? g.R / g.k : g.R) * f8_pitch(g.K) <= kApartBytes;
   // A workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end.  Of less than two
   // rounds each has its own: a few ids name no tile, and their compute units take the ones behind the 256th.
   const int64_t grid = tiles <= 2 * kTileGrid ? tiles : kTileGrid;
-  f8_tile_kernel<MODE><<<(unsigned)grid, kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
+  f8_tile_kernel<MODE><<<(unsigned)grid, kTileWaves * kWave, kTileLds, s>>>(h, n_ct);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }
@@ -1040,7 +1055,7 @@ int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
   // most of their columns empty.  us, turned / not, rows x columns, K:  800 x 8  2048 4.6 7.7, 8192 9.3 8.6;  800 x 64  2048 7.6 8.6, 4096 13 8.5;
   // 3000 x 16  2048 4.9 8.3, 4096 7.2 8.8, 8192 12 12;  16384 x 16  520 5.7 5.6, 4096 15 18, 8192 31 35 (fp32 40 55);  16384 x 64  2048 15 11, 8192 46 36
   if (m.M > 64 && (m.M < 4096 ? m.N <= 64 && (int64_t)m.K * (m.N + 16) <= 180000 : m.N <= 16)) {
-    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true, false};
+    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true, false, false};
     return bf16 ? launch_few<bf16_t>(t, m.N <= 32 ? 32 : 64, s) : launch_few<float>(t, m.N <= 32 ? 32 : 64, s);
   }
   Path path = out_path(m.M, 1, m.N, m.K, !bf16);

@@ -456,7 +456,9 @@ MATMULS = [(1, 8, 1), (1, 64, 128), (3, 40, 130), (16, 72, 256), (17, 128, 384),
            (301, 8, 2048), (1001, 40, 500), (3001, 64, 1024), (5003, 16, 8192), (16411, 16, 300), (9001, 256, 2304), (4100, 72, 2600), (20003, 136, 384),
            (6007, 512, 1300),
            # few workgroups of few rows; fp32 results over long sums
-           (250, 1000, 2048), (1500, 136, 700), (200, 2080, 8300)]
+           (250, 1000, 2048), (1500, 136, 700), (200, 2080, 8300),
+           # whole 16 blocks of K, where workgroups begin at different ones: tiles of 64, 128 and 256 rows
+           (1000, 4000, 4090), (1100, 4104, 2040), (500, 16600, 4096)]
 
 
 @gpu
@@ -643,7 +645,9 @@ def parts(xv, W, idx, gates, inv):
 
 
 LAYERS = [(1, 8, 8, 1, 1), (1, 256, 384, 4, 2), (3, 136, 264, 4, 4), (7, 520, 128, 3, 1), (40, 256, 200, 8, 3), (64, 264, 1376, 5, 2), (130, 128, 136, 256, 8),
-          (300, 384, 640, 2, 1), (513, 256, 520, 1, 1), (700, 512, 392, 6, 2), (2000, 128, 256, 3, 2), (900, 768, 904, 3, 2), (1500, 264, 1160, 2, 1), (4100, 136, 128, 256, 4), (600, 256, 8200, 2, 1), (24, 264, 200, 1, 1), (90, 136, 520, 4, 2), (1750, 1032, 2104, 2, 2), (500, 1032, 8200, 2, 2)]
+          (300, 384, 640, 2, 1), (513, 256, 520, 1, 1), (700, 512, 392, 6, 2), (2000, 128, 256, 3, 2), (900, 768, 904, 3, 2), (1500, 264, 1160, 2, 1), (4100, 136, 128, 256, 4), (600, 256, 8200, 2, 1), (24, 264, 200, 1, 1), (90, 136, 520, 4, 2), (1750, 1032, 2104, 2, 2), (500, 1032, 8200, 2, 2),
+          # whole 16 blocks of K, as for products
+          (5, 2048, 200, 4, 2), (90, 2040, 520, 4, 2), (150, 4096, 264, 1, 1), (900, 2048, 1200, 2, 2)]
 
 
 @gpu

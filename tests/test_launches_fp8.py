@@ -79,7 +79,8 @@ PATHS = [
     (257, 1024, 2048, "mid64", "mid64", True), (256, 1024, 2056, "mid64", "mid64", True), (700, 4096, 8300, "mid64", "mid128", False),
     (64, 4096, 11008, "mid64", "mid64", True), (1024, 4096, 4096, "mid64", "mid64", False), (1025, 4096, 4096, "mid128", "mid128", False),
     (2049, 4096, 4096, "tall", "mid128", False), (1376, 4096, 4001, "mid128", "mid128", False), (16384, 11008, 4096, "tall", "mid128", False),
-    (2048, 4096, 11008, "tall", "mid128", True),
+    (2048, 4096, 11008, "tall", "mid128", True), (1000, 4000, 4090, "mid64", "mid64", False), (1100, 4104, 2040, "mid128", "mid128", False),
+    (500, 16600, 4096, "tall", "mid128", False),
     # of few columns and many rows
     (65, 16, 2048, "few16", "few16", False), (4095, 64, 2048, "few16", "few16", False), (4095, 64, 2304, "mid64", "mid64", True),
     (4096, 64, 2048, "few16", "few16", False), (4097, 64, 2048, "mid64", "mid64", True), (5000, 16, 8192, "few16", "few16", False), (16384, 8, 520, "few64", "few16", False),
@@ -157,3 +158,10 @@ def test_limits(record):
         assert rc == want and (rc or all(fits(x) for x in found)) and (not rc or not found)
     (rc, found), = record(layer((1 << 25) - 64, 128, 8, 8, 8))
     assert rc == 0 and all(fits(x) for x in found)
+
+
+def test_layers_of_whole_16_blocks_take_each_kernel(record):
+    """(whose workgroups begin at different places of K there)"""
+    ups = ((5, 2048, 200, 4, 2), UP_FEW), ((90, 2040, 520, 4, 2), MID.format(0, 64)), ((150, 4096, 264, 1, 1), MID.format(0, 128)), ((900, 2048, 1200, 2, 2), TALL.format(0))
+    for (shape, up), (rc, found) in zip(ups, record(*[layer(*s) for s, _ in ups])):
+        assert shape in LAYERS and rc == 0 and name(found[0]) == up, (shape, name(found[0]))
