@@ -46,7 +46,6 @@ struct F8Args {
   int slices; float* sums;              // K ranges of a tile; more than one, or in32: their sums [slice][R][N] go there, and not to out
   bool turned;                          // few rows: these are the result's columns, and it is written [N][R]
   bool in32;
-  bool apart;                           // tall tiles of neighbouring columns begin at different places of K
 };
 
 struct Tile { int e, row0, row_end; };
@@ -539,7 +538,8 @@ constexpr uint32_t kB0 = 2 * kStage, kScale0 = 4 * kStage, kOffsets0 = kScale0 +
 constexpr int kTileLds = kOffsets0 + (kF8MaxExperts + 1) * 4;
 enum TileMode { kUp, kOut };                            // activations in 8 bits; bf16
 
-template <TileMode MODE>
+// APART: tiles of neighbouring columns begin at different places of K (an instance of its own: where it gains nothing it takes 1 %)
+template <TileMode MODE, bool APART>
 __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g, int n_ct) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr bool UP = MODE == kUp;
@@ -576,7 +576,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
           row0 = t.row0;
           row_end = t.row_end;
           col0 = tn * COLS;
-          first = k_first + (g.apart && slices == 1 && nk % 16 == 0 ? 4 * tn % nk : 0);
+          first = k_first + (APART ? 4 * tn % nk : 0);      // (whole 16 blocks, not cut)
           return true;
         }
       return false;
@@ -633,14 +633,17 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
     copy64(b_from, b_off, to_b + stage * kStage);
   };
   auto advance = [&] {
-    a1_from = a_from;
-    const int64_t to = --left == 0 ? (int64_t)(1 - nk) * kF8Block : (int64_t)kF8Block;
+    int64_t to = kF8Block;
+    if constexpr (APART) {
+      a1_from = a_from;
+      if (--left == 0) to = (int64_t)(1 - nk) * kF8Block;
+    }
     a_from += to;
     b_from += to;
   };
   auto copy_a1 = [&](int stage, uint64_t from) { copy32(from, a_off[2], a_off[3], to_a + stage * kStage + 64 * 128); };
   auto copy_scales = [&](int c) {                        // of k tiles 16 c ..
-    copy16(s_from + (uint64_t)(16 * c < k_first + nk ? c : c - nk / 16) * 16, s_off, to_s + (c & 1) * kScaleStage);
+    copy16(s_from + (uint64_t)(!APART || 16 * c < k_first + nk ? c : c - nk / 16) * 16, s_off, to_s + (c & 1) * kScaleStage);
   };
 
   // ---- fragments: lane l has row l % 16, chunks 2g and 2g + 1 of lane group g = l / 16
@@ -697,7 +700,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g,
         if (h == 0) read_b(stage);
       }
       if (h == 0) {
-        if (kt + 1 < nk) copy_a1(stage ^ 1, a1_from);
+        if (kt + 1 < nk) copy_a1(stage ^ 1, APART ? a1_from : a_from - kF8Block);
       } else {
         // the scales of the next 16 k tiles, where those of the 16 before were (the first two are there from the start)
         if (Q == 2) {
@@ -907,19 +910,21 @@ template <MidMode MODE> int launch_mid(const F8Args& g, int tile_rows, hipStream
 // 11008, 177 us and 168; 500, 2 of 8 of 4096 x 4096, 133 and 118.  Of more the tiles beside each other would read them from memory again: 16384 tokens of the
 // former 3.41 and 3.58 ms, 8 MB of rows as fast as together.
 constexpr int64_t kApartBytes = 2 << 20;
-template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
-  if (int rc = raise_lds<f8_tile_kernel<MODE>>(kTileLds)) return rc;
+template <TileMode MODE, bool APART> int launch_tiles_as(const F8Args& g, hipStream_t s) {
+  if (int rc = raise_lds<f8_tile_kernel<MODE, APART>>(kTileLds)) return rc;
   const int n_ct = ceil_div(g.N, MODE == kUp ? 128 : 256);
   const int64_t n_rt = g.offsets ? most_tiles(g.R, g.E, kTileRows) : ceil_div(g.R, kTileRows);
   const int64_t tiles = (n_rt * n_ct + kXcds) * g.slices;
-  F8Args h = g;
-  h.apart = (int64_t)(g.perm ? g.R / g.k : g.R) * f8_pitch(g.K) <= kApartBytes;
   // A workgroup for every compute unit, which takes every 256th tile: what begins its next one runs beside the last one's end.  Of less than two
   // rounds each has its own: a few ids name no tile, and their compute units take the ones behind the 256th.
   const int64_t grid = tiles <= 2 * kTileGrid ? tiles : kTileGrid;
-  f8_tile_kernel<MODE><<<(unsigned)grid, kTileWaves * kWave, kTileLds, s>>>(h, n_ct);
+  f8_tile_kernel<MODE, APART><<<(unsigned)grid, kTileWaves * kWave, kTileLds, s>>>(g, n_ct);
   BTX_LAUNCH_CHECK();
   return BTX_OK;
+}
+template <TileMode MODE> int launch_tiles(const F8Args& g, hipStream_t s) {
+  const bool apart = (int64_t)(g.perm ? g.R / g.k : g.R) * f8_pitch(g.K) <= kApartBytes && g.slices == 1 && f8_pitch(g.K) % (16 * kF8Block) == 0;
+  return apart ? launch_tiles_as<MODE, true>(g, s) : launch_tiles_as<MODE, false>(g, s);
 }
 
 // K ranges of the tiles: as many as fill the chip (`places` workgroups at once) where the tiles alone do not, of `shortest` k tiles or more each; no more
@@ -1036,8 +1041,10 @@ template <bool F32> int launch_out(F8Args& g, Path path, int most_slices, hipStr
 }  // namespace
 
 int f8_prepare() {
-  if (int rc = raise_lds<f8_tile_kernel<kUp>>(kTileLds)) return rc;
-  if (int rc = raise_lds<f8_tile_kernel<kOut>>(kTileLds)) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<kUp, false>>(kTileLds)) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<kUp, true>>(kTileLds)) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<kOut, false>>(kTileLds)) return rc;
+  if (int rc = raise_lds<f8_tile_kernel<kOut, true>>(kTileLds)) return rc;
   if (int rc = raise_lds<f8_mid_kernel<kMidUp, 64>>(Mid<64>::lds)) return rc;
   if (int rc = raise_lds<f8_mid_kernel<kMidUp, 128>>(Mid<128>::lds)) return rc;
   if (int rc = raise_lds<f8_mid_kernel<kMidOut, 64>>(Mid<64>::lds)) return rc;
@@ -1055,7 +1062,7 @@ int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
   // most of their columns empty.  us, turned / not, rows x columns, K:  800 x 8  2048 4.6 7.7, 8192 9.3 8.6;  800 x 64  2048 7.6 8.6, 4096 13 8.5;
   // 3000 x 16  2048 4.9 8.3, 4096 7.2 8.8, 8192 12 12;  16384 x 16  520 5.7 5.6, 4096 15 18, 8192 31 35 (fp32 40 55);  16384 x 64  2048 15 11, 8192 46 36
   if (m.M > 64 && (m.M < 4096 ? m.N <= 64 && (int64_t)m.K * (m.N + 16) <= 180000 : m.N <= 16)) {
-    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true, false, false};
+    const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true, false};
     return bf16 ? launch_few<bf16_t>(t, m.N <= 32 ? 32 : 64, s) : launch_few<float>(t, m.N <= 32 ? 32 : 64, s);
   }
   Path path = out_path(m.M, 1, m.N, m.K, !bf16);

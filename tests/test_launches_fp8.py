@@ -12,7 +12,7 @@ from test_fp8 import LAYERS, MATMULS
 
 MAX_THREADS = (1 << 32) - 1     # of one launch and direction of the grid
 UP_FEW, FEW16, FEW64 = "f8_few_kernel<true, 2, 2, 2, float>", "f8_few_kernel<false, {}, 1, 4, {}>", "f8_few_kernel<false, {}, 4, 2, {}>"
-MID, TALL = "f8_mid_kernel<(MidMode){}, {}>", "f8_tile_kernel<(TileMode){}>"
+MID, TALL = "f8_mid_kernel<(MidMode){}, {}>", "f8_tile_kernel<(TileMode){}, {}>"
 
 
 @pytest.fixture(scope="module")
@@ -107,7 +107,7 @@ def test_products(record, M, N, K, bf16, f32, cut):
 def all_kernels():
     ot = ("float", "unsigned short")
     few = {FEW16.format(rb, t) for rb in (2, 4) for t in ot} | {FEW64.format(rb, ot[1]) for rb in (2, 4)} | {UP_FEW}
-    return few | {MID.format(m, bm) for m in range(3) for bm in (64, 128)} | {TALL.format(m) for m in range(2)}
+    return few | {MID.format(m, bm) for m in range(3) for bm in (64, 128)} | {TALL.format(m, a) for m in range(2) for a in ("false", "true")}
 
 
 def test_the_shapes_of_the_parity_tests_reach_every_kernel(record):
@@ -120,7 +120,7 @@ def test_the_shapes_of_the_parity_tests_reach_every_kernel(record):
         if any(n.startswith("f8_add") for n in names) or any(n.startswith("combine_kernel") and n.endswith("false, true>") for n in names):
             cut |= {n for n in names if "mid" in n or "tile" in n}
     assert all_kernels() <= reached, all_kernels() - reached
-    assert cut >= {MID.format(1, 64), MID.format(2, 64), TALL.format(1)}, cut
+    assert cut >= {MID.format(1, 64), MID.format(2, 64), TALL.format(1, "false")}, cut
 
 
 def test_any_sizes_fit_their_launches_and_workspaces(record):
@@ -162,6 +162,6 @@ def test_limits(record):
 
 def test_layers_of_whole_16_blocks_take_each_kernel(record):
     """(whose workgroups begin at different places of K there)"""
-    ups = ((5, 2048, 200, 4, 2), UP_FEW), ((90, 2040, 520, 4, 2), MID.format(0, 64)), ((150, 4096, 264, 1, 1), MID.format(0, 128)), ((900, 2048, 1200, 2, 2), TALL.format(0))
+    ups = ((5, 2048, 200, 4, 2), UP_FEW), ((90, 2040, 520, 4, 2), MID.format(0, 64)), ((150, 4096, 264, 1, 1), MID.format(0, 128)), ((900, 2048, 1200, 2, 2), TALL.format(0, "true"))
     for (shape, up), (rc, found) in zip(ups, record(*[layer(*s) for s, _ in ups])):
         assert shape in LAYERS and rc == 0 and name(found[0]) == up, (shape, name(found[0]))
