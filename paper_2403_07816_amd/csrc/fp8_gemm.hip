@@ -907,7 +907,7 @@ template <MidMode MODE> int launch_mid(const F8Args& g, int tile_rows, hipStream
 }
 
 // Of so few rows, which an XCD's L2 keeps, neighbouring columns begin at different places of K, as the middling tiles' do: 301 tokens, 2 of 4 experts of 4096 x
-// 11008, 177 us and 168; 500, 2 of 8 of 4096 x 4096, 133 and 118.  Of more the tiles beside each other would read them from memory again: 16384 tokens of the
+// 11008, 172 us and 166; 500, 2 of 8 of 4096 x 4096, 133 and 118.  Of more the tiles beside each other would read them from memory again: 16384 tokens of the
 // former 3.41 and 3.58 ms, 8 MB of rows as fast as together.
 constexpr int64_t kApartBytes = 2 << 20;
 template <TileMode MODE, bool APART> int launch_tiles_as(const F8Args& g, hipStream_t s) {
