@@ -483,7 +483,7 @@ int btx_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, i
  * btx_moe_ff_forward_mx4 - the layer of 4-bit experts, for serving (forward only): btx_moe_ff_forward with both
  * operands of every product in microscaled 4-bit floats.  Token rows are quantised along d once each; per expert
  *     act = silu(xq W1_e) * (xq W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
- *     (but for up to 2^22 values and for sums that are cut into ranges, which stay in fp32; not with more than 8 experts a token, 4 of many tokens)
+ *     (but for sums that are cut into ranges, which stay in fp32)
  *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
  *   x [T,d] bf16;  residual [T,d] bf16, may be NULL;  out [T,d] bf16; aliasing as in btx_moe_ff_forward
  *   W1, W3: codes [E,f,d/2] and scales [E,f,btx_mx4_scale_pitch(d)];  W2: [E,d,f/2] and [E,d,btx_mx4_scale_pitch(f)], as
@@ -569,7 +569,9 @@ int btx_fp8_matmul(const uint8_t* A_codes, const uint8_t* A_scales, const uint8_
  * btx_moe_ff_forward_fp8 - the layer of 8-bit experts, for serving (forward only): btx_moe_ff_forward with both operands of every product in block-scaled
  * 8-bit floats.  Per expert
  *     act = silu(x W1_e) * (x W3_e)   (fp32 sums), quantised along f from its fp32 values;   y = actq W2_e, rounded to bf16
- *     (but for sums that are cut into ranges, which stay in fp32)
+ *     (but for up to 2^22 values, T*k*d of them, and for sums that are cut into ranges, which stay in fp32; with more than 8 experts a token, of 8192 tokens
+ *     and more with more than 4, all are rounded)
+ *     out[t] = residual[t] + sum_j gates[t,j] * y            as in btx_moe_ff_forward
  * Products as btx_fp8_matmul's: for act as its fp32 results' up to 64 rows an expert on average and in small layers, else as its bf16 ones', with which one
  * code in a few thousand is the neighbour of the one that exact sums have (out 2.1e-3 of its norm from the formula instead of 1.7e-3); for y as its bf16 ones'.
  *   x         codes [T,btx_fp8_code_pitch(d)] and scales [T,btx_fp8_scale_pitch(d)], as btx_rmsnorm_fp8 or btx_fp8_quantize (axis 1) writes them
