@@ -50,13 +50,13 @@ __device__ __forceinline__ void round_sum(const bf16_t*, float* v) {
   }
 }
 
-// TPR: threads that share a row, a wavefront or the workgroup; MAXC: pieces of 8 columns that each has.  (sum may be h or residual, whose
-// elements a thread has read by then: no __restrict__.)
+// TPR: threads that share a row, a wavefront (up to 512 columns) or the workgroup; MAXC: pieces of 8 columns that each has.  (sum may be h or
+// residual, whose elements a thread has read by then; those of another that it reads behind the row's end are dropped: no __restrict__.)
 template <typename XT, int TPR, int MAXC>
 __global__ __launch_bounds__(kThreads) void f8_norm_kernel(const XT* h, const XT* residual, const float* __restrict__ gain, float eps, int T, int d,
                                                            XT* sum, XT* __restrict__ xn, float* __restrict__ rstd, u32x2* __restrict__ codes,
                                                            uint8_t* __restrict__ scales) {
-  static_assert(TPR == kWave || TPR == kThreads, "a wavefront or the workgroup");
+  static_assert((TPR == kWave && MAXC == 1) || TPR == kThreads, "a wavefront or the workgroup");
   __shared__ double s_part[kThreads / kWave];
   const int lane = threadIdx.x & (kWave - 1), tid = TPR == kWave ? lane : threadIdx.x;
   const int64_t t = TPR == kWave ? (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave : blockIdx.x;
@@ -147,15 +147,12 @@ template <typename XT> int launch_typed(const F8NormArgs& a, hipStream_t s) {
           at(static_cast<XT*>(a.xn), a.d), a.rstd + t0, reinterpret_cast<u32x2*>(at(a.codes, f8_pitch(a.d))), at(a.scales, f8_scale_pitch(a.d)));
     }
   };
-  auto by_columns = [&](auto tpr) {
-    const int per = decltype(tpr)::value * 8;
-    if (a.d <= per) run(tpr, std::integral_constant<int, 1>{});
-    else if (a.d <= 2 * per) run(tpr, std::integral_constant<int, 2>{});
-    else if (a.d <= 4 * per) run(tpr, std::integral_constant<int, 4>{});
-    else run(tpr, std::integral_constant<int, 8>{});
-  };
-  if (a.d <= 512) by_columns(std::integral_constant<int, kWave>{});
-  else by_columns(std::integral_constant<int, kThreads>{});
+  const std::integral_constant<int, kThreads> block;
+  if (a.d <= kWave * 8) run(std::integral_constant<int, kWave>{}, std::integral_constant<int, 1>{});
+  else if (a.d <= kThreads * 8) run(block, std::integral_constant<int, 1>{});
+  else if (a.d <= 2 * kThreads * 8) run(block, std::integral_constant<int, 2>{});
+  else if (a.d <= 4 * kThreads * 8) run(block, std::integral_constant<int, 4>{});
+  else run(block, std::integral_constant<int, 8>{});
   BTX_LAUNCH_CHECK();
   return BTX_OK;
 }

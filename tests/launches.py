@@ -50,6 +50,12 @@ int hipFuncSetAttribute(const void*, int, int) { return 0; }
 int hipGetLastError() { return 0; }
 int hipEventRecord(void*, void*) { return 0; }
 int hipGetSymbolAddress(void** p, const void*) { *p = reinterpret_cast<void*>(0x1000); return 0; }
+const char* registered() {
+  static std::string out;
+  out.clear();
+  for (const auto& n : names) out += n.second + "\n";
+  return out.c_str();
+}
 const char* taken() { static std::string out; out.swap(log_text); log_text.clear(); return out.c_str(); }
 }
 """
@@ -73,6 +79,15 @@ print(json.dumps(out))
 """
 
 
+COMPILED = r"""
+import ctypes, sys
+log = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+log.registered.restype = ctypes.c_char_p
+lib = ctypes.CDLL(sys.argv[2])
+print(log.registered().decode(), end="")
+"""
+
+
 @dataclass(frozen=True)
 class Launch:
     kernel: str                # demangled name with its template arguments, without namespaces and parameters
@@ -93,12 +108,24 @@ def _short(name):
     return name
 
 
-def _recorded(calls, tmp_path):
+def _stand_in(tmp_path):
     source, stand_in = os.path.join(tmp_path, "stand_in.cpp"), os.path.join(tmp_path, "stand_in.so")
     if not os.path.exists(stand_in):
         with open(source, "w") as f:
             f.write(STAND_IN)
         subprocess.run(["g++", "-O1", "-shared", "-fPIC", source, "-o", stand_in], check=True)
+    return stand_in
+
+
+def compiled(tmp_path):
+    """The names, as Launch.kernel has them, of all kernels in the library."""
+    r = subprocess.run([sys.executable, "-c", COMPILED, _stand_in(tmp_path), B.LIB_PATH], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
+    return {_short(line) for line in r.stdout.splitlines()}
+
+
+def _recorded(calls, tmp_path):
+    stand_in = _stand_in(tmp_path)
     r = subprocess.run([sys.executable, "-c", CHILD, stand_in, B.LIB_PATH], input=json.dumps(calls), capture_output=True, text=True,
                        timeout=120)
     assert r.returncode == 0, r.stderr

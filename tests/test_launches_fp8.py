@@ -7,7 +7,7 @@ import pytest
 
 from paper_2403_07816_amd import binding as B
 
-from launches import P, PLENTY, launches
+from launches import P, PLENTY, compiled, launches
 from test_fp8 import LAYERS, MATMULS
 
 MAX_THREADS = (1 << 32) - 1     # of one launch and direction of the grid
@@ -165,3 +165,17 @@ def test_layers_of_whole_16_blocks_take_each_kernel(record):
     ups = ((5, 2048, 200, 4, 2), UP_FEW), ((90, 2040, 520, 4, 2), MID.format(0, 64)), ((150, 4096, 264, 1, 1), MID.format(0, 128)), ((900, 2048, 1200, 2, 2), TALL.format(0, "true"))
     for (shape, up), (rc, found) in zip(ups, record(*[layer(*s) for s, _ in ups])):
         assert shape in LAYERS and rc == 0 and name(found[0]) == up, (shape, name(found[0]))
+
+
+def norm(T, d, dtype):
+    return ("btx_rmsnorm_fp8", [P, P, dtype, P, 1e-5, T, d, P, 2 * P, P, P, P, 0])
+
+
+def test_every_kernel_that_is_compiled_can_be_launched(record, tmp_path):
+    types = (B.BTX_F32, B.BTX_BF16)
+    calls = [matmul(*c, dtype) for c in MATMULS for dtype in types] + [layer(*c) for c in LAYERS]
+    calls += [tensor(fn, 2, 301, cols, axis, dtype, br) for fn in "qd" for cols in (129, 264) for axis in (0, 1) for dtype in types for br in (1, 128)]
+    calls += [norm(3, d, dtype) for d in range(8, 16385, 8) for dtype in types]
+    reached = {name(x) for rc, found in record(*calls) for x in found}
+    have = {k for k in compiled(str(tmp_path)) if k.startswith("f8_")}
+    assert len(have) > 20 and have <= reached, sorted(have - reached)
