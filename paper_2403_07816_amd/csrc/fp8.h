@@ -8,8 +8,8 @@ namespace btx {
 
 constexpr int kF8Block = 128;
 constexpr int kF8MaxExperts = 256;
-constexpr int kF8MostRows = (1 << 28) - 256;          // T k, M: grids of every tile's height
-constexpr int kF8MostColumns = 65535 * 32;            // N, d, f and K: rows of the grid of few rows, and 32-bit offsets in a row tile
+constexpr int kF8MostRows = (1 << 28) - 256;          // T k, M: the grid of a product of few columns
+constexpr int kF8MostColumns = 65535 * 32;            // N, d, f and K: 32-bit offsets in a tile of 256 rows
 inline __host__ __device__ int64_t f8_pitch(int64_t K) { return (K + kF8Block - 1) / kF8Block * kF8Block; }
 // whole 16-byte pieces, which the products copy
 inline __host__ __device__ int64_t f8_scale_pitch(int64_t K) { return ((K + kF8Block - 1) / kF8Block + 15) / 16 * 16; }

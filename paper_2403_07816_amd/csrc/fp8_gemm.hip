@@ -290,8 +290,8 @@ template <typename OT> int launch_few(const F8Args& g, int tile_rows, hipStream_
 // 64 tokens, 32 of 4096 x 1376: 85, 86, 90)
 int launch_few_up(const F8Args& g, hipStream_t s) { return launch_few_shape<true, 2, 2, float>(g, 32, s); }
 
-// (tiles of 32 rows only where there are fewer than 25 an expert)
-static_assert(kF8MostColumns / 32 <= 65535 && (kF8MostRows / 64 + kF8MaxExperts + 0ll) * 8 * kWave < 1ll << 32, "the grid");
+// (of a turned product 16 rows are a workgroup's)
+static_assert((kF8MostRows / 16 + 0ll) * 4 * kWave < 1ll << 32, "a launch has fewer than 2^32 threads");
 
 // ---- a middling number of rows: BM x 128 tiles, BM 64 or 128 -----------------------------------------------------
 // Bound by reading B where rows are few, by LDS where they are many.  A k tile is a block: [row][128 bytes] of either operand, in a ring of NS stages that

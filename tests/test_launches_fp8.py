@@ -179,3 +179,9 @@ def test_every_kernel_that_is_compiled_can_be_launched(record, tmp_path):
     reached = {name(x) for rc, found in record(*calls) for x in found}
     have = {k for k in compiled(str(tmp_path)) if k.startswith("f8_")}
     assert len(have) > 20 and have <= reached, sorted(have - reached)
+
+
+def test_the_largest_turned_product(record):
+    """A workgroup of 256 threads for 16 rows, with fp32 results: the largest launch of all."""
+    (rc, found), = record(matmul((1 << 28) - 257, 8, 64, B.BTX_F32))
+    assert rc == 0 and name(found[0]) == FEW16.format(2, "float") and fits(found[0]) and found[0].grid[0] * found[0].block[0] == (1 << 32) - 4096
