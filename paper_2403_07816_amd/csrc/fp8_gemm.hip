@@ -893,10 +893,11 @@ template <auto KERNEL> int raise_lds(int bytes) {
   return BTX_OK;
 }
 
+int64_t mid_grid(int n_ct, int64_t n_rt) { return ceil_div((int64_t)n_ct, kXcds) * kXcds * n_rt; }
 template <MidMode MODE, int BM> int launch_mid_tiles(const F8Args& g, hipStream_t s) {
   if (int rc = raise_lds<f8_mid_kernel<MODE, BM>>(Mid<BM>::lds)) return rc;
   const int n_ct = ceil_div(g.N, MODE == kMidUp ? 64 : kMidCols);
-  const int64_t n_rt = g.offsets ? most_tiles(g.R, g.E, BM) : ceil_div(g.R, BM), grid = ceil_div((int64_t)n_ct * g.slices, kXcds) * kXcds * n_rt;
+  const int64_t grid = mid_grid(n_ct * g.slices, g.offsets ? most_tiles(g.R, g.E, BM) : ceil_div(g.R, BM));
   if (!grid_fits(grid, kMidWaves * kWave)) return BTX_ERR_UNSUPPORTED;
   f8_mid_kernel<MODE, BM><<<(unsigned)grid, kMidWaves * kWave, Mid<BM>::lds, s>>>(g, n_ct);
   BTX_LAUNCH_CHECK();
@@ -986,7 +987,8 @@ constexpr int kUpFewRows = 3, kUpMidRows = 64, kUpMidTiles = kTileGrid;
 Path up_path(int64_t R, int E, int f) {
   const Rows n(R, E);
   if (n.each <= kUpFewRows) return kFew32;
-  if (n.each <= kUpMidRows) return kMid64;
+  // (64 rows of 256 experts of 2 million columns are more workgroups than a launch has)
+  if (n.each <= kUpMidRows && grid_fits(mid_grid(ceil_div(f, 64), most_tiles((int)R, E, 64)), kMidWaves * kWave)) return kMid64;
   return n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
 }
 // Other products.  Of one matrix (sums of tiles that are cut along K are added by another launch), columns x K, rows, us:

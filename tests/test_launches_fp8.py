@@ -185,3 +185,10 @@ def test_the_largest_turned_product(record):
     """A workgroup of 256 threads for 16 rows, with fp32 results: the largest launch of all."""
     (rc, found), = record(matmul((1 << 28) - 257, 8, 64, B.BTX_F32))
     assert rc == 0 and name(found[0]) == FEW16.format(2, "float") and fits(found[0]) and found[0].grid[0] * found[0].block[0] == (1 << 32) - 4096
+
+
+def test_layers_of_the_most_columns_and_experts(record):
+    """64 rows of each in tiles of 64 rows and 64 columns would be 2^24 workgroups of 256 threads, which no launch has."""
+    for T, tall in ((2047, False), (2048, True)):
+        (rc, found), = record(layer(T, 8, 2097120, 256, 8))
+        assert rc == 0 and name(found[0]).startswith("f8_tile_kernel") == tall and all(fits(x) for x in found), T
