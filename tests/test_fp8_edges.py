@@ -1,10 +1,12 @@
 """Block-scaled 8-bit floats where the kernels of many rows, the matrix cores' own 8-bit product and sums that are cut along K can go wrong."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import fp8 as O
 from paper_2403_07816_amd import binding as B
 
-from test_fp8 import BF, DEV, make_layer, rng_of
+from test_fp8 import BF, DEV, F32, check_product, make_layer, rng_of
 from test_mx4 import experts, routing_of
 
 gpu = pytest.mark.gpu
@@ -39,3 +41,76 @@ def test_outputs_of_4_bit_experts_that_are_not_cut_are_rounded(T, d, f, E, k):
     r.gates.zero_()
     r.gates[:, 0] = 1.0
     assert not rest_of(lambda res: B.btx_moe_ff_forward_mx4(x, W1, W3, W2, r, residual=res)).any()
+
+
+# ---- products --------------------------------------------------------------------------------------------------
+
+# rows, columns, depth; the kernels of bf16 and of fp32 results (test_launches_fp8.py holds them to it)
+EDGE_PRODUCTS = [(5, 136, 700, "few16", "few16"), (40, 136, 700, "few16", "few16"), (5, 33000, 136, "few64", "few16"), (30, 33000, 300, "few64", "few16"), (300, 136, 2304, "mid64", "mid64"), (1100, 4104, 264, "mid128", "mid128"),
+                 (700, 2080, 8300, "mid64", "mid128"), (16500, 2048, 130, "tall", "mid128"), (500, 16600, 2040, "tall apart", "mid128"), (3001, 64, 1024, "few16", "few16")]
+SHAPES = [s[:3] for s in EDGE_PRODUCTS]
+
+
+def on_device(rows, K, seed, block_rows=1):
+    """(operand, the values that it stands for)"""
+    g = torch.Generator(device=DEV).manual_seed(1000 * seed + rows + K)
+    v = torch.randn((rows, K), generator=g, device=DEV) * torch.exp(0.5 * torch.randn((rows, 1), generator=g, device=DEV))
+    q = B.btx_fp8_quantize(v, block_rows=block_rows)
+    return q, B.btx_fp8_dequantize(q, F32).double().cpu().numpy()
+
+
+def some_rows(M):
+    return np.arange(M) if M <= 400 else np.unique(np.concatenate([np.arange(20), np.arange(M - 20, M), rng_of("rows", M).integers(0, M, 100)]))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_nan_stays_with_its_row_and_column(M, N, K, dtype):
+    """Scales that are NaN, over codes and over the zeros that a block with a NaN is quantised to, and the code that is NaN."""
+    (a, av), (b, bv) = on_device(M, K, 1), on_device(N, K, 2, 128)
+    last = (K - 1) // 128
+    rows, columns = [2, 3, 4, M - 1], [0, 33, 50, N - 1]
+    for q, at in ((a, rows), (b, columns)):
+        q.scales[at[0], 0] = 255
+        q.scales[at[1], last] = 255
+        q.codes[at[1], 128 * last:128 * last + 128] = 0
+        q.codes[at[2], K - 1] = 127
+        q.codes[at[3], 1] = 255
+    out = B.btx_fp8_matmul(a, b, dtype=dtype).cpu()
+    nan = torch.zeros((M, N), dtype=torch.bool)
+    nan[rows] = True
+    nan[:, columns] = True
+    assert torch.equal(torch.isnan(out), nan)
+    keep, kept = np.setdiff1d(some_rows(M), rows), np.setdiff1d(np.arange(N), columns)
+    check_product(out[keep][:, kept], av[keep], bv[kept])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_scales_from_the_smallest(M, N, K, dtype):
+    """Every code under scales from 2^-127 on, which no other test has in front of the matrix cores' own 8-bit product; none of a result that leaves fp32."""
+    g = torch.Generator(device=DEV).manual_seed(M + N + K)
+
+    def made(rows, lo, hi):
+        q = B.alloc_fp8((rows, K), -1, DEV)
+        q.codes.copy_(torch.randint(0, 127, q.codes.shape, generator=g, device=DEV) + 128 * torch.randint(0, 2, q.codes.shape, generator=g, device=DEV))
+        q.codes[:, K:] = 0
+        q.scales.zero_()
+        n = (K + 127) // 128
+        q.scales[:, :n] = torch.randint(lo, hi, (rows, n), generator=g, device=DEV).to(torch.uint8)
+        q.scales[:4, :n] = torch.tensor([[lo], [lo], [hi - 1], [lo + 1]], dtype=torch.uint8, device=DEV)
+        return q
+
+    a, b = made(M, 0, 60), made(N, 120, 200)
+    rows = some_rows(M)
+    av = O.values(a.codes[rows, :K].cpu().numpy().astype(np.int64), a.scales[rows].cpu().numpy().astype(np.int64))
+    bv = O.values(b.codes[:, :K].cpu().numpy().astype(np.int64), b.scales.cpu().numpy().astype(np.int64))
+    want, err = av @ bv.T, O.sums_error(av, bv, exact=dtype == F32)
+    # Below 2^-126 values are 2^-149 apart in fp32 and 2^-133 in bf16: sums of K products, results, and, in front of fp32 results, the values of a.
+    err = err + K * 2.0 ** -149 + (2.0 ** -134 * np.abs(bv).sum(1) if dtype == F32 else 0)
+    bound = err + torch.finfo(dtype).eps / 2 * (np.abs(want) + err) + (0 if dtype == F32 else 2.0 ** -134)
+    off = np.abs(B.btx_fp8_matmul(a, b, dtype=dtype)[rows].double().cpu().numpy() - want)
+    assert np.all(off <= bound), float((off / bound).max())
+    assert (np.abs(want) > 2 * bound).mean() > 0.9

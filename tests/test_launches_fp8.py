@@ -9,6 +9,7 @@ from paper_2403_07816_amd import binding as B
 
 from launches import P, PLENTY, compiled, launches
 from test_fp8 import LAYERS, MATMULS
+from test_fp8_edges import EDGE_PRODUCTS
 
 MAX_THREADS = (1 << 32) - 1     # of one launch and direction of the grid
 UP_FEW, FEW16, FEW64 = "f8_few_kernel<true, 2, 2, 2, float>", "f8_few_kernel<false, {}, 1, 4, {}>", "f8_few_kernel<false, {}, 4, 2, {}>"
@@ -192,3 +193,14 @@ def test_layers_of_the_most_columns_and_experts(record):
     for T, tall in ((2047, False), (2048, True)):
         (rc, found), = record(layer(T, 8, 2097120, 256, 8))
         assert rc == 0 and name(found[0]).startswith("f8_tile_kernel") == tall and all(fits(x) for x in found), T
+
+
+def test_the_shapes_of_the_edge_tests_reach_the_kernels_that_they_are_for(record):
+    seen = set()
+    for M, N, K, *kinds in EDGE_PRODUCTS:
+        for dtype, want in zip((B.BTX_BF16, B.BTX_F32), kinds):
+            (rc, found), = record(matmul(M, N, K, dtype))
+            got = kind(found[0]) + (" apart" if name(found[0]) == TALL.format(1, "true") else "")
+            assert rc == 0 and got == want, (M, N, K, dtype, got)
+            seen.add(name(found[0]))
+    assert all_kernels() - seen == {UP_FEW, MID.format(0, 64), MID.format(0, 128), TALL.format(0, "false"), TALL.format(0, "true")}
