@@ -114,3 +114,26 @@ def test_scales_from_the_smallest(M, N, K, dtype):
     off = np.abs(B.btx_fp8_matmul(a, b, dtype=dtype)[rows].double().cpu().numpy() - want)
     assert np.all(off <= bound), float((off / bound).max())
     assert (np.abs(want) > 2 * bound).mean() > 0.9
+
+
+# cut along K, and the kernel that does: bf16 results, fp32 results
+CUT_PRODUCTS = [(33, 2048, 11008, "mid64", "mid64"), (513, 264, 18000, "mid64", "mid64"), (200, 2080, 8300, "mid64", "mid128"), (2048, 4096, 8300, "tall", None),
+                (16, 512, 8192, "mid64", "mid64"), (301, 1032, 2177, "mid64", "mid64")]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N,K", [s[:3] for s in CUT_PRODUCTS])
+def test_sums_that_are_cut_lose_nothing(M, N, K, dtype):
+    """Whole numbers whose sums stay below 2^24: exact in fp32 in whatever order (and their products, 1 to 64, to the matrix cores' 8-bit product too); a bf16
+    result is that, rounded once."""
+    g = torch.Generator(device=DEV).manual_seed(M + N + K)
+    whole = lambda rows: torch.randint(-8, 9, (rows, K), generator=g, device=DEV).float()  # noqa: E731
+    av, bv = whole(M), whole(N)
+    a, b = B.btx_fp8_quantize(av), B.btx_fp8_quantize(bv)
+    assert torch.equal(B.btx_fp8_dequantize(a, F32), av) and torch.equal(B.btx_fp8_dequantize(b, F32), bv)
+    residual = torch.randint(-64, 65, (M, N), generator=g, device=DEV).to(dtype)
+    rows = torch.from_numpy(some_rows(M)).to(DEV)
+    want = av[rows].double() @ bv.double().T
+    assert torch.equal(B.btx_fp8_matmul(a, b, dtype=dtype)[rows], want.float().to(dtype))
+    assert torch.equal(B.btx_fp8_matmul(a, b, dtype=dtype, residual=residual)[rows], (want + residual[rows].double()).float().to(dtype))

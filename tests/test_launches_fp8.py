@@ -9,7 +9,7 @@ from paper_2403_07816_amd import binding as B
 
 from launches import P, PLENTY, compiled, launches
 from test_fp8 import LAYERS, MATMULS
-from test_fp8_edges import EDGE_PRODUCTS
+from test_fp8_edges import CUT_PRODUCTS, EDGE_PRODUCTS
 
 MAX_THREADS = (1 << 32) - 1     # of one launch and direction of the grid
 UP_FEW, FEW16, FEW64 = "f8_few_kernel<true, 2, 2, 2, float>", "f8_few_kernel<false, {}, 1, 4, {}>", "f8_few_kernel<false, {}, 4, 2, {}>"
@@ -204,3 +204,8 @@ def test_the_shapes_of_the_edge_tests_reach_the_kernels_that_they_are_for(record
             assert rc == 0 and got == want, (M, N, K, dtype, got)
             seen.add(name(found[0]))
     assert all_kernels() - seen == {UP_FEW, MID.format(0, 64), MID.format(0, 128), TALL.format(0, "false"), TALL.format(0, "true")}
+    for M, N, K, *kinds in CUT_PRODUCTS:
+        for dtype, want in zip((B.BTX_BF16, B.BTX_F32), kinds):
+            (rc, found), = record(matmul(M, N, K, dtype))
+            if want:
+                assert rc == 0 and kind(found[0]) == want and len(found) == 2 and name(found[1]).startswith("f8_add_slices_kernel"), (M, N, K, dtype, name(found[0]))
