@@ -137,3 +137,28 @@ def test_sums_that_are_cut_lose_nothing(M, N, K, dtype):
     want = av[rows].double() @ bv.double().T
     assert torch.equal(B.btx_fp8_matmul(a, b, dtype=dtype)[rows], want.float().to(dtype))
     assert torch.equal(B.btx_fp8_matmul(a, b, dtype=dtype, residual=residual)[rows], (want + residual[rows].double()).float().to(dtype))
+
+
+@gpu
+@pytest.mark.parametrize("T,d,n", [(190, 264, 136), (2100, 1032, 2056)])
+def test_training_of_a_linear_layer_in_bf16(T, d, n):
+    """y = x W^T and dx = dy W with results in bf16: against the values that the codes stand for, and dx against differences of the loss of exact products."""
+    rng = rng_of("training in bf16", T, d, n)
+    x, W, dY = (torch.tensor(rng.standard_normal(s)).to(BF) for s in ((T, d), (n, d), (T, n)))
+    q = {name: (B.btx_fp8_quantize(v.to(DEV), axis, rows), axis) for name, v, axis, rows in
+         (("x", x, -1, 1), ("W", W, -1, 128), ("Wt", W, -2, 128), ("dY", dY, -1, 1), ("dYt", dY, -2, 1), ("xt", x, -2, 1))}
+    v = {}
+    for name, (t, axis) in q.items():
+        back = B.btx_fp8_dequantize(t, F32, axis).double().cpu().numpy()
+        v[name] = back if axis == -1 else back.T
+    check_product(B.btx_fp8_matmul(q["x"][0], q["W"][0]), v["x"], v["W"])
+    dx = B.btx_fp8_matmul(q["dY"][0], q["Wt"][0])
+    check_product(dx, v["dY"], v["Wt"])
+    check_product(B.btx_fp8_matmul(q["dYt"][0], q["xt"][0], dtype=F32), v["dYt"], v["xt"])
+    step = rng.standard_normal((T, d))
+    x0, W0, dY0 = (t.double().numpy() for t in (x, W, dY))
+    loss = lambda m: float((dY0 * (m @ W0.T)).sum())  # noqa: E731
+    slope = (loss(x0 + 1e-5 * step) - loss(x0 - 1e-5 * step)) / 2e-5
+    got = dx.double().cpu().numpy()
+    # every factor of a product is off by half an e4m3 step, 2^-4 of it at most, at random: two factors
+    assert abs((got * step).sum() - slope) <= 2 * 2.0 ** -4 * np.linalg.norm(got) * np.linalg.norm(step)
