@@ -1,4 +1,6 @@
 """Block-scaled 8-bit floats where the kernels of many rows, the matrix cores' own 8-bit product and sums that are cut along K can go wrong."""
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
@@ -6,7 +8,8 @@ import torch
 from oracle import fp8 as O
 from paper_2403_07816_amd import binding as B
 
-from test_fp8 import BF, DEV, F32, check_product, make_layer, rng_of
+import test_fp8
+from test_fp8 import BF, DEV, F32, check_layer, check_product, make_layer, rng_of
 from test_mx4 import experts, routing_of
 
 gpu = pytest.mark.gpu
@@ -51,10 +54,10 @@ EDGE_PRODUCTS = [(5, 136, 700, "few16", "few16"), (40, 136, 700, "few16", "few16
 SHAPES = [s[:3] for s in EDGE_PRODUCTS]
 
 
-def on_device(rows, K, seed, block_rows=1):
+def on_device(rows, K, seed, block_rows=1, scale=1.0):
     """(operand, the values that it stands for)"""
     g = torch.Generator(device=DEV).manual_seed(1000 * seed + rows + K)
-    v = torch.randn((rows, K), generator=g, device=DEV) * torch.exp(0.5 * torch.randn((rows, 1), generator=g, device=DEV))
+    v = torch.randn((rows, K), generator=g, device=DEV) * torch.exp(0.5 * torch.randn((rows, 1), generator=g, device=DEV)) * scale
     q = B.btx_fp8_quantize(v, block_rows=block_rows)
     return q, B.btx_fp8_dequantize(q, F32).double().cpu().numpy()
 
@@ -162,3 +165,153 @@ def test_training_of_a_linear_layer_in_bf16(T, d, n):
     got = dx.double().cpu().numpy()
     # every factor of a product is off by half an e4m3 step, 2^-4 of it at most, at random: two factors
     assert abs((got * step).sum() - slope) <= 2 * 2.0 ** -4 * np.linalg.norm(got) * np.linalg.norm(step)
+
+
+# ---- the layer in tall tiles -------------------------------------------------------------------------------------
+
+# T, d, f, E, k; the kernels of UP and DOWN, whether DOWN's sums are cut (test_launches_fp8.py holds the sizes to them)
+TALL_LAYERS = [((9000, 520, 776, 4, 2), "tall", "tall", False), ((900, 2040, 1096, 4, 2), "tall apart", "mid64", True), ((1600, 520, 8200, 4, 1), "tall", "tall", True)]
+TALL_EXPERTS = (2200, 8192, 16400, 33, 1)
+tall = pytest.mark.parametrize("T,d,f,E,k", [s[0] for s in TALL_LAYERS])
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """make_layer() with operands from the device."""
+    monkeypatch.setattr(test_fp8, "operand", on_device)
+    return make_layer
+
+
+def poisoned(T, d, f, E, k):
+    return torch.full((B.load_library().btx_moe_ff_forward_fp8_workspace_bytes(T, d, f, E, k),), 255, dtype=torch.uint8, device=DEV)
+
+
+@gpu
+@tall
+@pytest.mark.parametrize("skew,drop", [(True, 0.0), (False, 0.4), (True, 0.9), (False, 1.0)])
+def test_tall_layer_of_a_favoured_expert_and_dropped_pairs(made, T, d, f, E, k, skew, drop):
+    x, xv, W, routing, idx, gates, inv = made(T, d, f, E, k, 3, skew, drop)
+    residual = torch.tensor(rng_of("dres", T).standard_normal((T, d))).to(BF).to(DEV)
+    out = torch.full((T + 1, d), 77.0, dtype=BF, device=DEV)
+    B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing, out=out[:T], residual=residual, workspace=poisoned(T, d, f, E, k))
+    check_layer(out[:T], xv, W, idx, gates, inv, residual)
+    assert (out[T] == 77.0).all()                          # rows behind the last token are left
+    if drop == 1.0:
+        assert torch.equal(out[:T], residual)
+
+
+@gpu
+@tall
+def test_tall_layer_of_one_expert_twice(made, T, d, f, E, k):
+    """A routing that names an expert in all of a token's slots and has one without tokens, and a workspace that holds NaN."""
+    x, xv, W, routing, _, gates, _ = made(T, d, f, E, k, 6)
+    idx = np.repeat(rng_of("twice", T).integers(0, E - 1, (T, 1)), k, 1)
+    perm = np.argsort(idx.reshape(-1), kind="stable")
+    inv = np.argsort(perm).reshape(T, k)
+    offsets = np.concatenate([[0], np.cumsum(np.bincount(idx.reshape(-1), minlength=E))])
+    for name, v in (("topk_idx", idx), ("perm", perm), ("inv_pos", inv), ("offsets", offsets)):
+        setattr(routing, name, torch.tensor(v, dtype=torch.int32, device=DEV))
+    ws = poisoned(T, d, f, E, k)
+    out = B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing, workspace=ws)
+    check_layer(out, xv, W, idx, gates, inv)
+    assert torch.equal(B.btx_moe_ff_forward_fp8(x, *[w for w, _ in W], routing, workspace=ws), out)
+
+
+@gpu
+@tall
+def test_tall_layer_keeps_nan_to_its_tokens(made, T, d, f, E, k):
+    """A token's scale, a block of W1 of one expert (whose tokens' block of activations is quantised to NaN in the kernel), a column of another's output."""
+    x, xv, W, routing, idx, gates, inv = made(T, d, f, E, k, 4)
+    q = [w for w, _ in W]
+    clean = B.btx_moe_ff_forward_fp8(x, *q, routing).cpu()
+    check_layer(clean, xv, W, idx, gates, inv)
+    x.scales[3, 1] = 255
+    x.scales[T - 1, (d - 1) // 128] = 255
+    q[0].scales[0, f - 1, 1] = 255
+    q[2].scales[1, 10, 2] = 255
+    out = B.btx_moe_ff_forward_fp8(x, *q, routing, workspace=poisoned(T, d, f, E, k)).cpu()
+    nan = torch.zeros(T, d, dtype=torch.bool)
+    nan[[3, T - 1]] = True
+    nan[torch.tensor((idx == 0).any(1))] = True
+    nan[torch.tensor((idx == 1).any(1)), 10] = True
+    assert torch.equal(torch.isnan(out), nan) and not nan.all(1).all()
+    assert torch.equal(out[~nan], clean[~nan])
+
+
+@gpu
+def test_tall_layer_of_weights_past_32_bit_offsets():
+    """The last of experts of more than 4 GiB in all; the others are zero."""
+    T, d, f, E, _ = TALL_EXPERTS
+    lib = B.load_library()
+    q, last = [], []
+    for n, K in ((f, d), (f, d), (d, f)):
+        w = B.Fp8(torch.zeros((E, n, lib.btx_fp8_code_pitch(K)), dtype=torch.uint8, device=DEV),
+                  torch.full((E, n, lib.btx_fp8_scale_pitch(K)), 127, dtype=torch.uint8, device=DEV), K)
+        part = B.btx_fp8_quantize(torch.randn((n, K), generator=torch.Generator(device=DEV).manual_seed(n + K), device=DEV) * K ** -0.5)
+        w.codes[E - 1], w.scales[E - 1] = part.codes, part.scales
+        q.append(w)
+        last.append(B.btx_fp8_dequantize(part, F32).double())
+    x = B.btx_fp8_quantize(torch.randn((T, d), generator=torch.Generator(device=DEV).manual_seed(T), device=DEV))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    half = T // 2                                          # tokens of expert 0, and of the last
+    routing = SimpleNamespace(topk_idx=i32([[0]] * half + [[E - 1]] * (T - half)), gates=torch.ones((T, 1), device=DEV), perm=i32(range(T)),
+                              offsets=i32([0] + [half] * (E - 1) + [T]), inv_pos=i32([[t] for t in range(T)]))
+    out = B.btx_moe_ff_forward_fp8(x, *q, routing).double()
+    assert not out[:half].any()
+    xv = B.btx_fp8_dequantize(x, F32).double()[half:]
+    h1, h3 = xv @ last[0].T, xv @ last[1].T
+    act = B.btx_fp8_dequantize(B.btx_fp8_quantize((h1 * torch.sigmoid(h1) * h3).float()), F32).double()
+    want = act @ last[2].T
+    # codes on the other side of a rounding, and two roundings to bf16: 2^-8 of the norm each at most
+    assert (out[half:] - want).norm() <= 2 * 2.0 ** -8 * want.norm()
+
+
+@gpu
+@tall
+def test_tall_layer_in_a_graph_and_on_two_streams(made, T, d, f, E, k):
+    _, _, W, routing, _, _, _ = made(T, d, f, E, k, 5)
+    q = [w for w, _ in W]
+    g = torch.Generator(device=DEV).manual_seed(T)
+    tokens = [torch.randn((T, d), generator=g, device=DEV) for _ in range(3)]
+    B.btx_init()
+
+    def buffers():
+        return SimpleNamespace(x=B.alloc_fp8((T, d), -1, DEV), out=torch.empty((T, d), dtype=BF, device=DEV), ws=poisoned(T, d, f, E, k))
+
+    def layer(b):
+        return B.btx_moe_ff_forward_fp8(b.x, *q, routing, out=b.out, workspace=b.ws)
+
+    def fill(b, i):
+        B.btx_fp8_quantize(tokens[i], out=b.x)
+        b.out.fill_(3.0)
+
+    eager, b = buffers(), buffers()
+    fill(b, 0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer(b)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer(b)
+    for i in (1, 2, 1, 0):
+        fill(b, i)
+        graph.replay()
+        fill(eager, i)
+        assert torch.equal(layer(eager), b.out)
+        torch.cuda.synchronize()
+    want = []
+    for x, i in ((b, 1), (eager, 2)):
+        fill(x, i)
+        want.append(layer(x).clone())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for x in (b, eager):
+            x.out.zero_()
+        torch.cuda.synchronize()
+        for stream, x in zip(streams, (b, eager)):
+            with torch.cuda.stream(stream):
+                layer(x)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.out, w) for x, w in zip((b, eager), want))

@@ -9,7 +9,7 @@ from paper_2403_07816_amd import binding as B
 
 from launches import P, PLENTY, compiled, launches
 from test_fp8 import LAYERS, MATMULS
-from test_fp8_edges import CUT_PRODUCTS, EDGE_PRODUCTS
+from test_fp8_edges import CUT_PRODUCTS, EDGE_PRODUCTS, TALL_EXPERTS, TALL_LAYERS
 
 MAX_THREADS = (1 << 32) - 1     # of one launch and direction of the grid
 UP_FEW, FEW16, FEW64 = "f8_few_kernel<true, 2, 2, 2, float>", "f8_few_kernel<false, {}, 1, 4, {}>", "f8_few_kernel<false, {}, 4, 2, {}>"
@@ -209,3 +209,12 @@ def test_the_shapes_of_the_edge_tests_reach_the_kernels_that_they_are_for(record
             (rc, found), = record(matmul(M, N, K, dtype))
             if want:
                 assert rc == 0 and kind(found[0]) == want and len(found) == 2 and name(found[1]).startswith("f8_add_slices_kernel"), (M, N, K, dtype, name(found[0]))
+
+
+def test_the_edge_tests_of_tall_layers_take_tall_tiles(record):
+    ups = {"tall": TALL.format(0, "false"), "tall apart": TALL.format(0, "true")}
+    downs = {"tall": TALL.format(1, "false"), "mid64": MID.format(1, 64)}
+    for (shape, up, down, cut) in TALL_LAYERS + [(TALL_EXPERTS, "tall", "tall", False)]:
+        (rc, found), = record(layer(*shape))
+        assert rc == 0 and [name(x) for x in found[:2]] == [ups[up], downs[down]], (shape, found)
+        assert name(found[2]).startswith("combine_kernel") and name(found[2]).endswith("false, true>") == cut, (shape, name(found[2]))
