@@ -511,7 +511,8 @@ int btx_moe_ff_forward_mx4(const void* x, const uint8_t* W1_codes, const uint8_t
  * btx_fp8_quantize: a block's scale is the smallest power of two, at least 2^-127, of which its largest magnitude is at most 448 times; its values
  * divided by that are rounded to the nearest e4m3 value, ties to the even one.  A block that holds an infinity or a NaN gets the scale
  * 255: all its values are NaN.
- * btx_fp8_dequantize: value of the code * scale, exact in fp32, and down to 2^-133 in bf16.
+ * btx_fp8_dequantize: value of the code * scale, exact in fp32, and down to 2^-133 in bf16; from 2^128 on an infinity (as fp32 values from 248 * 2^120 on are
+ * quantised to).
  *   x, out      [batch, rows, cols]  dtype (BTX_F32 or BTX_BF16)
  *   axis        1: blocks along the rows: K = cols, n = rows (activations: [T,d] with batch 1)
  *               0: blocks down the columns: K = rows, n = cols; codes and scales are [batch, cols, ..].  So are the experts' weights
@@ -550,9 +551,9 @@ int btx_rmsnorm_fp8(const void* h, const void* residual, int dtype, const float*
 
 /* ---------------------------------------------------------------------------
  * btx_fp8_matmul - out[m,n] = residual[m,n] + sum_k A[m,k] B[n,k] of two matrices in block-scaled 8-bit floats: sums in fp32 in an order that the sizes
- * fix (the same bits every time), rounded once.  fp32 results: exact products (of values under 2^-126, those to bf16's precision there).  bf16 results: of
- * every 8 neighbouring products what lies 13 bits or more below the largest is dropped before they are added up (2e-5 of the result's norm, where rounding
- * it to bf16 is 1.7e-3), in up to twice the rate.
+ * fix (the same bits every time), rounded once.  fp32 results: exact products (of values under 2^-126, those to bf16's precision there, and of infinities for
+ * those from 2^128 on).  bf16 results: of every 8 neighbouring products what lies 13 bits or more below the largest is dropped before they are added up (2e-5
+ * of the result's norm, where rounding it to bf16 is 1.7e-3), in up to twice the rate.
  *   A         codes [M,btx_fp8_code_pitch(K)], scales [M,btx_fp8_scale_pitch(K)];   B: the same with N rows
  *   residual  [M,N]  dtype, may be NULL; may be out itself (a gradient that is added to)
  *   out       [M,N]  dtype (BTX_F32 or BTX_BF16)

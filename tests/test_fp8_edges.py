@@ -315,3 +315,19 @@ def test_tall_layer_in_a_graph_and_on_two_streams(made, T, d, f, E, k):
                 layer(x)
         torch.cuda.synchronize()
         assert all(torch.equal(x.out, w) for x, w in zip((b, eager), want))
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_values_past_fp32(M, N, K):
+    """448 * 2^127 (a scale that no tensor of finite floats is quantised to) times 2^-127: in front of fp32 results a value is a bf16 value, and that one infinite;
+    bf16 results are of codes and scales as they are."""
+    a, b = (B.Fp8(torch.zeros((n, (K + 127) // 128 * 128), dtype=torch.uint8, device=DEV), torch.full((n, 16 * (((K + 127) // 128 + 15) // 16)), s, dtype=torch.uint8, device=DEV), K)
+            for n, s in ((M, 254), (N, 0)))
+    a.codes[2, K - 1] = 126
+    b.codes[:, K - 1] = 56
+    out = B.btx_fp8_matmul(a, b), B.btx_fp8_matmul(a, b, dtype=F32)
+    assert (out[0][2] == 448).all() and (out[1][2] == float("inf")).all()
+    assert all(int(o.count_nonzero()) == N for o in out)
+    q = B.btx_fp8_quantize(torch.full((1, 8), torch.finfo(F32).max, device=DEV))
+    assert int(q.scales[0, 0]) == 247 and torch.isinf(B.btx_fp8_dequantize(q, F32)).all()
