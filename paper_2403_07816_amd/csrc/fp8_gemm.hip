@@ -538,7 +538,8 @@ constexpr uint32_t kB0 = 2 * kStage, kScale0 = 4 * kStage, kOffsets0 = kScale0 +
 constexpr int kTileLds = kOffsets0 + (kF8MaxExperts + 1) * 4;
 enum TileMode { kUp, kOut };                            // activations in 8 bits; bf16
 
-// APART: tiles of neighbouring columns begin at different places of K (an instance of its own: where it gains nothing it takes 1 %)
+// APART: tiles of neighbouring columns begin at different places of K.  An instance of its own: with one for both, timed in turn on one card, layers that are not
+// apart took 0.2-0.5 % longer (16384 tokens 3.439 and 3.444 ms, 2048 582 and 584 us, 32 experts of width 1376 1154 and 1160 us), 16384 x 11008 x 4096 as long.
 template <TileMode MODE, bool APART>
 __global__ __launch_bounds__(kTileWaves* kWave, 2) void f8_tile_kernel(F8Args g, int n_ct) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -968,7 +969,9 @@ __global__ __launch_bounds__(kAddThreads) void f8_add_slices_kernel(const f32x4*
 // Which kernel, and the rows of its tiles
 enum Path { kFew32, kFew64, kMid64, kMid128, kTall };
 constexpr int kPathRows[] = {32, 64, 64, 128, kTileRows};
-// Rows of E experts (those that have a row: about as many each), in tiles
+// Rows of E experts (those that have a row: about as many each), in tiles.  Counts stay on the device, so a favoured expert takes the kernel of the mean: with one
+// that every token names, 301 tokens of 2 of 4 experts of 4096 x 11008 170 -> 181 us (the bf16 layer 258 -> 326), 16384 3.45 -> 3.46 ms, 64 of 8 of 32 of width
+// 1376 140 -> 139 us.
 struct Rows {
   int64_t busy, each;
   Rows(int64_t R, int E) : busy(std::min<int64_t>(E, R)), each((R + busy - 1) / busy) {}
@@ -978,11 +981,12 @@ struct Rows {
 // (2.5 us and more): a sum that is 2e-5 off is on the other side of a code's border now and then, or its block of a scale's, and over few tokens one such
 // block shows (3 tokens of 4 experts of 168 x 88: 0.0053 of the result's norm, and 0.0017).  That costs little where reading the weights bounds it:
 // 16 tokens of 2 of 4 experts of 4096 x 11008 122 -> 132 us, 64 131 -> 135.  Tall tiles' are on the matrix cores' own 8-bit products: 16384 tokens would
-// take twice as long, and the sums' errors average out over those.  A layer's time, us, with few / 64 / 128 / tall for UP:
-//   2 of 4 experts of 4096 x 11008, rows each:  1  66 66 80 73;  4  134 126 128 145;  16  152 133 139 153;  64  236 142 149 159;  95  316 179 162 164
-//   8 of 32 of 4096 x 1376:  4  124 129 142 137;  16  142 136 144 142;  50  216 147 153 149;  95  315 180 165 156
-//   2 of 8 of 2048 x 8192:  1  63 68 73 78;  16  108 98 104 106;  32  130 101 108 107;  63  188 127 122 115
-//   2 of 8 of 1024 x 2048:  1  15 18 21 23;  16  26 24 26 27;  64  39 31 32 30;  128  56 42 40 35
+// take twice as long, and the sums' errors average out over those.  A layer's time, us, with few / 64 / 128 / tall for UP (all experts with as many rows; of one
+// row two experts).  Up to 64 rows tall tiles are now and then a little faster, and not exact:
+//   2 of 4 experts of 4096 x 11008, rows each:  1  62 63 77 60;  4  134 126 129 134;  16  143 122 133 135;  64  231 139 151 147;  95  303 183 171 154
+//   8 of 32 of 4096 x 1376:  4  140 134 145 133;  16  146 131 137 135;  50  220 147 147 141;  95  301 181 168 148
+//   2 of 8 of 2048 x 8192:  1  31 32 36 36;  16  104 95 103 102;  32  118 97 106 103;  63  169 107 116 108
+//   2 of 8 of 1024 x 2048:  1  18 20 22 24;  16  25 24 27 27;  64  35 29 31 29;  128  54 34 33 32
 constexpr int kUpFewRows = 3, kUpMidRows = 64, kUpMidTiles = kTileGrid;
 Path up_path(int64_t R, int E, int f) {
   const Rows n(R, E);
@@ -992,20 +996,20 @@ Path up_path(int64_t R, int E, int f) {
   return n.tiles(128) * ceil_div(f, 64) <= kUpMidTiles ? kMid128 : kTall;
 }
 // Other products.  Of one matrix (sums of tiles that are cut along K are added by another launch), columns x K, rows, us:
-//   1024 x 1024: 64  5.1 7.3 8.3 13;  256  5.6 7.1 9.5 16;  1024  13 7.5 9.8 16;  16384  75 36 29 22
-//   4096 x 1376: 32  5.4 8.0 9.5 15;  96  8.5 8.4 11 17;  1024  27 12 13 20;  16384  366 207 143 97
-//   4096 x 4096: 16  7.4 9.6 11 15;  32  9.5 10 12 16;  64  15 12 13 17;  256  47 16 21 29;  1024  74 27 29 43;  2048  157 52 41 53;  16384  - 591 333 211
-//   4096 x 11008: 16  15 15 17 21;  64  33 18 20 24;  256  120 30 33 44;  1024  193 73 74 65;  2048  402 146 105 94
-//   512 x 8192: 16  11 9.3 10 15;  256  25 12 14 25;  2048  91 23 22 31        256 x 2048: 64  7.4 9.4 10 15;  1024  8.1 10 13 23;  16384  37 16 17 32
-//   11008 x 4096: 1  12 16 - -;  8  14 17 - -;  16  16 13 18 17;  32  23 14 18 19;  256  59 29 32 35;  512  118 45 40 44;  1024  216 76 70 46
-//   11008 x 2048: 16  8.8 9.6 - -;  32  12 11 - -        8192 x 8192: 4  16 19 - -;  12  19 17 - -        33000 x 512: 8  7.0 6.5;  48  11 7.7;
-//   33000 x 4096: 1  40 32 - -;  32  46 37 - -
-// In fp32:  1024 x 2048: 64  7.9 12 14;  200  8.4 12 15        4096 x 4001: 64  15 14 16;  400  - 29 29;  1376  - 63 59;  4096  - 171 128
-//   4096 x 16384: 40  38 20 23;  100  79 33 28;  400  - 104 81;  1024  - 156 147        512 x 8192: 400  - 15 19;  2048  - 34 29
+//   1024 x 1024: 64  5.8 7.2 8.6 12;  256  5.7 7.4 9.6 15;  1024  14 7.7 10 16;  16384  77 34 28 21
+//   4096 x 1376: 32  5.9 7.6 9.6 15;  96  8.7 8.5 11 17;  1024  28 12 13 20;  16384  367 207 134 86
+//   4096 x 4096: 16  8.0 10 10 14;  32  9.8 11 11 15;  64  14 12 12 17;  256  47 16 18 28;  1024  75 24 30 42;  2048  155 51 42 53;  16384  1141 595 325 200
+//   4096 x 11008: 16  15 14 15 20;  64  33 17 19 24;  256  120 28 28 38;  1024  192 64 67 62;  2048  399 137 102 91
+//   512 x 8192: 16  11 9.9 11 15;  256  25 13 14 25;  2048  91 23 23 31        256 x 2048: 64  7.5 9.9 10 15;  1024  8.2 10 13 23;  16384  38 16 17 31
+//   11008 x 4096: 1  11 13 14 15;  8  14 13 14 15;  16  16 12 15 16;  32  22 13 16 17;  256  58 23 27 34;  512  115 40 36 43;  1024  216 71 62 46
+//   11008 x 2048: 16  9.0 10 10 15;  32  12 11 12 16        8192 x 8192: 4  16 17 17 18;  12  19 15 18 19        33000 x 512: 8  7.1 6.2 6.7 11;
+//   48  10 7.3 7.9 10        33000 x 4096: 1  32 27 29 34;  32  44 31 31 35
+// In fp32:  1024 x 2048: 64  8.4 12 14;  200  8.4 13 16        4096 x 4001: 64  15 14 16;  400  73 29 29;  1376  239 66 60;  4096  - 174 132
+//   4096 x 16384: 40  38 21 24;  100  79 34 28;  400  282 107 81;  1024  - 155 148        512 x 8192: 400  25 15 19;  2048  91 34 30
 // Of experts (the sums of tiles that are cut are added where the rows are combined), rows each:
-//   4 of 11008 x 4096 (K x N): 4  42 44 46 43;  16  56 46 46 44;  32  86 47 48 45;  64  132 58 50 49;  150  297 86 79 59
-//   32 of 1376 x 4096: 4  37 36 37 41;  16  44 41 41 43;  32  52 43 43 44;  100  99 61 53 47       8 of 2048 x 1024: 4  8 9 10 15;  16  11 9 10 15;
-//   64  20 11 12 18;  256  51 16 19 27;  1024  166 38 38 45;      64 of 1024 x 2048: 4  29 31 31 36;  32  40 37 36 38;  64  57 42 41 39;  256  155 89 86 62
+//   4 of 11008 x 4096 (K x N): 4  40 47 47 45;  16  54 41 48 46;  32  76 42 50 48;  64  146 46 52 51;  150  351 90 81 62
+//   32 of 1376 x 4096: 4  40 38 39 42;  16  44 40 41 43;  32  50 43 44 47;  100  138 61 52 47       8 of 2048 x 1024: 4  8.2 9.1 10 15;  16  9.4 9.0 10 15;
+//   64  18 11 12 17;  256  54 15 16 25;  1024  205 34 30 30;      64 of 1024 x 2048: 4  30 31 31 34;  32  39 35 37 39;  64  61 38 40 39;  256  210 89 85 52
 Path out_path(int64_t R, int E, int N, int K, bool exact) {
   const Rows n(R, E);
   const int columns = ceil_div(N, kMidCols), n_blk = (int)(f8_pitch(K) / kF8Block);
@@ -1061,8 +1065,8 @@ int launch_f8_matmul(const F8Matmul& m, hipStream_t s) {
   F8Args g{m.a, m.b, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.M, m.N, m.K, nullptr, nullptr, m.out, m.residual, 1, static_cast<float*>(m.workspace)};
   const bool bf16 = m.dtype == BTX_BF16;
   // A result of few columns, turned: few rows of b, with the many of a for weights.  Tiles of 64 rows and 128 columns are cut along K for these, and have
-  // most of their columns empty.  us, turned / not, rows x columns, K:  800 x 8  2048 4.6 7.7, 8192 9.3 8.6;  800 x 64  2048 7.6 8.6, 4096 13 8.5;
-  // 3000 x 16  2048 4.9 8.3, 4096 7.2 8.8, 8192 12 12;  16384 x 16  520 5.7 5.6, 4096 15 18, 8192 31 35 (fp32 40 55);  16384 x 64  2048 15 11, 8192 46 36
+  // most of their columns empty.  us, turned / not, rows x columns, K:  800 x 8  2048 5.1 7.2, 8192 9.7 9.8;  800 x 64  2048 7.9 7.8, 4096 14 10;
+  // 3000 x 16  2048 5.8 7.9, 4096 7.2 10, 8192 12 13;  16384 x 16  520 6.0 5.9, 4096 15 18, 8192 26 32 (fp32 38 55);  16384 x 64  2048 15 11, 8192 42 32
   if (m.M > 64 && (m.M < 4096 ? m.N <= 64 && (int64_t)m.K * (m.N + 16) <= 180000 : m.N <= 16)) {
     const F8Args t{m.b, m.a, {nullptr, nullptr}, nullptr, nullptr, 1, 1, m.N, m.M, m.K, nullptr, nullptr, m.out, m.residual, 1, nullptr, true, false};
     return bf16 ? launch_few<bf16_t>(t, m.N <= 32 ? 32 : 64, s) : launch_few<float>(t, m.N <= 32 ? 32 : 64, s);
